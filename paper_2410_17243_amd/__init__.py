@@ -27,6 +27,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libinfcl.so")
 HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "infcl.h")
 ABLATION_HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "infcl_ablation.h")
+TOWER_HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "infcl_tower.h")
 
 INFCL_OK, INFCL_ERR_INVALID, INFCL_ERR_UNSUPPORTED, INFCL_ERR_WORKSPACE, INFCL_ERR_HIP = range(5)
 INFCL_BF16, INFCL_F32, INFCL_F16 = 0, 1, 2
@@ -346,3 +347,17 @@ def clip_loss(img, txt, scale):
     if _ClipLoss is None:
         _ClipLoss = _make_function()
     return _ClipLoss.apply(img, txt, scale)
+
+
+# The text tower's operators (tower.py) under the package's own name; the module
+# is imported when one is first asked for.
+_TOWER = ("embed", "embed_fwd", "embed_bwd", "Ckpt8", "ckpt8_pack", "ckpt8_unpack", "ckpt8_act_fwd", "ckpt8_act_bwd",
+          "ckpt8_wgrad", "linear8", "mlp8", "packed_attn", "packed_attn_qkv", "packed_attn_fwd", "packed_attn_bwd")
+
+
+def __getattr__(name):
+    if name in _TOWER:
+        from . import tower
+
+        return getattr(tower, name)
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

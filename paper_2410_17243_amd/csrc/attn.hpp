@@ -1,0 +1,255 @@
+// Shared parts of the packed-attention kernels (gfx950).
+//
+// Every kernel keeps 32 rows of one side per wave in registers as the column
+// operand of the 32x32x16 MFMA and sweeps tiles of the other side through LDS.
+// A product of swept rows (A) with own rows (B) leaves in lane L the own row
+// L % 32 and, in register r of a 32-row block, the swept row
+// 8 (r / 4) + 4 (L / 32) + r % 4: softmax statistics of own rows are sums over a
+// lane's registers and one exchange with lane L ^ 32, and registers 8t .. 8t + 7,
+// rounded to 16 bits, are the column operand of the next product over swept
+// rows 16t .. 16t + 15 as they stand, if the transposing LDS reads of its row
+// operand take those rows in the same order (lane half h, slot e:
+// 16t + 8 (e / 4) + 4h + e % 4).
+//
+// Tiles in LDS: rows of DP features (64 or 128; heads of fewer features are
+// filled up with zeros), 16-byte chunks at chunk ^ attn_sw(row), so that reads
+// of one chunk of 16 rows, and the 4 rows x 4 chunks of a half-wave's
+// transposing reads, each touch all 64 banks once.
+#pragma once
+
+#include "common.hpp"
+#include "infcl_tower.h"
+
+namespace infcl {
+
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+
+// What the kernels get of a call.  Strides in elements.
+struct AttnArgs {
+  const uint16_t *q, *k, *v;
+  int64_t qs, qh, ks, kh, vs, vh;  // from token to token, from head to head
+  const int32_t *cu_q, *cu_k;
+  int64_t tq, tk;
+  int32_t nseq, heads, kvh, group, hd, causal;
+  float scale, sl2;  // of the scores; times log2(e)
+};
+
+// How a forward call is cut up, and its workspace.
+struct AttnFwdPlan {
+  int nw, tiles, parts;  // waves of a workgroup; row tiles of a sequence; parts of its keys
+  size_t o, ml, total;
+};
+
+// Sequence z's queries [q0, q0 + m) and keys [k0, k0 + n), cut to the arrays
+// whatever the offsets say.  z = nseq: the rows past the last sequence, as
+// queries without keys (or keys without queries).
+struct AttnSeq {
+  int64_t q0, k0;
+  int32_t m, n;
+};
+__device__ __forceinline__ AttnSeq attn_seq(const AttnArgs& a, int z) {
+  AttnSeq s;
+  const int64_t q0 = a.cu_q[z], k0 = a.cu_k[z];
+  const int64_t q1 = z < a.nseq ? a.cu_q[z + 1] : a.tq, k1 = z < a.nseq ? a.cu_k[z + 1] : a.tk;
+  s.q0 = q0 < 0 ? 0 : q0 > a.tq ? a.tq : q0;
+  s.k0 = k0 < 0 ? 0 : k0 > a.tk ? a.tk : k0;
+  const int64_t e = q1 > a.tq ? a.tq : q1, f = k1 > a.tk ? a.tk : k1;
+  s.m = (int32_t)(e > s.q0 ? e - s.q0 : 0);
+  s.n = (int32_t)(f > s.k0 ? f - s.k0 : 0);
+  return s;
+}
+
+template <int DP>
+__host__ __device__ __forceinline__ int attn_sw(int r) {
+  return DP == 128 ? 4 * (r & 3) + ((r >> 2) & 3) : 4 * ((r >> 1) & 1) + ((r >> 2) & 3);
+}
+
+// Copies of a tile of KT rows to LDS by NW waves: instruction k = wave + NW kk
+// fills 1024 bytes.  The chunk order depends on k only modulo kPeriod, so a
+// lane keeps one source offset for each of kVar instructions.  Chunks past the
+// head's features have an offset past every tile: zeros.
+template <int DP, int NW, int KT>
+struct AttnTile {
+  static constexpr int kCh = DP / 8, kRows = 64 / kCh, kInstr = KT / kRows, kPer = kInstr / NW;
+  static constexpr int kPeriod = DP == 128 ? 4 : 2, kVar = kPeriod / NW > 1 ? kPeriod / NW : 1;
+  static constexpr int kBytes = KT * DP * 2, kRow = DP * 2;
+  static_assert(kPer >= 1 && kInstr % NW == 0, "layout");
+
+  static __host__ __device__ __forceinline__ void offsets(uint32_t (&off)[kVar], int wave, int lane, uint32_t stride, int hd) {
+#pragma unroll
+    for (int i = 0; i < kVar; ++i) {
+      const int r = ((wave + NW * i) % kPeriod) * kRows + lane / kCh, c = (lane % kCh) ^ attn_sw<DP>(r);
+      off[i] = 8 * c < hd ? (uint32_t)(lane / kCh) * stride + 16 * c : 0x80000000u;
+    }
+  }
+  // rows: how many there are from base on (any number; at most KT are read).
+  static __device__ __forceinline__ void issue(const uint16_t* base, int rows, uint32_t stride, int hd,
+                                               INFCL_LDS char* lds, const uint32_t (&off)[kVar], int wave) {
+    int n = rows > KT ? KT : rows;
+    n = n < 0 ? 0 : n;
+    const uint64_t at = (uint64_t)base;
+    u32x4 rs;
+    rs[0] = (uint32_t)at, rs[1] = (uint32_t)(at >> 32) & 0xFFFFu, rs[3] = 0x00020000u;
+    rs[2] = n ? (uint32_t)(n - 1) * stride + 2 * hd : 0;
+#pragma unroll
+    for (int kk = 0; kk < kPer; ++kk) {
+      const int k = wave + NW * kk;
+      dma16_asm(rs, lds + 1024 * k, off[kk % kVar], (uint32_t)(k * kRows) * stride);
+    }
+  }
+};
+
+// Addresses in a tile: row fragments (swept rows as A operand: row L % 32, chunk
+// 2i + h) and transposed ones (32-feature block fb, rows 16t + 8tt + 4h + e).
+template <int DP>
+struct AttnLanes {
+  static constexpr int kI = DP / 16, kFb = DP / 32;
+  int row[kI], tr[2][kFb];
+  __host__ __device__ __forceinline__ void init(int lane) {
+    const int r = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < kI; ++i) row[i] = r * DP * 2 + 16 * ((2 * i + h) ^ attn_sw<DP>(r));
+    const int l16 = lane & 15, e = l16 >> 2, qq = l16 & 3, nb = (lane >> 4) & 1;
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      const int tr_row = 8 * tt + 4 * h + e;
+#pragma unroll
+      for (int fb = 0; fb < kFb; ++fb)
+        tr[tt][fb] =
+            tr_row * DP * 2 + 16 * ((4 * fb + 2 * nb + (qq >> 1)) ^ attn_sw<DP>(tr_row)) + 8 * (qq & 1);
+    }
+  }
+};
+
+__device__ __forceinline__ bf16x8 attn_row(const INFCL_LDS char* p) { return *(const INFCL_LDS bf16x8*)p; }
+__device__ __forceinline__ bf16x8 attn_tr(const INFCL_LDS char* p0, const INFCL_LDS char* p1) {
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((INFCL_LDS s16x4*)p0);
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((INFCL_LDS s16x4*)p1);
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Registers 8t .. 8t + 7 of a 32-row block as the column operand of step t.
+template <bool F16>
+__device__ __forceinline__ bf16x8 attn_pack(const f32x16& x, int t) {
+  bf16x8 r;
+  if constexpr (F16) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = to16<true>(x[8 * t + e]);
+  } else {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = pk_bf16(x[8 * t + 2 * e], x[8 * t + 2 * e + 1]);
+    r = __builtin_bit_cast(bf16x8, w);
+  }
+  return r;
+}
+
+// x of this lane and of lane ^ 32.
+__device__ __forceinline__ void attn_both(float x, float& a, float& b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  a = __uint_as_float(r[0]);
+  b = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float attn_max2(float x) {
+  float a, b;
+  attn_both(x, a, b);
+  return fmaxf(a, b);
+}
+__device__ __forceinline__ float attn_sum2(float x) {
+  float a, b;
+  attn_both(x, a, b);
+  return a + b;
+}
+
+__device__ __forceinline__ f32x16 f32x16_zero() {
+  f32x16 z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
+}
+
+// Swept row of register r in lane half h, within its 32-row block.
+__host__ __device__ __forceinline__ int attn_reg_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
+
+// One own row's 16-byte chunk 2i + h (of hd / 8), or zeros.
+__device__ __forceinline__ bf16x8 attn_own(const uint16_t* row, int i, int h, int hd, bool live) {
+  u32x4 c = {0, 0, 0, 0};
+  if (live && 8 * (2 * i + h) < hd) c = *(const u32x4*)(row + 8 * (2 * i + h));
+  return __builtin_bit_cast(bf16x8, c);
+}
+
+// Stores a transposed accumulator (own row in the lane, features in the
+// registers) times f as 16-bit elements.
+template <bool F16, int FB>
+__device__ __forceinline__ void attn_store(uint16_t* row, const f32x16 (&acc)[FB], float f, int h, int hd) {
+#pragma unroll
+  for (int fb = 0; fb < FB; ++fb)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int d = 32 * fb + 8 * j + 4 * h;
+      if (d >= hd) continue;
+      u32x2 w;
+      if constexpr (F16) {
+        typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+        f16x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (_Float16)(acc[fb][4 * j + e] * f);
+        w = __builtin_bit_cast(u32x2, x);
+      } else {
+        w[0] = pk_bf16(acc[fb][4 * j] * f, acc[fb][4 * j + 1] * f);
+        w[1] = pk_bf16(acc[fb][4 * j + 2] * f, acc[fb][4 * j + 3] * f);
+      }
+      *(u32x2*)(row + d) = w;
+    }
+}
+
+// Whether an accumulator holds a NaN (x 0 is NaN for infinities too).
+template <int FB>
+__device__ __forceinline__ bool attn_bad(const f32x16 (&acc)[FB]) {
+  float t = 0.f;
+#pragma unroll
+  for (int fb = 0; fb < FB; ++fb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) t = fmaf(acc[fb][r], 0.f, t);
+  return !(t == 0.f);
+}
+
+// ---- The exact form of a tile with masked entries.  A masked weight is zero,
+// but zero times an infinity or a NaN of a masked row would reach the product.
+// A workgroup whose sums are not finite therefore sweeps again and takes the
+// tiles that hold masked entries row by row: no masked row is read into a sum.
+
+// <own row, swept row j> over this lane's half of the features, both halves added.
+template <int DP, bool F16>
+__device__ __forceinline__ float attn_dot(const bf16x8 (&own)[DP / 16], const INFCL_LDS char* tile, int j, int h) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < DP / 16; ++i) {
+    const bf16x8 x = attn_row(tile + j * DP * 2 + 16 * ((2 * i + h) ^ attn_sw<DP>(j)));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fmaf(from16<F16>(own[i][e]), from16<F16>(x[e]), s);
+  }
+  return attn_sum2(s);
+}
+// acc += w row j, where live.
+template <int DP, bool F16>
+__device__ __forceinline__ void attn_axpy(f32x16 (&acc)[DP / 32], float w, bool live, const INFCL_LDS char* tile, int j,
+                                          int h) {
+#pragma unroll
+  for (int fb = 0; fb < DP / 32; ++fb)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      const bf16x4 x = *(const INFCL_LDS bf16x4*)(tile + j * DP * 2 + 16 * ((4 * fb + q) ^ attn_sw<DP>(j)) + 8 * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (live) acc[fb][4 * q + e] = fmaf(w, from16<F16>(x[e]), acc[fb][4 * q + e]);
+    }
+}
+
+// Barrier of the workgroup after all of this wave's copies and LDS reads.
+__device__ __forceinline__ void attn_barrier() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+}  // namespace infcl

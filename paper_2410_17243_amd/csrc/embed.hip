@@ -1,0 +1,506 @@
+// Token embedding with scaling, and the table's gradient by sorted tokens.
+//
+//   out_t    = scale W[tok_t]
+//   dW_v     = scale sum_{t: tok_t = v} dout_t
+//
+// Both are bound by memory.  The forward is one copy of rows.  The gradient
+// has to read dout once and write the table once; a token's rows are spread
+// over dout, so the positions are first sorted by token (a stable radix sort:
+// 12 bytes per token, against 2 d bytes of its row) and each table row is then
+// one group of lanes that adds its rows in order of t: no atomics on floats,
+// one write per table row, and the order of every sum is fixed.  Tokens with
+// more than kPart rows (those that open and close every caption) are summed in
+// parts of kPart sorted positions, joined in order.
+#include "infcl_tower.h"
+#include "rows.hpp"
+
+namespace infcl {
+namespace {
+
+// ------------------------------------------------------------------- forward
+
+// A group of 1 << ls lanes copies a row; each group takes kFwdRows rows at a
+// time so that as many loads are in flight.
+constexpr int kFwdRows = 4;
+
+template <int T, typename Tok>
+__global__ void __launch_bounds__(256) embed_fwd_kernel(const Tok* __restrict__ tok, int64_t n,
+                                                        const u32x4* __restrict__ table, int64_t vocab, int c, int ls,
+                                                        float scale, u32x4* __restrict__ out) {
+  const int gl = threadIdx.x & ((1 << ls) - 1);
+  const int64_t g = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> ls, ng = (int64_t)gridDim.x * 256 >> ls;
+  for (int64_t t0 = g * kFwdRows; t0 < n; t0 += ng * kFwdRows) {
+    int64_t v[kFwdRows];
+#pragma unroll
+    for (int k = 0; k < kFwdRows; ++k) {
+      v[k] = t0 + k < n ? (int64_t)tok[t0 + k] : -1;
+      if (v[k] >= vocab) v[k] = -1;
+    }
+    for (int i = gl; i < c; i += 1 << ls) {
+      u32x4 r[kFwdRows];
+#pragma unroll
+      for (int k = 0; k < kFwdRows; ++k) {
+        r[k] = u32x4{0, 0, 0, 0};
+        if (v[k] >= 0) r[k] = table[v[k] * c + i];
+      }
+#pragma unroll
+      for (int k = 0; k < kFwdRows; ++k) {
+        if (v[k] >= 0) {
+          float x[Chunk<T>::N];
+          Chunk<T>::load(r[k], x);
+#pragma unroll
+          for (int e = 0; e < Chunk<T>::N; ++e) x[e] *= scale;
+          r[k] = Chunk<T>::store(x);
+        }
+        if (t0 + k < n) out[(t0 + k) * c + i] = r[k];
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------- sort
+
+// Least significant digit first, `bits` bits a pass (at most kMaxBits).  A
+// block of 4 waves owns kTile consecutive elements, a wave a quarter of them,
+// 64 at a time in order.
+constexpr int kTile = 4096, kMaxBits = 10;
+
+template <typename Tok>
+__device__ __forceinline__ uint32_t token_key(Tok t, uint32_t vocab) {
+  return t >= 0 && (uint64_t)t < vocab ? (uint32_t)t : vocab;  // (invalid ones last)
+}
+
+// Counts of a tile's digits.  first: keys are made from the tokens.  Also
+// clears the next pass's counts.
+template <typename Tok>
+__global__ void __launch_bounds__(256) sort_count(const Tok* __restrict__ tok, int64_t n, uint32_t vocab, int bits,
+                                                  uint32_t* __restrict__ hist, uint32_t* __restrict__ next) {
+  __shared__ uint32_t cnt[1 << kMaxBits];
+  const int bins = 1 << bits;
+  for (int i = threadIdx.x; i < bins; i += 256) {
+    cnt[i] = 0;
+    next[(int64_t)blockIdx.x * bins + i] = 0;
+  }
+  __syncthreads();
+  const int64_t t0 = (int64_t)blockIdx.x * kTile;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < kTile; i += 256)
+    if (t0 + i < n) atomicAdd(&cnt[token_key(tok[t0 + i], vocab) & (bins - 1)], 1u);
+  __syncthreads();
+  for (int i = threadIdx.x; i < bins; i += 256) hist[(int64_t)blockIdx.x * bins + i] = cnt[i];
+}
+
+// One pass: every element to its place.  The place is the number of elements
+// with smaller digits (all tiles), plus those of its digit in earlier tiles,
+// plus those earlier in this tile.  hist holds every tile's counts; with next,
+// the places' counts of the following digit are added up there (integer
+// atomics: the counts do not depend on their order).
+template <typename Tok, bool FIRST>
+__global__ void __launch_bounds__(256) sort_scatter(const Tok* __restrict__ tok, const uint2* __restrict__ in,
+                                                    int64_t n, uint32_t vocab, int shift, int bits,
+                                                    const uint32_t* __restrict__ hist, uint32_t* __restrict__ next,
+                                                    uint2* __restrict__ out) {
+  __shared__ uint32_t base[1 << kMaxBits], wcnt[4][1 << kMaxBits], wsum[4];
+  const int bins = 1 << bits, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int tiles = gridDim.x;
+  // a thread's share of the bins: 1 to 4 consecutive ones
+  const int per = bins > 256 ? bins >> 8 : 1;
+  uint32_t before[4] = {0, 0, 0, 0}, all[4] = {0, 0, 0, 0}, mine = 0;
+  if ((int)threadIdx.x * per < bins) {
+    for (int t = 0; t < tiles; ++t) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < per) {
+          const uint32_t h = hist[(int64_t)t * bins + threadIdx.x * per + k];
+          all[k] += h;
+          before[k] += t < (int)blockIdx.x ? h : 0;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mine += all[k];
+  }
+  // exclusive scan over the threads
+  uint32_t inc = mine;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const uint32_t o = __shfl_up(inc, s);
+    if (lane >= s) inc += o;
+  }
+  if (lane == 63) wsum[wave] = inc;
+  for (int i = threadIdx.x; i < 4 * bins; i += 256) wcnt[i >> bits][i & (bins - 1)] = 0;
+  __syncthreads();
+  uint32_t off = inc - mine;
+  for (int w = 0; w < wave; ++w) off += wsum[w];
+  if ((int)threadIdx.x * per < bins) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < per) {
+        base[threadIdx.x * per + k] = off + before[k];
+        off += all[k];
+      }
+  }
+  // this wave's quarter: counts, then places
+  constexpr int kWave = kTile / 4;
+  const int64_t w0 = (int64_t)blockIdx.x * kTile + wave * kWave;
+  uint2 el[kWave / 64];
+#pragma unroll
+  for (int i = 0; i < kWave / 64; ++i) {
+    const int64_t t = w0 + 64 * i + lane;
+    el[i] = make_uint2(0, 0);
+    if (t < n) el[i] = FIRST ? make_uint2(token_key(tok[t], vocab), (uint32_t)t) : in[t];
+  }
+#pragma unroll
+  for (int i = 0; i < kWave / 64; ++i)
+    if (w0 + 64 * i + lane < n) atomicAdd(&wcnt[wave][(el[i].x >> shift) & (bins - 1)], 1u);
+  __syncthreads();
+  for (int i = threadIdx.x; i < bins; i += 256) {
+    uint32_t o = base[i];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t h = wcnt[w][i];
+      wcnt[w][i] = o;
+      o += h;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kWave / 64; ++i) {
+    const bool live = w0 + 64 * i + lane < n;
+    const uint32_t dg = (el[i].x >> shift) & (bins - 1);
+    uint64_t same = __ballot(live);
+    for (int k = 0; k < bits; ++k) {  // lanes with this lane's digit
+      const bool bit = (dg >> k) & 1;
+      const uint64_t m = __ballot(bit);
+      same &= bit ? m : ~m;
+    }
+    const int ahead = __popcll(same & ((1ull << lane) - 1)), count = __popcll(same);
+    uint32_t place = 0;
+    if (live) place = wcnt[wave][dg] + ahead;
+    __builtin_amdgcn_wave_barrier();
+    if (live && ahead == 0) wcnt[wave][dg] += count;
+    __builtin_amdgcn_wave_barrier();
+    if (live) {
+      out[place] = el[i];
+      if (next) atomicAdd(&next[(int64_t)(place / kTile) * bins + ((el[i].x >> (shift + bits)) & (bins - 1))], 1u);
+    }
+  }
+}
+
+// start[v] = first sorted position whose token is >= v, v = 0 .. vocab.
+__global__ void __launch_bounds__(256) row_starts(const uint2* __restrict__ sorted, int64_t n, uint32_t vocab,
+                                                  uint32_t* __restrict__ start) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i > n) return;
+  const int64_t lo = i ? (int64_t)sorted[i - 1].x + 1 : 0, hi = i < n ? (int64_t)sorted[i].x : (int64_t)vocab;
+  for (int64_t v = lo; v <= hi && v <= vocab; ++v) start[v] = (uint32_t)i;
+}
+
+// ------------------------------------------------------------- sums by token
+
+constexpr int kPart = 128;  // sorted positions that one group of lanes sums at most
+
+// Sum of the rows at sorted positions [a, b), chunk i of c, in order.
+template <int T>
+__device__ __forceinline__ void sum_rows(const uint2* __restrict__ sorted, const u32x4* __restrict__ dout, int c, int i,
+                                         uint32_t a, uint32_t b, float (&s)[Chunk<T>::N]) {
+  constexpr int N = Chunk<T>::N, U = 8;
+#pragma unroll
+  for (int e = 0; e < N; ++e) s[e] = 0.f;
+  for (; a < b; a += U) {
+    u32x4 r[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (a + k < b) r[k] = dout[(int64_t)sorted[a + k].y * c + i];
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (a + k < b) {
+        float x[N];
+        Chunk<T>::load(r[k], x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) s[e] += x[e];
+      }
+  }
+}
+
+template <int T, int G>
+__device__ __forceinline__ void put_row(void* dtable, int64_t v, int c, int i, const float (&s)[Chunk<T>::N],
+                                        float scale) {
+  constexpr int N = Chunk<T>::N;
+  float x[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) x[e] = s[e] * scale;
+  if constexpr (G == T) {
+    ((u32x4*)dtable)[v * c + i] = Chunk<T>::store(x);
+  } else {  // fp32 from 16-bit rows
+    f32x4* p = (f32x4*)dtable + (v * c + i) * 2;
+    p[0] = f32x4{x[0], x[1], x[2], x[3]};
+    p[1] = f32x4{x[4], x[5], x[6], x[7]};
+  }
+}
+
+// Blocks [0, row_blocks): table rows of at most kPart tokens, a group of lanes
+// each.  The others: sorted positions [128 p, 128 p + 128) of tokens with more
+// than kPart rows.  Such a stretch holds parts of at most two of them (one
+// inside it would be too short): sums in slots 2p (the run that holds its first
+// position) and 2p + 1 (the one of its last, if another).
+template <int T, int G>
+__global__ void __launch_bounds__(256) embed_sum(const uint2* __restrict__ sorted, int64_t n,
+                                                 const u32x4* __restrict__ dout, const uint32_t* __restrict__ start,
+                                                 uint32_t vocab, int c, int ls, float scale, void* __restrict__ dtable,
+                                                 float* __restrict__ part, uint32_t row_blocks) {
+  constexpr int N = Chunk<T>::N;
+  const int gl = threadIdx.x & ((1 << ls) - 1);
+  const uint32_t per = 256u >> ls;
+  if (blockIdx.x < row_blocks) {
+    const uint32_t v = blockIdx.x * per + (threadIdx.x >> ls);
+    if (v >= vocab) return;
+    const uint32_t a = start[v], b = start[v + 1];
+    if (b - a > kPart) return;
+    for (int i = gl; i < c; i += 1 << ls) {
+      float s[N];
+      sum_rows<T>(sorted, dout, c, i, a, b, s);
+      put_row<T, G>(dtable, v, c, i, s, scale);
+    }
+    return;
+  }
+  const int64_t p = (int64_t)(blockIdx.x - row_blocks) * per + (threadIdx.x >> ls);
+  const int64_t s0 = p * kPart;
+  if (s0 >= n) return;
+  const uint32_t a0 = (uint32_t)s0, b0 = (uint32_t)(s0 + kPart < n ? s0 + kPart : n);
+  const uint32_t v0 = sorted[a0].x, v1 = sorted[b0 - 1].x;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t v = h ? v1 : v0;
+    if (v >= vocab || (h && v1 == v0)) continue;
+    uint32_t a = start[v], b = start[v + 1];
+    if (b - a <= kPart) continue;
+    a = a > a0 ? a : a0;
+    b = b < b0 ? b : b0;
+    for (int i = gl; i < c; i += 1 << ls) {
+      float s[N];
+      sum_rows<T>(sorted, dout, c, i, a, b, s);
+      float* q = part + ((2 * p + h) * c + i) * N;
+#pragma unroll
+      for (int e = 0; e < N; e += 4) *(f32x4*)(q + e) = f32x4{s[e], s[e + 1], s[e + 2], s[e + 3]};
+    }
+  }
+}
+
+// The parts of a token with more than kPart rows, in order: block p joins the
+// run that begins in stretch p, if one does.  Four waves take a quarter of the
+// parts each; blockIdx.y is a group of 64 chunks of the row.
+template <int T, int G>
+__global__ void __launch_bounds__(256) embed_join(const uint2* __restrict__ sorted, int64_t n,
+                                                  const uint32_t* __restrict__ start, uint32_t vocab, int c,
+                                                  float scale, const float* __restrict__ part,
+                                                  void* __restrict__ dtable) {
+  constexpr int N = Chunk<T>::N;
+  const int64_t p = blockIdx.x, s0 = p * kPart, last = (s0 + kPart < n ? s0 + kPart : n) - 1;
+  const uint32_t v = sorted[last].x;  // (a long run that begins here holds the stretch's last position)
+  if (v >= vocab) return;
+  const int64_t a = start[v], b = start[v + 1];
+  if (b - a <= kPart || a < s0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int i = blockIdx.y * 64 + lane;
+  const int64_t p1 = (b - 1) / kPart, cnt = p1 - p + 1, q = (cnt + 3) / 4;
+  float s[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) s[e] = 0.f;
+  if (i < c) {
+    const int64_t k1 = (wave + 1) * q < cnt ? (wave + 1) * q : cnt;
+#pragma unroll 4
+    for (int64_t k = wave * q; k < k1; ++k) {
+      // the first part is the run's own slot of stretch p, the others start their stretch
+      const int64_t slot = 2 * (p + k) + (k == 0 && a > s0 && sorted[s0].x != v ? 1 : 0);
+      const float* r = part + (slot * c + i) * N;
+#pragma unroll
+      for (int e = 0; e < N; e += 4) {
+        const f32x4 x = *(const f32x4*)(r + e);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[e + j] += x[j];
+      }
+    }
+  }
+  __shared__ float red[3][64][N + 1];
+  if (wave)
+#pragma unroll
+    for (int e = 0; e < N; ++e) red[wave - 1][lane][e] = s[e];
+  __syncthreads();
+  if (wave || i >= c) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w)
+#pragma unroll
+    for (int e = 0; e < N; ++e) s[e] += red[w][lane][e];
+  put_row<T, G>(dtable, v, c, i, s, scale);
+}
+
+__global__ void __launch_bounds__(256) fill_zero(u32x4* p, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
+    p[i] = u32x4{0, 0, 0, 0};
+}
+
+// ---------------------------------------------------------------------- host
+
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+struct SortPlan {
+  int bits, passes;  // bits of a digit
+  int64_t tiles;
+  size_t el0, el1, hist0, hist1, start, part, total;
+};
+
+SortPlan sort_plan(int64_t n, int64_t vocab, int64_t d) {
+  SortPlan s;
+  int kb = 1;
+  while (((int64_t)1 << kb) <= vocab) ++kb;  // keys 0 .. vocab
+  s.passes = (kb + kMaxBits - 1) / kMaxBits;
+  s.bits = (kb + s.passes - 1) / s.passes;
+  s.tiles = (n + kTile - 1) / kTile;
+  size_t off = 0;
+  s.el0 = off; off = up256(off + (size_t)n * 8);
+  s.el1 = off; off = up256(off + (size_t)n * 8);
+  s.hist0 = off; off = up256(off + ((size_t)s.tiles << s.bits) * 4);
+  s.hist1 = off; off = up256(off + ((size_t)s.tiles << s.bits) * 4);
+  s.start = off; off = up256(off + (size_t)(vocab + 1) * 4);
+  s.part = off; off = up256(off + (size_t)((n + kPart - 1) / kPart) * 2 * (size_t)d * 4);
+  s.total = off;
+  return s;
+}
+
+bool aligned(const void* p, size_t a) { return p != nullptr && ((uintptr_t)p % a) == 0; }
+bool known(int t) { return t == INFCL_BF16 || t == INFCL_F32 || t == INFCL_F16; }
+int64_t chunks_of(int64_t d, int dtype) { return d * (dtype == INFCL_F32 ? 4 : 2) / 16; }
+bool rows_ok(int64_t d, int dtype) { return d % (dtype == INFCL_F32 ? 4 : 8) == 0; }
+constexpr int64_t kMaxN = ((int64_t)1 << 31) - 2, kMaxD = (int64_t)1 << 20;
+
+template <int T>
+int embed_fwd_t(const void* tokens, int tb, int64_t n, const void* table, int64_t vocab, int64_t d, float scale,
+                void* out, hipStream_t st) {
+  const int64_t c = chunks_of(d, T);
+  const int ls = row_lanes_log2(c, 1);
+  const int64_t groups = (n + kFwdRows - 1) / kFwdRows;
+  int64_t blocks = ((groups << ls) + 255) / 256;
+  if (blocks > 16384) blocks = 16384;
+  if (tb == 4)
+    hipLaunchKernelGGL((embed_fwd_kernel<T, int32_t>), dim3((unsigned)blocks), dim3(256), 0, st, (const int32_t*)tokens,
+                       n, (const u32x4*)table, vocab, (int)c, ls, scale, (u32x4*)out);
+  else
+    hipLaunchKernelGGL((embed_fwd_kernel<T, int64_t>), dim3((unsigned)blocks), dim3(256), 0, st, (const int64_t*)tokens,
+                       n, (const u32x4*)table, vocab, (int)c, ls, scale, (u32x4*)out);
+  return hipGetLastError() == hipSuccess ? INFCL_OK : INFCL_ERR_HIP;
+}
+
+template <typename Tok>
+int sort_tokens(const void* tokens, int64_t n, int64_t vocab, const SortPlan& s, char* ws, const uint2** sorted,
+                hipStream_t st) {
+  const Tok* tok = (const Tok*)tokens;
+  uint2* el[2] = {(uint2*)(ws + s.el0), (uint2*)(ws + s.el1)};
+  uint32_t* hist[2] = {(uint32_t*)(ws + s.hist0), (uint32_t*)(ws + s.hist1)};
+  const dim3 grid((unsigned)s.tiles);
+  hipLaunchKernelGGL((sort_count<Tok>), grid, dim3(256), 0, st, tok, n, (uint32_t)vocab, s.bits, hist[0], hist[1]);
+  if (hipGetLastError() != hipSuccess) return INFCL_ERR_HIP;
+  for (int p = 0; p < s.passes; ++p) {
+    uint32_t* next = p + 1 < s.passes ? hist[(p + 1) & 1] : nullptr;
+    if (p >= 1 && next) {  // (the count clears the first one's)
+      const int64_t q = ((s.tiles << s.bits) * 4 + 15) / 16;
+      hipLaunchKernelGGL(fill_zero, dim3((unsigned)(q / 256 + 1 < 1024 ? q / 256 + 1 : 1024)), dim3(256), 0, st,
+                         (u32x4*)next, q);
+    }
+    if (p == 0)
+      hipLaunchKernelGGL((sort_scatter<Tok, true>), grid, dim3(256), 0, st, tok, (const uint2*)nullptr, n,
+                         (uint32_t)vocab, 0, s.bits, hist[0], next, el[0]);
+    else
+      hipLaunchKernelGGL((sort_scatter<Tok, false>), grid, dim3(256), 0, st, tok, (const uint2*)el[(p + 1) & 1], n,
+                         (uint32_t)vocab, p * s.bits, s.bits, hist[p & 1], next, el[p & 1]);
+    if (hipGetLastError() != hipSuccess) return INFCL_ERR_HIP;
+  }
+  *sorted = el[(s.passes + 1) & 1];
+  return INFCL_OK;
+}
+
+template <int T, int G>
+int embed_bwd_t(const void* tokens, int tb, int64_t n, const void* dout, int64_t vocab, int64_t d, float scale,
+                void* dtable, char* ws, hipStream_t st) {
+  const int64_t c = chunks_of(d, T);
+  if (n == 0) {
+    const int64_t q = (vocab * d * (G == kF32 ? 4 : 2)) / 16;
+    hipLaunchKernelGGL(fill_zero, dim3((unsigned)(q / 256 + 1 < 16384 ? q / 256 + 1 : 16384)), dim3(256), 0, st,
+                       (u32x4*)dtable, q);
+    return hipGetLastError() == hipSuccess ? INFCL_OK : INFCL_ERR_HIP;
+  }
+  const SortPlan s = sort_plan(n, vocab, d);
+  const uint2* sorted;
+  const int rc = tb == 4 ? sort_tokens<int32_t>(tokens, n, vocab, s, ws, &sorted, st)
+                         : sort_tokens<int64_t>(tokens, n, vocab, s, ws, &sorted, st);
+  if (rc != INFCL_OK) return rc;
+  uint32_t* start = (uint32_t*)(ws + s.start);
+  hipLaunchKernelGGL(row_starts, dim3((unsigned)(n / 256 + 1)), dim3(256), 0, st, sorted, n, (uint32_t)vocab, start);
+  const int ls = row_lanes_log2(c, 1);
+  const int64_t per = 256 >> ls, parts = (n + kPart - 1) / kPart;
+  const int64_t rb = (vocab + per - 1) / per, pb = n > kPart ? (parts + per - 1) / per : 0;
+  hipLaunchKernelGGL((embed_sum<T, G>), dim3((unsigned)(rb + pb)), dim3(256), 0, st, sorted, n, (const u32x4*)dout,
+                     start, (uint32_t)vocab, (int)c, ls, scale, dtable, (float*)(ws + s.part), (uint32_t)rb);
+  if (pb)
+    hipLaunchKernelGGL((embed_join<T, G>), dim3((unsigned)parts, (unsigned)((c + 63) / 64)), dim3(256), 0, st, sorted,
+                       n, start, (uint32_t)vocab, (int)c, scale, (const float*)(ws + s.part), dtable);
+  return hipGetLastError() == hipSuccess ? INFCL_OK : INFCL_ERR_HIP;
+}
+
+}  // namespace
+}  // namespace infcl
+
+using namespace infcl;
+
+extern "C" infcl_status infcl_embed_fwd(const void* tokens, int token_bytes, int64_t n, const void* table,
+                                        int64_t vocab, int64_t d, int dtype, float scale, void* out, void* stream) {
+  if (n < 0 || vocab < 1 || d < 1 || !known(dtype) || (token_bytes != 4 && token_bytes != 8)) return INFCL_ERR_INVALID;
+  if (!rows_ok(d, dtype) || d > kMaxD || n > kMaxN || vocab > kMaxN) return INFCL_ERR_UNSUPPORTED;
+  if (n == 0) return INFCL_OK;
+  if (!aligned(tokens, (size_t)token_bytes) || !aligned(table, 16) || !aligned(out, 16)) return INFCL_ERR_INVALID;
+  hipStream_t st = (hipStream_t)stream;
+  int rc;
+  if (dtype == INFCL_BF16)
+    rc = embed_fwd_t<kBF16>(tokens, token_bytes, n, table, vocab, d, scale, out, st);
+  else if (dtype == INFCL_F16)
+    rc = embed_fwd_t<kF16>(tokens, token_bytes, n, table, vocab, d, scale, out, st);
+  else
+    rc = embed_fwd_t<kF32>(tokens, token_bytes, n, table, vocab, d, scale, out, st);
+  return (infcl_status)rc;
+}
+
+extern "C" infcl_status infcl_embed_bwd_workspace(int64_t n, int64_t vocab, int64_t d, size_t* bytes) {
+  if (!bytes || n < 0 || vocab < 1 || d < 1) return INFCL_ERR_INVALID;
+  if (d > kMaxD || n > kMaxN || vocab > kMaxN) return INFCL_ERR_UNSUPPORTED;
+  *bytes = sort_plan(n, vocab, d).total;
+  return INFCL_OK;
+}
+
+extern "C" infcl_status infcl_embed_bwd(const void* tokens, int token_bytes, int64_t n, const void* dout,
+                                        int64_t vocab, int64_t d, int dtype, float scale, void* dtable, int grad_dtype,
+                                        void* workspace, size_t ws_bytes, void* stream) {
+  if (n < 0 || vocab < 1 || d < 1 || !known(dtype) || !known(grad_dtype) || (token_bytes != 4 && token_bytes != 8))
+    return INFCL_ERR_INVALID;
+  if (!rows_ok(d, dtype) || d > kMaxD || n > kMaxN || vocab > kMaxN ||
+      (grad_dtype != INFCL_F32 && grad_dtype != dtype))
+    return INFCL_ERR_UNSUPPORTED;
+  if (!aligned(dtable, 16)) return INFCL_ERR_INVALID;
+  if (n > 0) {
+    if (!aligned(tokens, (size_t)token_bytes) || !aligned(dout, 16) || !aligned(workspace, 256))
+      return INFCL_ERR_INVALID;
+    if (ws_bytes < sort_plan(n, vocab, d).total) return INFCL_ERR_WORKSPACE;
+  }
+  hipStream_t st = (hipStream_t)stream;
+  char* ws = (char*)workspace;
+  int rc;
+  if (dtype == INFCL_F32)
+    rc = embed_bwd_t<kF32, kF32>(tokens, token_bytes, n, dout, vocab, d, scale, dtable, ws, st);
+  else if (dtype == INFCL_BF16 && grad_dtype == INFCL_F32)
+    rc = embed_bwd_t<kBF16, kF32>(tokens, token_bytes, n, dout, vocab, d, scale, dtable, ws, st);
+  else if (dtype == INFCL_BF16)
+    rc = embed_bwd_t<kBF16, kBF16>(tokens, token_bytes, n, dout, vocab, d, scale, dtable, ws, st);
+  else if (grad_dtype == INFCL_F32)
+    rc = embed_bwd_t<kF16, kF32>(tokens, token_bytes, n, dout, vocab, d, scale, dtable, ws, st);
+  else
+    rc = embed_bwd_t<kF16, kF16>(tokens, token_bytes, n, dout, vocab, d, scale, dtable, ws, st);
+  return (infcl_status)rc;
+}

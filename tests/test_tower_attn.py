@@ -1,0 +1,305 @@
+"""Packed attention on the GPU against 64 bits: values and gradients with
+element-wise bounds, masks, lengths, views, and what masked rows may hold.
+
+Bounds.  The kernel's products are exact and accumulated in fp32; the weights p
+and ds are rounded to 16 bits (relative eps = 2^-p) for
+the second products, results once more.  So with the oracle's sums of absolute
+terms:  |out - ref| <= eps (out_abs + |ref|), and the same for dv; for dq and dk
+eps (dq_abs + |ref|) plus, as D_i comes from out rounded to 16 bits,
+eps dq_dlt.  To these an fp32 part: scores of at most hd = 128 products of unit
+entries are off by less than 2^-17 (128 2^-24), which is their weights' relative
+error; 2^-15 of the sums covers it, the exponentials and the accumulations."""
+
+import math
+
+import pytest
+import torch
+
+import paper_2410_17243_amd as infcl
+from oracle import tower
+
+DT = {"bf16": torch.bfloat16, "f16": torch.float16}
+EPS = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}  # one rounding to nearest
+F32 = 2.0 ** -15
+TINY = {"bf16": 1e-30, "f16": 2.0 ** -25}  # below the type's normal numbers
+
+
+def _cu(lens):
+    return [0] + torch.tensor(lens).cumsum(0).tolist()
+
+
+def _inputs(tq, tk, heads, kv, hd, dtype, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    mk = lambda t, h: torch.randn((t, h, hd), generator=g).to(DT[dtype])  # noqa: E731
+    return mk(tq, heads), mk(tk, kv), mk(tk, kv), mk(tq, heads)
+
+
+def _dev(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda") if isinstance(x, list) else x.cuda()
+
+
+def _near(got, ref, tol, what):
+    got = got.detach().cpu().double()
+    assert torch.isfinite(got).all(), what
+    over = (got - ref).abs() - tol
+    assert (over <= 0).all(), (what, float(over.max()), float((got - ref).abs().max()))
+
+
+def _check_fwd(out, lse, r, dtype):
+    e = EPS[dtype]
+    _near(out, r["out"], (e + F32) * r["out_abs"] + e * r["out"].abs() + TINY[dtype], "out")
+    lse = lse.cpu().double()
+    assert torch.equal(torch.isinf(lse), torch.isinf(r["lse"]))
+    ok = torch.isfinite(r["lse"])
+    # scores off by 2^-17 at most, and the fp32 of the value itself
+    assert ((lse - r["lse"])[ok].abs() <= 2.0 ** -16 + 2.0 ** -22 * r["lse"][ok].abs()).all()
+
+
+def _check_bwd(grads, r, dtype):
+    e = EPS[dtype]
+    for name, got in zip(("dq", "dk", "dv"), grads):
+        tol = (e + F32) * r[name + "_abs"] + e * r[name].abs() + TINY[dtype]
+        if name != "dv":
+            tol = tol + (e + F32) * r[name + "_dlt"]
+        _near(got, r[name], tol, name)
+
+
+def _run(lens_q, lens_k, heads, kv, hd, dtype, causal, scale=None, seed=0, extra=0):
+    cu_q, cu_k = _cu(lens_q), _cu(lens_k)
+    q, k, v, do = _inputs(cu_q[-1] + extra, cu_k[-1] + extra, heads, kv, hd, dtype, seed)
+    scale = hd ** -0.5 if scale is None else scale
+    r = tower.attention(q, k, v, cu_q, cu_k, causal, scale, do)
+    a = [_dev(t) for t in (q, k, v)]
+    off = (_dev(cu_q), max(lens_q), _dev(cu_k), max(lens_k))
+    out, lse = infcl.packed_attn_fwd(*a, *off, causal=causal, scale=scale)
+    _check_fwd(out, lse, r, dtype)
+    grads = infcl.packed_attn_bwd(*a, out, lse, _dev(do), *off, causal=causal, scale=scale)
+    _check_bwd(grads, r, dtype)
+    return out, lse, grads, r
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,heads,kv,hd,dtype", [
+    ([1], 1, 1, 8, "bf16"), ([1, 2, 3], 2, 1, 64, "f16"), ([31, 32, 33], 2, 2, 64, "bf16"),
+    ([5, 0, 77, 1, 16], 8, 8, 64, "bf16"), ([64, 65, 63], 4, 2, 128, "f16"), ([127, 129], 3, 1, 72, "bf16"),
+    ([200, 0, 0, 90], 6, 2, 80, "f16"), ([257], 4, 1, 32, "bf16"), ([128, 300], 2, 1, 128, "bf16"), ([20] * 40, 3, 3, 96, "bf16"),
+])
+@pytest.mark.parametrize("causal", [True, False])
+def test_self_attention(lens, heads, kv, hd, dtype, causal):
+    _run(lens, lens, heads, kv, hd, dtype, causal)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens_q,lens_k,heads,kv,hd", [
+    ([1, 1, 1], [40, 1, 0], 8, 2, 64),            # one query token: prefix, none, no keys at all
+    ([3, 70, 9], [300, 70, 40], 4, 4, 64),        # a cached prefix
+    ([50, 140], [20, 130], 2, 1, 128),            # more queries than keys: the first see none
+    ([33], [1000], 6, 1, 40), ([0, 2], [5, 0], 2, 2, 64),
+])
+@pytest.mark.parametrize("causal", [True, False])
+def test_queries_and_keys_of_other_lengths(lens_q, lens_k, heads, kv, hd, causal):
+    _run(lens_q, lens_k, heads, kv, hd, "bf16", causal)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,most,heads,kv,hd,dtype", [(1, 777, 8, 8, 64, "bf16"), (3, 2000, 8, 1, 128, "f16"),
+                                                     (2, 5000, 6, 3, 72, "bf16"), (2, 4097, 40, 1, 64, "bf16")])
+def test_one_token_over_many_keys(n, most, heads, kv, hd, dtype):
+    """Keys are cut into parts here; the longest sequence is not all of them."""
+    lens = [max(0, most - 700 * i) for i in range(n)]
+    q, k, v, _ = _inputs(n, sum(lens), heads, kv, hd, dtype, 5)
+    r = tower.attention(q, k, v, list(range(n + 1)), _cu(lens), True, hd ** -0.5)
+    out, lse = infcl.packed_attn_fwd(*[_dev(t) for t in (q, k, v)], _dev(list(range(n + 1))), 1, _dev(_cu(lens)), most)
+    _check_fwd(out, lse, r, dtype)
+    alone, none = infcl.packed_attn_fwd(*[_dev(t) for t in (q, k, v)], _dev(list(range(n + 1))), 1, _dev(_cu(lens)), most,
+                                        need_lse=False)
+    assert none is None and torch.equal(alone, out)
+
+
+@pytest.mark.gpu
+def test_long_sequence():
+    _run([1300, 700], [1300, 700], 2, 1, 64, "bf16", True, seed=3)
+
+
+@pytest.mark.gpu
+def test_large_scores_keep_their_weights():
+    """Scores up to about 100: the running maximum moves by many powers of two.
+    A score of 100 is off by 100 2^-21 at most (fp32 sums of 64 products)."""
+    lens = [150]
+    q, k, v, _ = _inputs(150, 150, 2, 2, 64, "bf16", 9)
+    r = tower.attention(q, k, v, _cu(lens), _cu(lens), True, 3.0)
+    out, _ = infcl.packed_attn_fwd(_dev(q), _dev(k), _dev(v), _dev(_cu(lens)), 150, scale=3.0)
+    tol = (EPS["bf16"] + 2.0 ** -12) * r["out_abs"] + EPS["bf16"] * r["out"].abs()
+    _near(out, r["out"], tol, "out")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hd", [64, 128])
+def test_gradient_against_differences(hd):
+    """The kernel's gradients against central differences of the 64-bit forward
+    along a random direction; the bound is the sum of the element-wise ones."""
+    cu = _cu([40, 9])
+    q, k, v, do = _inputs(49, 49, 4, 2, hd, "f16", 2)
+    a = [_dev(t) for t in (q, k, v)]
+    out, lse = infcl.packed_attn_fwd(*a, _dev(cu), 40)
+    grads = infcl.packed_attn_bwd(*a, out, lse, _dev(do), _dev(cu), 40)
+    r = tower.attention(q, k, v, cu, cu, True, hd ** -0.5, do)
+    for i, name in enumerate(("dq", "dk", "dv")):
+        step = torch.randn([q, k, v][i].shape, generator=torch.Generator().manual_seed(7), dtype=torch.float64)
+        f = []
+        for h in (1e-4, -1e-4):
+            x = [t.double() for t in (q, k, v)]
+            x[i] = x[i] + h * step
+            f.append(float((tower.attention(*x, cu, cu, True, hd ** -0.5)["out"] * do.double()).sum()))
+        e = EPS["f16"]
+        tol = (e + F32) * (r[name + "_abs"] + r.get(name + "_dlt", 0)) + e * r[name].abs() + TINY["f16"]
+        assert abs((f[0] - f[1]) / 2e-4 - float((grads[i].cpu().double() * step).sum())) <= float((tol * step.abs()).sum())
+
+
+@pytest.mark.gpu
+def test_views_of_one_projection_and_autograd():
+    lens, heads, kv, hd = [60, 7, 133], 4, 2, 64
+    cu = _cu(lens)
+    g = torch.Generator().manual_seed(1)
+    qkv = torch.randn((200, heads + 2 * kv, hd), generator=g).bfloat16()
+    do = torch.randn((200, heads, hd), generator=g).bfloat16()
+    q, k, v = qkv[:, :heads], qkv[:, heads:heads + kv], qkv[:, heads + kv:]
+    r = tower.attention(q, k, v, cu, cu, True, hd ** -0.5, do)
+    x = qkv.cuda().requires_grad_()
+    out = infcl.packed_attn_qkv(x, heads, kv, _dev(cu), 133)
+    out.backward(do.cuda())
+    d = x.grad
+    _check_bwd((d[:, :heads], d[:, heads:heads + kv], d[:, heads + kv:]), r, "bf16")
+    a = [t.contiguous().cuda().requires_grad_() for t in (q, k, v)]
+    same = infcl.packed_attn(*a, _dev(cu), 133)
+    same.backward(do.cuda())
+    assert torch.equal(same, out) and torch.equal(a[0].grad, d[:, :heads]) and torch.equal(a[2].grad, d[:, heads + kv:])
+    swapped = [t.transpose(0, 1).contiguous().cuda().transpose(0, 1) for t in (q, k, v)]  # [heads][tokens] in memory
+    assert torch.equal(infcl.packed_attn_fwd(*swapped, _dev(cu), 133)[0], out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,hd", [([20, 45], 64), ([150, 300], 64), ([40], 128), ([200], 128)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_masked_rows_may_hold_anything(lens, hd, bad):
+    """Keys and values no query of the first half sees yet, and whole other
+    sequences, hold NaN or infinity: earlier rows are bit for bit as without."""
+    cu, heads, kv = _cu(lens), 2, 1
+    t = cu[-1]
+    q, k, v, do = _inputs(t, t, heads, kv, hd, "bf16", 4)
+    late = cu[-2] + (lens[-1] // 2)  # from here on the last sequence's rows are bad
+    k2, v2, q2, do2 = k.clone(), v.clone(), q.clone(), do.clone()
+    k2[late:], v2[late:], q2[late:] = bad, bad, bad
+    clean = infcl.packed_attn_fwd(_dev(q), _dev(k), _dev(v), _dev(cu), max(lens))
+    out, lse = infcl.packed_attn_fwd(_dev(q2), _dev(k2), _dev(v2), _dev(cu), max(lens))
+    e = EPS["bf16"]
+    r = tower.attention(q, k, v, cu, cu, True, hd ** -0.5, do)
+    for x, y in ((out[:late], clean[0][:late]), (lse[:, :late], clean[1][:, :late])):
+        # (rows of tiles taken again row by row keep fp32 weights: as near as any)
+        assert torch.isfinite(x).all() and float((x - y).abs().max()) <= 2.0 ** -6
+    _near(out[:late], r["out"][:late], ((e + F32) * r["out_abs"] + e * r["out"].abs())[:late], "out")
+    assert not torch.isfinite(out[late:]).all()
+    # backward, with good keys and values: queries and dout before a key's own do not reach it
+    q3, do3 = q.clone(), do.clone()
+    early = cu[-2] + lens[-1] // 2
+    q3[cu[-2]:early], do3[cu[-2]:early] = bad, bad
+    out, lse = infcl.packed_attn_fwd(_dev(q), _dev(k), _dev(v), _dev(cu), max(lens))
+    dq, dk, dv = infcl.packed_attn_bwd(_dev(q3), _dev(k), _dev(v), out, lse, _dev(do3), _dev(cu), max(lens))
+    for got, name in ((dk, "dk"), (dv, "dv"), (dq, "dq")):
+        tol = (e + F32) * (r[name + "_abs"] + r.get(name + "_dlt", 0)) + e * r[name].abs()
+        _near(got[early:], r[name][early:], tol[early:], name)
+    # ... and keys and values after a query do not reach its gradient
+    dq, _, _ = infcl.packed_attn_bwd(_dev(q), _dev(k2), _dev(v2), clean[0], clean[1], _dev(do), _dev(cu), max(lens))
+    tol = (e + F32) * (r["dq_abs"] + r["dq_dlt"]) + e * r["dq"].abs()
+    _near(dq[:late], r["dq"][:late], tol[:late], "dq")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+def test_rows_past_the_last_sequence(causal):
+    """Rows of the arrays that no sequence has: NaN there reaches no one, and
+    their own results are zeros."""
+    lens, t = [30, 70], 140
+    cu = _cu(lens)
+    q, k, v, do = _inputs(t, t, 2, 2, 64, "bf16", 6)
+    r = tower.attention(q[:100], k[:100], v[:100], cu, cu, causal, 0.125, do[:100])
+    for x in (q, k, v, do):
+        x[100:] = math.nan
+    out, lse = infcl.packed_attn_fwd(_dev(q), _dev(k), _dev(v), _dev(cu), 70, causal=causal)
+    _check_fwd(out[:100], lse[:, :100], r, "bf16")
+    assert (out[100:] == 0).all() and (lse[:, 100:] == -math.inf).all()
+    grads = infcl.packed_attn_bwd(_dev(q), _dev(k), _dev(v), out, lse, _dev(do), _dev(cu), 70, causal=causal)
+    _check_bwd([x[:100] for x in grads], r, "bf16")
+    assert all((x[100:] == 0).all() for x in grads)
+
+
+@pytest.mark.gpu
+def test_longer_than_said():
+    """max_q and max_k below the true lengths cost time, not rows."""
+    lens = [150, 300]
+    cu = _cu(lens)
+    q, k, v, do = _inputs(450, 450, 2, 1, 64, "bf16", 8)
+    r = tower.attention(q, k, v, cu, cu, True, 0.125, do)
+    a = [_dev(t) for t in (q, k, v)]
+    out, lse = infcl.packed_attn_fwd(*a, _dev(cu), 40)
+    _check_fwd(out, lse, r, "bf16")
+    _check_bwd(infcl.packed_attn_bwd(*a, out, lse, _dev(do), _dev(cu), 40), r, "bf16")
+
+
+@pytest.mark.gpu
+def test_captured_step_replays_on_another_stream():
+    cu = _dev(_cu([100, 3, 40]))
+    q, k, v, do = [_dev(t) for t in _inputs(143, 143, 4, 2, 64, "bf16", 3)]
+
+    def step():
+        out, lse = infcl.packed_attn_fwd(q, k, v, cu, 100)
+        return (out, lse, *infcl.packed_attn_bwd(q, k, v, out, lse, do, cu, 100))
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        ref = step()
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = step()
+    for _ in range(3):
+        for x in got:
+            x.fill_(float("nan"))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for x, y, w in zip(got, ref, step()):
+            assert torch.equal(x, y) and torch.equal(w, y)
+
+
+@pytest.mark.gpu
+def test_refusals():
+    cu = _dev([0, 4])
+    q, k, v, do = [_dev(t) for t in _inputs(4, 4, 4, 2, 64, "bf16")]
+    ok = infcl.packed_attn_fwd(q, k, v, cu, 4)
+    with pytest.raises(TypeError):
+        infcl.packed_attn_fwd(q.float(), k.float(), v.float(), cu, 4)
+    with pytest.raises(ValueError):
+        infcl.packed_attn_fwd(q, k.half(), v, cu, 4)
+    with pytest.raises(ValueError):
+        infcl.packed_attn_fwd(q[:, :3], k, v, cu, 4)  # three heads for two
+    with pytest.raises(ValueError):
+        infcl.packed_attn_fwd(q, k[:3], v[:3], cu, 4)
+    with pytest.raises(ValueError):
+        infcl.packed_attn_fwd(q, k, v, cu.long(), 4)
+    with pytest.raises(ValueError):
+        infcl.packed_attn_fwd(q, k, v, cu, 4, cu)  # no max_k
+    with pytest.raises(ValueError):
+        infcl.packed_attn_fwd(q.transpose(1, 2), k, v, cu, 4)
+    with pytest.raises(ValueError):
+        infcl.packed_attn_fwd(q.cpu(), k, v, cu, 4)
+    with pytest.raises(infcl.InfclError):
+        infcl.packed_attn_fwd(q, k, v, cu, 4, scale=-1.0)
+    with pytest.raises(infcl.InfclError):
+        wide = torch.zeros((4, 2, 136), dtype=torch.bfloat16, device="cuda")
+        infcl.packed_attn_fwd(wide, wide, wide, cu, 4)
+    with pytest.raises(ValueError):
+        infcl.packed_attn_bwd(q, k, v, ok[0], ok[1][:, :3], do, cu, 4)
+    with pytest.raises(ValueError):
+        infcl.packed_attn_bwd(q, k, v, ok[0], ok[1], do[:3], cu, 4)

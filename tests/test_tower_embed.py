@@ -1,0 +1,107 @@
+"""Token embedding and its gradient on the GPU against 64 bits."""
+
+import math
+
+import pytest
+import torch
+
+import paper_2410_17243_amd as infcl
+from oracle import tower
+
+DT = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+EPS = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11, "f32": 2.0 ** -24}  # one rounding to nearest
+STEP = {"bf16": 0.0, "f16": 2.0 ** -25, "f32": 0.0}  # half the step of subnormal fp16 (the others' do not occur here)
+
+
+def _tokens(n, vocab, seed, ids):
+    g = torch.Generator().manual_seed(seed)
+    t = (torch.rand(n, generator=g, dtype=torch.float64) ** 4 * vocab).long()
+    if n > 3:
+        t[1::7] = vocab - 1                      # one token that a seventh of the rows have
+        t[n // 2], t[n // 3] = -1, vocab + 5     # two that stand for nothing
+    return t.to(ids)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,vocab,d,dtype,ids", [
+    (1, 1, 8, "bf16", torch.int64), (7, 3, 8, "f16", torch.int32), (130, 5, 512, "bf16", torch.int64),
+    (1000, 997, 72, "f32", torch.int32), (4097, 100, 520, "bf16", torch.int32), (4097, 70000, 128, "f16", torch.int64),
+    (20000, 2, 40, "f32", torch.int64), (9000, 1 << 20, 16, "bf16", torch.int64), (300, 1 << 21, 8, "f16", torch.int32),
+])
+def test_forward_and_gradient(n, vocab, d, dtype, ids):
+    tok = _tokens(n, vocab, n, ids)
+    g = torch.Generator().manual_seed(d)
+    table, dout = torch.randn((vocab, d), generator=g).to(DT[dtype]), torch.randn((n, d), generator=g).to(DT[dtype])
+    scale = math.sqrt(d)
+    s32 = float(torch.tensor(scale, dtype=torch.float32))
+    out = infcl.embed_fwd(tok.cuda(), table.cuda(), scale).cpu()
+    ref = tower.embedding(tok, table, s32)
+    assert out.dtype == DT[dtype] and ((out.double() - ref).abs() <= EPS[dtype] * ref.abs()).all()
+    ref, size, count = tower.embedding_grad(tok, dout, vocab, s32)
+    dw = infcl.embed_bwd(tok.cuda(), dout.cuda(), vocab, scale).cpu()
+    # fp32 sums of c terms: at most c roundings of partial sums that |terms| bound, and the scale's
+    tol = (count[:, None] + 2) * 2.0 ** -24 * size
+    assert dw.dtype == torch.float32 and ((dw.double() - ref).abs() <= tol).all()
+    if dtype != "f32":
+        dw = infcl.embed_bwd(tok.cuda(), dout.cuda(), vocab, scale, grad_dtype=DT[dtype]).cpu()
+        assert dw.dtype == DT[dtype]
+        assert ((dw.double() - ref).abs() <= tol * 2 + EPS[dtype] * ref.abs() + STEP[dtype]).all()
+    if not (ids == torch.int32 and n == 1000):
+        return
+    w = table.cuda().requires_grad_()
+    infcl.embed(tok.cuda().view(8, 125), w, scale).backward(dout.cuda().view(8, 125, d))
+    assert w.grad.dtype == DT[dtype] and ((w.grad.cpu().double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.gpu
+def test_repeats_bit_for_bit_and_on_another_stream():
+    tok, dout = _tokens(5000, 50, 3, torch.int64).cuda(), torch.randn((5000, 64), device="cuda")
+    a = infcl.embed_bwd(tok, dout, 50, 0.5)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        b = infcl.embed_bwd(tok, dout, 50, 0.5)
+    s.synchronize()
+    assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+def test_no_tokens():
+    t, w = torch.empty(0, dtype=torch.int64, device="cuda"), torch.randn((6, 8), device="cuda")
+    assert infcl.embed_fwd(t, w).shape == (0, 8)
+    assert (infcl.embed_bwd(t, w[:0], 6) == 0).all()
+
+
+@pytest.mark.gpu
+def test_captured_gradient_replays():
+    tok, dout = _tokens(9000, 3000, 3, torch.int64).cuda(), torch.randn((9000, 64), device="cuda")
+    ref = infcl.embed_bwd(tok, dout, 3000)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = infcl.embed_bwd(tok, dout, 3000)
+    for _ in range(3):
+        got.fill_(float("nan"))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, ref)
+        assert torch.equal(infcl.embed_bwd(tok, dout, 3000), ref)
+
+
+@pytest.mark.gpu
+def test_refusals():
+    t, w = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros((6, 8), device="cuda")
+    with pytest.raises(TypeError):
+        infcl.embed_fwd(t.float(), w)
+    with pytest.raises(TypeError):
+        infcl.embed_fwd(t, w.double())
+    with pytest.raises(ValueError):
+        infcl.embed_fwd(t.cpu(), w)
+    with pytest.raises(ValueError):
+        infcl.embed_fwd(t, w.t())
+    with pytest.raises(ValueError):
+        infcl.embed_bwd(t, w, 6)  # six rows for four tokens
+    with pytest.raises(TypeError):
+        infcl.embed_bwd(t, w[:4], 6, grad_dtype=torch.float16)
+    with pytest.raises(infcl.InfclError):
+        infcl.embed_fwd(t, torch.zeros((6, 6), device="cuda"))  # rows of 24 bytes
