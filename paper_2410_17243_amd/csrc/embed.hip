@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(const Tok* __restrict__ 
           for (int e = 0; e < Chunk<T>::N; ++e) x[e] *= scale;
           r[k] = Chunk<T>::store(x);
         }
-        if (t0 + k < n) out[(t0 + k) * c + i] = r[k];
+        if (t0 + k < n) __builtin_nontemporal_store(r[k], &out[(t0 + k) * c + i]);
       }
     }
   }
@@ -60,86 +60,120 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(const Tok* __restrict__ 
 
 // ---------------------------------------------------------------------- sort
 
-// Least significant digit first, `bits` bits a pass (at most kMaxBits).  A
-// block of 4 waves owns kTile consecutive elements, a wave a quarter of them,
-// 64 at a time in order.
-constexpr int kTile = 4096, kMaxBits = 10;
-
 template <typename Tok>
 __device__ __forceinline__ uint32_t token_key(Tok t, uint32_t vocab) {
   return t >= 0 && (uint64_t)t < vocab ? (uint32_t)t : vocab;  // (invalid ones last)
 }
 
-// Counts of a tile's digits.  first: keys are made from the tokens.  Also
-// clears the next pass's counts.
+// Where the rows of one token begin and end in sorted order: by table row
+// (start, of many tokens) or by sorted position (few tokens).
+struct Runs {
+  const uint2* sorted;    // (token, position), n of them
+  const uint32_t* start;  // by row: first sorted position whose token is >= v, v = 0 .. vocab
+  const uint2* run;       // by position: [begin, end) of its run; null: by row
+};
+
+__device__ __forceinline__ void run_of(const Runs& r, int64_t at, uint32_t v, uint32_t& a, uint32_t& b) {
+  if (r.run) {
+    const uint2 x = r.run[at];
+    a = x.x, b = x.y;
+  } else {
+    a = r.start[v], b = r.start[v + 1];
+  }
+}
+
+__device__ __forceinline__ void zero_rows(u32x4* p, int64_t n, int64_t i, int64_t step) {
+  for (; i < n; i += step) p[i] = u32x4{0, 0, 0, 0};
+}
+
+// Few tokens (up to kFew): a token's place is the number of smaller ones, plus
+// that of its equals before it, and the former and the number of its equals are
+// its run.  n^2 comparisons, which the whole chip shares: 16 tokens to a
+// workgroup, each counted by 16 groups of lanes (n = 4096: 1 M comparisons per
+// SIMD, 5 us; a bitonic network in one workgroup took 24 us at n = 2001, a radix
+// sort 32 us in two launches).  The other workgroups clear the table meanwhile,
+// whose absent rows no one else writes.
+constexpr int kFew = 4096, kRankTokens = 16;
+
 template <typename Tok>
-__global__ void __launch_bounds__(256) sort_count(const Tok* __restrict__ tok, int64_t n, uint32_t vocab, int bits,
-                                                  uint32_t* __restrict__ hist, uint32_t* __restrict__ next) {
+__global__ void __launch_bounds__(256) sort_few(const Tok* __restrict__ tok, int n, uint32_t vocab, unsigned rank_blocks,
+                                                uint2* __restrict__ sorted, uint2* __restrict__ run,
+                                                u32x4* __restrict__ table, int64_t chunks) {
+  if (blockIdx.x >= rank_blocks) {
+    zero_rows(table, chunks, ((int64_t)blockIdx.x - rank_blocks) * 256 + threadIdx.x,
+              ((int64_t)gridDim.x - rank_blocks) * 256);
+    return;
+  }
+  __shared__ __attribute__((aligned(16))) uint32_t key[kFew];
+  __shared__ uint32_t red[4][kRankTokens][3];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n4 = (n + 3) & ~3;
+#pragma unroll 4
+  for (int i = tid; i < n4; i += 256) key[i] = i < n ? token_key(tok[i], vocab) : 0xFFFFFFFFu;  // (no token's key)
+  __syncthreads();
+  const int i0 = (int)blockIdx.x * kRankTokens, i = i0 + (lane & 15), sub = wave * 4 + (lane >> 4);
+  const uint32_t mine = i < n ? key[i] : 0xFFFFFFFEu;
+  uint32_t less = 0, same = 0, ahead = 0;
+#pragma unroll 4
+  for (int j = 4 * sub; j < n4; j += 64) {
+    const u32x4 k = *(const u32x4*)&key[j];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      less += k[e] < mine;
+      same += k[e] == mine;
+      ahead += k[e] == mine && j + e < i;
+    }
+  }
+#pragma unroll
+  for (int s = 16; s <= 32; s <<= 1) {
+    less += __shfl_xor(less, s);
+    same += __shfl_xor(same, s);
+    ahead += __shfl_xor(ahead, s);
+  }
+  if (lane < 16) red[wave][lane][0] = less, red[wave][lane][1] = same, red[wave][lane][2] = ahead;
+  __syncthreads();
+  if (tid >= kRankTokens || i0 + tid >= n) return;
+  uint32_t t[3] = {0, 0, 0};
+  for (int w = 0; w < 4; ++w)
+    for (int e = 0; e < 3; ++e) t[e] += red[w][tid][e];
+  sorted[t[0] + t[2]] = make_uint2(mine, (uint32_t)i);
+  run[t[0] + t[2]] = make_uint2(t[0], t[0] + t[1]);
+}
+
+// More tokens: a radix sort, least significant digit first, `bits` bits a pass
+// (at most kMaxBits).  A block of 4 waves owns kTile consecutive elements, a
+// wave a quarter of them, 64 at a time in order.
+constexpr int kTile = 4096, kMaxBits = 10;
+
+// Counts of a tile's digits.
+template <typename Tok, bool FIRST>
+__global__ void __launch_bounds__(256) sort_count(const Tok* __restrict__ tok, const uint2* __restrict__ in, int64_t n,
+                                                  uint32_t vocab, int shift, int bits, uint32_t* __restrict__ hist) {
   __shared__ uint32_t cnt[1 << kMaxBits];
   const int bins = 1 << bits;
-  for (int i = threadIdx.x; i < bins; i += 256) {
-    cnt[i] = 0;
-    next[(int64_t)blockIdx.x * bins + i] = 0;
-  }
+  for (int i = threadIdx.x; i < bins; i += 256) cnt[i] = 0;
   __syncthreads();
   const int64_t t0 = (int64_t)blockIdx.x * kTile;
-#pragma unroll 4
+#pragma unroll 8
   for (int i = threadIdx.x; i < kTile; i += 256)
-    if (t0 + i < n) atomicAdd(&cnt[token_key(tok[t0 + i], vocab) & (bins - 1)], 1u);
+    if (t0 + i < n) {
+      const uint32_t k = FIRST ? token_key(tok[t0 + i], vocab) : in[t0 + i].x;
+      atomicAdd(&cnt[(k >> shift) & (bins - 1)], 1u);
+    }
   __syncthreads();
   for (int i = threadIdx.x; i < bins; i += 256) hist[(int64_t)blockIdx.x * bins + i] = cnt[i];
 }
 
 // One pass: every element to its place.  The place is the number of elements
 // with smaller digits (all tiles), plus those of its digit in earlier tiles,
-// plus those earlier in this tile.  hist holds every tile's counts; with next,
-// the places' counts of the following digit are added up there (integer
-// atomics: the counts do not depend on their order).
+// plus those earlier in this tile.
 template <typename Tok, bool FIRST>
 __global__ void __launch_bounds__(256) sort_scatter(const Tok* __restrict__ tok, const uint2* __restrict__ in,
                                                     int64_t n, uint32_t vocab, int shift, int bits,
-                                                    const uint32_t* __restrict__ hist, uint32_t* __restrict__ next,
-                                                    uint2* __restrict__ out) {
+                                                    const uint32_t* __restrict__ hist, uint2* __restrict__ out) {
   __shared__ uint32_t base[1 << kMaxBits], wcnt[4][1 << kMaxBits], wsum[4];
   const int bins = 1 << bits, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int tiles = gridDim.x;
-  // a thread's share of the bins: 1 to 4 consecutive ones
-  const int per = bins > 256 ? bins >> 8 : 1;
-  uint32_t before[4] = {0, 0, 0, 0}, all[4] = {0, 0, 0, 0}, mine = 0;
-  if ((int)threadIdx.x * per < bins) {
-    for (int t = 0; t < tiles; ++t) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k < per) {
-          const uint32_t h = hist[(int64_t)t * bins + threadIdx.x * per + k];
-          all[k] += h;
-          before[k] += t < (int)blockIdx.x ? h : 0;
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) mine += all[k];
-  }
-  // exclusive scan over the threads
-  uint32_t inc = mine;
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const uint32_t o = __shfl_up(inc, s);
-    if (lane >= s) inc += o;
-  }
-  if (lane == 63) wsum[wave] = inc;
-  for (int i = threadIdx.x; i < 4 * bins; i += 256) wcnt[i >> bits][i & (bins - 1)] = 0;
-  __syncthreads();
-  uint32_t off = inc - mine;
-  for (int w = 0; w < wave; ++w) off += wsum[w];
-  if ((int)threadIdx.x * per < bins) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (k < per) {
-        base[threadIdx.x * per + k] = off + before[k];
-        off += all[k];
-      }
-  }
-  // this wave's quarter: counts, then places
   constexpr int kWave = kTile / 4;
   const int64_t w0 = (int64_t)blockIdx.x * kTile + wave * kWave;
   uint2 el[kWave / 64];
@@ -149,6 +183,47 @@ __global__ void __launch_bounds__(256) sort_scatter(const Tok* __restrict__ tok,
     el[i] = make_uint2(0, 0);
     if (t < n) el[i] = FIRST ? make_uint2(token_key(tok[t], vocab), (uint32_t)t) : in[t];
   }
+  for (int i = threadIdx.x; i < 4 * bins; i += 256) wcnt[i >> bits][i & (bins - 1)] = 0;
+  // a thread's share of the bins: 1 to 4 consecutive ones
+  const int per = bins > 256 ? bins >> 8 : 1;
+  uint32_t all[4] = {0, 0, 0, 0}, mine = 0;
+  if ((int)threadIdx.x * per < bins) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k >= per) break;
+      const uint32_t* h = hist + threadIdx.x * per + k;
+      uint32_t before = 0, sum = 0;
+#pragma unroll 16
+      for (int t = 0; t < tiles; ++t) {
+        const uint32_t x = h[(int64_t)t << bits];
+        sum += x;
+        before += t < (int)blockIdx.x ? x : 0;
+      }
+      all[k] = sum;
+      base[threadIdx.x * per + k] = before;
+      mine += sum;
+    }
+  }
+  // exclusive scan over the threads
+  uint32_t inc = mine;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const uint32_t o = __shfl_up(inc, s);
+    if (lane >= s) inc += o;
+  }
+  if (lane == 63) wsum[wave] = inc;
+  __syncthreads();
+  uint32_t off = inc - mine;
+  for (int w = 0; w < wave; ++w) off += wsum[w];
+  if ((int)threadIdx.x * per < bins) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < per) {
+        base[threadIdx.x * per + k] += off;
+        off += all[k];
+      }
+  }
+  // counts of this wave's quarter, then places
 #pragma unroll
   for (int i = 0; i < kWave / 64; ++i)
     if (w0 + 64 * i + lane < n) atomicAdd(&wcnt[wave][(el[i].x >> shift) & (bins - 1)], 1u);
@@ -179,10 +254,7 @@ __global__ void __launch_bounds__(256) sort_scatter(const Tok* __restrict__ tok,
     __builtin_amdgcn_wave_barrier();
     if (live && ahead == 0) wcnt[wave][dg] += count;
     __builtin_amdgcn_wave_barrier();
-    if (live) {
-      out[place] = el[i];
-      if (next) atomicAdd(&next[(int64_t)(place / kTile) * bins + ((el[i].x >> (shift + bits)) & (bins - 1))], 1u);
-    }
+    if (live) out[place] = el[i];
   }
 }
 
@@ -197,28 +269,36 @@ __global__ void __launch_bounds__(256) row_starts(const uint2* __restrict__ sort
 
 // ------------------------------------------------------------- sums by token
 
-constexpr int kPart = 128;  // sorted positions that one group of lanes sums at most
+constexpr int kPart = 32;  // sorted positions that one group of lanes sums at most
 
-// Sum of the rows at sorted positions [a, b), chunk i of c, in order.
+// Sum of the rows at sorted positions [a, b), chunk i of c, in order.  The 1 << ls
+// lanes of the group read their positions together.
 template <int T>
 __device__ __forceinline__ void sum_rows(const uint2* __restrict__ sorted, const u32x4* __restrict__ dout, int c, int i,
-                                         uint32_t a, uint32_t b, float (&s)[Chunk<T>::N]) {
+                                         int gl, int ls, uint32_t a, uint32_t b, float (&s)[Chunk<T>::N]) {
   constexpr int N = Chunk<T>::N, U = 8;
 #pragma unroll
   for (int e = 0; e < N; ++e) s[e] = 0.f;
-  for (; a < b; a += U) {
-    u32x4 r[U];
+  for (; a < b; a += 1u << ls) {
+    const uint32_t mine = a + gl < b ? sorted[a + gl].y : 0;
+    const int m = (int)(b - a < (1u << ls) ? b - a : 1u << ls);
+    for (int k0 = 0; k0 < m; k0 += U) {
+      u32x4 r[U];
 #pragma unroll
-    for (int k = 0; k < U; ++k)
-      if (a + k < b) r[k] = dout[(int64_t)sorted[a + k].y * c + i];
-#pragma unroll
-    for (int k = 0; k < U; ++k)
-      if (a + k < b) {
-        float x[N];
-        Chunk<T>::load(r[k], x);
-#pragma unroll
-        for (int e = 0; e < N; ++e) s[e] += x[e];
+      for (int k = 0; k < U; ++k) {
+        const uint32_t row = __shfl(mine, (k0 + k) & ((1 << ls) - 1), 1 << ls);
+        r[k] = u32x4{0, 0, 0, 0};
+        if (k0 + k < m && i < c) r[k] = dout[(int64_t)row * c + i];
       }
+#pragma unroll
+      for (int k = 0; k < U; ++k)
+        if (k0 + k < m) {
+          float x[N];
+          Chunk<T>::load(r[k], x);
+#pragma unroll
+          for (int e = 0; e < N; ++e) s[e] += x[e];
+        }
+    }
   }
 }
 
@@ -238,105 +318,138 @@ __device__ __forceinline__ void put_row(void* dtable, int64_t v, int c, int i, c
   }
 }
 
-// Blocks [0, row_blocks): table rows of at most kPart tokens, a group of lanes
-// each.  The others: sorted positions [128 p, 128 p + 128) of tokens with more
-// than kPart rows.  Such a stretch holds parts of at most two of them (one
-// inside it would be too short): sums in slots 2p (the run that holds its first
-// position) and 2p + 1 (the one of its last, if another).
+// Blocks [0, row_blocks): table rows (or sorted positions that begin a run) of at most kPart tokens, a group
+// of lanes each.  The others: stretches [kPart p, kPart (p + 1)) of the sorted
+// positions, for tokens with more than kPart rows.  Such a stretch holds parts of
+// at most two of them (one inside it would be too short): sums in slots 2p (the
+// run that holds its first position) and 2p + 1 (the one of its last, if
+// another).  blockIdx.y: a slice of 1 << ls chunks of the row.
 template <int T, int G>
-__global__ void __launch_bounds__(256) embed_sum(const uint2* __restrict__ sorted, int64_t n,
-                                                 const u32x4* __restrict__ dout, const uint32_t* __restrict__ start,
-                                                 uint32_t vocab, int c, int ls, float scale, void* __restrict__ dtable,
+__global__ void __launch_bounds__(256) embed_sum(Runs r, int64_t n, const u32x4* __restrict__ dout, uint32_t vocab,
+                                                 int c, int ls, float scale, void* __restrict__ dtable,
                                                  float* __restrict__ part, uint32_t row_blocks) {
   constexpr int N = Chunk<T>::N;
-  const int gl = threadIdx.x & ((1 << ls) - 1);
+  const int gl = threadIdx.x & ((1 << ls) - 1), i = ((int)blockIdx.y << ls) + gl;
   const uint32_t per = 256u >> ls;
+  float s[N];
   if (blockIdx.x < row_blocks) {
-    const uint32_t v = blockIdx.x * per + (threadIdx.x >> ls);
-    if (v >= vocab) return;
-    const uint32_t a = start[v], b = start[v + 1];
-    if (b - a > kPart) return;
-    for (int i = gl; i < c; i += 1 << ls) {
-      float s[N];
-      sum_rows<T>(sorted, dout, c, i, a, b, s);
-      put_row<T, G>(dtable, v, c, i, s, scale);
+    uint32_t v = blockIdx.x * per + (threadIdx.x >> ls), a, b;
+    if (r.run) {  // a run by its first position
+      if (v >= n) return;
+      a = r.run[v].x, b = r.run[v].y;
+      if (a != v) return;
+      v = r.sorted[v].x;
     }
+    if (v >= vocab) return;
+    if (!r.run) a = r.start[v], b = r.start[v + 1];
+    if (b - a > kPart) return;
+    sum_rows<T>(r.sorted, dout, c, i, gl, ls, a, b, s);
+    if (i < c) put_row<T, G>(dtable, v, c, i, s, scale);
     return;
   }
   const int64_t p = (int64_t)(blockIdx.x - row_blocks) * per + (threadIdx.x >> ls);
   const int64_t s0 = p * kPart;
   if (s0 >= n) return;
   const uint32_t a0 = (uint32_t)s0, b0 = (uint32_t)(s0 + kPart < n ? s0 + kPart : n);
-  const uint32_t v0 = sorted[a0].x, v1 = sorted[b0 - 1].x;
+  const uint32_t v0 = r.sorted[a0].x, v1 = r.sorted[b0 - 1].x;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const uint32_t v = h ? v1 : v0;
     if (v >= vocab || (h && v1 == v0)) continue;
-    uint32_t a = start[v], b = start[v + 1];
+    uint32_t a, b;
+    run_of(r, h ? b0 - 1 : a0, v, a, b);
     if (b - a <= kPart) continue;
-    a = a > a0 ? a : a0;
-    b = b < b0 ? b : b0;
-    for (int i = gl; i < c; i += 1 << ls) {
-      float s[N];
-      sum_rows<T>(sorted, dout, c, i, a, b, s);
-      float* q = part + ((2 * p + h) * c + i) * N;
+    sum_rows<T>(r.sorted, dout, c, i, gl, ls, a > a0 ? a : a0, b < b0 ? b : b0, s);
+    if (i >= c) continue;
+    float* q = part + ((2 * p + h) * c + i) * N;
 #pragma unroll
-      for (int e = 0; e < N; e += 4) *(f32x4*)(q + e) = f32x4{s[e], s[e + 1], s[e + 2], s[e + 3]};
-    }
+    for (int e = 0; e < N; e += 4) *(f32x4*)(q + e) = f32x4{s[e], s[e + 1], s[e + 2], s[e + 3]};
   }
 }
 
-// The parts of a token with more than kPart rows, in order: block p joins the
-// run that begins in stretch p, if one does.  Four waves take a quarter of the
-// parts each; blockIdx.y is a group of 64 chunks of the row.
-template <int T, int G>
-__global__ void __launch_bounds__(256) embed_join(const uint2* __restrict__ sorted, int64_t n,
-                                                  const uint32_t* __restrict__ start, uint32_t vocab, int c,
-                                                  float scale, const float* __restrict__ part,
-                                                  void* __restrict__ dtable) {
-  constexpr int N = Chunk<T>::N;
-  const int64_t p = blockIdx.x, s0 = p * kPart, last = (s0 + kPart < n ? s0 + kPart : n) - 1;
-  const uint32_t v = sorted[last].x;  // (a long run that begins here holds the stretch's last position)
-  if (v >= vocab) return;
-  const int64_t a = start[v], b = start[v + 1];
-  if (b - a <= kPart || a < s0) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int i = blockIdx.y * 64 + lane;
-  const int64_t p1 = (b - 1) / kPart, cnt = p1 - p + 1, q = (cnt + 3) / 4;
-  float s[N];
+// The parts of tokens with more than kPart rows, in order.  A workgroup looks at
+// 64 stretches, a lane of every wave at one: runs that begin there and have at
+// most kWaveParts parts are joined by a wave each, longer ones by all of them.
+// A wave adds four interleaved quarters of its parts, 16 chunks of the row at a
+// time (blockIdx.y: the slice).
+constexpr int kJoinWaves = 8, kWaveParts = 32;
+
+// Sum of parts [k0, k1) of the run that begins in stretch p, in the second slot
+// of it if inside; every lane of a chunk's four gets it.
+template <int N>
+__device__ __forceinline__ void join_parts(const float* __restrict__ part, int64_t p, bool inside, int64_t k0,
+                                           int64_t k1, int c, int i, int u, float (&s)[N]) {
 #pragma unroll
   for (int e = 0; e < N; ++e) s[e] = 0.f;
   if (i < c) {
-    const int64_t k1 = (wave + 1) * q < cnt ? (wave + 1) * q : cnt;
-#pragma unroll 4
-    for (int64_t k = wave * q; k < k1; ++k) {
-      // the first part is the run's own slot of stretch p, the others start their stretch
-      const int64_t slot = 2 * (p + k) + (k == 0 && a > s0 && sorted[s0].x != v ? 1 : 0);
-      const float* r = part + (slot * c + i) * N;
+#pragma unroll 8
+    for (int64_t k = k0 + u; k < k1; k += 4) {
+      const int64_t slot = 2 * (p + k) + (k == 0 && inside ? 1 : 0);
+      const float* x = part + (slot * c + i) * N;
 #pragma unroll
       for (int e = 0; e < N; e += 4) {
-        const f32x4 x = *(const f32x4*)(r + e);
+        const f32x4 y = *(const f32x4*)(x + e);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[e + j] += x[j];
+        for (int j = 0; j < 4; ++j) s[e + j] += y[j];
       }
     }
   }
-  __shared__ float red[3][64][N + 1];
-  if (wave)
 #pragma unroll
-    for (int e = 0; e < N; ++e) red[wave - 1][lane][e] = s[e];
-  __syncthreads();
-  if (wave || i >= c) return;
+  for (int m = 16; m <= 32; m <<= 1)
 #pragma unroll
-  for (int w = 0; w < 3; ++w)
+    for (int e = 0; e < N; ++e) s[e] += __shfl_xor(s[e], m);
+}
+
+template <int T, int G>
+__global__ void __launch_bounds__(64 * kJoinWaves)
+    embed_join(Runs r, int64_t n, uint32_t vocab, int c, float scale, const float* __restrict__ part,
+               void* __restrict__ dtable) {
+  constexpr int N = Chunk<T>::N;
+  __shared__ float red[kJoinWaves - 1][16][N + 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int i = blockIdx.y * 16 + (lane & 15), u = lane >> 4;
+  const int64_t p0 = (int64_t)blockIdx.x * 64, s0 = (p0 + lane) * kPart;
+  uint32_t v = vocab, a = 0, b = 0;
+  if (s0 < n) {
+    const int64_t last = (s0 + kPart < n ? s0 + kPart : n) - 1;
+    v = r.sorted[last].x;  // (a long run that begins here holds the stretch's last position)
+    if (v < vocab) run_of(r, last, v, a, b);
+  }
+  const bool starts = v < vocab && b - a > kPart && a >= s0;
+  const uint32_t cnt = starts ? (b - 1) / kPart - (uint32_t)(p0 + lane) + 1 : 0;
+  const bool inside = a > s0;
+  float s[N];
+  int k = 0;
+  for (uint64_t m = __ballot(starts && cnt <= kWaveParts); m; m &= m - 1, ++k) {
+    if (k % kJoinWaves != wave) continue;
+    const int l = __ffsll((unsigned long long)m) - 1;
+    join_parts<N>(part, p0 + l, __shfl((int)inside, l) != 0, 0, __shfl(cnt, l), c, i, u, s);
+    const uint32_t row = __shfl(v, l);
+    if (i < c && u == 0) put_row<T, G>(dtable, row, c, i, s, scale);
+  }
+  for (uint64_t m = __ballot(starts && cnt > kWaveParts); m; m &= m - 1) {  // (the same in every wave)
+    const int l = __ffsll((unsigned long long)m) - 1;
+    const int64_t all = __shfl(cnt, l), q = (all + kJoinWaves - 1) / kJoinWaves;
+    const int64_t k1 = (wave + 1) * q < all ? (wave + 1) * q : all;
+    join_parts<N>(part, p0 + l, __shfl((int)inside, l) != 0, wave * q, k1, c, i, u, s);
+    const uint32_t row = __shfl(v, l);
+    if (wave && u == 0)
 #pragma unroll
-    for (int e = 0; e < N; ++e) s[e] += red[w][lane][e];
-  put_row<T, G>(dtable, v, c, i, s, scale);
+      for (int e = 0; e < N; ++e) red[wave - 1][lane][e] = s[e];
+    __syncthreads();
+    if (wave == 0 && i < c && u == 0) {
+#pragma unroll
+      for (int w = 0; w < kJoinWaves - 1; ++w)
+#pragma unroll
+        for (int e = 0; e < N; ++e) s[e] += red[w][lane][e];
+      put_row<T, G>(dtable, row, c, i, s, scale);
+    }
+    __syncthreads();
+  }
 }
 
 __global__ void __launch_bounds__(256) fill_zero(u32x4* p, int64_t n) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
-    p[i] = u32x4{0, 0, 0, 0};
+  zero_rows(p, n, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
 }
 
 // ---------------------------------------------------------------------- host
@@ -344,24 +457,29 @@ __global__ void __launch_bounds__(256) fill_zero(u32x4* p, int64_t n) {
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct SortPlan {
+  bool few;
   int bits, passes;  // bits of a digit
   int64_t tiles;
-  size_t el0, el1, hist0, hist1, start, part, total;
+  size_t el0, el1, hist, start, run, part, total;
 };
 
 SortPlan sort_plan(int64_t n, int64_t vocab, int64_t d) {
-  SortPlan s;
+  SortPlan s = {};
   int kb = 1;
   while (((int64_t)1 << kb) <= vocab) ++kb;  // keys 0 .. vocab
+  s.few = n <= kFew;
   s.passes = (kb + kMaxBits - 1) / kMaxBits;
   s.bits = (kb + s.passes - 1) / s.passes;
   s.tiles = (n + kTile - 1) / kTile;
   size_t off = 0;
   s.el0 = off; off = up256(off + (size_t)n * 8);
-  s.el1 = off; off = up256(off + (size_t)n * 8);
-  s.hist0 = off; off = up256(off + ((size_t)s.tiles << s.bits) * 4);
-  s.hist1 = off; off = up256(off + ((size_t)s.tiles << s.bits) * 4);
-  s.start = off; off = up256(off + (size_t)(vocab + 1) * 4);
+  if (s.few) {
+    s.run = off; off = up256(off + (size_t)n * 8);
+  } else {
+    s.el1 = off; off = up256(off + (size_t)n * 8);
+    s.hist = off; off = up256(off + ((size_t)s.tiles << s.bits) * 4);
+    s.start = off; off = up256(off + (size_t)(vocab + 1) * 4);
+  }
   s.part = off; off = up256(off + (size_t)((n + kPart - 1) / kPart) * 2 * (size_t)d * 4);
   s.total = off;
   return s;
@@ -390,59 +508,68 @@ int embed_fwd_t(const void* tokens, int tb, int64_t n, const void* table, int64_
   return hipGetLastError() == hipSuccess ? INFCL_OK : INFCL_ERR_HIP;
 }
 
+unsigned fill_blocks(int64_t chunks, int threads) {
+  const int64_t b = chunks / (4 * threads) + 1;
+  return (unsigned)(b < 2048 ? b : 2048);
+}
+
 template <typename Tok>
-int sort_tokens(const void* tokens, int64_t n, int64_t vocab, const SortPlan& s, char* ws, const uint2** sorted,
-                hipStream_t st) {
+int sort_tokens(const void* tokens, int64_t n, int64_t vocab, const SortPlan& s, char* ws, void* dtable,
+                int64_t chunks, Runs& r, hipStream_t st) {
   const Tok* tok = (const Tok*)tokens;
   uint2* el[2] = {(uint2*)(ws + s.el0), (uint2*)(ws + s.el1)};
-  uint32_t* hist[2] = {(uint32_t*)(ws + s.hist0), (uint32_t*)(ws + s.hist1)};
+  if (s.few) {
+    const unsigned rb = (unsigned)((n + kRankTokens - 1) / kRankTokens);
+    r.sorted = el[0], r.run = (const uint2*)(ws + s.run);
+    hipLaunchKernelGGL((sort_few<Tok>), dim3(rb + fill_blocks(chunks, 256)), dim3(256), 0, st, tok, (int)n,
+                       (uint32_t)vocab, rb, el[0], (uint2*)(ws + s.run), (u32x4*)dtable, chunks);
+    return hipGetLastError() == hipSuccess ? INFCL_OK : INFCL_ERR_HIP;
+  }
+  uint32_t* hist = (uint32_t*)(ws + s.hist);
   const dim3 grid((unsigned)s.tiles);
-  hipLaunchKernelGGL((sort_count<Tok>), grid, dim3(256), 0, st, tok, n, (uint32_t)vocab, s.bits, hist[0], hist[1]);
-  if (hipGetLastError() != hipSuccess) return INFCL_ERR_HIP;
   for (int p = 0; p < s.passes; ++p) {
-    uint32_t* next = p + 1 < s.passes ? hist[(p + 1) & 1] : nullptr;
-    if (p >= 1 && next) {  // (the count clears the first one's)
-      const int64_t q = ((s.tiles << s.bits) * 4 + 15) / 16;
-      hipLaunchKernelGGL(fill_zero, dim3((unsigned)(q / 256 + 1 < 1024 ? q / 256 + 1 : 1024)), dim3(256), 0, st,
-                         (u32x4*)next, q);
+    const uint2* in = el[(p + 1) & 1];
+    if (p == 0) {
+      hipLaunchKernelGGL((sort_count<Tok, true>), grid, dim3(256), 0, st, tok, in, n, (uint32_t)vocab, 0, s.bits, hist);
+      hipLaunchKernelGGL((sort_scatter<Tok, true>), grid, dim3(256), 0, st, tok, in, n, (uint32_t)vocab, 0, s.bits,
+                         hist, el[0]);
+    } else {
+      hipLaunchKernelGGL((sort_count<Tok, false>), grid, dim3(256), 0, st, tok, in, n, (uint32_t)vocab, p * s.bits,
+                         s.bits, hist);
+      hipLaunchKernelGGL((sort_scatter<Tok, false>), grid, dim3(256), 0, st, tok, in, n, (uint32_t)vocab, p * s.bits,
+                         s.bits, hist, el[p & 1]);
     }
-    if (p == 0)
-      hipLaunchKernelGGL((sort_scatter<Tok, true>), grid, dim3(256), 0, st, tok, (const uint2*)nullptr, n,
-                         (uint32_t)vocab, 0, s.bits, hist[0], next, el[0]);
-    else
-      hipLaunchKernelGGL((sort_scatter<Tok, false>), grid, dim3(256), 0, st, tok, (const uint2*)el[(p + 1) & 1], n,
-                         (uint32_t)vocab, p * s.bits, s.bits, hist[p & 1], next, el[p & 1]);
     if (hipGetLastError() != hipSuccess) return INFCL_ERR_HIP;
   }
-  *sorted = el[(s.passes + 1) & 1];
-  return INFCL_OK;
+  r.sorted = el[(s.passes + 1) & 1];
+  r.start = (const uint32_t*)(ws + s.start);
+  hipLaunchKernelGGL(row_starts, dim3((unsigned)(n / 256 + 1)), dim3(256), 0, st, r.sorted, n, (uint32_t)vocab,
+                     (uint32_t*)(ws + s.start));
+  return hipGetLastError() == hipSuccess ? INFCL_OK : INFCL_ERR_HIP;
 }
 
 template <int T, int G>
 int embed_bwd_t(const void* tokens, int tb, int64_t n, const void* dout, int64_t vocab, int64_t d, float scale,
                 void* dtable, char* ws, hipStream_t st) {
-  const int64_t c = chunks_of(d, T);
+  const int64_t c = chunks_of(d, T), chunks = chunks_of(vocab * d, G);
   if (n == 0) {
-    const int64_t q = (vocab * d * (G == kF32 ? 4 : 2)) / 16;
-    hipLaunchKernelGGL(fill_zero, dim3((unsigned)(q / 256 + 1 < 16384 ? q / 256 + 1 : 16384)), dim3(256), 0, st,
-                       (u32x4*)dtable, q);
+    hipLaunchKernelGGL(fill_zero, dim3(fill_blocks(chunks, 256)), dim3(256), 0, st, (u32x4*)dtable, chunks);
     return hipGetLastError() == hipSuccess ? INFCL_OK : INFCL_ERR_HIP;
   }
   const SortPlan s = sort_plan(n, vocab, d);
-  const uint2* sorted;
-  const int rc = tb == 4 ? sort_tokens<int32_t>(tokens, n, vocab, s, ws, &sorted, st)
-                         : sort_tokens<int64_t>(tokens, n, vocab, s, ws, &sorted, st);
+  Runs r = {};
+  const int rc = tb == 4 ? sort_tokens<int32_t>(tokens, n, vocab, s, ws, dtable, chunks, r, st)
+                         : sort_tokens<int64_t>(tokens, n, vocab, s, ws, dtable, chunks, r, st);
   if (rc != INFCL_OK) return rc;
-  uint32_t* start = (uint32_t*)(ws + s.start);
-  hipLaunchKernelGGL(row_starts, dim3((unsigned)(n / 256 + 1)), dim3(256), 0, st, sorted, n, (uint32_t)vocab, start);
   const int ls = row_lanes_log2(c, 1);
-  const int64_t per = 256 >> ls, parts = (n + kPart - 1) / kPart;
-  const int64_t rb = (vocab + per - 1) / per, pb = n > kPart ? (parts + per - 1) / per : 0;
-  hipLaunchKernelGGL((embed_sum<T, G>), dim3((unsigned)(rb + pb)), dim3(256), 0, st, sorted, n, (const u32x4*)dout,
-                     start, (uint32_t)vocab, (int)c, ls, scale, dtable, (float*)(ws + s.part), (uint32_t)rb);
+  const int64_t per = 256 >> ls, rows = s.few ? n : vocab, parts = (n + kPart - 1) / kPart;
+  const int64_t rb = (rows + per - 1) / per, pb = n > kPart ? (parts + per - 1) / per : 0;
+  const unsigned slices = (unsigned)((c + (1 << ls) - 1) >> ls);
+  hipLaunchKernelGGL((embed_sum<T, G>), dim3((unsigned)(rb + pb), slices), dim3(256), 0, st, r, n, (const u32x4*)dout,
+                     (uint32_t)vocab, (int)c, ls, scale, dtable, (float*)(ws + s.part), (uint32_t)rb);
   if (pb)
-    hipLaunchKernelGGL((embed_join<T, G>), dim3((unsigned)parts, (unsigned)((c + 63) / 64)), dim3(256), 0, st, sorted,
-                       n, start, (uint32_t)vocab, (int)c, scale, (const float*)(ws + s.part), dtable);
+    hipLaunchKernelGGL((embed_join<T, G>), dim3((unsigned)((parts + 63) / 64), (unsigned)((c + 15) / 16)),
+                       dim3(64 * kJoinWaves), 0, st, r, n, (uint32_t)vocab, (int)c, scale, (const float*)(ws + s.part), dtable);
   return hipGetLastError() == hipSuccess ? INFCL_OK : INFCL_ERR_HIP;
 }
 
