@@ -214,37 +214,40 @@ __device__ __forceinline__ bool attn_bad(const f32x16 (&acc)[FB]) {
   return !(t == 0.f);
 }
 
-// ---- The exact form of a tile with masked entries.  A masked weight is zero,
-// but zero times an infinity or a NaN of a masked row would reach the product.
-// A workgroup whose sums are not finite therefore sweeps again and takes the
-// tiles that hold masked entries row by row: no masked row is read into a sum.
+// ---- The row-by-row form.  A masked weight is zero, but zero times an infinity
+// or a NaN of a masked row would reach the product.  A wave whose sums are not
+// finite therefore takes its rows again on the vector unit, in fp32, from
+// memory, without reading any row that is masked.  Only such rows take the time
+// (a thousand times a sweep's).  The functions are calls, not inlined, with few
+// registers, so that the sweeps keep theirs: they go through the features 8 at a
+// time, with all weights anew.  Lanes L and L ^ 32 share an own row and take
+// every other 8 features of it.
 
-// <own row, swept row j> over this lane's half of the features, both halves added.
-template <int DP, bool F16>
-__device__ __forceinline__ float attn_dot(const bf16x8 (&own)[DP / 16], const INFCL_LDS char* tile, int j, int h) {
+// <x, y>, over both lanes' features.
+template <bool F16>
+__device__ __forceinline__ float attn_dot(const uint16_t* x, const uint16_t* y, int h, int hd) {
   float s = 0.f;
+#pragma unroll 1
+  for (int d = 8 * h; d < hd; d += 16) {
+    const bf16x8 a = *(const bf16x8*)(x + d), b = *(const bf16x8*)(y + d);
 #pragma unroll
-  for (int i = 0; i < DP / 16; ++i) {
-    const bf16x8 x = attn_row(tile + j * DP * 2 + 16 * ((2 * i + h) ^ attn_sw<DP>(j)));
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s = fmaf(from16<F16>(own[i][e]), from16<F16>(x[e]), s);
+    for (int e = 0; e < 8; ++e) s = fmaf(from16<F16>(a[e]), from16<F16>(b[e]), s);
   }
   return attn_sum2(s);
 }
-// acc += w row j, where live.
-template <int DP, bool F16>
-__device__ __forceinline__ void attn_axpy(f32x16 (&acc)[DP / 32], float w, bool live, const INFCL_LDS char* tile, int j,
-                                          int h) {
+// acc += w x[0 .. 7]
+template <bool F16>
+__device__ __forceinline__ void attn_axpy8(float (&acc)[8], float w, const uint16_t* x) {
+  const bf16x8 a = *(const bf16x8*)x;
 #pragma unroll
-  for (int fb = 0; fb < DP / 32; ++fb)
+  for (int e = 0; e < 8; ++e) acc[e] = fmaf(w, from16<F16>(a[e]), acc[e]);
+}
+template <bool F16>
+__device__ __forceinline__ void attn_store8(uint16_t* x, const float (&acc)[8], float f) {
+  bf16x8 a;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-      const bf16x4 x = *(const INFCL_LDS bf16x4*)(tile + j * DP * 2 + 16 * ((4 * fb + q) ^ attn_sw<DP>(j)) + 8 * h);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (live) acc[fb][4 * q + e] = fmaf(w, from16<F16>(x[e]), acc[fb][4 * q + e]);
-    }
+  for (int e = 0; e < 8; ++e) a[e] = to16<F16>(acc[e] * f);
+  *(bf16x8*)x = a;
 }
 
 // Barrier of the workgroup after all of this wave's copies and LDS reads.

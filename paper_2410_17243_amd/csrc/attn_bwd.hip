@@ -24,19 +24,77 @@ struct AttnGrads {
   const uint16_t *out, *dout;
   int64_t os, oh, dos, doh;
   const float* lse;
-  float *lse2, *dlt;  // [heads][trow]: 64 entries past the tokens may be read
+  float* stat;  // [heads][trow][2]: lse log2(e), D; 32 entries past the tokens may be read
   int64_t trow;
   uint16_t *dq, *dk, *dv;
   int64_t dqs, dqh, dks, dkh, dvs, dvh;
 };
 
+// Row by row (attn.hpp): dq of the lane's row from keys [0, lim).  own_d: D is
+// the sum of p dp.  Returns D.
+template <bool F16>
+__device__ __attribute__((noinline)) float attn_dq_rows(const uint16_t* q, const uint16_t* dout,
+                                                        const uint16_t* out, const uint16_t* k, const uint16_t* v,
+                                                        int64_t ks, int64_t vs, int lim, float scale, float lse,
+                                                        bool own_d, int hd, int h, uint16_t* dq) {
+  const float sl2 = scale * kLog2e, lse2 = lse == -__builtin_inff() ? 0.f : lse * kLog2e;
+  float D = 0.f;
+  if (lse != -__builtin_inff() && !own_d) D = attn_dot<F16>(dout, out, h, hd);
+  if (own_d) {
+#pragma unroll 1
+    for (int j = 0; j < lim; ++j) {
+      const float p = exp2_hw(fmaf(attn_dot<F16>(q, k + j * ks, h, hd), sl2, -lse2));
+      D = fmaf(p, attn_dot<F16>(dout, v + j * vs, h, hd), D);
+    }
+  }
+#pragma unroll 1
+  for (int d = 0; d < hd; d += 16) {
+    float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const int at = d + 8 * h;
+#pragma unroll 1
+    for (int j = 0; j < lim; ++j) {
+      const float p = exp2_hw(fmaf(attn_dot<F16>(q, k + j * ks, h, hd), sl2, -lse2));
+      const float ds = p * (attn_dot<F16>(dout, v + j * vs, h, hd) - D);
+      if (at < hd) attn_axpy8<F16>(acc, ds, k + j * ks + at);
+    }
+    if (at < hd) attn_store8<F16>(dq + at, acc, scale);
+  }
+  return D;
+}
+
+// ... dk and dv of the lane's key from queries [first, m) of the group's heads.
+template <bool F16>
+__device__ __attribute__((noinline)) void attn_dkv_rows(const uint16_t* k, const uint16_t* v, const uint16_t* q,
+                                                        const uint16_t* dout, int64_t qs, int64_t qh, int64_t ds_,
+                                                        int64_t dh, const float* stat, int64_t trow, int first, int m, int group, float scale, int hd, int h,
+                                                        uint16_t* dk, uint16_t* dv) {
+  const float sl2 = scale * kLog2e;
+#pragma unroll 1
+  for (int d = 0; d < hd; d += 16) {
+    float ak[8] = {0, 0, 0, 0, 0, 0, 0, 0}, av[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const int at = d + 8 * h;
+#pragma unroll 1
+    for (int g = 0; g < group; ++g)
+#pragma unroll 1
+      for (int i = first < 0 ? 0 : first; i < m; ++i) {
+        const uint16_t* qr = q + g * qh + i * qs;
+        const uint16_t* dr = dout + g * dh + i * ds_;
+        const float p = exp2_hw(fmaf(attn_dot<F16>(k, qr, h, hd), sl2, -stat[(g * trow + i) * 2]));
+        const float ds = p * (attn_dot<F16>(v, dr, h, hd) - stat[(g * trow + i) * 2 + 1]);
+        if (at >= hd) continue;
+        attn_axpy8<F16>(av, p, dr + at);
+        attn_axpy8<F16>(ak, ds, qr + at);
+      }
+    if (at < hd) attn_store8<F16>(dk + at, ak, scale), attn_store8<F16>(dv + at, av, 1.f);
+  }
+}
+
 // Owns rows (query, head of the group); sweeps the keys they see.
 template <int DP, int NW, int KT, bool F16>
-__global__ void __launch_bounds__(64 * NW) attn_dq_kernel(AttnArgs a, AttnGrads w, int tiles) {
+__global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGrads w, int tiles) {
   constexpr int kFb = DP / 32, kI = DP / 16, kKb = KT / 32;
   typedef AttnTile<DP, NW, KT> Tile;
   __shared__ __attribute__((aligned(1024))) char lds_[4 * Tile::kBytes];
-  __shared__ int redo;
   INFCL_LDS char* lds = (INFCL_LDS char*)lds_;
   const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int h = lane >> 5;
@@ -59,6 +117,7 @@ __global__ void __launch_bounds__(64 * NW) attn_dq_kernel(AttnArgs a, AttnGrads 
   const uint16_t* kb = a.k + sq.k0 * a.ks + kv * a.kh;
   const uint16_t* vb = a.v + sq.k0 * a.vs + kv * a.vh;
 
+  bool bad = false;  // this wave's sums may hold what masked rows hold
   for (uint32_t t = (uint32_t)t0; t * (uint64_t)(32 * NW) < rows; t += (uint32_t)tiles) {
     const uint32_t r = t * (32 * NW) + wave * 32 + (lane & 31);
     const bool live = r < rows;
@@ -94,8 +153,7 @@ __global__ void __launch_bounds__(64 * NW) attn_dq_kernel(AttnArgs a, AttnGrads 
 
     f32x16 acc[kFb];
     attn_barrier();
-    if (threadIdx.x == 0) redo = 0;
-    for (int exact = 0;; exact = 1) {
+    {
 #pragma unroll
       for (int fb = 0; fb < kFb; ++fb) acc[fb] = f32x16_zero();
       if (0 < kend) {
@@ -127,10 +185,17 @@ __global__ void __launch_bounds__(64 * NW) attn_dq_kernel(AttnArgs a, AttnGrads 
 #pragma unroll
         for (int b = 0; b < kKb; ++b)
 #pragma unroll
-          for (int x = 0; x < 16; ++x) {
-            p[b][x] = exp2_hw(fmaf(p[b][x], a.sl2, -lse2));
-            if (masked && k + 32 * b + attn_reg_row(x, h) >= lim) p[b][x] = 0.f, dp[b][x] = 0.f;
-          }
+          for (int x = 0; x < 16; ++x) p[b][x] = exp2_hw(fmaf(p[b][x], a.sl2, -lse2));
+        if (masked) {
+#pragma unroll
+          for (int b = 0; b < kKb; ++b)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+              const bool out = k + 32 * b + attn_reg_row(x, h) >= lim;
+              p[b][x] = out ? 0.f : p[b][x];
+              dp[b][x] = out ? 0.f : dp[b][x];
+            }
+        }
         if (sq.n <= KT) {
           float s = 0.f;
 #pragma unroll
@@ -138,14 +203,6 @@ __global__ void __launch_bounds__(64 * NW) attn_dq_kernel(AttnArgs a, AttnGrads 
 #pragma unroll
             for (int x = 0; x < 16; ++x) s = fmaf(p[b][x], dp[b][x], s);
           D = attn_sum2(s);
-        }
-        if (exact && masked) {
-          for (int j = 0; j < KT && k + j < kend; ++j) {
-            const float pj = exp2_hw(fmaf(attn_dot<DP, F16>(qf, kt, j, h), a.sl2, -lse2));
-            const float ds = pj * (attn_dot<DP, F16>(df, vt, j, h) - D);
-            attn_axpy<DP, F16>(acc, ds, k + j < lim, kt, j, h);
-          }
-          continue;
         }
 #pragma unroll
         for (int b = 0; b < kKb; ++b) {
@@ -161,32 +218,49 @@ __global__ void __launch_bounds__(64 * NW) attn_dq_kernel(AttnArgs a, AttnGrads 
           }
         }
       }
-      if (!a.causal || exact) break;
-      attn_barrier();
-      if (wave_any(attn_bad(acc)) && lane == 0) redo = 1;
-      attn_barrier();
-      if (!redo) break;
     }
+    bad |= a.causal && wave_any(live && attn_bad(acc));
     if (!live) continue;
     attn_store<F16>(w.dq + token * w.dqs + head * w.dqh, acc, a.scale, h, a.hd);
-    if (h == 0) {
-      w.lse2[(int64_t)head * w.trow + token] = lse2;
-      w.dlt[(int64_t)head * w.trow + token] = D;
-    }
+    w.stat[((int64_t)head * w.trow + token) * 2 + h] = h ? D : lse2;
+  }
+  if (!bad) return;
+  wait_dma();  // (the stores of these rows are done: other lanes write them again)
+  for (uint64_t r = (uint64_t)t0 * (32 * NW) + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31); r < rows;
+       r += (uint64_t)tiles * (32 * NW)) {
+    const int pos = (int)((uint32_t)r / (uint32_t)a.group), head = kv * a.group + (int)((uint32_t)r % (uint32_t)a.group);
+    const int64_t token = sq.q0 + pos;
+    const int lim = pos + sq.n - sq.m + 1;
+    const float D = attn_dq_rows<F16>(
+        a.q + token * a.qs + head * a.qh, w.dout + token * w.dos + head * w.doh, w.out + token * w.os + head * w.oh,
+        a.k + sq.k0 * a.ks + kv * a.kh, a.v + sq.k0 * a.vs + kv * a.vh, a.ks, a.vs, lim < sq.n ? lim : sq.n, a.scale,
+        w.lse[(int64_t)head * a.tq + token], sq.n <= KT, a.hd, (threadIdx.x >> 5) & 1,
+        w.dq + token * w.dqs + head * w.dqh);
+    if (threadIdx.x & 32) w.stat[((int64_t)head * w.trow + token) * 2 + 1] = D;
   }
 }
 
-// Owns keys; sweeps the queries that see them, one head of the group after
-// another.
-template <int DP, int NW, bool F16>
-__global__ void __launch_bounds__(64 * NW) attn_dkv_kernel(AttnArgs a, AttnGrads w, int tiles) {
+// Owns 32 NW keys; sweeps the queries that see them, one head of the group after
+// another.  NG groups of NW waves own the same keys and take every NG-th tile of
+// queries each: the sweep of one workgroup, which is the longest chain of a call
+// (all heads of the group times all later queries), is NG times shorter, and the
+// groups' sums are added through LDS at its end.
+// At 128 features the own keys, the two sums and a tile's weights fill the
+// registers of two waves per SIMD: the own values stay in LDS there (a fifth of
+// the sweep's LDS reads), for a register spilled in the sweep costs far more (its
+// reload waits for the tile copies in flight).
+template <int DP, int NW, int NG, bool F16>
+__global__ void __launch_bounds__(64 * NW * NG, 2) attn_dkv_kernel(AttnArgs a, AttnGrads w, int tiles) {
   constexpr int kFb = DP / 32, kI = DP / 16, QT = 32;
+  constexpr bool kVLds = DP == 128;
   typedef AttnTile<DP, NW, QT> Tile;
-  __shared__ __attribute__((aligned(1024))) char lds_[4 * Tile::kBytes];
-  __shared__ int redo;
+  typedef AttnTile<DP, NW * NG, 32 * NW> Own;
+  __shared__ __attribute__((aligned(1024))) char lds_[4 * NG * Tile::kBytes + (kVLds ? Own::kBytes : 0)];
+  __shared__ __attribute__((aligned(16))) float stat_[NW * NG][64];  // a tile's pairs of lse log2(e) and D
   INFCL_LDS char* lds = (INFCL_LDS char*)lds_;
-  const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int h = lane >> 5;
+  const int wave = NW * NG == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int h = lane >> 5, wk = wave % NW, grp = wave / NW;
+  INFCL_LDS float* stat = (INFCL_LDS float*)stat_[wave];
   const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
   const int t0 = (int)(blockIdx.x / groups);
   const uint32_t gz = blockIdx.x % groups;
@@ -199,102 +273,164 @@ __global__ void __launch_bounds__(64 * NW) attn_dkv_kernel(AttnArgs a, AttnGrads
   ln.init(lane);
   const uint32_t qst = (uint32_t)(a.qs * 2), dst = (uint32_t)(w.dos * 2);
   uint32_t qoff[Tile::kVar], doff[Tile::kVar];
-  Tile::offsets(qoff, wave, lane, qst, a.hd);
-  Tile::offsets(doff, wave, lane, dst, a.hd);
+  Tile::offsets(qoff, wk, lane, qst, a.hd);
+  Tile::offsets(doff, wk, lane, dst, a.hd);
 
+  bool bad = false;  // this wave's sums may hold what masked rows hold
   for (int64_t t = t0; t * (32 * NW) < sq.n; t += tiles) {
-    const int key0 = (int)(t * (32 * NW)), kw = key0 + 32 * wave, key = kw + (lane & 31);
-    const bool live = key < sq.n;
-    const int64_t token = sq.k0 + key;
-    bf16x8 kf[kI], vf[kI];
-#pragma unroll
-    for (int i = 0; i < kI; ++i) {
-      kf[i] = attn_own(a.k + (live ? token * a.ks : 0) + kv * a.kh, i, h, a.hd, live);
-      vf[i] = attn_own(a.v + (live ? token * a.vs : 0) + kv * a.vh, i, h, a.hd, live);
-    }
-    // queries from `first` on see this lane's key, from wall on all the wave's;
-    // none before qbeg sees one of the workgroup's
+    const int key0 = (int)(t * (32 * NW)), kw = key0 + 32 * wk;
+    bf16x8 kf[kI], vf[kVLds ? 1 : kI];
     const int shift = sq.n - sq.m;
-    const int first = a.causal ? key - shift : 0;
+    int first;  // queries from here on see this lane's key
+    {
+      const int key = kw + (lane & 31);
+      const bool live = key < sq.n;
+      const int64_t token = sq.k0 + (live ? key : 0);
+#pragma unroll
+      for (int i = 0; i < kI; ++i) {
+        kf[i] = attn_own(a.k + token * a.ks + kv * a.kh, i, h, a.hd, live);
+        if constexpr (!kVLds) vf[i] = attn_own(a.v + token * a.vs + kv * a.vh, i, h, a.hd, live);
+      }
+      first = a.causal ? key - shift : 0;
+    }
+    // from wall on all the wave's keys; none before qbeg sees one of the workgroup's
     const int wall = a.causal ? kw + 31 - shift : 0, wany = a.causal ? kw - shift : 0;
     int qbeg = a.causal ? key0 - shift : 0;
     qbeg = qbeg < 0 ? 0 : qbeg / QT * QT;
 
     f32x16 dk[kFb], dv[kFb];
     attn_barrier();
-    if (threadIdx.x == 0) redo = 0;
-    for (int exact = 0;; exact = 1) {
+    const INFCL_LDS char* own = lds + 4 * NG * Tile::kBytes + wk * 32 * Tile::kRow;
+    if constexpr (kVLds) {
+      uint32_t off[Own::kVar];
+      Own::offsets(off, wave, lane, (uint32_t)(a.vs * 2), a.hd);
+      Own::issue(a.v + (sq.k0 + key0) * a.vs + kv * a.vh, sq.n - key0, (uint32_t)(a.vs * 2), a.hd,
+                 lds + 4 * NG * Tile::kBytes, off, wave);
+    }
 #pragma unroll
-      for (int fb = 0; fb < kFb; ++fb) dk[fb] = f32x16_zero(), dv[fb] = f32x16_zero();
-      // tiles of all heads of the group, as one sequence
-      const int per = sq.m > qbeg ? (sq.m - qbeg + QT - 1) / QT : 0;
-      const int64_t count = (int64_t)per * a.group;
-      auto issue = [&](int g, int i, int b) {
-        const int head = kv * a.group + g;
-        INFCL_LDS char* to = lds + b * 2 * Tile::kBytes;
-        Tile::issue(a.q + (sq.q0 + i) * a.qs + head * a.qh, sq.m - i, qst, a.hd, to, qoff, wave);
-        Tile::issue(w.dout + (sq.q0 + i) * w.dos + head * w.doh, sq.m - i, dst, a.hd, to + Tile::kBytes, doff, wave);
-      };
-      if (count) issue(0, qbeg, 0);
-      int g = 0, i0 = qbeg, buf = 0;
-      for (int64_t c = 0; c < count; ++c, buf ^= 1) {
-        int gn = g, in = i0 + QT;
-        if (in >= sq.m) ++gn, in = qbeg;
-        attn_barrier();
-        if (c + 1 < count) issue(gn, in, buf ^ 1);
-        const int head = kv * a.group + g, i1 = i0;
-        g = gn, i0 = in;
-        if (i1 + QT <= wany || kw >= sq.n) continue;  // (no query of the tile sees a key of this wave)
-        const float* pl = w.lse2 + (int64_t)head * w.trow + sq.q0 + i1;
-        const float* pd = w.dlt + (int64_t)head * w.trow + sq.q0 + i1;
-        const INFCL_LDS char* qt = lds + buf * 2 * Tile::kBytes;
-        const INFCL_LDS char* dt = qt + Tile::kBytes;
-        f32x16 p = f32x16_zero(), dp = f32x16_zero(), L, Dv;
+    for (int fb = 0; fb < kFb; ++fb) dk[fb] = f32x16_zero(), dv[fb] = f32x16_zero();
+    // tiles of all heads of the group, as one sequence; this group's are grp, grp + NG, ..
+    const int per = sq.m > qbeg ? (sq.m - qbeg + QT - 1) / QT : 0;
+    const int64_t count = (int64_t)per * a.group;
+    INFCL_LDS char* mylds = lds + grp * 4 * Tile::kBytes;
+    // the lanes fetch a tile's 32 pairs a tile ahead
+    const float* row = w.stat + sq.q0 * 2;
+    float ahead = 0.f;
+    int g = 0, i0 = qbeg;  // the tile in hand, then the next
+    auto step = [&]() {
+      i0 += NG * QT;
+      while (i0 >= qbeg + per * QT && g < a.group) i0 -= per * QT, ++g;
+    };
+    auto issue = [&](int b) {
+      const int head = kv * a.group + g;
+      INFCL_LDS char* to = mylds + b * 2 * Tile::kBytes;
+      Tile::issue(a.q + (sq.q0 + i0) * a.qs + head * a.qh, sq.m - i0, qst, a.hd, to, qoff, wk);
+      Tile::issue(w.dout + (sq.q0 + i0) * w.dos + head * w.doh, sq.m - i0, dst, a.hd, to + Tile::kBytes, doff, wk);
+      ahead = row[((int64_t)head * w.trow + i0) * 2 + lane];
+    };
+    if (count) {
+      i0 += grp * QT;
+      while (i0 >= qbeg + per * QT && g < a.group) i0 -= per * QT, ++g;
+      if (g < a.group) issue(0);
+    }
+    int buf = 0;
+    for (int64_t c = 0; c < count; c += NG, buf ^= 1) {
+      const int i1 = i0;
+      const bool none = g >= a.group || i1 + QT <= wany || kw >= sq.n;  // (no query of the tile sees a key of this wave)
+      stat[lane] = ahead;
+      step();
+      attn_barrier();
+      if (g < a.group) issue(buf ^ 1);
+      if (none) continue;
+      const INFCL_LDS char* qt = mylds + buf * 2 * Tile::kBytes;
+      const INFCL_LDS char* dt = qt + Tile::kBytes;
+      f32x16 p = f32x16_zero(), dp = f32x16_zero();
 #pragma unroll
-        for (int x = 0; x < 16; ++x) L[x] = pl[attn_reg_row(x, h)], Dv[x] = pd[attn_reg_row(x, h)];
+      for (int i = 0; i < kI; ++i) p = mfma16<F16>(attn_row(qt + ln.row[i]), kf[i], p);
+      if constexpr (kVLds) __builtin_amdgcn_sched_barrier(0);  // (fewer fragments held at a time)
 #pragma unroll
-        for (int i = 0; i < kI; ++i) {
-          p = mfma16<F16>(attn_row(qt + ln.row[i]), kf[i], p);
+      for (int i = 0; i < kI; ++i) {
+        if constexpr (kVLds)
+          dp = mfma16<F16>(attn_row(dt + ln.row[i]), attn_row(own + ln.row[i]), dp);
+        else
           dp = mfma16<F16>(attn_row(dt + ln.row[i]), vf[i], dp);
-        }
-        const bool masked = i1 < wall || i1 + QT > sq.m;
+      }
+      const bool masked = i1 < wall || i1 + QT > sq.m;
 #pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          p[x] = exp2_hw(fmaf(p[x], a.sl2, -L[x]));
-          dp[x] -= Dv[x];
-          const int i = i1 + attn_reg_row(x, h);
-          if (masked && (i < first || i >= sq.m)) p[x] = 0.f, dp[x] = 0.f;
-          dp[x] *= p[x];
-        }
-        if (exact && masked) {
-          for (int j = 0; j < QT && i1 + j < sq.m; ++j) {
-            const float pj = exp2_hw(fmaf(attn_dot<DP, F16>(kf, qt, j, h), a.sl2, -pl[j]));
-            const float ds = pj * (attn_dot<DP, F16>(vf, dt, j, h) - pd[j]);
-            attn_axpy<DP, F16>(dv, pj, i1 + j >= first, dt, j, h);
-            attn_axpy<DP, F16>(dk, ds, i1 + j >= first, qt, j, h);
-          }
-          continue;
-        }
+      for (int x4 = 0; x4 < 4; ++x4) {
+        const f32x4 lo = *(const INFCL_LDS f32x4*)(stat + 2 * attn_reg_row(4 * x4, h));
+        const f32x4 hi = *(const INFCL_LDS f32x4*)(stat + 2 * attn_reg_row(4 * x4, h) + 4);
+        const float L[4] = {lo[0], lo[2], hi[0], hi[2]}, D[4] = {lo[1], lo[3], hi[1], hi[3]};
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const bf16x8 pw = attn_pack<F16>(p, u), ds = attn_pack<F16>(dp, u);
-          const int ro = 16 * u * Tile::kRow;
-#pragma unroll
-          for (int fb = 0; fb < kFb; ++fb) {
-            dv[fb] = mfma16<F16>(attn_tr(dt + ro + ln.tr[0][fb], dt + ro + ln.tr[1][fb]), pw, dv[fb]);
-            dk[fb] = mfma16<F16>(attn_tr(qt + ro + ln.tr[0][fb], qt + ro + ln.tr[1][fb]), ds, dk[fb]);
-          }
+        for (int e = 0; e < 4; ++e) {
+          const int x = 4 * x4 + e;
+          p[x] = exp2_hw(fmaf(p[x], a.sl2, -L[e]));
+          dp[x] = p[x] * (dp[x] - D[e]);
         }
       }
-      if (!a.causal || exact) break;
-      attn_barrier();
-      if ((wave_any(attn_bad(dk)) || wave_any(attn_bad(dv))) && lane == 0) redo = 1;
-      attn_barrier();
-      if (!redo) break;
+      if (masked) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const int i = i1 + attn_reg_row(x, h);
+          const bool out = i < first || i >= sq.m;
+          p[x] = out ? 0.f : p[x];
+          dp[x] = out ? 0.f : dp[x];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8 pw = attn_pack<F16>(p, u), ds = attn_pack<F16>(dp, u);
+        const int ro = 16 * u * Tile::kRow;
+#pragma unroll
+        for (int fb = 0; fb < kFb; ++fb) {
+          dv[fb] = mfma16<F16>(attn_tr(dt + ro + ln.tr[0][fb], dt + ro + ln.tr[1][fb]), pw, dv[fb]);
+          dk[fb] = mfma16<F16>(attn_tr(qt + ro + ln.tr[0][fb], qt + ro + ln.tr[1][fb]), ds, dk[fb]);
+        }
+      }
     }
-    if (!live) continue;
-    attn_store<F16>(w.dk + token * w.dks + kv * w.dkh, dk, a.scale, h, a.hd);
-    attn_store<F16>(w.dv + token * w.dvs + kv * w.dvh, dv, 1.f, h, a.hd);
+    if constexpr (NG == 2) {
+      INFCL_LDS float* red = (INFCL_LDS float*)lds + wk * kFb * 16 * 64 + lane;
+      static_assert(NW * kFb * 16 * 64 * 4 <= 4 * NG * Tile::kBytes, "room");
+#pragma unroll
+      for (int both = 0; both < 2; ++both) {
+        f32x16(&acc)[kFb] = both ? dv : dk;
+        attn_barrier();
+        if (grp) {
+#pragma unroll
+          for (int fb = 0; fb < kFb; ++fb)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) red[(fb * 16 + x) * 64] = acc[fb][x];
+        }
+        attn_barrier();
+        if (!grp) {
+#pragma unroll
+          for (int fb = 0; fb < kFb; ++fb)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) acc[fb][x] += red[(fb * 16 + x) * 64];
+        }
+      }
+    }
+    int own_lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(own_lane));  // (addresses made here, not kept through the sweep)
+    const int own_key = kw + (own_lane & 31);
+    const bool mine = own_key < sq.n && grp == 0;
+    bad |= a.causal && wave_any(mine && (attn_bad(dk) || attn_bad(dv)));
+    if (!mine) continue;
+    const int64_t at = sq.k0 + own_key;
+    attn_store<F16>(w.dk + at * w.dks + kv * w.dkh, dk, a.scale, own_lane >> 5, a.hd);
+    attn_store<F16>(w.dv + at * w.dvs + kv * w.dvh, dv, 1.f, own_lane >> 5, a.hd);
+  }
+  if (!bad) return;
+  wait_dma();  // (the stores of these rows are done: other lanes write them again)
+  const int h0 = kv * a.group;
+  for (int64_t key = (int64_t)t0 * (32 * NW) + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31); key < sq.n;
+       key += (int64_t)tiles * (32 * NW)) {
+    const int64_t token = sq.k0 + key;
+    attn_dkv_rows<F16>(a.k + token * a.ks + kv * a.kh, a.v + token * a.vs + kv * a.vh, a.q + sq.q0 * a.qs + h0 * a.qh,
+                       w.dout + sq.q0 * w.dos + h0 * w.doh, a.qs, a.qh, w.dos, w.doh,
+                       w.stat + (h0 * w.trow + sq.q0) * 2, w.trow, (int)key - (sq.n - sq.m), sq.m, a.group, a.scale,
+                       a.hd, (threadIdx.x >> 5) & 1, w.dk + token * w.dks + kv * w.dkh,
+                       w.dv + token * w.dvs + kv * w.dvh);
   }
 }
 
@@ -304,8 +440,9 @@ void launch_both(const AttnArgs& a, const AttnGrads& w, int64_t max_q, int64_t m
   const int64_t tq = ((max_q < 1 ? 1 : max_q) * a.group + own - 1) / own, tk = ((max_k < 1 ? 1 : max_k) + own - 1) / own;
   hipLaunchKernelGGL((attn_dq_kernel<DP, NW, KT, F16>), dim3((unsigned)(tq * groups)), dim3(64 * NW), 0, st, a, w,
                      (int)tq);
-  hipLaunchKernelGGL((attn_dkv_kernel<DP, NW, F16>), dim3((unsigned)(tk * groups)), dim3(64 * NW), 0, st, a, w,
-                     (int)tk);
+  constexpr int NG = NW == 1 ? 1 : 2;
+  hipLaunchKernelGGL((attn_dkv_kernel<DP, NW, NG, F16>), dim3((unsigned)(tk * groups)), dim3(64 * NW * NG), 0, st, a,
+                     w, (int)tk);
 }
 
 template <bool F16>
@@ -340,8 +477,7 @@ int launch_attn_bwd(const AttnArgs& a, int dtype, int64_t max_q, int64_t max_k, 
   w.out = out, w.os = os, w.oh = oh, w.lse = lse, w.dout = dout, w.dos = dos, w.doh = doh;
   w.dq = dq, w.dqs = dqs, w.dqh = dqh, w.dk = dk, w.dks = dks, w.dkh = dkh, w.dv = dv, w.dvs = dvs, w.dvh = dvh;
   w.trow = (int64_t)(((size_t)a.tq + 64 + 63) / 64 * 64);
-  w.lse2 = (float*)ws;
-  w.dlt = w.lse2 + w.trow * a.heads;
+  w.stat = (float*)ws;
   if (dtype == INFCL_F16)
     launch_t<true>(a, w, max_q, max_k, st);
   else

@@ -29,34 +29,56 @@ struct AttnParts {
   int64_t rows;
 };
 
-// Workgroup idx takes rows [32 NW t, +32 NW) of sequence z's group of heads kv,
-// t descending (with causal masks the last rows see most keys), and part
-// `part` of its keys.
+// Row by row (attn.hpp): keys [kbeg, kstop) of the lane's row q, results as the
+// sweep leaves them.
+template <bool F16>
+__device__ __attribute__((noinline)) void attn_fwd_rows(const uint16_t* q, const uint16_t* k, const uint16_t* v,
+                                                        int64_t ks, int64_t vs, int kbeg, int kstop, float scale, int hd,
+                                                        int h, float* po, float* ml, uint16_t* out, float* lse) {
+  const float sl2 = scale * kLog2e;
+  float M = -__builtin_inff(), l = 0.f;
+#pragma unroll 1
+  for (int j = kbeg; j < kstop; ++j) M = fmaxf(M, attn_dot<F16>(q, k + j * ks, h, hd));
+  const float ref = M == -__builtin_inff() ? 0.f : M * sl2;
+#pragma unroll 1
+  for (int j = kbeg; j < kstop; ++j) l += exp2_hw(fmaf(attn_dot<F16>(q, k + j * ks, h, hd), sl2, -ref));
+  const float inv = po ? 1.f : l == 0.f ? 0.f : 1.f / l;
+#pragma unroll 1
+  for (int d = 0; d < hd; d += 16) {
+    float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const int at = d + 8 * h;
+#pragma unroll 1
+    for (int j = kbeg; j < kstop; ++j) {
+      const float p = exp2_hw(fmaf(attn_dot<F16>(q, k + j * ks, h, hd), sl2, -ref));
+      if (at < hd) attn_axpy8<F16>(acc, p, v + j * vs + at);
+    }
+    if (at >= hd) continue;
+    if (po) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) po[at + e] = acc[e];
+    } else {
+      attn_store8<F16>(out + at, acc, inv);
+    }
+  }
+  if (h) return;
+  if (po)
+    ml[0] = l > 0.f || l != l ? ref : -__builtin_inff(), ml[1] = l;
+  else if (lse)
+    *lse = l == 0.f ? -__builtin_inff() : fmaf(M, scale, logf(l));
+}
+
+// One workgroup's tile t of sequence sq's rows (query, head of the group kv), over
+// its part of the keys.  Returns whether the wave's sums were not finite: they
+// may hold what masked rows hold, and its rows are to be taken row by row.
 template <int DP, int NW, int KT, bool F16, bool SPLIT>
-__global__ void __launch_bounds__(64 * NW)
-    attn_fwd_kernel(AttnArgs a, uint16_t* __restrict__ out, int64_t os, int64_t oh, float* __restrict__ lse, int tiles,
-                    int parts, AttnParts pw) {
+__device__ __forceinline__ bool attn_fwd_tile(const AttnArgs& a, uint16_t* __restrict__ out, int64_t os, int64_t oh,
+                                              float* __restrict__ lse, int parts, const AttnParts& pw,
+                                              const AttnSeq& sq, int kv, int part, uint32_t t, uint32_t rows,
+                                              INFCL_LDS char* lds) {
   constexpr int kFb = DP / 32, kI = DP / 16, kKb = KT / 32;
   typedef AttnTile<DP, NW, KT> Tile;
-  __shared__ __attribute__((aligned(1024))) char lds_[4 * Tile::kBytes];
-  __shared__ int redo;
-  INFCL_LDS char* lds = (INFCL_LDS char*)lds_;
   const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int h = lane >> 5;
-
-  uint32_t idx = blockIdx.x;
-  const int part = SPLIT ? (int)(idx % (uint32_t)parts) : 0;
-  if (SPLIT) idx /= (uint32_t)parts;
-  const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
-  const int t0 = tiles - 1 - (int)(idx / groups);
-  const uint32_t gz = idx % groups;
-  const int z = (int)(gz / (uint32_t)a.kvh), kv = (int)(gz % (uint32_t)a.kvh);
-  AttnSeq sq = attn_seq(a, z);
-  if (z == a.nseq) sq.n = 0;
-  const int64_t rows64 = (int64_t)sq.m * a.group;
-  const uint32_t rows = rows64 > 0x7FFFFFFF ? 0x7FFFFFFFu : (uint32_t)rows64;
-  if ((int64_t)t0 * (32 * NW) >= rows) return;
-
   AttnLanes<DP> ln;
   ln.init(lane);
   const uint32_t kst = (uint32_t)(a.ks * 2), vst = (uint32_t)(a.vs * 2);
@@ -70,142 +92,162 @@ __global__ void __launch_bounds__(64 * NW)
   const int kbeg = SPLIT ? (part * per < sq.n ? part * per : sq.n) : 0;
   const int kstop = SPLIT ? (kbeg + per < sq.n ? kbeg + per : sq.n) : sq.n;
 
-  // (one tile, unless sequences are longer than the caller said)
-  for (uint32_t t = (uint32_t)t0; t * (uint64_t)(32 * NW) < rows; t += (uint32_t)tiles) {
-    const uint32_t r = t * (32 * NW) + wave * 32 + (lane & 31);
-    const bool live = r < rows;
-    const int pos = live ? (int)(r / (uint32_t)a.group) : 0, g = live ? (int)(r % (uint32_t)a.group) : 0;
-    const int head = kv * a.group + g;
-    const int64_t token = sq.q0 + pos;
-    bf16x8 qf[kI];
+  const uint32_t r = t * (32 * NW) + wave * 32 + (lane & 31);
+  const bool live = r < rows;
+  const int pos = live ? (int)(r / (uint32_t)a.group) : 0, g = live ? (int)(r % (uint32_t)a.group) : 0;
+  const int head = kv * a.group + g;
+  const int64_t token = sq.q0 + pos;
+  bf16x8 qf[kI];
 #pragma unroll
-    for (int i = 0; i < kI; ++i) qf[i] = attn_own(a.q + token * a.qs + head * a.qh, i, h, a.hd, live);
+  for (int i = 0; i < kI; ++i) qf[i] = attn_own(a.q + token * a.qs + head * a.qh, i, h, a.hd, live);
 
-    // keys [0, lim) are seen by this lane's row; every row of the wave sees
-    // those below wmin, none of the workgroup those from kend on
-    const int shift = sq.n - sq.m + 1;
-    int lim = a.causal ? pos + shift : sq.n;
-    lim = lim < 0 ? 0 : lim;
-    if (!live) lim = 0;
-    const uint32_t rl = t * (uint64_t)(32 * NW) + 32 * NW < rows ? t * (32 * NW) + 32 * NW - 1 : rows - 1;
-    int kend = a.causal ? (int)(rl / (uint32_t)a.group) + shift : sq.n;
-    kend = kend < kstop ? kend : kstop;
-    const uint32_t rw = t * (32 * NW) + wave * 32;  // the wave's first row, and its last
-    const uint32_t rv = rw + 31 < rows ? rw + 31 : rows - 1;
-    const int wmin = rw >= rows ? 0 : a.causal ? (int)(rw / (uint32_t)a.group) + shift : sq.n;
-    const int wmax = rw >= rows ? 0 : a.causal ? (int)(rv / (uint32_t)a.group) + shift : sq.n;
+  // keys [0, lim) are seen by this lane's row; every row of the wave sees
+  // those below wmin, none of the workgroup those from kend on
+  const int shift = sq.n - sq.m + 1;
+  int lim = a.causal ? pos + shift : sq.n;
+  lim = lim < 0 ? 0 : lim;
+  if (!live) lim = 0;
+  const uint32_t rl = t * (uint64_t)(32 * NW) + 32 * NW < rows ? t * (32 * NW) + 32 * NW - 1 : rows - 1;
+  int kend = a.causal ? (int)(rl / (uint32_t)a.group) + shift : sq.n;
+  kend = kend < kstop ? kend : kstop;
+  const uint32_t rw = t * (32 * NW) + wave * 32;  // the wave's first row, and its last
+  const uint32_t rv = rw + 31 < rows ? rw + 31 : rows - 1;
+  const int wmin = rw >= rows ? 0 : a.causal ? (int)(rw / (uint32_t)a.group) + shift : sq.n;
+  const int wmax = rw >= rows ? 0 : a.causal ? (int)(rv / (uint32_t)a.group) + shift : sq.n;
 
-    f32x16 acc[kFb];
-    float M, l;
+  f32x16 acc[kFb];
+#pragma unroll
+  for (int fb = 0; fb < kFb; ++fb) acc[fb] = f32x16_zero();
+  float M = -__builtin_inff(), l = 0.f;
+  attn_barrier();
+  if (kbeg < kend) {
+    Tile::issue(kb + (int64_t)kbeg * a.ks, sq.n - kbeg, kst, a.hd, lds, koff, wave);
+    Tile::issue(vb + (int64_t)kbeg * a.vs, sq.n - kbeg, vst, a.hd, lds + Tile::kBytes, voff, wave);
+  }
+  int buf = 0;
+  for (int k = kbeg; k < kend; k += KT, buf ^= 1) {
     attn_barrier();
-    if (threadIdx.x == 0) redo = 0;
-    for (int exact = 0;; exact = 1) {
-#pragma unroll
-      for (int fb = 0; fb < kFb; ++fb) acc[fb] = f32x16_zero();
-      M = -__builtin_inff(), l = 0.f;
-      if (kbeg < kend) {
-        Tile::issue(kb + (int64_t)kbeg * a.ks, sq.n - kbeg, kst, a.hd, lds, koff, wave);
-        Tile::issue(vb + (int64_t)kbeg * a.vs, sq.n - kbeg, vst, a.hd, lds + Tile::kBytes, voff, wave);
-      }
-      int buf = 0;
-      for (int k = kbeg; k < kend; k += KT, buf ^= 1) {
-        attn_barrier();
-        if (k + KT < kend) {
-          INFCL_LDS char* nx = lds + (buf ^ 1) * 2 * Tile::kBytes;
-          Tile::issue(kb + (int64_t)(k + KT) * a.ks, sq.n - k - KT, kst, a.hd, nx, koff, wave);
-          Tile::issue(vb + (int64_t)(k + KT) * a.vs, sq.n - k - KT, vst, a.hd, nx + Tile::kBytes, voff, wave);
-        }
-        if (k >= wmax) continue;
-        const INFCL_LDS char* kt = lds + buf * 2 * Tile::kBytes;
-        const INFCL_LDS char* vt = kt + Tile::kBytes;
-        f32x16 s[kKb];
-#pragma unroll
-        for (int b = 0; b < kKb; ++b) {
-          s[b] = f32x16_zero();
-#pragma unroll
-          for (int i = 0; i < kI; ++i) s[b] = mfma16<F16>(attn_row(kt + b * 32 * Tile::kRow + ln.row[i]), qf[i], s[b]);
-        }
-        const bool masked = k + KT > wmin;
-        if (masked) {
-#pragma unroll
-          for (int b = 0; b < kKb; ++b)
-#pragma unroll
-            for (int x = 0; x < 16; ++x)
-              if (k + 32 * b + attn_reg_row(x, h) >= lim) s[b][x] = -__builtin_inff();
-        }
-        float top = s[0][0];
-#pragma unroll
-        for (int b = 0; b < kKb; ++b)
-#pragma unroll
-          for (int x = 0; x < 16; ++x) top = fmaxf(top, s[b][x]);
-        top = attn_max2(top);
-        const bool up = top * a.sl2 > M * a.sl2 + kSlack || (M == -__builtin_inff() && top > M);
-        if (wave_any(up)) {
-          const float Mn = up ? top : M;
-          const float f = up && M != -__builtin_inff() ? exp2_hw((M - Mn) * a.sl2) : 1.f;  // (nothing summed yet: 0)
-          M = Mn;
-          l *= f;
-#pragma unroll
-          for (int fb = 0; fb < kFb; ++fb)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) acc[fb][x] *= f;
-        }
-        const float ref = M == -__builtin_inff() ? 0.f : M * a.sl2;
-#pragma unroll
-        for (int b = 0; b < kKb; ++b)
-#pragma unroll
-          for (int x = 0; x < 16; ++x) {
-            s[b][x] = exp2_hw(fmaf(s[b][x], a.sl2, -ref));
-            l += s[b][x];
-          }
-        if (exact && masked) {
-          for (int j = 0; j < KT && k + j < kend; ++j) {
-            const float p = exp2_hw(fmaf(attn_dot<DP, F16>(qf, kt, j, h), a.sl2, -ref));
-            attn_axpy<DP, F16>(acc, p, k + j < lim, vt, j, h);
-          }
-          continue;
-        }
-#pragma unroll
-        for (int b = 0; b < kKb; ++b)
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const bf16x8 p = attn_pack<F16>(s[b], u);
-            const int ro = (32 * b + 16 * u) * Tile::kRow;
-#pragma unroll
-            for (int fb = 0; fb < kFb; ++fb)
-              acc[fb] = mfma16<F16>(attn_tr(vt + ro + ln.tr[0][fb], vt + ro + ln.tr[1][fb]), p, acc[fb]);
-          }
-      }
-      if (!a.causal || exact) break;
-      attn_barrier();
-      if (wave_any(attn_bad(acc)) && lane == 0) redo = 1;
-      attn_barrier();
-      if (!redo) break;
+    if (k + KT < kend) {
+      INFCL_LDS char* nx = lds + (buf ^ 1) * 2 * Tile::kBytes;
+      Tile::issue(kb + (int64_t)(k + KT) * a.ks, sq.n - k - KT, kst, a.hd, nx, koff, wave);
+      Tile::issue(vb + (int64_t)(k + KT) * a.vs, sq.n - k - KT, vst, a.hd, nx + Tile::kBytes, voff, wave);
     }
-    l = attn_sum2(l);
-    if constexpr (SPLIT) {
-      if (!live) continue;
-      const int64_t id = token * a.heads + head;
-      float* po = pw.o + ((int64_t)part * pw.rows + id) * a.hd;
+    if (k >= wmax) continue;
+    const INFCL_LDS char* kt = lds + buf * 2 * Tile::kBytes;
+    const INFCL_LDS char* vt = kt + Tile::kBytes;
+    f32x16 s[kKb];
+#pragma unroll
+    for (int b = 0; b < kKb; ++b) {
+      s[b] = f32x16_zero();
+#pragma unroll
+      for (int i = 0; i < kI; ++i) s[b] = mfma16<F16>(attn_row(kt + b * 32 * Tile::kRow + ln.row[i]), qf[i], s[b]);
+    }
+    const bool masked = k + KT > wmin;
+    if (masked) {
+#pragma unroll
+      for (int b = 0; b < kKb; ++b)
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+          if (k + 32 * b + attn_reg_row(x, h) >= lim) s[b][x] = -__builtin_inff();
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int b = 0; b < kKb; ++b)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) top = fmaxf(top, s[b][x]);
+    top = attn_max2(top);
+    const bool up = top * a.sl2 > M * a.sl2 + kSlack || (M == -__builtin_inff() && top > M);
+    if (wave_any(up)) {
+      const float Mn = up ? top : M;
+      const float f = up && M != -__builtin_inff() ? exp2_hw((M - Mn) * a.sl2) : 1.f;  // (nothing summed yet: 0)
+      M = Mn;
+      l *= f;
 #pragma unroll
       for (int fb = 0; fb < kFb; ++fb)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int d = 32 * fb + 8 * j + 4 * h;
-          if (d < a.hd)
-            *(f32x4*)(po + d) = f32x4{acc[fb][4 * j], acc[fb][4 * j + 1], acc[fb][4 * j + 2], acc[fb][4 * j + 3]};
-        }
-      if (h == 0) {
-        float* ml = pw.ml + ((int64_t)part * pw.rows + id) * 2;
-        ml[0] = l > 0.f || l != l ? M * a.sl2 : -__builtin_inff();
-        ml[1] = l;
-      }
-    } else {
-      if (!live) continue;
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      attn_store<F16>(out + token * os + head * oh, acc, inv, h, a.hd);
-      if (lse && h == 0) lse[(int64_t)head * a.tq + token] = l == 0.f ? -__builtin_inff() : fmaf(M, a.scale, logf(l));
+        for (int x = 0; x < 16; ++x) acc[fb][x] *= f;
     }
+    const float ref = M == -__builtin_inff() ? 0.f : M * a.sl2;
+#pragma unroll
+    for (int b = 0; b < kKb; ++b)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        s[b][x] = exp2_hw(fmaf(s[b][x], a.sl2, -ref));
+        l += s[b][x];
+      }
+#pragma unroll
+    for (int b = 0; b < kKb; ++b)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8 p = attn_pack<F16>(s[b], u);
+        const int ro = (32 * b + 16 * u) * Tile::kRow;
+#pragma unroll
+        for (int fb = 0; fb < kFb; ++fb)
+          acc[fb] = mfma16<F16>(attn_tr(vt + ro + ln.tr[0][fb], vt + ro + ln.tr[1][fb]), p, acc[fb]);
+      }
+  }
+  l = attn_sum2(l);
+  const int64_t id = token * a.heads + head;
+  float* po = SPLIT ? pw.o + ((int64_t)part * pw.rows + id) * a.hd : nullptr;
+  float* ml = SPLIT ? pw.ml + ((int64_t)part * pw.rows + id) * 2 : nullptr;
+  const bool bad = a.causal && wave_any(live && attn_bad(acc));
+  if (!live) return bad;
+  if constexpr (SPLIT) {
+#pragma unroll
+    for (int fb = 0; fb < kFb; ++fb)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int d = 32 * fb + 8 * j + 4 * h;
+        if (d < a.hd)
+          *(f32x4*)(po + d) = f32x4{acc[fb][4 * j], acc[fb][4 * j + 1], acc[fb][4 * j + 2], acc[fb][4 * j + 3]};
+      }
+    if (h == 0) ml[0] = l > 0.f || l != l ? M * a.sl2 : -__builtin_inff(), ml[1] = l;
+  } else {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    attn_store<F16>(out + token * os + head * oh, acc, inv, h, a.hd);
+    if (lse && h == 0) lse[(int64_t)head * a.tq + token] = l == 0.f ? -__builtin_inff() : fmaf(M, a.scale, logf(l));
+  }
+  return bad;
+}
+
+// Workgroup idx takes rows [32 NW t, +32 NW) of sequence z's group of heads kv,
+// t descending (with causal masks the last rows see most keys), and part
+// `part` of its keys.
+template <int DP, int NW, int KT, bool F16, bool SPLIT>
+__global__ void __launch_bounds__(64 * NW, 2)
+    attn_fwd_kernel(AttnArgs a, uint16_t* __restrict__ out, int64_t os, int64_t oh, float* __restrict__ lse, int tiles,
+                    int parts, AttnParts pw) {
+  __shared__ __attribute__((aligned(1024))) char lds[4 * AttnTile<DP, NW, KT>::kBytes];
+  uint32_t idx = blockIdx.x;
+  const int part = SPLIT ? (int)(idx % (uint32_t)parts) : 0;
+  if (SPLIT) idx /= (uint32_t)parts;
+  const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
+  const int t0 = tiles - 1 - (int)(idx / groups);
+  const uint32_t gz = idx % groups;
+  const int z = (int)(gz / (uint32_t)a.kvh), kv = (int)(gz % (uint32_t)a.kvh);
+  AttnSeq sq = attn_seq(a, z);
+  if (z == a.nseq) sq.n = 0;
+  const int64_t rows64 = (int64_t)sq.m * a.group;
+  const uint32_t rows = rows64 > 0x7FFFFFFF ? 0x7FFFFFFFu : (uint32_t)rows64;
+  // (one tile, unless sequences are longer than the caller said)
+  bool bad = false;
+  for (uint32_t t = (uint32_t)t0; t * (uint64_t)(32 * NW) < rows; t += (uint32_t)tiles)
+    bad |= attn_fwd_tile<DP, NW, KT, F16, SPLIT>(a, out, os, oh, lse, parts, pw, sq, kv, part, t, rows,
+                                                 (INFCL_LDS char*)lds);
+  if (!bad) return;
+  wait_dma();  // (the stores of these rows are done: other lanes write them again)
+  const int h = (threadIdx.x >> 5) & 1;
+  const int per = SPLIT ? ((sq.n + parts - 1) / parts + KT - 1) / KT * KT : sq.n;
+  for (uint64_t r = (uint64_t)t0 * (32 * NW) + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31); r < rows;
+       r += (uint64_t)tiles * (32 * NW)) {
+    const int pos = (int)((uint32_t)r / (uint32_t)a.group), head = kv * a.group + (int)((uint32_t)r % (uint32_t)a.group);
+    const int64_t token = sq.q0 + pos, id = token * a.heads + head;
+    const int lim = pos + sq.n - sq.m + 1, kbeg = part * per, kend = kbeg + per < sq.n ? kbeg + per : sq.n;
+    attn_fwd_rows<F16>(a.q + token * a.qs + head * a.qh, a.k + sq.k0 * a.ks + kv * a.kh, a.v + sq.k0 * a.vs + kv * a.vh,
+                       a.ks, a.vs, kbeg, lim < kend ? lim : kend, a.scale, a.hd, h,
+                       SPLIT ? pw.o + ((int64_t)part * pw.rows + id) * a.hd : nullptr,
+                       SPLIT ? pw.ml + ((int64_t)part * pw.rows + id) * 2 : nullptr, out + token * os + head * oh,
+                       lse ? lse + (int64_t)head * a.tq + token : nullptr);
   }
 }
 
