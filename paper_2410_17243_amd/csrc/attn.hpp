@@ -40,6 +40,14 @@ struct AttnFwdPlan {
   size_t o, ml, total;
 };
 
+// ... and a backward call.
+struct AttnBwdPlan {
+  bool few;
+  int parts;     // of the sweeps over queries
+  int64_t trow;  // pairs of a head in stat
+  size_t stat, part, total;
+};
+
 // Sequence z's queries [q0, q0 + m) and keys [k0, k0 + n), cut to the arrays
 // whatever the offsets say.  z = nseq: the rows past the last sequence, as
 // queries without keys (or keys without queries).

@@ -5,11 +5,11 @@ namespace infcl {
 AttnFwdPlan attn_fwd_plan(const AttnArgs& a, int64_t max_q, int64_t max_k);
 int launch_attn_fwd(const AttnArgs& a, const AttnFwdPlan& p, int dtype, uint16_t* out, int64_t os, int64_t oh,
                     float* lse, char* ws, hipStream_t st);
-size_t attn_bwd_bytes(const AttnArgs& a);
-int launch_attn_bwd(const AttnArgs& a, int dtype, int64_t max_q, int64_t max_k, const uint16_t* out, int64_t os,
-                    int64_t oh, const float* lse, const uint16_t* dout, int64_t dos, int64_t doh, uint16_t* dq,
-                    int64_t dqs, int64_t dqh, uint16_t* dk, int64_t dks, int64_t dkh, uint16_t* dv, int64_t dvs,
-                    int64_t dvh, char* ws, hipStream_t st);
+AttnBwdPlan attn_bwd_plan(const AttnArgs& a, int64_t max_q, int64_t max_k);
+int launch_attn_bwd(const AttnArgs& a, const AttnBwdPlan& p, int dtype, int64_t max_q, int64_t max_k,
+                    const uint16_t* out, int64_t os, int64_t oh, const float* lse, const uint16_t* dout, int64_t dos,
+                    int64_t doh, uint16_t* dq, int64_t dqs, int64_t dqh, uint16_t* dk, int64_t dks, int64_t dkh,
+                    uint16_t* dv, int64_t dvs, int64_t dvh, char* ws, hipStream_t st);
 }  // namespace infcl
 
 using namespace infcl;
@@ -71,7 +71,7 @@ extern "C" infcl_status infcl_attn_workspace(const infcl_attn_shape* s, size_t* 
   const infcl_attn_view none = {nullptr, 0, 0};
   const AttnArgs a = args_of(s, none, none, none, nullptr, nullptr);
   if (fwd_bytes) *fwd_bytes = attn_fwd_plan(a, least(s->max_q, s->total_q), least(s->max_k, s->total_k)).total;
-  if (bwd_bytes) *bwd_bytes = attn_bwd_bytes(a);
+  if (bwd_bytes) *bwd_bytes = attn_bwd_plan(a, least(s->max_q, s->total_q), least(s->max_k, s->total_k)).total;
   return fwd_bytes || bwd_bytes ? INFCL_OK : INFCL_ERR_INVALID;
 }
 
@@ -112,9 +112,11 @@ extern "C" infcl_status infcl_attn_bwd(const infcl_attn_shape* s, infcl_attn_vie
       !view_supported(dout) || !view_supported(dq) || !view_supported(dk) || !view_supported(dv))
     return INFCL_ERR_UNSUPPORTED;
   const AttnArgs a = args_of(s, q, k, v, cu_q, cu_k);
-  if (ws_bytes < attn_bwd_bytes(a)) return INFCL_ERR_WORKSPACE;
+  const int64_t mq = least(s->max_q, s->total_q), mk = least(s->max_k, s->total_k);
+  const AttnBwdPlan p = attn_bwd_plan(a, mq, mk);
+  if (ws_bytes < p.total) return INFCL_ERR_WORKSPACE;
   return (infcl_status)launch_attn_bwd(
-      a, s->dtype, least(s->max_q, s->total_q), least(s->max_k, s->total_k), (const uint16_t*)out.data,
+      a, p, s->dtype, mq, mk, (const uint16_t*)out.data,
       out.token_stride, out.head_stride, lse, (const uint16_t*)dout.data, dout.token_stride, dout.head_stride,
       (uint16_t*)dq.data, dq.token_stride, dq.head_stride, (uint16_t*)dk.data, dk.token_stride, dk.head_stride,
       (uint16_t*)dv.data, dv.token_stride, dv.head_stride, (char*)workspace, (hipStream_t)stream);

@@ -20,12 +20,15 @@
 namespace infcl {
 namespace {
 
+constexpr int64_t kBwdGroups = 768;  // workgroups that the sweeps over queries are cut into, about
+
 struct AttnGrads {
   const uint16_t *out, *dout;
   int64_t os, oh, dos, doh;
   const float* lse;
   float* stat;  // [heads][trow][2]: lse log2(e), D; 32 entries past the tokens may be read
   int64_t trow;
+  float* part;  // [parts][dk, dv][tokens][kvh][hd]: sums of parts of the sweeps
   uint16_t *dq, *dk, *dv;
   int64_t dqs, dqh, dks, dkh, dvs, dvh;
 };
@@ -240,29 +243,31 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGra
   }
 }
 
-// Owns 32 NW keys; sweeps the queries that see them, one head of the group after
-// another.  NG groups of NW waves own the same keys and take every NG-th tile of
-// queries each: the sweep of one workgroup, which is the longest chain of a call
-// (all heads of the group times all later queries), is NG times shorter, and the
-// groups' sums are added through LDS at its end.
-// At 128 features the own keys, the two sums and a tile's weights fill the
-// registers of two waves per SIMD: the own values stay in LDS there (a fifth of
-// the sweep's LDS reads), for a register spilled in the sweep costs far more (its
-// reload waits for the tile copies in flight).
-template <int DP, int NW, int NG, bool F16>
-__global__ void __launch_bounds__(64 * NW * NG, 2) attn_dkv_kernel(AttnArgs a, AttnGrads w, int tiles) {
+// Owns 32 NW keys; sweeps the queries that see them, of all heads of the group:
+// tiles from the last queries down, the heads of a tile one after another.  All
+// workgroups of a sequence's key head begin with the same tiles that way and go
+// through them together, so that the copies find them in L2.
+// At 128 features the own rows, the two sums and a tile's weights are more than
+// the registers of two waves per SIMD: the own values stay in LDS there (a fifth
+// of the sweep's LDS reads), for a register spilled in the sweep costs far more
+// (its reload waits for the tile copies in flight).
+// SPLIT: a workgroup takes one of several parts of the tiles and leaves its sums in
+// fp32 for attn_dkv_join.
+template <int DP, int NW, bool F16, bool SPLIT>
+__global__ void __launch_bounds__(64 * NW, 2) attn_dkv_kernel(AttnArgs a, AttnGrads w, int tiles, int parts) {
   constexpr int kFb = DP / 32, kI = DP / 16, QT = 32;
   constexpr bool kVLds = DP == 128;
   typedef AttnTile<DP, NW, QT> Tile;
-  typedef AttnTile<DP, NW * NG, 32 * NW> Own;
-  __shared__ __attribute__((aligned(1024))) char lds_[4 * NG * Tile::kBytes + (kVLds ? Own::kBytes : 0)];
-  __shared__ __attribute__((aligned(16))) float stat_[NW * NG][64];  // a tile's pairs of lse log2(e) and D
+  typedef AttnTile<DP, NW, 32 * NW> Own;
+  __shared__ __attribute__((aligned(1024))) char lds_[4 * Tile::kBytes + (kVLds ? Own::kBytes : 0)];
+  __shared__ __attribute__((aligned(16))) float stat_[NW][64];  // a tile's pairs of lse log2(e) and D
   INFCL_LDS char* lds = (INFCL_LDS char*)lds_;
-  const int wave = NW * NG == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int h = lane >> 5, wk = wave % NW, grp = wave / NW;
+  const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int h = lane >> 5;
   INFCL_LDS float* stat = (INFCL_LDS float*)stat_[wave];
   const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
-  const int t0 = (int)(blockIdx.x / groups);
+  // (longest sweeps first: the first keys' parts)
+  const int t0 = (int)(blockIdx.x / groups) / (SPLIT ? parts : 1), part = SPLIT ? (int)(blockIdx.x / groups) % parts : 0;
   const uint32_t gz = blockIdx.x % groups;
   const int z = (int)(gz / (uint32_t)a.kvh), kv = (int)(gz % (uint32_t)a.kvh);
   AttnSeq sq = attn_seq(a, z);
@@ -273,15 +278,15 @@ __global__ void __launch_bounds__(64 * NW * NG, 2) attn_dkv_kernel(AttnArgs a, A
   ln.init(lane);
   const uint32_t qst = (uint32_t)(a.qs * 2), dst = (uint32_t)(w.dos * 2);
   uint32_t qoff[Tile::kVar], doff[Tile::kVar];
-  Tile::offsets(qoff, wk, lane, qst, a.hd);
-  Tile::offsets(doff, wk, lane, dst, a.hd);
+  Tile::offsets(qoff, wave, lane, qst, a.hd);
+  Tile::offsets(doff, wave, lane, dst, a.hd);
 
   bool bad = false;  // this wave's sums may hold what masked rows hold
   for (int64_t t = t0; t * (32 * NW) < sq.n; t += tiles) {
-    const int key0 = (int)(t * (32 * NW)), kw = key0 + 32 * wk;
+    const int key0 = (int)(t * (32 * NW)), kw = key0 + 32 * wave;
     bf16x8 kf[kI], vf[kVLds ? 1 : kI];
     const int shift = sq.n - sq.m;
-    int first;  // queries from here on see this lane's key
+    const int first = a.causal ? kw + (lane & 31) - shift : 0;  // queries from here on see this lane's key
     {
       const int key = kw + (lane & 31);
       const bool live = key < sq.n;
@@ -291,7 +296,6 @@ __global__ void __launch_bounds__(64 * NW * NG, 2) attn_dkv_kernel(AttnArgs a, A
         kf[i] = attn_own(a.k + token * a.ks + kv * a.kh, i, h, a.hd, live);
         if constexpr (!kVLds) vf[i] = attn_own(a.v + token * a.vs + kv * a.vh, i, h, a.hd, live);
       }
-      first = a.causal ? key - shift : 0;
     }
     // from wall on all the wave's keys; none before qbeg sees one of the workgroup's
     const int wall = a.causal ? kw + 31 - shift : 0, wany = a.causal ? kw - shift : 0;
@@ -300,60 +304,51 @@ __global__ void __launch_bounds__(64 * NW * NG, 2) attn_dkv_kernel(AttnArgs a, A
 
     f32x16 dk[kFb], dv[kFb];
     attn_barrier();
-    const INFCL_LDS char* own = lds + 4 * NG * Tile::kBytes + wk * 32 * Tile::kRow;
+    const INFCL_LDS char* vown = lds + 4 * Tile::kBytes + wave * 32 * Tile::kRow;
     if constexpr (kVLds) {
       uint32_t off[Own::kVar];
       Own::offsets(off, wave, lane, (uint32_t)(a.vs * 2), a.hd);
       Own::issue(a.v + (sq.k0 + key0) * a.vs + kv * a.vh, sq.n - key0, (uint32_t)(a.vs * 2), a.hd,
-                 lds + 4 * NG * Tile::kBytes, off, wave);
+                 lds + 4 * Tile::kBytes, off, wave);
     }
 #pragma unroll
     for (int fb = 0; fb < kFb; ++fb) dk[fb] = f32x16_zero(), dv[fb] = f32x16_zero();
-    // tiles of all heads of the group, as one sequence; this group's are grp, grp + NG, ..
+    // this part's tiles [c0, c1): tile c is head c % group of queries qbeg + QT (per - 1 - c / group) on
     const int per = sq.m > qbeg ? (sq.m - qbeg + QT - 1) / QT : 0;
-    const int64_t count = (int64_t)per * a.group;
-    INFCL_LDS char* mylds = lds + grp * 4 * Tile::kBytes;
+    int64_t c0 = 0, c1 = (int64_t)per * a.group;
+    if (SPLIT) {
+      const int64_t share = (c1 + parts - 1) / parts;
+      c0 = share * part < c1 ? share * part : c1;
+      c1 = c0 + share < c1 ? c0 + share : c1;
+    }
     // the lanes fetch a tile's 32 pairs a tile ahead
     const float* row = w.stat + sq.q0 * 2;
     float ahead = 0.f;
-    int g = 0, i0 = qbeg;  // the tile in hand, then the next
-    auto step = [&]() {
-      i0 += NG * QT;
-      while (i0 >= qbeg + per * QT && g < a.group) i0 -= per * QT, ++g;
-    };
+    int g = (int)(c0 % a.group), i0 = qbeg + QT * (per - 1 - (int)(c0 / a.group));  // the tile in hand, then the next
     auto issue = [&](int b) {
       const int head = kv * a.group + g;
-      INFCL_LDS char* to = mylds + b * 2 * Tile::kBytes;
-      Tile::issue(a.q + (sq.q0 + i0) * a.qs + head * a.qh, sq.m - i0, qst, a.hd, to, qoff, wk);
-      Tile::issue(w.dout + (sq.q0 + i0) * w.dos + head * w.doh, sq.m - i0, dst, a.hd, to + Tile::kBytes, doff, wk);
+      INFCL_LDS char* to = lds + b * 2 * Tile::kBytes;
+      Tile::issue(a.q + (sq.q0 + i0) * a.qs + head * a.qh, sq.m - i0, qst, a.hd, to, qoff, wave);
+      Tile::issue(w.dout + (sq.q0 + i0) * w.dos + head * w.doh, sq.m - i0, dst, a.hd, to + Tile::kBytes, doff, wave);
       ahead = row[((int64_t)head * w.trow + i0) * 2 + lane];
     };
-    if (count) {
-      i0 += grp * QT;
-      while (i0 >= qbeg + per * QT && g < a.group) i0 -= per * QT, ++g;
-      if (g < a.group) issue(0);
-    }
+    if (c0 < c1) issue(0);
     int buf = 0;
-    for (int64_t c = 0; c < count; c += NG, buf ^= 1) {
+    for (int64_t c = c0; c < c1; ++c, buf ^= 1) {
       const int i1 = i0;
-      const bool none = g >= a.group || i1 + QT <= wany || kw >= sq.n;  // (no query of the tile sees a key of this wave)
+      const bool none = i1 + QT <= wany || kw >= sq.n;  // (no query of the tile sees a key of this wave)
       stat[lane] = ahead;
-      step();
+      if (++g == a.group) g = 0, i0 -= QT;
       attn_barrier();
-      if (g < a.group) issue(buf ^ 1);
+      if (c + 1 < c1) issue(buf ^ 1);
       if (none) continue;
-      const INFCL_LDS char* qt = mylds + buf * 2 * Tile::kBytes;
+      const INFCL_LDS char* qt = lds + buf * 2 * Tile::kBytes;
       const INFCL_LDS char* dt = qt + Tile::kBytes;
       f32x16 p = f32x16_zero(), dp = f32x16_zero();
 #pragma unroll
-      for (int i = 0; i < kI; ++i) p = mfma16<F16>(attn_row(qt + ln.row[i]), kf[i], p);
-      if constexpr (kVLds) __builtin_amdgcn_sched_barrier(0);  // (fewer fragments held at a time)
-#pragma unroll
       for (int i = 0; i < kI; ++i) {
-        if constexpr (kVLds)
-          dp = mfma16<F16>(attn_row(dt + ln.row[i]), attn_row(own + ln.row[i]), dp);
-        else
-          dp = mfma16<F16>(attn_row(dt + ln.row[i]), vf[i], dp);
+        p = mfma16<F16>(attn_row(qt + ln.row[i]), kf[i], p);
+        dp = mfma16<F16>(attn_row(dt + ln.row[i]), kVLds ? attn_row(vown + ln.row[i]) : vf[kVLds ? 0 : i], dp);
       }
       const bool masked = i1 < wall || i1 + QT > sq.m;
 #pragma unroll
@@ -388,37 +383,30 @@ __global__ void __launch_bounds__(64 * NW * NG, 2) attn_dkv_kernel(AttnArgs a, A
         }
       }
     }
-    if constexpr (NG == 2) {
-      INFCL_LDS float* red = (INFCL_LDS float*)lds + wk * kFb * 16 * 64 + lane;
-      static_assert(NW * kFb * 16 * 64 * 4 <= 4 * NG * Tile::kBytes, "room");
-#pragma unroll
-      for (int both = 0; both < 2; ++both) {
-        f32x16(&acc)[kFb] = both ? dv : dk;
-        attn_barrier();
-        if (grp) {
-#pragma unroll
-          for (int fb = 0; fb < kFb; ++fb)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) red[(fb * 16 + x) * 64] = acc[fb][x];
-        }
-        attn_barrier();
-        if (!grp) {
-#pragma unroll
-          for (int fb = 0; fb < kFb; ++fb)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) acc[fb][x] += red[(fb * 16 + x) * 64];
-        }
-      }
-    }
     int own_lane = threadIdx.x & 63;
     asm volatile("" : "+v"(own_lane));  // (addresses made here, not kept through the sweep)
     const int own_key = kw + (own_lane & 31);
-    const bool mine = own_key < sq.n && grp == 0;
-    bad |= a.causal && wave_any(mine && (attn_bad(dk) || attn_bad(dv)));
-    if (!mine) continue;
+    const bool mine = own_key < sq.n;
     const int64_t at = sq.k0 + own_key;
-    attn_store<F16>(w.dk + at * w.dks + kv * w.dkh, dk, a.scale, own_lane >> 5, a.hd);
-    attn_store<F16>(w.dv + at * w.dvs + kv * w.dvh, dv, 1.f, own_lane >> 5, a.hd);
+    if constexpr (SPLIT) {
+      if (!mine) continue;
+      const int64_t rows = a.tk * a.kvh;
+      float* pk = w.part + ((int64_t)part * 2 * rows + at * a.kvh + kv) * a.hd;
+#pragma unroll
+      for (int fb = 0; fb < kFb; ++fb)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int d = 32 * fb + 8 * j + 4 * (own_lane >> 5);
+          if (d >= a.hd) continue;
+          *(f32x4*)(pk + d) = f32x4{dk[fb][4 * j], dk[fb][4 * j + 1], dk[fb][4 * j + 2], dk[fb][4 * j + 3]};
+          *(f32x4*)(pk + rows * a.hd + d) = f32x4{dv[fb][4 * j], dv[fb][4 * j + 1], dv[fb][4 * j + 2], dv[fb][4 * j + 3]};
+        }
+    } else {
+      bad |= a.causal && wave_any(mine && (attn_bad(dk) || attn_bad(dv)));
+      if (!mine) continue;
+      attn_store<F16>(w.dk + at * w.dks + kv * w.dkh, dk, a.scale, own_lane >> 5, a.hd);
+      attn_store<F16>(w.dv + at * w.dvs + kv * w.dvh, dv, 1.f, own_lane >> 5, a.hd);
+    }
   }
   if (!bad) return;
   wait_dma();  // (the stores of these rows are done: other lanes write them again)
@@ -434,54 +422,125 @@ __global__ void __launch_bounds__(64 * NW * NG, 2) attn_dkv_kernel(AttnArgs a, A
   }
 }
 
+// The parts' dk and dv, in order.  A wave takes 32 rows of one sequence's key head,
+// 16 lanes to a row; if one of them is not finite, all again row by row.
+template <bool F16>
+__global__ void __launch_bounds__(256) attn_dkv_join(AttnArgs a, AttnGrads w, int tiles, int parts) {
+  const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
+  const uint32_t gz = blockIdx.x % groups;
+  const int z = (int)(gz / (uint32_t)a.kvh), kv = (int)(gz % (uint32_t)a.kvh);
+  AttnSeq sq = attn_seq(a, z);
+  if (z == a.nseq) sq.m = 0;
+  const int lane = threadIdx.x & 63, d = 8 * (lane & 15);
+  const int64_t step = a.tk * a.kvh * a.hd;  // from dk to dv of a part, and on to the next part's dk
+  for (int64_t key0 = (int64_t)(blockIdx.x / groups) * 128 + (threadIdx.x >> 6) * 32; key0 < sq.n;
+       key0 += (int64_t)tiles * 128) {
+    float sum = 0.f;
+    for (int r = lane >> 4; r < 32; r += 4) {
+      const int64_t token = sq.k0 + key0 + r;
+      if (key0 + r >= sq.n || d >= a.hd) continue;
+      const float* src = w.part + (token * a.kvh + kv) * a.hd + d;
+      float ak[8] = {0, 0, 0, 0, 0, 0, 0, 0}, av[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 4
+      for (int p = 0; p < parts; ++p) {
+        const f32x4 *x = (const f32x4*)(src + 2 * p * step), *y = (const f32x4*)(src + (2 * p + 1) * step);
+        const f32x4 x0 = x[0], x1 = x[1], y0 = y[0], y1 = y[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ak[e] += x0[e], ak[4 + e] += x1[e], av[e] += y0[e], av[4 + e] += y1[e];
+      }
+      attn_store8<F16>(w.dk + token * w.dks + kv * w.dkh + d, ak, a.scale);
+      attn_store8<F16>(w.dv + token * w.dvs + kv * w.dvh + d, av, 1.f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf(ak[e], 0.f, fmaf(av[e], 0.f, sum));
+    }
+    if (!a.causal || !wave_any(!(sum == 0.f))) continue;
+    wait_dma();  // (the stores of these rows are done: other lanes write them again)
+    const int64_t key = key0 + (lane & 31), token = sq.k0 + key;
+    const int h0 = kv * a.group;
+    if (key < sq.n)
+      attn_dkv_rows<F16>(a.k + token * a.ks + kv * a.kh, a.v + token * a.vs + kv * a.vh, a.q + sq.q0 * a.qs + h0 * a.qh,
+                         w.dout + sq.q0 * w.dos + h0 * w.doh, a.qs, a.qh, w.dos, w.doh,
+                         w.stat + (h0 * w.trow + sq.q0) * 2, w.trow, (int)key - (sq.n - sq.m), sq.m, a.group, a.scale,
+                         a.hd, lane >> 5, w.dk + token * w.dks + kv * w.dkh, w.dv + token * w.dvs + kv * w.dvh);
+  }
+}
+
 template <int DP, bool F16, int NW, int KT>
-void launch_both(const AttnArgs& a, const AttnGrads& w, int64_t max_q, int64_t max_k, hipStream_t st) {
-  const int64_t groups = (int64_t)(a.nseq + 1) * a.kvh, own = 32 * NW;
-  const int64_t tq = ((max_q < 1 ? 1 : max_q) * a.group + own - 1) / own, tk = ((max_k < 1 ? 1 : max_k) + own - 1) / own;
+void launch_both(const AttnArgs& a, const AttnGrads& w, const AttnBwdPlan& p, int64_t max_q, int64_t max_k,
+                 hipStream_t st) {
+  const int64_t groups = (int64_t)(a.nseq + 1) * a.kvh;
+  const int64_t tq = ((max_q < 1 ? 1 : max_q) * a.group + 32 * NW - 1) / (32 * NW);
+  const int64_t tk = ((max_k < 1 ? 1 : max_k) + 32 * NW - 1) / (32 * NW);
   hipLaunchKernelGGL((attn_dq_kernel<DP, NW, KT, F16>), dim3((unsigned)(tq * groups)), dim3(64 * NW), 0, st, a, w,
                      (int)tq);
-  constexpr int NG = NW == 1 ? 1 : 2;
-  hipLaunchKernelGGL((attn_dkv_kernel<DP, NW, NG, F16>), dim3((unsigned)(tk * groups)), dim3(64 * NW * NG), 0, st, a,
-                     w, (int)tk);
+  const dim3 grid((unsigned)(tk * groups * p.parts));
+  if (p.parts == 1) {
+    hipLaunchKernelGGL((attn_dkv_kernel<DP, NW, F16, false>), grid, dim3(64 * NW), 0, st, a, w, (int)tk, 1);
+  } else if constexpr (NW > 1) {
+    hipLaunchKernelGGL((attn_dkv_kernel<DP, NW, F16, true>), grid, dim3(64 * NW), 0, st, a, w, (int)tk, p.parts);
+    hipLaunchKernelGGL((attn_dkv_join<F16>), dim3((unsigned)(tk * groups)), dim3(256), 0, st, a, w, (int)tk, p.parts);
+  }
 }
 
 template <bool F16>
-void launch_t(const AttnArgs& a, const AttnGrads& w, int64_t max_q, int64_t max_k, hipStream_t st) {
-  // as in the forward: short sequences run one wave to a workgroup
-  const bool few = max_q * a.group <= 128 && max_k <= 128;
+void launch_t(const AttnArgs& a, const AttnGrads& w, const AttnBwdPlan& p, int64_t max_q, int64_t max_k,
+              hipStream_t st) {
   if (a.hd <= 64) {
-    if (few)
-      launch_both<64, F16, 1, 32>(a, w, max_q, max_k, st);
+    if (p.few)
+      launch_both<64, F16, 1, 32>(a, w, p, max_q, max_k, st);
     else
-      launch_both<64, F16, 4, 64>(a, w, max_q, max_k, st);
+      launch_both<64, F16, 4, 64>(a, w, p, max_q, max_k, st);
   } else {
-    if (few)
-      launch_both<128, F16, 1, 32>(a, w, max_q, max_k, st);
+    if (p.few)
+      launch_both<128, F16, 1, 32>(a, w, p, max_q, max_k, st);
     else
-      launch_both<128, F16, 4, 32>(a, w, max_q, max_k, st);
+      launch_both<128, F16, 4, 32>(a, w, p, max_q, max_k, st);
   }
 }
 
 }  // namespace
 
-size_t attn_bwd_bytes(const AttnArgs& a) {
-  const size_t row = ((size_t)a.tq + 64 + 63) / 64 * 64;
-  return 2 * row * (size_t)a.heads * sizeof(float) + 256;
+// As in the forward, short sequences run one wave to a workgroup.  Otherwise the
+// sweeps of the key tiles are cut into parts where there are fewer than two
+// workgroups for a compute unit: their lengths differ (with causal masks from
+// none to all queries), and one long sweep would be waited for.
+AttnBwdPlan attn_bwd_plan(const AttnArgs& a, int64_t max_q, int64_t max_k) {
+  AttnBwdPlan p;
+  p.few = max_q * a.group <= 128 && max_k <= 128;
+  p.parts = 1;
+  if (!p.few) {
+    const int64_t most = a.nseq * ((max_k + 127) / 128), about = a.tk / 128 + a.nseq;
+    const int64_t wgs = (most < about ? most : about) * a.kvh;
+    const int64_t sweep = (max_q + 31) / 32 * a.group;  // tiles of the longest
+    int64_t parts = wgs > 0 ? (kBwdGroups + wgs - 1) / wgs : 1;
+    if (parts > sweep / 16) parts = sweep / 16;
+    if (parts > 16) parts = 16;
+    p.parts = (int)(parts < 1 ? 1 : parts);
+  }
+  const size_t row = ((size_t)a.tq + 32 + 63) / 64 * 64;
+  size_t off = 0;
+  p.trow = (int64_t)row;
+  p.stat = off, off = (off + 2 * row * (size_t)a.heads * sizeof(float) + 255) & ~(size_t)255;
+  p.part = off;
+  if (p.parts > 1) off += 2 * (size_t)p.parts * (size_t)a.tk * (size_t)a.kvh * (size_t)a.hd * sizeof(float);
+  p.total = (off + 255) & ~(size_t)255;
+  return p;
 }
 
-int launch_attn_bwd(const AttnArgs& a, int dtype, int64_t max_q, int64_t max_k, const uint16_t* out, int64_t os,
-                    int64_t oh, const float* lse, const uint16_t* dout, int64_t dos, int64_t doh, uint16_t* dq,
-                    int64_t dqs, int64_t dqh, uint16_t* dk, int64_t dks, int64_t dkh, uint16_t* dv, int64_t dvs,
-                    int64_t dvh, char* ws, hipStream_t st) {
+int launch_attn_bwd(const AttnArgs& a, const AttnBwdPlan& p, int dtype, int64_t max_q, int64_t max_k,
+                    const uint16_t* out, int64_t os, int64_t oh, const float* lse, const uint16_t* dout, int64_t dos,
+                    int64_t doh, uint16_t* dq, int64_t dqs, int64_t dqh, uint16_t* dk, int64_t dks, int64_t dkh,
+                    uint16_t* dv, int64_t dvs, int64_t dvh, char* ws, hipStream_t st) {
   AttnGrads w;
   w.out = out, w.os = os, w.oh = oh, w.lse = lse, w.dout = dout, w.dos = dos, w.doh = doh;
   w.dq = dq, w.dqs = dqs, w.dqh = dqh, w.dk = dk, w.dks = dks, w.dkh = dkh, w.dv = dv, w.dvs = dvs, w.dvh = dvh;
-  w.trow = (int64_t)(((size_t)a.tq + 64 + 63) / 64 * 64);
-  w.stat = (float*)ws;
+  w.trow = p.trow;
+  w.stat = (float*)(ws + p.stat);
+  w.part = (float*)(ws + p.part);
   if (dtype == INFCL_F16)
-    launch_t<true>(a, w, max_q, max_k, st);
+    launch_t<true>(a, w, p, max_q, max_k, st);
   else
-    launch_t<false>(a, w, max_q, max_k, st);
+    launch_t<false>(a, w, p, max_q, max_k, st);
   return hipGetLastError() == hipSuccess ? INFCL_OK : INFCL_ERR_HIP;
 }
 
