@@ -67,6 +67,22 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs& a, int z) {
   return s;
 }
 
+// Workgroup idx of a grid of `tiles` tiles for each of `groups` (sequence, key head)
+// pairs: tile t, 0 the first to run, of pair g.  With many pairs a pair's tiles
+// follow one another on one XCD, whose L2 then holds what they share; with few,
+// all first tiles come first (the longest, where lengths differ by tile), spread
+// over the XCDs, so that none of them is left waiting.
+constexpr uint32_t kAttnManyGroups = 64;
+struct AttnPlace {
+  uint32_t t, g;
+};
+__host__ __device__ __forceinline__ AttnPlace attn_place(uint32_t idx, uint32_t tiles, uint32_t groups) {
+  if (groups < kAttnManyGroups) return AttnPlace{idx / groups, idx % groups};
+  const uint32_t even = groups & ~7u;
+  if (idx < even * tiles) return AttnPlace{(idx >> 3) % tiles, (idx >> 3) / tiles * 8 + (idx & 7)};
+  return AttnPlace{(idx - even * tiles) % tiles, even + (idx - even * tiles) / tiles};
+}
+
 template <int DP>
 __host__ __device__ __forceinline__ int attn_sw(int r) {
   return DP == 128 ? 4 * (r & 3) + ((r >> 2) & 3) : 4 * ((r >> 1) & 1) + ((r >> 2) & 3);
@@ -150,6 +166,13 @@ __device__ __forceinline__ bf16x8 attn_pack(const f32x16& x, int t) {
     r = __builtin_bit_cast(bf16x8, w);
   }
   return r;
+}
+
+// x, as a value the compiler knows nothing of (a comparison with it is one
+// instruction, not one for each of the conditions it came from).
+__device__ __forceinline__ int attn_opaque(int x) {
+  asm("" : "+v"(x));
+  return x;
 }
 
 // x of this lane and of lane ^ 32.

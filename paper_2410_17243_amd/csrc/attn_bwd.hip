@@ -102,9 +102,9 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGra
   const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int h = lane >> 5;
   const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
-  const int t0 = tiles - 1 - (int)(blockIdx.x / groups);
-  const uint32_t gz = blockIdx.x % groups;
-  const int z = (int)(gz / (uint32_t)a.kvh), kv = (int)(gz % (uint32_t)a.kvh);
+  const AttnPlace at = attn_place(blockIdx.x, (uint32_t)tiles, groups);
+  const int t0 = tiles - 1 - (int)at.t;
+  const int z = (int)(at.g / (uint32_t)a.kvh), kv = (int)(at.g % (uint32_t)a.kvh);
   AttnSeq sq = attn_seq(a, z);
   if (z == a.nseq) sq.n = 0;
   const int64_t rows64 = (int64_t)sq.m * a.group;
@@ -267,9 +267,9 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dkv_kernel(AttnArgs a, AttnGr
   INFCL_LDS float* stat = (INFCL_LDS float*)stat_[wave];
   const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
   // (longest sweeps first: the first keys' parts)
-  const int t0 = (int)(blockIdx.x / groups) / (SPLIT ? parts : 1), part = SPLIT ? (int)(blockIdx.x / groups) % parts : 0;
-  const uint32_t gz = blockIdx.x % groups;
-  const int z = (int)(gz / (uint32_t)a.kvh), kv = (int)(gz % (uint32_t)a.kvh);
+  const AttnPlace where = attn_place(blockIdx.x, (uint32_t)(tiles * parts), groups);
+  const int t0 = (int)where.t / (SPLIT ? parts : 1), part = SPLIT ? (int)where.t % parts : 0;
+  const int z = (int)(where.g / (uint32_t)a.kvh), kv = (int)(where.g % (uint32_t)a.kvh);
   AttnSeq sq = attn_seq(a, z);
   if (z == a.nseq) sq.m = 0;
   if ((int64_t)t0 * (32 * NW) >= sq.n) return;

@@ -135,20 +135,40 @@ __device__ __forceinline__ bool attn_fwd_tile(const AttnArgs& a, uint16_t* __res
     if (k >= wmax) continue;
     const INFCL_LDS char* kt = lds + buf * 2 * Tile::kBytes;
     const INFCL_LDS char* vt = kt + Tile::kBytes;
+    // All row fragments first, then the products, and the transposed fragments of
+    // the second product while the weights are formed: left to itself the compiler
+    // waits for each LDS read right before its product.
+    bf16x8 kf[kKb][kI];
+#pragma unroll
+    for (int b = 0; b < kKb; ++b)
+#pragma unroll
+      for (int i = 0; i < kI; ++i) kf[b][i] = attn_row(kt + b * 32 * Tile::kRow + ln.row[i]);
+    __builtin_amdgcn_sched_barrier(0);
     f32x16 s[kKb];
 #pragma unroll
     for (int b = 0; b < kKb; ++b) {
       s[b] = f32x16_zero();
 #pragma unroll
-      for (int i = 0; i < kI; ++i) s[b] = mfma16<F16>(attn_row(kt + b * 32 * Tile::kRow + ln.row[i]), qf[i], s[b]);
+      for (int i = 0; i < kI; ++i) s[b] = mfma16<F16>(kf[b][i], qf[i], s[b]);
     }
-    const bool masked = k + KT > wmin;
-    if (masked) {
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8 vf[kKb][2][kFb];
+#pragma unroll
+    for (int b = 0; b < kKb; ++b)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int fb = 0; fb < kFb; ++fb) {
+          const int ro = (32 * b + 16 * u) * Tile::kRow;
+          vf[b][u][fb] = attn_tr(vt + ro + ln.tr[0][fb], vt + ro + ln.tr[1][fb]);
+        }
+    __builtin_amdgcn_sched_barrier(0);
+    if (k + KT > wmin) {
+      const int left = attn_opaque(lim - k - 4 * h);
 #pragma unroll
       for (int b = 0; b < kKb; ++b)
 #pragma unroll
-        for (int x = 0; x < 16; ++x)
-          if (k + 32 * b + attn_reg_row(x, h) >= lim) s[b][x] = -__builtin_inff();
+        for (int x = 0; x < 16; ++x) s[b][x] = 32 * b + attn_reg_row(x, 0) < left ? s[b][x] : -__builtin_inff();
     }
     float top = s[0][0];
 #pragma unroll
@@ -180,10 +200,8 @@ __device__ __forceinline__ bool attn_fwd_tile(const AttnArgs& a, uint16_t* __res
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const bf16x8 p = attn_pack<F16>(s[b], u);
-        const int ro = (32 * b + 16 * u) * Tile::kRow;
 #pragma unroll
-        for (int fb = 0; fb < kFb; ++fb)
-          acc[fb] = mfma16<F16>(attn_tr(vt + ro + ln.tr[0][fb], vt + ro + ln.tr[1][fb]), p, acc[fb]);
+        for (int fb = 0; fb < kFb; ++fb) acc[fb] = mfma16<F16>(vf[b][u][fb], p, acc[fb]);
       }
   }
   l = attn_sum2(l);
@@ -222,9 +240,9 @@ __global__ void __launch_bounds__(64 * NW, 2)
   const int part = SPLIT ? (int)(idx % (uint32_t)parts) : 0;
   if (SPLIT) idx /= (uint32_t)parts;
   const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
-  const int t0 = tiles - 1 - (int)(idx / groups);
-  const uint32_t gz = idx % groups;
-  const int z = (int)(gz / (uint32_t)a.kvh), kv = (int)(gz % (uint32_t)a.kvh);
+  const AttnPlace at = attn_place(idx, (uint32_t)tiles, groups);
+  const int t0 = tiles - 1 - (int)at.t;
+  const int z = (int)(at.g / (uint32_t)a.kvh), kv = (int)(at.g % (uint32_t)a.kvh);
   AttnSeq sq = attn_seq(a, z);
   if (z == a.nseq) sq.n = 0;
   const int64_t rows64 = (int64_t)sq.m * a.group;
