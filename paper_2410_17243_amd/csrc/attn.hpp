@@ -175,6 +175,15 @@ __device__ __forceinline__ int attn_opaque(int x) {
   return x;
 }
 
+// Waits for fragments loaded from memory: here, once, and not at their first use
+// in a sweep, where the wait would be for the copies under way as well, every time
+// around.
+template <int N>
+__device__ __forceinline__ void attn_settle(bf16x8 (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
+
 // x of this lane and of lane ^ 32.
 __device__ __forceinline__ void attn_both(float x, float& a, float& b) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);

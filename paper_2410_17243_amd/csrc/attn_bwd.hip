@@ -127,21 +127,6 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGra
     const int pos = live ? (int)(r / (uint32_t)a.group) : 0, g = live ? (int)(r % (uint32_t)a.group) : 0;
     const int head = kv * a.group + g;
     const int64_t token = sq.q0 + pos;
-    bf16x8 qf[kI], df[kI];
-    float D = 0.f;
-#pragma unroll
-    for (int i = 0; i < kI; ++i) {
-      qf[i] = attn_own(a.q + token * a.qs + head * a.qh, i, h, a.hd, live);
-      df[i] = attn_own(w.dout + token * w.dos + head * w.doh, i, h, a.hd, live);
-      const bf16x8 of = attn_own(w.out + token * w.os + head * w.oh, i, h, a.hd, live);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) D = fmaf(from16<F16>(df[i][e]), from16<F16>(of[e]), D);
-    }
-    D = attn_sum2(D);
-    float lse2 = 0.f;
-    if (live) lse2 = w.lse[(int64_t)head * a.tq + token] * kLog2e;
-    if (lse2 == -__builtin_inff()) lse2 = 0.f, D = 0.f;
-
     const int shift = sq.n - sq.m + 1;
     int lim = a.causal ? pos + shift : sq.n;
     lim = lim < 0 ? 0 : lim;
@@ -154,15 +139,37 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGra
     const int wmin = rw >= rows ? 0 : a.causal ? (int)(rw / (uint32_t)a.group) + shift : sq.n;
     const int wmax = rw >= rows ? 0 : a.causal ? (int)(rv / (uint32_t)a.group) + shift : sq.n;
 
-    f32x16 acc[kFb];
-    attn_barrier();
-    {
+    if (t != (uint32_t)t0) attn_barrier();
+    if (0 < kend) {
+      Tile::issue(kb, sq.n, kst, a.hd, lds, koff, wave);
+      Tile::issue(vb, sq.n, vst, a.hd, lds + Tile::kBytes, voff, wave);
+    }
+    bf16x8 qf[kI], df[kI];
+    float D = 0.f;
 #pragma unroll
-      for (int fb = 0; fb < kFb; ++fb) acc[fb] = f32x16_zero();
-      if (0 < kend) {
-        Tile::issue(kb, sq.n, kst, a.hd, lds, koff, wave);
-        Tile::issue(vb, sq.n, vst, a.hd, lds + Tile::kBytes, voff, wave);
+    for (int i = 0; i < kI; ++i) {
+      qf[i] = attn_own(a.q + token * a.qs + head * a.qh, i, h, a.hd, live);
+      df[i] = attn_own(w.dout + token * w.dos + head * w.doh, i, h, a.hd, live);
+    }
+    if (sq.n > KT) {
+#pragma unroll
+      for (int i = 0; i < kI; ++i) {
+        const bf16x8 of = attn_own(w.out + token * w.os + head * w.oh, i, h, a.hd, live);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) D = fmaf(from16<F16>(df[i][e]), from16<F16>(of[e]), D);
       }
+      D = attn_sum2(D);
+    }
+    float lse2 = 0.f;
+    if (live) lse2 = w.lse[(int64_t)head * a.tq + token] * kLog2e;
+    if (lse2 == -__builtin_inff()) lse2 = 0.f, D = 0.f;
+    attn_settle(qf);
+    attn_settle(df);
+    asm volatile("" : "+v"(lse2));
+    f32x16 acc[kFb];
+#pragma unroll
+    for (int fb = 0; fb < kFb; ++fb) acc[fb] = f32x16_zero();
+    {
       int buf = 0;
       for (int k = 0; k < kend; k += KT, buf ^= 1) {
         attn_barrier();
@@ -184,19 +191,19 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGra
             dp[b] = mfma16<F16>(attn_row(vt + b * 32 * Tile::kRow + ln.row[i]), df[i], dp[b]);
           }
         }
-        const bool masked = k + KT > wmin;
 #pragma unroll
         for (int b = 0; b < kKb; ++b)
 #pragma unroll
           for (int x = 0; x < 16; ++x) p[b][x] = exp2_hw(fmaf(p[b][x], a.sl2, -lse2));
-        if (masked) {
+        if (k + KT > wmin) {
+          const int left = attn_opaque(lim - k - 4 * h);
 #pragma unroll
           for (int b = 0; b < kKb; ++b)
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
-              const bool out = k + 32 * b + attn_reg_row(x, h) >= lim;
-              p[b][x] = out ? 0.f : p[b][x];
-              dp[b][x] = out ? 0.f : dp[b][x];
+              const bool seen = 32 * b + attn_reg_row(x, 0) < left;
+              p[b][x] = seen ? p[b][x] : 0.f;
+              dp[b][x] = seen ? dp[b][x] : 0.f;
             }
         }
         if (sq.n <= KT) {
@@ -303,7 +310,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dkv_kernel(AttnArgs a, AttnGr
     qbeg = qbeg < 0 ? 0 : qbeg / QT * QT;
 
     f32x16 dk[kFb], dv[kFb];
-    attn_barrier();
+    if (t != t0) attn_barrier();
     const INFCL_LDS char* vown = lds + 4 * Tile::kBytes + wave * 32 * Tile::kRow;
     if constexpr (kVLds) {
       uint32_t off[Own::kVar];
@@ -350,7 +357,6 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dkv_kernel(AttnArgs a, AttnGr
         p = mfma16<F16>(attn_row(qt + ln.row[i]), kf[i], p);
         dp = mfma16<F16>(attn_row(dt + ln.row[i]), kVLds ? attn_row(vown + ln.row[i]) : vf[kVLds ? 0 : i], dp);
       }
-      const bool masked = i1 < wall || i1 + QT > sq.m;
 #pragma unroll
       for (int x4 = 0; x4 < 4; ++x4) {
         const f32x4 lo = *(const INFCL_LDS f32x4*)(stat + 2 * attn_reg_row(4 * x4, h));
@@ -363,13 +369,13 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dkv_kernel(AttnArgs a, AttnGr
           dp[x] = p[x] * (dp[x] - D[e]);
         }
       }
-      if (masked) {
+      if (i1 < wall || i1 + QT > sq.m) {
+        const int lo = attn_opaque(first - i1 - 4 * h), hi = attn_opaque(sq.m - i1 - 4 * h);
 #pragma unroll
         for (int x = 0; x < 16; ++x) {
-          const int i = i1 + attn_reg_row(x, h);
-          const bool out = i < first || i >= sq.m;
-          p[x] = out ? 0.f : p[x];
-          dp[x] = out ? 0.f : dp[x];
+          const bool seen = attn_reg_row(x, 0) >= lo && attn_reg_row(x, 0) < hi;
+          p[x] = seen ? p[x] : 0.f;
+          dp[x] = seen ? dp[x] : 0.f;
         }
       }
 #pragma unroll

@@ -68,13 +68,13 @@ __device__ __attribute__((noinline)) void attn_fwd_rows(const uint16_t* q, const
 }
 
 // One workgroup's tile t of sequence sq's rows (query, head of the group kv), over
-// its part of the keys.  Returns whether the wave's sums were not finite: they
+// its part of the keys.  again: LDS is in use.  Returns whether the wave's sums were not finite: they
 // may hold what masked rows hold, and its rows are to be taken row by row.
 template <int DP, int NW, int KT, bool F16, bool SPLIT>
 __device__ __forceinline__ bool attn_fwd_tile(const AttnArgs& a, uint16_t* __restrict__ out, int64_t os, int64_t oh,
                                               float* __restrict__ lse, int parts, const AttnParts& pw,
                                               const AttnSeq& sq, int kv, int part, uint32_t t, uint32_t rows,
-                                              INFCL_LDS char* lds) {
+                                              INFCL_LDS char* lds, bool again) {
   constexpr int kFb = DP / 32, kI = DP / 16, kKb = KT / 32;
   typedef AttnTile<DP, NW, KT> Tile;
   const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -97,9 +97,6 @@ __device__ __forceinline__ bool attn_fwd_tile(const AttnArgs& a, uint16_t* __res
   const int pos = live ? (int)(r / (uint32_t)a.group) : 0, g = live ? (int)(r % (uint32_t)a.group) : 0;
   const int head = kv * a.group + g;
   const int64_t token = sq.q0 + pos;
-  bf16x8 qf[kI];
-#pragma unroll
-  for (int i = 0; i < kI; ++i) qf[i] = attn_own(a.q + token * a.qs + head * a.qh, i, h, a.hd, live);
 
   // keys [0, lim) are seen by this lane's row; every row of the wave sees
   // those below wmin, none of the workgroup those from kend on
@@ -119,11 +116,15 @@ __device__ __forceinline__ bool attn_fwd_tile(const AttnArgs& a, uint16_t* __res
 #pragma unroll
   for (int fb = 0; fb < kFb; ++fb) acc[fb] = f32x16_zero();
   float M = -__builtin_inff(), l = 0.f;
-  attn_barrier();
+  if (again) attn_barrier();
   if (kbeg < kend) {
     Tile::issue(kb + (int64_t)kbeg * a.ks, sq.n - kbeg, kst, a.hd, lds, koff, wave);
     Tile::issue(vb + (int64_t)kbeg * a.vs, sq.n - kbeg, vst, a.hd, lds + Tile::kBytes, voff, wave);
   }
+  bf16x8 qf[kI];
+#pragma unroll
+  for (int i = 0; i < kI; ++i) qf[i] = attn_own(a.q + token * a.qs + head * a.qh, i, h, a.hd, live);
+  attn_settle(qf);
   int buf = 0;
   for (int k = kbeg; k < kend; k += KT, buf ^= 1) {
     attn_barrier();
@@ -251,7 +252,7 @@ __global__ void __launch_bounds__(64 * NW, 2)
   bool bad = false;
   for (uint32_t t = (uint32_t)t0; t * (uint64_t)(32 * NW) < rows; t += (uint32_t)tiles)
     bad |= attn_fwd_tile<DP, NW, KT, F16, SPLIT>(a, out, os, oh, lse, parts, pw, sq, kv, part, t, rows,
-                                                 (INFCL_LDS char*)lds);
+                                                 (INFCL_LDS char*)lds, t != (uint32_t)t0);
   if (!bad) return;
   wait_dma();  // (the stores of these rows are done: other lanes write them again)
   const int h = (threadIdx.x >> 5) & 1;
