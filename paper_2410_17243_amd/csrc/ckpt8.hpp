@@ -7,25 +7,52 @@ namespace infcl {
 
 constexpr int kActNone = 0, kActGelu = 1, kActQuickGelu = 2;
 
-// f(x): x Phi(x) (erf), or x sigma(1.702 x).
+// Phi(-|x|): with E = e^(-x^2/2) and t = 1 / (1 + |x| / sqrt(8)),
+// the scaled complementary error function is a smooth function of t on [0, 1], and
+// Phi(-|x|) = E t Q(t), Q its least relative error polynomial of degree 8 (fitted by
+// reweighted least squares against erfcx in 64 bits: 4e-8; in fp32, with the
+// reciprocal and exponential of the hardware, 9e-7 of the value up to |x| = 4, 2e-7
+// absolute).  15 instructions and two of quarter rate; the library's erf takes
+// three times as many, which showed where f is taken from 8 bits (65536 x 4096:
+// 210 us with it).
+__device__ __forceinline__ float phi_tail(float x, float& E) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.35355339f, fabsf(x), 1.f));
+  float q = -2.959678322e-02f;
+  q = fmaf(q, t, 1.425919682e-01f);
+  q = fmaf(q, t, -2.442315370e-01f);
+  q = fmaf(q, t, 1.397574842e-01f);
+  q = fmaf(q, t, -1.381248608e-02f);
+  q = fmaf(q, t, 1.015552655e-01f);
+  q = fmaf(q, t, 1.214982346e-01f);
+  q = fmaf(q, t, 1.411950439e-01f);
+  q = fmaf(q, t, 1.410427839e-01f);
+  E = exp2_hw(-0.5f * kLog2e * x * x);
+  return q * t * E;
+}
+
+// f(x): x Phi(x), or x sigma(1.702 x).
 template <int ACT>
 __device__ __forceinline__ float act_value(float x) {
-  if constexpr (ACT == kActGelu)
-    return 0.5f * x * (1.f + erff(x * 0.70710678118654752f));
-  else if constexpr (ACT == kActQuickGelu)
-    return x / (1.f + exp2_hw(-1.702f * kLog2e * x));
-  else
+  if constexpr (ACT == kActGelu) {
+    float E;
+    const float q = phi_tail(x, E);
+    return x * (x > 0.f ? 1.f - q : q);
+  } else if constexpr (ACT == kActQuickGelu) {
+    return x * __builtin_amdgcn_rcpf(1.f + exp2_hw(-1.702f * kLog2e * x));
+  } else {
     return x;
+  }
 }
 // f'(x): Phi(x) + x phi(x), or s (1 + 1.702 x (1 - s)) with s = sigma(1.702 x).
 // Far on the negative side s is 0 and x (1 - s) finite: the product is 0.
 template <int ACT>
 __device__ __forceinline__ float act_slope(float x) {
   if constexpr (ACT == kActGelu) {
-    return 0.5f * (1.f + erff(x * 0.70710678118654752f)) +
-           x * (0.39894228040143268f * exp2_hw(-0.5f * kLog2e * x * x));
+    float E;
+    const float q = phi_tail(x, E);
+    return fmaf(x * 0.39894228040143268f, E, x > 0.f ? 1.f - q : q);
   } else {
-    const float s = 1.f / (1.f + exp2_hw(-1.702f * kLog2e * x));
+    const float s = __builtin_amdgcn_rcpf(1.f + exp2_hw(-1.702f * kLog2e * x));
     return s * (1.f + 1.702f * x * (1.f - s));
   }
 }
