@@ -12,9 +12,11 @@
 // lse log2(e), rows with no keys as 0, for the second.
 //
 // p and ds are rounded to 16 bits for the second products, as the inputs are.
-// D comes from o as stored, except where all keys of a sequence are in one
-// tile: there it is the sum of p dp in the registers, which no rounding of o
-// touches (with few keys o is not small beside dp, and its rounding would show).
+// D comes from o as stored, except for rows that see the first tile of keys only:
+// there it is the sum of p dp in the registers, which no rounding of o touches.
+// (The error of D from o's rounding, beside that of rounding ds, is the sum of
+// p^2 over a row in the mean square: near 1 for a row that sees few keys, 3 / n
+// over n keys of similar scores.)
 #include "attn.hpp"
 
 namespace infcl {
@@ -151,7 +153,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGra
       qf[i] = attn_own(a.q + token * a.qs + head * a.qh, i, h, a.hd, live);
       df[i] = attn_own(w.dout + token * w.dos + head * w.doh, i, h, a.hd, live);
     }
-    if (sq.n > KT) {
+    if (wmax > KT) {
 #pragma unroll
       for (int i = 0; i < kI; ++i) {
         const bf16x8 of = attn_own(w.out + token * w.os + head * w.oh, i, h, a.hd, live);
@@ -206,7 +208,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGra
               dp[b][x] = seen ? dp[b][x] : 0.f;
             }
         }
-        if (sq.n <= KT) {
+        if (wmax <= KT) {
           float s = 0.f;
 #pragma unroll
           for (int b = 0; b < kKb; ++b)
@@ -244,7 +246,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGra
     const float D = attn_dq_rows<F16>(
         a.q + token * a.qs + head * a.qh, w.dout + token * w.dos + head * w.doh, w.out + token * w.os + head * w.oh,
         a.k + sq.k0 * a.ks + kv * a.kh, a.v + sq.k0 * a.vs + kv * a.vh, a.ks, a.vs, lim < sq.n ? lim : sq.n, a.scale,
-        w.lse[(int64_t)head * a.tq + token], sq.n <= KT, a.hd, (threadIdx.x >> 5) & 1,
+        w.lse[(int64_t)head * a.tq + token], lim <= KT, a.hd, (threadIdx.x >> 5) & 1,
         w.dq + token * w.dqs + head * w.dqh);
     if (threadIdx.x & 32) w.stat[((int64_t)head * w.trow + token) * 2 + 1] = D;
   }

@@ -184,7 +184,7 @@ WPlan wgrad_plan(int64_t n, int64_t d, int64_t m) {
   w.tm = (int)((m + bm - 1) / bm), w.tn = (int)((d + bm - 1) / bm);
   const int64_t tiles = (int64_t)w.tm * w.tn, slots = w.big ? 256 : 512;
   int64_t parts = slots / tiles;
-  if (parts > stages / 4) parts = stages / 4;  // a part worth its sums
+  if (parts > stages / 8) parts = stages / 8;  // a part worth its sums
   if (parts > 64) parts = 64;
   if (parts < 1) parts = 1;
   w.steps = (stages + parts - 1) / parts;
