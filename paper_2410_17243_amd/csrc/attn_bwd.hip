@@ -430,7 +430,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dkv_kernel(AttnArgs a, AttnGr
   }
 }
 
-// The parts' dk and dv, in order.  A wave takes 32 rows of one sequence's key head,
+// The parts' dk and dv, in order.  A wave takes 8 rows of one sequence's key head,
 // 16 lanes to a row; if one of them is not finite, all again row by row.
 template <bool F16>
 __global__ void __launch_bounds__(256) attn_dkv_join(AttnArgs a, AttnGrads w, int tiles, int parts) {
@@ -441,10 +441,11 @@ __global__ void __launch_bounds__(256) attn_dkv_join(AttnArgs a, AttnGrads w, in
   if (z == a.nseq) sq.m = 0;
   const int lane = threadIdx.x & 63, d = 8 * (lane & 15);
   const int64_t step = a.tk * a.kvh * a.hd;  // from dk to dv of a part, and on to the next part's dk
-  for (int64_t key0 = (int64_t)(blockIdx.x / groups) * 128 + (threadIdx.x >> 6) * 32; key0 < sq.n;
-       key0 += (int64_t)tiles * 128) {
+  for (int64_t key0 = (int64_t)(blockIdx.x / groups) * 32 + (threadIdx.x >> 6) * 8; key0 < sq.n;
+       key0 += (int64_t)tiles * 32) {
     float sum = 0.f;
-    for (int r = lane >> 4; r < 32; r += 4) {
+#pragma unroll
+    for (int r = lane >> 4; r < 8; r += 4) {
       const int64_t token = sq.k0 + key0 + r;
       if (key0 + r >= sq.n || d >= a.hd) continue;
       const float* src = w.part + (token * a.kvh + kv) * a.hd + d;
@@ -465,7 +466,7 @@ __global__ void __launch_bounds__(256) attn_dkv_join(AttnArgs a, AttnGrads w, in
     wait_dma();  // (the stores of these rows are done: other lanes write them again)
     const int64_t key = key0 + (lane & 31), token = sq.k0 + key;
     const int h0 = kv * a.group;
-    if (key < sq.n)
+    if ((lane & 31) < 8 && key < sq.n)
       attn_dkv_rows<F16>(a.k + token * a.ks + kv * a.kh, a.v + token * a.vs + kv * a.vh, a.q + sq.q0 * a.qs + h0 * a.qh,
                          w.dout + sq.q0 * w.dos + h0 * w.doh, a.qs, a.qh, w.dos, w.doh,
                          w.stat + (h0 * w.trow + sq.q0) * 2, w.trow, (int)key - (sq.n - sq.m), sq.m, a.group, a.scale,
@@ -486,7 +487,8 @@ void launch_both(const AttnArgs& a, const AttnGrads& w, const AttnBwdPlan& p, in
     hipLaunchKernelGGL((attn_dkv_kernel<DP, NW, F16, false>), grid, dim3(64 * NW), 0, st, a, w, (int)tk, 1);
   } else if constexpr (NW > 1) {
     hipLaunchKernelGGL((attn_dkv_kernel<DP, NW, F16, true>), grid, dim3(64 * NW), 0, st, a, w, (int)tk, p.parts);
-    hipLaunchKernelGGL((attn_dkv_join<F16>), dim3((unsigned)(tk * groups)), dim3(256), 0, st, a, w, (int)tk, p.parts);
+    hipLaunchKernelGGL((attn_dkv_join<F16>), dim3((unsigned)(4 * tk * groups)), dim3(256), 0, st, a, w, (int)(4 * tk),
+                       p.parts);
   }
 }
 

@@ -150,11 +150,18 @@ __global__ void __launch_bounds__(256) wgrad_sum(const f32x4* __restrict__ part,
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 2;  // 8 values
   if (i >= n4) return;
   float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll 4
-  for (int p = 0; p < parts; ++p) {
-    const f32x4 a = part[p * n4 + i], b = part[p * n4 + i + 1];
+  for (int p0 = 0; p0 < parts; p0 += 8) {  // eight parts' loads at a time
+    f32x4 x[8][2];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] += a[e], s[4 + e] += b[e];
+    for (int p = 0; p < 8; ++p) {
+      const int64_t at = (int64_t)(p0 + p < parts ? p0 + p : p0) * n4 + i;
+      x[p][0] = part[at], x[p][1] = part[at + 1];
+    }
+#pragma unroll
+    for (int p = 0; p < 8; ++p)
+      if (p0 + p < parts)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += x[p][0][e], s[4 + e] += x[p][1][e];
   }
   if constexpr (OUT == kF32) {
     ((f32x4*)out)[i] = f32x4{s[0], s[1], s[2], s[3]};

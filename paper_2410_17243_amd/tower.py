@@ -26,10 +26,11 @@ Packed attention
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
-from . import (INFCL_BF16, INFCL_F16, INFCL_F32, _check, _raw_stream, load_library)
+from . import INFCL_BF16, INFCL_F16, INFCL_F32, _check, _ptr, _raw_stream, load_library
 
 _CODES = {torch.bfloat16: INFCL_BF16, torch.float16: INFCL_F16, torch.float32: INFCL_F32}
 ACTS = {"none": 0, "gelu": 1, "quick_gelu": 2}
@@ -95,10 +96,19 @@ def _code(t, name):
     return c
 
 
-def _workspace(fn, where, dev, *sizes):
+# Small calls are bound by host time (an activation of 9 x 64: 12 us of it, 4 of
+# them the library's), so what depends on sizes alone is asked for once for each
+# set of them.
+
+@functools.lru_cache(maxsize=4096)
+def _workspace_bytes(name, *sizes) -> int:
     n = ctypes.c_size_t(0)
-    _check(fn(*sizes, ctypes.byref(n)), where)
-    return torch.empty(max(n.value, 256), dtype=torch.uint8, device=dev)
+    _check(getattr(_load(), name)(*sizes, ctypes.byref(n)), name)
+    return max(n.value, 256)
+
+
+def _workspace(name, dev, *sizes):
+    return torch.empty(_workspace_bytes(name, *sizes), dtype=torch.uint8, device=dev)
 
 
 # ------------------------------------------------------------ token embedding
@@ -140,7 +150,7 @@ def embed_bwd(tokens, dout, vocab: int, scale: float = 1.0, grad_dtype=None):
         raise TypeError(f"grad_dtype must be float32 or dout's dtype {dout.dtype}, got {gdt}")
     n, d = tokens.numel(), dout.shape[-1]
     lib = _load()
-    ws = _workspace(lib.infcl_embed_bwd_workspace, "infcl_embed_bwd_workspace", dev, n, int(vocab), d)
+    ws = _workspace("infcl_embed_bwd_workspace", dev, n, int(vocab), d)
     dtable = torch.empty((int(vocab), d), dtype=gdt, device=dev)
     _check(lib.infcl_embed_bwd(tokens.data_ptr(), size, n, dout.data_ptr(), int(vocab), d, code, float(scale),
                                dtable.data_ptr(), _CODES[gdt], ws.data_ptr(), ws.numel(), _raw_stream(dev)),
@@ -168,25 +178,24 @@ def embed(tokens, table, scale: float = 1.0):
 
 # ----------------------------------------------------------- packed attention
 
-def _view(t):
-    st, sh, _ = t.stride()
-    return _View(t.data_ptr(), st, sh)
+@functools.lru_cache(maxsize=4096)
+def _plan(*fields):
+    """(infcl_attn_shape, workspace bytes of the forward and of the backward) for its fields."""
+    sh, f, b = _Shape(*fields), ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(_load().infcl_attn_workspace(ctypes.byref(sh), ctypes.byref(f), ctypes.byref(b)), "infcl_attn_workspace")
+    return ctypes.byref(sh), f.value, b.value
 
 
 def _heads_view(t, name, like=None):
     """t as [tokens, heads, head_dim] with features next to each other and rows of
     16-byte units (strides of dimensions of one or no entry do not matter)."""
-    if t.dim() != 3 or t.stride(2) != 1 and t.shape[2] > 1:
-        raise ValueError(f"{name} must be [tokens, heads, head_dim] with contiguous features, got {tuple(t.shape)}, "
-                         f"strides {t.stride()}")
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or strides[2] != 1 and shape[2] > 1:
+        raise ValueError(f"{name} must be [tokens, heads, head_dim] with contiguous features, got {tuple(shape)}, "
+                         f"strides {strides}")
     if like is not None and t.dtype != like.dtype:
         raise ValueError(f"{name} must be {like.dtype}, got {t.dtype}")
-    st, sh, _ = t.stride()
-    if t.shape[0] < 2:
-        st = t.shape[1] * t.shape[2]
-    if t.shape[1] < 2:
-        sh = 0
-    return _View(t.data_ptr(), st, sh)
+    return _View(t.data_ptr(), strides[0] if shape[0] > 1 else shape[1] * shape[2], strides[1] if shape[1] > 1 else 0)
 
 
 def _cu(cu, name, dev):
@@ -195,18 +204,21 @@ def _cu(cu, name, dev):
                          f"{tuple(cu.shape)} on {cu.device}")
 
 
-def _attn_shape(q, k, v, cu_q, max_q, cu_k, max_k, causal, scale):
+def _attn_call(q, k, v, cu_q, max_q, cu_k, max_k, causal, scale):
+    """Checks the arguments; (device, plan, views of q, k and v, cu_k)."""
     dev = _device(("q", q), ("k", k), ("v", v))
     if q.dtype not in (torch.bfloat16, torch.float16):
         raise TypeError(f"q must be bfloat16 or float16, got {q.dtype}")
     vq, vk, vv = _heads_view(q, "q"), _heads_view(k, "k", q), _heads_view(v, "v", q)
-    if k.shape != v.shape or k.shape[2] != q.shape[2] or k.shape[1] < 1 or q.shape[1] % k.shape[1]:
-        raise ValueError(f"k and v must be [tokens, kv_heads, {q.shape[2]}], kv_heads a divisor of {q.shape[1]}, got "
+    tq, heads, hd = q.shape
+    tk, kv, khd = k.shape
+    if k.shape != v.shape or khd != hd or kv < 1 or heads % kv:
+        raise ValueError(f"k and v must be [tokens, kv_heads, {hd}], kv_heads a divisor of {heads}, got "
                          f"{tuple(k.shape)}, {tuple(v.shape)}")
     _cu(cu_q, "cu_q", dev)
     if cu_k is None:
-        if k.shape[0] != q.shape[0]:
-            raise ValueError(f"without cu_k there are as many keys as queries, got {k.shape[0]} and {q.shape[0]}")
+        if tk != tq:
+            raise ValueError(f"without cu_k there are as many keys as queries, got {tk} and {tq}")
         cu_k, max_k = cu_q, max_q
     else:
         _cu(cu_k, "cu_k", dev)
@@ -214,11 +226,9 @@ def _attn_shape(q, k, v, cu_q, max_q, cu_k, max_k, causal, scale):
             raise ValueError(f"cu_q and cu_k must have as many entries, got {cu_q.numel()} and {cu_k.numel()}")
         if max_k is None:
             raise ValueError("cu_k comes with max_k")
-    if scale is None:
-        scale = q.shape[2] ** -0.5
-    sh = _Shape(q.shape[0], k.shape[0], cu_q.numel() - 1, q.shape[1], k.shape[1], q.shape[2], _CODES[q.dtype],
-                1 if causal else 0, int(max_q), int(max_k), float(scale))
-    return dev, sh, vq, vk, vv, cu_k
+    plan = _plan(tq, tk, cu_q.numel() - 1, heads, kv, hd, _CODES[q.dtype], 1 if causal else 0, int(max_q), int(max_k),
+                 hd ** -0.5 if scale is None else float(scale))
+    return dev, plan, vq, vk, vv, cu_k
 
 
 def packed_attn_fwd(q, k, v, cu_q, max_q: int, cu_k=None, max_k=None, causal: bool = True, scale=None,
@@ -228,43 +238,38 @@ def packed_attn_fwd(q, k, v, cu_q, max_q: int, cu_k=None, max_k=None, causal: bo
     cu_k[z] .. cu_k[z+1] (cu_q's without cu_k) of k and v.  max_q, max_k: the longest
     lengths.  Returns out [tokens, heads, head_dim] and lse [heads, tokens] float32
     (None without need_lse).  scale: 1 / sqrt(head_dim) by default."""
-    dev, sh, vq, vk, vv, cu_k = _attn_shape(q, k, v, cu_q, max_q, cu_k, max_k, causal, scale)
-    lib = _load()
-    n = ctypes.c_size_t(0)
-    _check(lib.infcl_attn_workspace(ctypes.byref(sh), ctypes.byref(n), None), "infcl_attn_workspace")
-    out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=dev) if need_lse else None
-    ws = torch.empty(n.value, dtype=torch.uint8, device=dev) if n.value else None
-    _check(lib.infcl_attn_fwd(ctypes.byref(sh), vq, vk, vv, cu_q.data_ptr(), cu_k.data_ptr(), _view(out),
-                              None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), n.value,
-                              _raw_stream(dev)), "infcl_attn_fwd")
+    dev, (sh, n, _), vq, vk, vv, cu_k = _attn_call(q, k, v, cu_q, max_q, cu_k, max_k, causal, scale)
+    tq, heads, hd = q.shape
+    out = torch.empty((tq, heads, hd), dtype=q.dtype, device=dev)
+    lse = torch.empty((heads, tq), dtype=torch.float32, device=dev) if need_lse else None
+    ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    _check(_load().infcl_attn_fwd(sh, vq, vk, vv, cu_q.data_ptr(), cu_k.data_ptr(),
+                                  _View(out.data_ptr(), heads * hd, hd), _ptr(lse), _ptr(ws), n, _raw_stream(dev)),
+           "infcl_attn_fwd")
     return out, lse
 
 
 def packed_attn_bwd(q, k, v, out, lse, dout, cu_q, max_q: int, cu_k=None, max_k=None, causal: bool = True, scale=None,
                     grads=None):
     """dq, dk, dv of packed_attn_fwd; written into grads = (dq, dk, dv) where given."""
-    dev, sh, vq, vk, vv, cu_k = _attn_shape(q, k, v, cu_q, max_q, cu_k, max_k, causal, scale)
+    dev, (sh, _, n), vq, vk, vv, cu_k = _attn_call(q, k, v, cu_q, max_q, cu_k, max_k, causal, scale)
     _device(("q", q), ("out", out), ("lse", lse), ("dout", dout))
     if out.shape != q.shape or dout.shape != q.shape:
         raise ValueError(f"out and dout must be {tuple(q.shape)}, got {tuple(out.shape)}, {tuple(dout.shape)}")
     if lse.shape != (q.shape[1], q.shape[0]) or lse.dtype != torch.float32 or not lse.is_contiguous():
         raise ValueError(f"lse must be contiguous float32 [heads, tokens], got {lse.dtype} {tuple(lse.shape)}")
     if grads is None:
-        grads = (torch.empty(q.shape, dtype=q.dtype, device=dev), torch.empty(k.shape, dtype=q.dtype, device=dev),
-                 torch.empty(v.shape, dtype=q.dtype, device=dev))
-    dq, dk, dv = grads
-    _device(("q", q), ("dq", dq), ("dk", dk), ("dv", dv))
-    if dq.shape != q.shape or dk.shape != k.shape or dv.shape != v.shape:
-        raise ValueError("grads must have the shapes of q, k and v")
-    vo, vd = _heads_view(out, "out", q), _heads_view(dout, "dout", q)
-    views = [_heads_view(t, name, q) for t, name in ((dq, "dq"), (dk, "dk"), (dv, "dv"))]
-    lib = _load()
-    n = ctypes.c_size_t(0)
-    _check(lib.infcl_attn_workspace(ctypes.byref(sh), None, ctypes.byref(n)), "infcl_attn_workspace")
-    ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
-    _check(lib.infcl_attn_bwd(ctypes.byref(sh), vq, vk, vv, cu_q.data_ptr(), cu_k.data_ptr(), vo, lse.data_ptr(), vd,
-                              *views, ws.data_ptr(), n.value, _raw_stream(dev)), "infcl_attn_bwd")
+        dq, dk, dv = (torch.empty(t.shape, dtype=q.dtype, device=dev) for t in (q, k, v))
+    else:
+        dq, dk, dv = grads
+        _device(("q", q), ("dq", dq), ("dk", dk), ("dv", dv))
+        if dq.shape != q.shape or dk.shape != k.shape or dv.shape != v.shape:
+            raise ValueError("grads must have the shapes of q, k and v")
+    ws = torch.empty(n, dtype=torch.uint8, device=dev)
+    _check(_load().infcl_attn_bwd(sh, vq, vk, vv, cu_q.data_ptr(), cu_k.data_ptr(), _heads_view(out, "out", q),
+                                  lse.data_ptr(), _heads_view(dout, "dout", q), _heads_view(dq, "dq", q),
+                                  _heads_view(dk, "dk", q), _heads_view(dv, "dv", q), ws.data_ptr(), n,
+                                  _raw_stream(dev)), "infcl_attn_bwd")
     return dq, dk, dv
 
 
@@ -429,7 +434,7 @@ def ckpt8_wgrad(dy, kept: Ckpt8, act: str = "none", grad_dtype=None):
     n, m, stride = _rows(dy, "dy")
     d = kept.q.shape[-1]
     lib = _load()
-    ws = _workspace(lib.infcl_ckpt8_wgrad_workspace, "infcl_ckpt8_wgrad_workspace", dev, n, d, m)
+    ws = _workspace("infcl_ckpt8_wgrad_workspace", dev, n, d, m)
     dw = torch.empty((m, d), dtype=gdt, device=dev)
     _check(lib.infcl_ckpt8_wgrad(dy.data_ptr(), stride, kept.q.data_ptr(), kept.exps.data_ptr(), n, d, m,
                                  _CODES[dy.dtype], a, dw.data_ptr(), _CODES[gdt], ws.data_ptr(), ws.numel(),
