@@ -86,10 +86,13 @@ typedef struct {
 /* Bytes of workspace of the two calls (either pointer may be NULL). */
 infcl_status infcl_attn_workspace(const infcl_attn_shape* shape, size_t* fwd_bytes, size_t* bwd_bytes);
 
-/* lse [heads][total_q] float (may be NULL): what the backward needs. */
+/* lse [heads][total_q] float (may be NULL): what the backward needs.
+ * len_k [nseq] int32 (device, may be NULL): how many of a sequence's keys, from
+ * its first on, there are, where its rows of k and v are room for more (a cache
+ * that grows); n above is then the lesser of the two. */
 infcl_status infcl_attn_fwd(const infcl_attn_shape* shape, infcl_attn_view q, infcl_attn_view k, infcl_attn_view v,
-                            const int32_t* cu_q, const int32_t* cu_k, infcl_attn_view out, float* lse, void* workspace,
-                            size_t ws_bytes, void* stream);
+                            const int32_t* cu_q, const int32_t* cu_k, const int32_t* len_k, infcl_attn_view out,
+                            float* lse, void* workspace, size_t ws_bytes, void* stream);
 
 /* dq, dk, dv of dtype; out and lse as infcl_attn_fwd left them. */
 infcl_status infcl_attn_bwd(const infcl_attn_shape* shape, infcl_attn_view q, infcl_attn_view k, infcl_attn_view v,

@@ -28,7 +28,7 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 struct AttnArgs {
   const uint16_t *q, *k, *v;
   int64_t qs, qh, ks, kh, vs, vh;  // from token to token, from head to head
-  const int32_t *cu_q, *cu_k;
+  const int32_t *cu_q, *cu_k, *len_k;  // (len_k: may be null)
   int64_t tq, tk;
   int32_t nseq, heads, kvh, group, hd, causal;
   float scale, sl2;  // of the scores; times log2(e)
@@ -64,6 +64,10 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnArgs& a, int z) {
   const int64_t e = q1 > a.tq ? a.tq : q1, f = k1 > a.tk ? a.tk : k1;
   s.m = (int32_t)(e > s.q0 ? e - s.q0 : 0);
   s.n = (int32_t)(f > s.k0 ? f - s.k0 : 0);
+  if (a.len_k && z < a.nseq) {
+    const int32_t used = a.len_k[z] < 0 ? 0 : a.len_k[z];
+    s.n = used < s.n ? used : s.n;
+  }
   return s;
 }
 

@@ -48,12 +48,12 @@ bool view_supported(const infcl_attn_view& v) {
 }
 
 AttnArgs args_of(const infcl_attn_shape* s, const infcl_attn_view& q, const infcl_attn_view& k,
-                 const infcl_attn_view& v, const int32_t* cu_q, const int32_t* cu_k) {
+                 const infcl_attn_view& v, const int32_t* cu_q, const int32_t* cu_k, const int32_t* len_k) {
   AttnArgs a;
   a.q = (const uint16_t*)q.data, a.k = (const uint16_t*)k.data, a.v = (const uint16_t*)v.data;
   a.qs = q.token_stride, a.qh = q.head_stride, a.ks = k.token_stride, a.kh = k.head_stride;
   a.vs = v.token_stride, a.vh = v.head_stride;
-  a.cu_q = cu_q, a.cu_k = cu_k;
+  a.cu_q = cu_q, a.cu_k = cu_k, a.len_k = len_k;
   a.tq = s->total_q, a.tk = s->total_k;
   a.nseq = s->nseq, a.heads = s->heads, a.kvh = s->kv_heads, a.group = s->heads / s->kv_heads;
   a.hd = s->head_dim, a.causal = s->causal;
@@ -69,25 +69,27 @@ extern "C" infcl_status infcl_attn_workspace(const infcl_attn_shape* s, size_t* 
   const infcl_status st = shape_status(s);
   if (st != INFCL_OK) return st;
   const infcl_attn_view none = {nullptr, 0, 0};
-  const AttnArgs a = args_of(s, none, none, none, nullptr, nullptr);
+  const AttnArgs a = args_of(s, none, none, none, nullptr, nullptr, nullptr);
   if (fwd_bytes) *fwd_bytes = attn_fwd_plan(a, least(s->max_q, s->total_q), least(s->max_k, s->total_k)).total;
   if (bwd_bytes) *bwd_bytes = attn_bwd_plan(a, least(s->max_q, s->total_q), least(s->max_k, s->total_k)).total;
   return fwd_bytes || bwd_bytes ? INFCL_OK : INFCL_ERR_INVALID;
 }
 
 extern "C" infcl_status infcl_attn_fwd(const infcl_attn_shape* s, infcl_attn_view q, infcl_attn_view k,
-                                       infcl_attn_view v, const int32_t* cu_q, const int32_t* cu_k, infcl_attn_view out,
-                                       float* lse, void* workspace, size_t ws_bytes, void* stream) {
+                                       infcl_attn_view v, const int32_t* cu_q, const int32_t* cu_k,
+                                       const int32_t* len_k, infcl_attn_view out, float* lse, void* workspace,
+                                       size_t ws_bytes, void* stream) {
   const infcl_status st = shape_status(s);
   if (st != INFCL_OK) return st;
   if (s->total_q == 0) return INFCL_OK;
   const int64_t hd = s->head_dim;
   if (!view_ok(q, s->total_q, hd) || !view_ok(k, s->total_k, hd) || !view_ok(v, s->total_k, hd) ||
-      !view_ok(out, s->total_q, hd) || !aligned(cu_q, 4) || !aligned(cu_k, 4) || (lse && !aligned(lse, 4)))
+      !view_ok(out, s->total_q, hd) || !aligned(cu_q, 4) || !aligned(cu_k, 4) ||
+      (len_k && !aligned(len_k, 4)) || (lse && !aligned(lse, 4)))
     return INFCL_ERR_INVALID;
   if (!view_supported(q) || !view_supported(k) || !view_supported(v) || !view_supported(out))
     return INFCL_ERR_UNSUPPORTED;
-  const AttnArgs a = args_of(s, q, k, v, cu_q, cu_k);
+  const AttnArgs a = args_of(s, q, k, v, cu_q, cu_k, len_k);
   const AttnFwdPlan p = attn_fwd_plan(a, least(s->max_q, s->total_q), least(s->max_k, s->total_k));
   if (p.total > 0 && !aligned(workspace, 256)) return INFCL_ERR_INVALID;
   if (ws_bytes < p.total) return INFCL_ERR_WORKSPACE;
@@ -111,7 +113,7 @@ extern "C" infcl_status infcl_attn_bwd(const infcl_attn_shape* s, infcl_attn_vie
   if (!view_supported(q) || !view_supported(k) || !view_supported(v) || !view_supported(out) ||
       !view_supported(dout) || !view_supported(dq) || !view_supported(dk) || !view_supported(dv))
     return INFCL_ERR_UNSUPPORTED;
-  const AttnArgs a = args_of(s, q, k, v, cu_q, cu_k);
+  const AttnArgs a = args_of(s, q, k, v, cu_q, cu_k, nullptr);
   const int64_t mq = least(s->max_q, s->total_q), mk = least(s->max_k, s->total_k);
   const AttnBwdPlan p = attn_bwd_plan(a, mq, mk);
   if (ws_bytes < p.total) return INFCL_ERR_WORKSPACE;

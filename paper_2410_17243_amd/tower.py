@@ -10,7 +10,8 @@ Token embedding
     embed_bwd(tokens, dout, vocab, scale=1.0, grad_dtype=None) -> dtable
     embed(tokens, table, scale=1.0) -> out   (torch.autograd.Function)
 Packed attention
-    packed_attn_fwd(q, k, v, cu_q, max_q, cu_k=None, max_k=None, causal=True, scale=None, need_lse=True) -> (out, lse)
+    packed_attn_fwd(q, k, v, cu_q, max_q, cu_k=None, max_k=None, causal=True, scale=None, need_lse=True,
+                    len_k=None) -> (out, lse)
     packed_attn_bwd(q, k, v, out, lse, dout, cu_q, max_q, ...) -> (dq, dk, dv)
     packed_attn(q, k, v, cu_q, max_q, ...) -> out   (torch.autograd.Function)
     packed_attn_qkv(qkv, heads, kv_heads, cu, max_len, ...) -> out, of one projection [tokens, heads + 2 kv_heads, hd]
@@ -62,7 +63,7 @@ def _load():
             "infcl_embed_bwd_workspace": [i64, i64, i64, psz],
             "infcl_embed_bwd": [vp, ip, i64, vp, i64, i64, ip, fl, vp, ip, vp, sz, vp],
             "infcl_attn_workspace": [ctypes.POINTER(_Shape), psz, psz],
-            "infcl_attn_fwd": [ctypes.POINTER(_Shape), _View, _View, _View, vp, vp, _View, vp, vp, sz, vp],
+            "infcl_attn_fwd": [ctypes.POINTER(_Shape), _View, _View, _View, vp, vp, vp, _View, vp, vp, sz, vp],
             "infcl_attn_bwd": [ctypes.POINTER(_Shape), _View, _View, _View, vp, vp, _View, vp, _View, _View, _View,
                                _View, vp, sz, vp],
             "infcl_ckpt8_pack": [vp, i64, i64, i64, ip, vp, vp, vp],
@@ -200,7 +201,7 @@ def _heads_view(t, name, like=None):
 
 def _cu(cu, name, dev):
     if cu.dtype != torch.int32 or cu.dim() != 1 or cu.numel() < 1 or not cu.is_contiguous() or cu.device != dev:
-        raise ValueError(f"{name} must be a contiguous int32 tensor of offsets on {dev}, got {cu.dtype} "
+        raise ValueError(f"{name} must be a contiguous int32 vector on {dev}, got {cu.dtype} "
                          f"{tuple(cu.shape)} on {cu.device}")
 
 
@@ -232,18 +233,23 @@ def _attn_call(q, k, v, cu_q, max_q, cu_k, max_k, causal, scale):
 
 
 def packed_attn_fwd(q, k, v, cu_q, max_q: int, cu_k=None, max_k=None, causal: bool = True, scale=None,
-                    need_lse: bool = True):
+                    need_lse: bool = True, len_k=None):
     """Attention over packed sequences: q [tokens, heads, head_dim], k, v [tokens,
     kv_heads, head_dim]; sequence z has the rows cu_q[z] .. cu_q[z+1] of q and
     cu_k[z] .. cu_k[z+1] (cu_q's without cu_k) of k and v.  max_q, max_k: the longest
     lengths.  Returns out [tokens, heads, head_dim] and lse [heads, tokens] float32
-    (None without need_lse).  scale: 1 / sqrt(head_dim) by default."""
+    (None without need_lse).  scale: 1 / sqrt(head_dim) by default.  len_k [sequences]
+    int32: the keys in use, where cu_k gives each sequence room for more."""
     dev, (sh, n, _), vq, vk, vv, cu_k = _attn_call(q, k, v, cu_q, max_q, cu_k, max_k, causal, scale)
+    if len_k is not None:
+        _cu(len_k, "len_k", dev)
+        if len_k.numel() != cu_q.numel() - 1:
+            raise ValueError(f"len_k must have an entry for each of {cu_q.numel() - 1} sequences, got {len_k.numel()}")
     tq, heads, hd = q.shape
     out = torch.empty((tq, heads, hd), dtype=q.dtype, device=dev)
     lse = torch.empty((heads, tq), dtype=torch.float32, device=dev) if need_lse else None
     ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
-    _check(_load().infcl_attn_fwd(sh, vq, vk, vv, cu_q.data_ptr(), cu_k.data_ptr(),
+    _check(_load().infcl_attn_fwd(sh, vq, vk, vv, cu_q.data_ptr(), cu_k.data_ptr(), _ptr(len_k),
                                   _View(out.data_ptr(), heads * hd, hd), _ptr(lse), _ptr(ws), n, _raw_stream(dev)),
            "infcl_attn_fwd")
     return out, lse

@@ -303,3 +303,24 @@ def test_refusals():
         infcl.packed_attn_bwd(q, k, v, ok[0], ok[1][:, :3], do, cu, 4)
     with pytest.raises(ValueError):
         infcl.packed_attn_bwd(q, k, v, ok[0], ok[1], do[:3], cu, 4)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+def test_a_cache_with_room(causal):
+    """len_k: of each sequence's rows of k and v the first few are in use, the rest
+    hold NaN; none in use at all for one of them."""
+    cap, used, lens_q = 70, [1, 70, 33, 0], [1, 2, 5, 1]
+    q, k, v, _ = _inputs(sum(lens_q), cap * 4, 4, 2, 64, "bf16", 11)
+    at = [list(range(cap * i, cap * i + n)) for i, n in enumerate(used)]
+    rows = torch.tensor(sum(at, []))
+    r = tower.attention(q, k[rows], v[rows], _cu(lens_q), _cu(used), causal, 0.125)
+    free = torch.ones(cap * 4, dtype=torch.bool)
+    free[rows] = False
+    k[free], v[free] = math.nan, math.nan
+    out, lse = infcl.packed_attn_fwd(_dev(q), _dev(k), _dev(v), _dev(_cu(lens_q)), 5, _dev([cap * i for i in range(5)]),
+                                     cap, causal=causal, len_k=_dev(used))
+    _check_fwd(out, lse, r, "bf16")
+    with pytest.raises(ValueError):
+        infcl.packed_attn_fwd(_dev(q), _dev(k), _dev(v), _dev(_cu(lens_q)), 5, _dev([cap * i for i in range(5)]), cap,
+                              len_k=_dev(used[:3]))
