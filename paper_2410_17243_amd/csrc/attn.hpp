@@ -43,10 +43,25 @@ struct AttnFwdPlan {
 // ... and a backward call.
 struct AttnBwdPlan {
   bool few;
-  int parts;     // of the sweeps over queries
-  int64_t trow;  // pairs of a head in stat
-  size_t stat, part, total;
+  int parts, parts_q;  // of the sweeps over queries, over keys
+  int64_t trow;        // pairs of a head in stat
+  size_t stat, part, part_q, total;
 };
+
+// Tiles of nseq sequences, of which none has more than `most` and all together
+// about `sum`.
+inline int64_t attn_tiles(int64_t nseq, int64_t most, int64_t sum) {
+  const int64_t a = nseq * most, b = sum + nseq;
+  return a < b ? a : b;
+}
+// Parts into which each of `have` sweeps is cut so that there are `want` of them,
+// at most `most` and 16.
+inline int attn_parts(int64_t have, int64_t want, int64_t most) {
+  int64_t p = have > 0 ? (want + have - 1) / have : 1;
+  p = p < most ? p : most;
+  p = p < 16 ? p : 16;
+  return (int)(p < 1 ? 1 : p);
+}
 
 // Sequence z's queries [q0, q0 + m) and keys [k0, k0 + n), cut to the arrays
 // whatever the offsets say.  z = nseq: the rows past the last sequence, as

@@ -22,7 +22,8 @@
 namespace infcl {
 namespace {
 
-constexpr int64_t kBwdGroups = 768;  // workgroups that the sweeps over queries are cut into, about
+// Workgroups that the sweeps over queries, and over keys, are cut into, about.
+constexpr int64_t kBwdGroups = 768, kBwdRowGroups = 384;
 
 struct AttnGrads {
   const uint16_t *out, *dout;
@@ -30,7 +31,8 @@ struct AttnGrads {
   const float* lse;
   float* stat;  // [heads][trow][2]: lse log2(e), D; 32 entries past the tokens may be read
   int64_t trow;
-  float* part;  // [parts][dk, dv][tokens][kvh][hd]: sums of parts of the sweeps
+  float* part;    // [parts][dk, dv][tokens][kvh][hd]: sums of parts of the sweeps over queries
+  float* part_q;  // [parts][tokens][heads][hd]: ... over keys
   uint16_t *dq, *dk, *dv;
   int64_t dqs, dqh, dks, dkh, dvs, dvh;
 };
@@ -94,9 +96,25 @@ __device__ __attribute__((noinline)) void attn_dkv_rows(const uint16_t* k, const
   }
 }
 
-// Owns rows (query, head of the group); sweeps the keys they see.
-template <int DP, int NW, int KT, bool F16>
-__global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGrads w, int tiles) {
+// The lane's row r of a sequence's key head, row by row.
+template <int KT, bool F16>
+__device__ __forceinline__ void attn_dq_again(const AttnArgs& a, const AttnGrads& w, const AttnSeq& sq, int kv,
+                                              uint32_t r) {
+  const int pos = (int)(r / (uint32_t)a.group), head = kv * a.group + (int)(r % (uint32_t)a.group);
+  const int64_t token = sq.q0 + pos;
+  const int lim = pos + sq.n - sq.m + 1;
+  const float D = attn_dq_rows<F16>(
+      a.q + token * a.qs + head * a.qh, w.dout + token * w.dos + head * w.doh, w.out + token * w.os + head * w.oh,
+      a.k + sq.k0 * a.ks + kv * a.kh, a.v + sq.k0 * a.vs + kv * a.vh, a.ks, a.vs, lim < sq.n ? lim : sq.n, a.scale,
+      w.lse[(int64_t)head * a.tq + token], lim <= KT, a.hd, (threadIdx.x >> 5) & 1,
+      w.dq + token * w.dqs + head * w.dqh);
+  if (threadIdx.x & 32) w.stat[((int64_t)head * w.trow + token) * 2 + 1] = D;
+}
+
+// Owns rows (query, head of the group); sweeps the keys they see.  SPLIT: one of
+// several parts of the keys, whose sums are left in fp32 for attn_dq_join.
+template <int DP, int NW, int KT, bool F16, bool SPLIT>
+__global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGrads w, int tiles, int parts) {
   constexpr int kFb = DP / 32, kI = DP / 16, kKb = KT / 32;
   typedef AttnTile<DP, NW, KT> Tile;
   __shared__ __attribute__((aligned(1024))) char lds_[4 * Tile::kBytes];
@@ -104,8 +122,8 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGra
   const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int h = lane >> 5;
   const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
-  const AttnPlace at = attn_place(blockIdx.x, (uint32_t)tiles, groups);
-  const int t0 = tiles - 1 - (int)at.t;
+  const AttnPlace at = attn_place(blockIdx.x, (uint32_t)(tiles * parts), groups);
+  const int t0 = tiles - 1 - (int)at.t / (SPLIT ? parts : 1), part = SPLIT ? (int)at.t % parts : 0;
   const int z = (int)(at.g / (uint32_t)a.kvh), kv = (int)(at.g % (uint32_t)a.kvh);
   AttnSeq sq = attn_seq(a, z);
   if (z == a.nseq) sq.n = 0;
@@ -136,15 +154,21 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGra
     const uint32_t rl = t * (uint64_t)(32 * NW) + 32 * NW < rows ? t * (32 * NW) + 32 * NW - 1 : rows - 1;
     int kend = a.causal ? (int)(rl / (uint32_t)a.group) + shift : sq.n;
     kend = kend < sq.n ? kend : sq.n;
+    int kbeg = 0;
+    if (SPLIT) {  // shares of the keys that this tile sees
+      const int share = ((kend > 0 ? kend : 0) + parts * KT - 1) / (parts * KT) * KT;
+      kbeg = share * part;
+      kend = kbeg + share < kend ? kbeg + share : kend;
+    }
     const uint32_t rw = t * (32 * NW) + wave * 32;
     const uint32_t rv = rw + 31 < rows ? rw + 31 : rows - 1;
     const int wmin = rw >= rows ? 0 : a.causal ? (int)(rw / (uint32_t)a.group) + shift : sq.n;
     const int wmax = rw >= rows ? 0 : a.causal ? (int)(rv / (uint32_t)a.group) + shift : sq.n;
 
     if (t != (uint32_t)t0) attn_barrier();
-    if (0 < kend) {
-      Tile::issue(kb, sq.n, kst, a.hd, lds, koff, wave);
-      Tile::issue(vb, sq.n, vst, a.hd, lds + Tile::kBytes, voff, wave);
+    if (kbeg < kend) {
+      Tile::issue(kb + (int64_t)kbeg * a.ks, sq.n - kbeg, kst, a.hd, lds, koff, wave);
+      Tile::issue(vb + (int64_t)kbeg * a.vs, sq.n - kbeg, vst, a.hd, lds + Tile::kBytes, voff, wave);
     }
     bf16x8 qf[kI], df[kI];
     float D = 0.f;
@@ -173,7 +197,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGra
     for (int fb = 0; fb < kFb; ++fb) acc[fb] = f32x16_zero();
     {
       int buf = 0;
-      for (int k = 0; k < kend; k += KT, buf ^= 1) {
+      for (int k = kbeg; k < kend; k += KT, buf ^= 1) {
         attn_barrier();
         if (k + KT < kend) {
           INFCL_LDS char* nx = lds + (buf ^ 1) * 2 * Tile::kBytes;
@@ -231,24 +255,66 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGra
         }
       }
     }
-    bad |= a.causal && wave_any(live && attn_bad(acc));
+    if (!SPLIT) bad |= a.causal && wave_any(live && attn_bad(acc));
     if (!live) continue;
-    attn_store<F16>(w.dq + token * w.dqs + head * w.dqh, acc, a.scale, h, a.hd);
-    w.stat[((int64_t)head * w.trow + token) * 2 + h] = h ? D : lse2;
+    if (!SPLIT || part == 0) w.stat[((int64_t)head * w.trow + token) * 2 + h] = h ? D : lse2;
+    if constexpr (SPLIT) {
+      float* po = w.part_q + (((int64_t)part * a.tq + token) * a.heads + head) * a.hd;
+#pragma unroll
+      for (int fb = 0; fb < kFb; ++fb)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int d = 32 * fb + 8 * j + 4 * h;
+          if (d < a.hd)
+            *(f32x4*)(po + d) = f32x4{acc[fb][4 * j], acc[fb][4 * j + 1], acc[fb][4 * j + 2], acc[fb][4 * j + 3]};
+        }
+    } else {
+      attn_store<F16>(w.dq + token * w.dqs + head * w.dqh, acc, a.scale, h, a.hd);
+    }
   }
   if (!bad) return;
   wait_dma();  // (the stores of these rows are done: other lanes write them again)
   for (uint64_t r = (uint64_t)t0 * (32 * NW) + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31); r < rows;
-       r += (uint64_t)tiles * (32 * NW)) {
-    const int pos = (int)((uint32_t)r / (uint32_t)a.group), head = kv * a.group + (int)((uint32_t)r % (uint32_t)a.group);
-    const int64_t token = sq.q0 + pos;
-    const int lim = pos + sq.n - sq.m + 1;
-    const float D = attn_dq_rows<F16>(
-        a.q + token * a.qs + head * a.qh, w.dout + token * w.dos + head * w.doh, w.out + token * w.os + head * w.oh,
-        a.k + sq.k0 * a.ks + kv * a.kh, a.v + sq.k0 * a.vs + kv * a.vh, a.ks, a.vs, lim < sq.n ? lim : sq.n, a.scale,
-        w.lse[(int64_t)head * a.tq + token], lim <= KT, a.hd, (threadIdx.x >> 5) & 1,
-        w.dq + token * w.dqs + head * w.dqh);
-    if (threadIdx.x & 32) w.stat[((int64_t)head * w.trow + token) * 2 + 1] = D;
+       r += (uint64_t)tiles * (32 * NW))
+    attn_dq_again<KT, F16>(a, w, sq, kv, (uint32_t)r);
+}
+
+// The parts' dq, in order.  A wave takes 8 rows of a sequence's key head, 16 lanes to
+// a row; if one of them is not finite, all again row by row.
+template <int KT, bool F16>
+__global__ void __launch_bounds__(256) attn_dq_join(AttnArgs a, AttnGrads w, int tiles, int parts) {
+  const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
+  const uint32_t gz = blockIdx.x % groups;
+  const int z = (int)(gz / (uint32_t)a.kvh), kv = (int)(gz % (uint32_t)a.kvh);
+  AttnSeq sq = attn_seq(a, z);
+  if (z == a.nseq) sq.n = 0;
+  const int64_t rows = (int64_t)sq.m * a.group, step = a.tq * a.heads * a.hd;
+  const int lane = threadIdx.x & 63, d = 8 * (lane & 15);
+  for (int64_t r0 = (int64_t)(blockIdx.x / groups) * 32 + (threadIdx.x >> 6) * 8; r0 < rows; r0 += (int64_t)tiles * 32) {
+    float sum = 0.f;
+#pragma unroll
+    for (int i = lane >> 4; i < 8; i += 4) {
+      if (r0 + i >= rows || d >= a.hd) continue;
+      const uint32_t r = (uint32_t)(r0 + i);
+      const int64_t token = sq.q0 + r / (uint32_t)a.group;
+      const int head = kv * a.group + (int)(r % (uint32_t)a.group);
+      const float* src = w.part_q + (token * a.heads + head) * a.hd + d;
+      float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 4
+      for (int p = 0; p < parts; ++p) {
+        const f32x4* x = (const f32x4*)(src + p * step);
+        const f32x4 x0 = x[0], x1 = x[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += x0[e], acc[4 + e] += x1[e];
+      }
+      attn_store8<F16>(w.dq + token * w.dqs + head * w.dqh + d, acc, a.scale);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf(acc[e], 0.f, sum);
+    }
+    if (!a.causal || !wave_any(!(sum == 0.f))) continue;
+    wait_dma();  // (the stores of these rows are done: other lanes write them again)
+    const int64_t r = r0 + (lane & 31);
+    if ((lane & 31) < 8 && r < rows) attn_dq_again<KT, F16>(a, w, sq, kv, (uint32_t)r);
   }
 }
 
@@ -265,7 +331,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGra
 template <int DP, int NW, bool F16, bool SPLIT>
 __global__ void __launch_bounds__(64 * NW, 2) attn_dkv_kernel(AttnArgs a, AttnGrads w, int tiles, int parts) {
   constexpr int kFb = DP / 32, kI = DP / 16, QT = 32;
-  constexpr bool kVLds = DP == 128;
+  constexpr bool kVLds = DP == 128 && NW > 1;  // (a lone wave's tiles leave it a SIMD's registers)
   typedef AttnTile<DP, NW, QT> Tile;
   typedef AttnTile<DP, NW, 32 * NW> Own;
   __shared__ __attribute__((aligned(1024))) char lds_[4 * Tile::kBytes + (kVLds ? Own::kBytes : 0)];
@@ -480,8 +546,14 @@ void launch_both(const AttnArgs& a, const AttnGrads& w, const AttnBwdPlan& p, in
   const int64_t groups = (int64_t)(a.nseq + 1) * a.kvh;
   const int64_t tq = ((max_q < 1 ? 1 : max_q) * a.group + 32 * NW - 1) / (32 * NW);
   const int64_t tk = ((max_k < 1 ? 1 : max_k) + 32 * NW - 1) / (32 * NW);
-  hipLaunchKernelGGL((attn_dq_kernel<DP, NW, KT, F16>), dim3((unsigned)(tq * groups)), dim3(64 * NW), 0, st, a, w,
-                     (int)tq);
+  const dim3 qgrid((unsigned)(tq * groups * p.parts_q));
+  if (p.parts_q == 1) {
+    hipLaunchKernelGGL((attn_dq_kernel<DP, NW, KT, F16, false>), qgrid, dim3(64 * NW), 0, st, a, w, (int)tq, 1);
+  } else if constexpr (NW > 1) {
+    hipLaunchKernelGGL((attn_dq_kernel<DP, NW, KT, F16, true>), qgrid, dim3(64 * NW), 0, st, a, w, (int)tq, p.parts_q);
+    hipLaunchKernelGGL((attn_dq_join<KT, F16>), dim3((unsigned)(NW * tq * groups)), dim3(256), 0, st, a, w,
+                       (int)(NW * tq), p.parts_q);
+  }
   const dim3 grid((unsigned)(tk * groups * p.parts));
   if (p.parts == 1) {
     hipLaunchKernelGGL((attn_dkv_kernel<DP, NW, F16, false>), grid, dim3(64 * NW), 0, st, a, w, (int)tk, 1);
@@ -511,21 +583,18 @@ void launch_t(const AttnArgs& a, const AttnGrads& w, const AttnBwdPlan& p, int64
 }  // namespace
 
 // As in the forward, short sequences run one wave to a workgroup.  Otherwise the
-// sweeps of the key tiles are cut into parts where there are fewer than two
-// workgroups for a compute unit: their lengths differ (with causal masks from
-// none to all queries), and one long sweep would be waited for.
+// sweeps are cut into parts where there are fewer workgroups than it takes to
+// fill the chip evenly: their lengths differ (with causal masks from none to all
+// of the other side), and one long sweep would be waited for.
 AttnBwdPlan attn_bwd_plan(const AttnArgs& a, int64_t max_q, int64_t max_k) {
   AttnBwdPlan p;
   p.few = max_q * a.group <= 128 && max_k <= 128;
-  p.parts = 1;
+  p.parts = p.parts_q = 1;
   if (!p.few) {
-    const int64_t most = a.nseq * ((max_k + 127) / 128), about = a.tk / 128 + a.nseq;
-    const int64_t wgs = (most < about ? most : about) * a.kvh;
-    const int64_t sweep = (max_q + 31) / 32 * a.group;  // tiles of the longest
-    int64_t parts = wgs > 0 ? (kBwdGroups + wgs - 1) / wgs : 1;
-    if (parts > sweep / 16) parts = sweep / 16;
-    if (parts > 16) parts = 16;
-    p.parts = (int)(parts < 1 ? 1 : parts);
+    const int64_t tiles = max_k > 0 ? attn_tiles(a.nseq, (max_k + 127) / 128, a.tk / 128) * a.kvh : 0;
+    p.parts = attn_parts(tiles, kBwdGroups, (max_q + 31) / 32 * a.group / 16);  // at least 16 tiles a part
+    const int64_t rows = (max_q * a.group + 127) / 128;
+    p.parts_q = attn_parts(attn_tiles(a.nseq, rows, a.tq * a.group / 128) * a.kvh, kBwdRowGroups, max_k / 256);
   }
   const size_t row = ((size_t)a.tq + 32 + 63) / 64 * 64;
   size_t off = 0;
@@ -533,6 +602,11 @@ AttnBwdPlan attn_bwd_plan(const AttnArgs& a, int64_t max_q, int64_t max_k) {
   p.stat = off, off = (off + 2 * row * (size_t)a.heads * sizeof(float) + 255) & ~(size_t)255;
   p.part = off;
   if (p.parts > 1) off += 2 * (size_t)p.parts * (size_t)a.tk * (size_t)a.kvh * (size_t)a.hd * sizeof(float);
+  p.part_q = p.part;  // (joined before the other sweep begins)
+  if (p.parts_q > 1) {
+    const size_t end = p.part + (size_t)p.parts_q * (size_t)a.tq * (size_t)a.heads * (size_t)a.hd * sizeof(float);
+    off = off > end ? off : end;
+  }
   p.total = (off + 255) & ~(size_t)255;
   return p;
 }
@@ -547,6 +621,7 @@ int launch_attn_bwd(const AttnArgs& a, const AttnBwdPlan& p, int dtype, int64_t 
   w.trow = p.trow;
   w.stat = (float*)(ws + p.stat);
   w.part = (float*)(ws + p.part);
+  w.part_q = (float*)(ws + p.part_q);
   if (dtype == INFCL_F16)
     launch_t<true>(a, w, p, max_q, max_k, st);
   else

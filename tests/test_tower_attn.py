@@ -179,7 +179,7 @@ def test_views_of_one_projection_and_autograd():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("lens,hd", [([20, 45], 64), ([150, 300], 64), ([40], 128), ([200], 128)])
+@pytest.mark.parametrize("lens,hd", [([20, 45], 64), ([150, 300], 64), ([40], 128), ([200], 128), ([900], 64), ([640], 128)])
 @pytest.mark.parametrize("bad", [math.nan, math.inf])
 def test_masked_rows_may_hold_anything(lens, hd, bad):
     """Keys and values no query of the first half sees yet, and whole other
