@@ -490,6 +490,8 @@ bool known(int t) { return t == INFCL_BF16 || t == INFCL_F32 || t == INFCL_F16; 
 int64_t chunks_of(int64_t d, int dtype) { return d * (dtype == INFCL_F32 ? 4 : 2) / 16; }
 bool rows_ok(int64_t d, int dtype) { return d % (dtype == INFCL_F32 ? 4 : 8) == 0; }
 constexpr int64_t kMaxN = ((int64_t)1 << 31) - 2, kMaxD = (int64_t)1 << 20;
+// (every workgroup of a sort pass reads all tiles' counts: 2^14 tiles are 0.3 s)
+constexpr int64_t kMaxSort = (int64_t)1 << 26;
 
 template <int T>
 int embed_fwd_t(const void* tokens, int tb, int64_t n, const void* table, int64_t vocab, int64_t d, float scale,
@@ -597,7 +599,7 @@ extern "C" infcl_status infcl_embed_fwd(const void* tokens, int token_bytes, int
 
 extern "C" infcl_status infcl_embed_bwd_workspace(int64_t n, int64_t vocab, int64_t d, size_t* bytes) {
   if (!bytes || n < 0 || vocab < 1 || d < 1) return INFCL_ERR_INVALID;
-  if (d > kMaxD || n > kMaxN || vocab > kMaxN) return INFCL_ERR_UNSUPPORTED;
+  if (d > kMaxD || n > kMaxSort || vocab > kMaxN) return INFCL_ERR_UNSUPPORTED;
   *bytes = sort_plan(n, vocab, d).total;
   return INFCL_OK;
 }
@@ -607,7 +609,7 @@ extern "C" infcl_status infcl_embed_bwd(const void* tokens, int token_bytes, int
                                         void* workspace, size_t ws_bytes, void* stream) {
   if (n < 0 || vocab < 1 || d < 1 || !known(dtype) || !known(grad_dtype) || (token_bytes != 4 && token_bytes != 8))
     return INFCL_ERR_INVALID;
-  if (!rows_ok(d, dtype) || d > kMaxD || n > kMaxN || vocab > kMaxN ||
+  if (!rows_ok(d, dtype) || d > kMaxD || n > kMaxSort || vocab > kMaxN ||
       (grad_dtype != INFCL_F32 && grad_dtype != dtype))
     return INFCL_ERR_UNSUPPORTED;
   if (!aligned(dtable, 16)) return INFCL_ERR_INVALID;

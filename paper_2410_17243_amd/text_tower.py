@@ -107,13 +107,17 @@ class TextTower(torch.nn.Module):
         dev = self.table.device
         cu = torch.arange(n + 1, dtype=torch.int32, device=dev)
         kv = [torch.zeros((2, n * self.max_len, b.kv_heads, b.hd), dtype=self.dtype, device=dev) for b in self.blocks]
-        return {"kv": kv, "cu_q": cu, "cu_k": cu * self.max_len, "len": torch.zeros(n, dtype=torch.int32, device=dev)}
+        return {"kv": kv, "cu_q": cu, "cu_k": cu * self.max_len, "len": torch.zeros(n, dtype=torch.int32, device=dev),
+                "taken": 0}
 
     @torch.no_grad()
     def extend(self, tokens, cache):
         """One more token of every caption (tokens [n]): its feature rows, as forward
-        gives them for the captions so far; keys and values go to the cache.  At
-        most max_len tokens a caption (the caller counts)."""
+        gives them for the captions so far; keys and values go to the cache, which
+        has room for max_len tokens of each."""
+        if cache["taken"] == self.max_len or tokens.numel() != cache["len"].numel():
+            raise ValueError(f"a token for each of {cache['len'].numel()} captions, {self.max_len} times at most")
+        cache["taken"] += 1
         at = cache["cu_k"][:-1].long() + cache["len"].long()
         x = embed(tokens, self.table) + embed(cache["len"], self.places)
         cache["len"] += 1

@@ -71,7 +71,9 @@ def test_extending_token_by_token_gives_the_whole_captions_features(kv):
     for i in range(9):
         last = t.extend(tokens[:, i].contiguous(), cache)
     assert cache["len"].tolist() == [9] * 5
-    assert float((whole - last).norm(dim=1).max()) < 8 * 2.0 ** -8
+    assert float((whole - last).detach().norm(dim=1).max()) < 8 * 2.0 ** -8
+    with pytest.raises(ValueError):
+        t.extend(tokens[:2, 0].contiguous(), cache)
 
 
 @pytest.mark.gpu

@@ -118,3 +118,9 @@ def test_workspaces_are_what_the_parts_need(lib):
     one = fwd(tq=1, tk=100000, nseq=1, mq=1, mk=100000)
     assert one % 256 == 0 and 0 < one <= 2048 * 4 * (64 + 2) * 4 + 512
     assert fwd(tq=1 << 20, tk=1 << 20, nseq=8192, mq=128, mk=128) == 0
+
+
+def test_token_counts_that_the_sort_would_take_too_long_for(lib):
+    n = ctypes.c_size_t(0)
+    assert lib.infcl_embed_bwd_workspace(1 << 26, 100, 8, ctypes.byref(n)) == OK
+    assert lib.infcl_embed_bwd_workspace((1 << 26) + 1, 100, 8, ctypes.byref(n)) == UNSUPPORTED

@@ -324,3 +324,37 @@ def test_a_cache_with_room(causal):
     with pytest.raises(ValueError):
         infcl.packed_attn_fwd(_dev(q), _dev(k), _dev(v), _dev(_cu(lens_q)), 5, _dev([cap * i for i in range(5)]), cap,
                               len_k=_dev(used[:3]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tq,tk", [(0, 5), (5, 0), (0, 0)])
+def test_no_queries_or_no_keys_at_all(tq, tk):
+    q, k, v, do = [_dev(t) for t in _inputs(tq, tk, 4, 2, 64, "bf16")]
+    cu = (_dev([0, tq]), tq, _dev([0, tk]), tk)
+    out, lse = infcl.packed_attn_fwd(q, k, v, *cu)
+    assert out.shape == (tq, 4, 64) and (out == 0).all() and (lse == -math.inf).all()
+    grads = infcl.packed_attn_bwd(q, k, v, out, lse, do, *cu)
+    assert [g.shape[0] for g in grads] == [tq, tk, tk] and all((g == 0).all() for g in grads)
+    none = _dev([0])  # no sequence: rows that no one has
+    out, lse = infcl.packed_attn_fwd(q, k, v, none, 0, none, 0)
+    assert (out == 0).all() and (lse == -math.inf).all()
+
+
+@pytest.mark.gpu
+def test_far_rows():
+    """Rows more than 2^32 bytes into the arrays: the last of three sequences of a
+    long cache."""
+    kv, hd, far = 8, 128, 2_200_000  # 4.5 GB of keys
+    k = torch.zeros((far + 300, kv, hd), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    q, ks, vs, do = _inputs(40, 300, 8, kv, hd, "bf16", 12)
+    k[far:], v[far:] = ks.cuda(), vs.cuda()
+    lens_q, lens_k = [0, 0, 40], [5, far - 5, 300]
+    r = tower.attention(q, ks, vs, [0, 40], [0, 300], True, hd ** -0.5, do)
+    a = (_dev(q), k, v)
+    off = (_dev(_cu(lens_q)), 40, _dev(_cu(lens_k)), 300)
+    out, lse = infcl.packed_attn_fwd(*a, *off)
+    _check_fwd(out, lse, r, "bf16")
+    dq, dk, dv = infcl.packed_attn_bwd(*a, out, lse, _dev(do), *off)
+    _check_bwd((dq, dk[far:], dv[far:]), r, "bf16")
+    assert int(dk[:far].count_nonzero()) == 0 and int(dv[:far].count_nonzero()) == 0
