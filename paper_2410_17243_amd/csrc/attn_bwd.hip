@@ -16,13 +16,23 @@
 // there it is the sum of p dp in the registers, which no rounding of o touches.
 // (The error of D from o's rounding, beside that of rounding ds, is the sum of
 // p^2 over a row in the mean square: near 1 for a row that sees few keys, 3 / n
-// over n keys of similar scores.)
+// over n keys of similar scores.)  ds is rounded as it stands: in fp16 its range is
+// that of the gradients times 1 / scale, which loss scaling has to respect.
+//
+// 4 sequences of up to 4096 tokens, 16 heads of 128 over 4: dq 229 us (910 TFLOP/s),
+// dk and dv 335 us (825) and 25 us to join their parts; bound by the latency of
+// each tile's chain (products, weights, products) at two waves per SIMD, which is
+// what 128 features' accumulators leave.  1024 captions of about 17 tokens, 8
+// heads of 64: 30 and 32 us; a wave's chain of loads for one tile of work.
 #include "attn.hpp"
 
 namespace infcl {
 namespace {
 
-// Workgroups that the sweeps over queries, and over keys, are cut into, about.
+// Workgroups that the sweeps over queries, and over keys, are cut into, about (4
+// sequences of up to 4096 tokens, 4 key heads: dk and dv with their join 560 us
+// uncut, 511, 413, 422 and 425 at 512, 768, 1024 and 1536; 3 of up to 3371 tokens, one
+// key head: dq 115 us uncut, 81 so).
 constexpr int64_t kBwdGroups = 768, kBwdRowGroups = 384;
 
 struct AttnGrads {
