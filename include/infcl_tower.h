@@ -44,7 +44,7 @@ infcl_status infcl_embed_fwd(const void* tokens, int token_bytes, int64_t n, con
  *   dtable_v = scale * sum over t with token_t = v of dout_t,
  * every row written (rows of absent tokens with zeros).  dout [n, d] of dtype.
  * The tokens are sorted (stable), the rows of one token summed in fp32 in order
- * of t, in parts of 32 where there are more.  n <= 2^26,
+ * of t, in parts of 32 or 64 where there are more.  n <= 2^26,
  * vocab < 2^31 - 1. */
 infcl_status infcl_embed_bwd_workspace(int64_t n, int64_t vocab, int64_t d, size_t* bytes);
 infcl_status infcl_embed_bwd(const void* tokens, int token_bytes, int64_t n, const void* dout, int64_t vocab,

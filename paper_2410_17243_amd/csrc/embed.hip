@@ -9,12 +9,12 @@
 // 12 bytes per token, against 2 d bytes of its row) and each table row is then
 // one group of lanes that adds its rows in order of t: no atomics on floats,
 // one write per table row, and the order of every sum is fixed.  Tokens with
-// more than kPart rows (those that open and close every caption) are summed in
-// parts of kPart sorted positions, joined in order.
+// many rows (those that open and close every caption) are summed in parts of 32
+// or 64 sorted positions, joined in order.
 //
 // 524288 tokens, 512 features of bf16, vocabulary 50000: forward 147 us (4.0 TB/s of
-// the 588 MB), sort 53 us in five launches, sums 139 us (638 MB at 4.6 TB/s), joins 39
-// us (the parts of the two tokens that every caption has are one chain).  2001
+// the 588 MB), sort 53 us in five launches, sums 140 us (638 MB at 4.6 TB/s), joins 15
+// us (the parts of the two tokens that every caption has are a chain each).  2001
 // tokens, 512 features of fp32, vocabulary 8192: 4 + 11 + 8 + 4 us, launches and the
 // latency of dependent reads.
 #include "infcl_tower.h"
@@ -77,6 +77,7 @@ struct Runs {
   const uint2* sorted;    // (token, position), n of them
   const uint32_t* start;  // by row: first sorted position whose token is >= v, v = 0 .. vocab
   const uint2* run;       // by position: [begin, end) of its run; null: by row
+  int lg;                 // log2 of the positions of a part
 };
 
 __device__ __forceinline__ void run_of(const Runs& r, int64_t at, uint32_t v, uint32_t& a, uint32_t& b) {
@@ -274,7 +275,10 @@ __global__ void __launch_bounds__(256) row_starts(const uint2* __restrict__ sort
 
 // ------------------------------------------------------------- sums by token
 
-constexpr int kPart = 32;  // sorted positions that one group of lanes sums at most
+// Sorted positions that one group of lanes sums at most, as a power of two: few
+// tokens are bound by that chain, many by the joins of the longest runs (2001
+// tokens: 25 us a step with 32, 27 with 64; 524288: 375 and 352).
+constexpr int kPartFew = 5, kPartMany = 6;
 
 // Sum of the rows at sorted positions [a, b), chunk i of c, in order.  The 1 << ls
 // lanes of the group read their positions together.
@@ -323,9 +327,9 @@ __device__ __forceinline__ void put_row(void* dtable, int64_t v, int c, int i, c
   }
 }
 
-// Blocks [0, row_blocks): table rows (or sorted positions that begin a run) of at most kPart tokens, a group
-// of lanes each.  The others: stretches [kPart p, kPart (p + 1)) of the sorted
-// positions, for tokens with more than kPart rows.  Such a stretch holds parts of
+// Blocks [0, row_blocks): table rows (or sorted positions that begin a run) of at
+// most one part, P positions, a group of lanes each.  The others: stretches
+// [P p, P (p + 1)) of the sorted positions, for tokens with more rows.  Such a stretch holds parts of
 // at most two of them (one inside it would be too short): sums in slots 2p (the
 // run that holds its first position) and 2p + 1 (the one of its last, if
 // another).  blockIdx.y: a slice of 1 << ls chunks of the row.
@@ -347,15 +351,15 @@ __global__ void __launch_bounds__(256) embed_sum(Runs r, int64_t n, const u32x4*
     }
     if (v >= vocab) return;
     if (!r.run) a = r.start[v], b = r.start[v + 1];
-    if (b - a > kPart) return;
+    if (b - a > 1u << r.lg) return;
     sum_rows<T>(r.sorted, dout, c, i, gl, ls, a, b, s);
     if (i < c) put_row<T, G>(dtable, v, c, i, s, scale);
     return;
   }
   const int64_t p = (int64_t)(blockIdx.x - row_blocks) * per + (threadIdx.x >> ls);
-  const int64_t s0 = p * kPart;
+  const int64_t s0 = p << r.lg;
   if (s0 >= n) return;
-  const uint32_t a0 = (uint32_t)s0, b0 = (uint32_t)(s0 + kPart < n ? s0 + kPart : n);
+  const uint32_t a0 = (uint32_t)s0, b0 = (uint32_t)(s0 + (1 << r.lg) < n ? s0 + (1 << r.lg) : n);
   const uint32_t v0 = r.sorted[a0].x, v1 = r.sorted[b0 - 1].x;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -363,7 +367,7 @@ __global__ void __launch_bounds__(256) embed_sum(Runs r, int64_t n, const u32x4*
     if (v >= vocab || (h && v1 == v0)) continue;
     uint32_t a, b;
     run_of(r, h ? b0 - 1 : a0, v, a, b);
-    if (b - a <= kPart) continue;
+    if (b - a <= 1u << r.lg) continue;
     sum_rows<T>(r.sorted, dout, c, i, gl, ls, a > a0 ? a : a0, b < b0 ? b : b0, s);
     if (i >= c) continue;
     float* q = part + ((2 * p + h) * c + i) * N;
@@ -372,7 +376,7 @@ __global__ void __launch_bounds__(256) embed_sum(Runs r, int64_t n, const u32x4*
   }
 }
 
-// The parts of tokens with more than kPart rows, in order.  A workgroup looks at
+// The parts of tokens with more rows than a part has, in order.  A workgroup looks at
 // 64 stretches, a lane of every wave at one: runs that begin there and have at
 // most kWaveParts parts are joined by a wave each, longer ones by all of them.
 // A wave adds four interleaved quarters of its parts, 16 chunks of the row at a
@@ -413,15 +417,15 @@ __global__ void __launch_bounds__(64 * kJoinWaves)
   __shared__ float red[kJoinWaves - 1][16][N + 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int i = blockIdx.y * 16 + (lane & 15), u = lane >> 4;
-  const int64_t p0 = (int64_t)blockIdx.x * 64, s0 = (p0 + lane) * kPart;
+  const int64_t p0 = (int64_t)blockIdx.x * 64, s0 = (p0 + lane) << r.lg;
   uint32_t v = vocab, a = 0, b = 0;
   if (s0 < n) {
-    const int64_t last = (s0 + kPart < n ? s0 + kPart : n) - 1;
+    const int64_t last = (s0 + (1 << r.lg) < n ? s0 + (1 << r.lg) : n) - 1;
     v = r.sorted[last].x;  // (a long run that begins here holds the stretch's last position)
     if (v < vocab) run_of(r, last, v, a, b);
   }
-  const bool starts = v < vocab && b - a > kPart && a >= s0;
-  const uint32_t cnt = starts ? (b - 1) / kPart - (uint32_t)(p0 + lane) + 1 : 0;
+  const bool starts = v < vocab && b - a > 1u << r.lg && a >= s0;
+  const uint32_t cnt = starts ? ((b - 1) >> r.lg) - (uint32_t)(p0 + lane) + 1 : 0;
   const bool inside = a > s0;
   float s[N];
   int k = 0;
@@ -464,6 +468,7 @@ size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 struct SortPlan {
   bool few;
   int bits, passes;  // bits of a digit
+  int lg;            // log2 of a part
   int64_t tiles;
   size_t el0, el1, hist, start, run, part, total;
 };
@@ -485,7 +490,8 @@ SortPlan sort_plan(int64_t n, int64_t vocab, int64_t d) {
     s.hist = off; off = up256(off + ((size_t)s.tiles << s.bits) * 4);
     s.start = off; off = up256(off + (size_t)(vocab + 1) * 4);
   }
-  s.part = off; off = up256(off + (size_t)((n + kPart - 1) / kPart) * 2 * (size_t)d * 4);
+  s.lg = s.few ? kPartFew : kPartMany;
+  s.part = off; off = up256(off + (size_t)((n + (1 << s.lg) - 1) >> s.lg) * 2 * (size_t)d * 4);
   s.total = off;
   return s;
 }
@@ -565,12 +571,13 @@ int embed_bwd_t(const void* tokens, int tb, int64_t n, const void* dout, int64_t
   }
   const SortPlan s = sort_plan(n, vocab, d);
   Runs r = {};
+  r.lg = s.lg;
   const int rc = tb == 4 ? sort_tokens<int32_t>(tokens, n, vocab, s, ws, dtable, chunks, r, st)
                          : sort_tokens<int64_t>(tokens, n, vocab, s, ws, dtable, chunks, r, st);
   if (rc != INFCL_OK) return rc;
   const int ls = row_lanes_log2(c, 1);
-  const int64_t per = 256 >> ls, rows = s.few ? n : vocab, parts = (n + kPart - 1) / kPart;
-  const int64_t rb = (rows + per - 1) / per, pb = n > kPart ? (parts + per - 1) / per : 0;
+  const int64_t per = 256 >> ls, rows = s.few ? n : vocab, parts = (n + (1 << s.lg) - 1) >> s.lg;
+  const int64_t rb = (rows + per - 1) / per, pb = n > 1 << s.lg ? (parts + per - 1) / per : 0;
   const unsigned slices = (unsigned)((c + (1 << ls) - 1) >> ls);
   hipLaunchKernelGGL((embed_sum<T, G>), dim3((unsigned)(rb + pb), slices), dim3(256), 0, st, r, n, (const u32x4*)dout,
                      (uint32_t)vocab, (int)c, ls, scale, dtable, (float*)(ws + s.part), (uint32_t)rb);
