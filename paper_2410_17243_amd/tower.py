@@ -4,6 +4,8 @@ What an encoder trained beside the contrastive loss runs: token embedding,
 attention over packed sequences, and activation checkpoints in 8 bits.  As in
 the package itself this module only marshals arguments; the work is done by
 the HIP kernels of libinfcl.so on the current stream, and nothing falls back.
+The autograd functions are differentiable once: a gradient of their gradient is
+an error.
 
 Token embedding
     embed_fwd(tokens, table, scale=1.0) -> out
@@ -30,6 +32,7 @@ import ctypes
 import functools
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import INFCL_BF16, INFCL_F16, INFCL_F32, _check, _ptr, _raw_stream, load_library
 
@@ -167,6 +170,7 @@ class _Embed(torch.autograd.Function):
         return embed_fwd(tokens, table, scale)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         (tokens,) = ctx.saved_tensors
         return None, embed_bwd(tokens, dout.contiguous(), ctx.vocab, ctx.scale, dout.dtype), None
@@ -288,6 +292,7 @@ class _PackedAttn(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         q, k, v, out, lse, cu_q, cu_k = ctx.saved_tensors
         max_q, max_k, causal, scale = ctx.rest
@@ -310,6 +315,7 @@ class _PackedAttnQkv(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         qkv, out, lse, cu = ctx.saved_tensors
         heads, kv_heads, max_len, causal, scale = ctx.rest
@@ -457,6 +463,7 @@ class _Linear8(torch.autograd.Function):
         return torch.nn.functional.linear(x, w, b)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         q, exps, w = ctx.saved_tensors
         dy = dy.contiguous()
@@ -483,6 +490,7 @@ class _Mlp8(torch.autograd.Function):
         return torch.nn.functional.linear(a, w2, b2)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         xq, xe, hq, he, w1, w2 = ctx.saved_tensors
         dy = dy.contiguous()

@@ -1,0 +1,72 @@
+"""The tower's autograd functions as the graph sees them, without a GPU: the
+kernels' places are taken by torch products that leave no graph, as the kernels
+leave none."""
+
+import math
+
+import pytest
+import torch
+
+import paper_2410_17243_amd as infcl
+from oracle import tower as oracle
+from paper_2410_17243_amd import tower
+
+
+@pytest.fixture
+def plain_kernels(monkeypatch):
+    """Stand-ins that compute in the inputs' type on the CPU and keep x as it is."""
+    keep = lambda x: tower.Ckpt8(x.detach().clone(), torch.zeros((*x.shape[:-1], 1), dtype=torch.uint8), x.dtype)  # noqa: E731
+
+    def wgrad(dy, kept, act="none", grad_dtype=None):
+        x = oracle.act(kept.q.reshape(-1, kept.q.shape[-1]), act)
+        return (dy.detach().reshape(-1, dy.shape[-1]).T @ x).to(grad_dtype or torch.float32)
+
+    def attn_fwd(q, k, v, cu_q, max_q, *rest, **kw):
+        r = oracle.attention(q.detach(), k.detach(), v.detach(), cu_q.tolist(), cu_q.tolist(), True, q.shape[2] ** -0.5)
+        return r["out"].to(q.dtype), r["lse"].float()
+
+    def attn_bwd(q, k, v, out, lse, dout, cu_q, max_q, *rest, grads=None, **kw):
+        r = oracle.attention(q.detach(), k.detach(), v.detach(), cu_q.tolist(), cu_q.tolist(), True, q.shape[2] ** -0.5,
+                             dout.detach())
+        got = tuple(r[n].to(q.dtype) for n in ("dq", "dk", "dv"))
+        for to, x in zip(grads or (), got):
+            to.copy_(x)
+        return got
+
+    for name, fn in {
+        "ckpt8_pack": keep, "ckpt8_act_fwd": lambda x, act: (oracle.act(x.detach(), act), keep(x)), "ckpt8_wgrad": wgrad,
+        "ckpt8_act_bwd": lambda dy, kept, act: dy.detach() * oracle.act_slope(kept.q, act),
+        "embed_fwd": lambda tok, table, scale=1.0: scale * table.detach()[tok],
+        "embed_bwd": lambda tok, dout, vocab, scale=1.0, gdt=None: torch.zeros((vocab, dout.shape[-1]), dtype=gdt).index_add_(
+            0, tok.reshape(-1), scale * dout.detach().reshape(-1, dout.shape[-1])),
+        "packed_attn_fwd": attn_fwd, "packed_attn_bwd": attn_bwd,
+    }.items():
+        monkeypatch.setattr(tower, name, fn)
+
+
+def _call(name):
+    """(the function of its differentiable arguments, those arguments)."""
+    g = torch.Generator().manual_seed(3)
+    r = lambda *s: (torch.randn(s, generator=g) / math.sqrt(s[-1])).requires_grad_()  # noqa: E731
+    cu = torch.tensor([0, 4, 6], dtype=torch.int32)
+    return {
+        "embed": (lambda w: infcl.embed(torch.tensor([1, 0, 3]), w, 2.0), [r(5, 8)]),
+        "linear8": (infcl.linear8, [r(6, 8), r(16, 8), r(16)]),
+        "mlp8": (lambda *a: infcl.mlp8(*a, act="gelu"), [r(6, 8), r(16, 8), r(16), r(8, 16), r(8)]),
+        "packed_attn": (lambda q, k, v: infcl.packed_attn(q, k, v, cu, 4), [r(6, 2, 8), r(6, 1, 8), r(6, 1, 8)]),
+        "packed_attn_qkv": (lambda x: infcl.packed_attn_qkv(x, 2, 1, cu, 4), [r(6, 4, 8)]),
+    }[name]
+
+
+NAMES = ["embed", "linear8", "mlp8", "packed_attn", "packed_attn_qkv"]
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_second_derivatives_are_refused(plain_kernels, name):
+    """The kernels leave no graph: a gradient of a gradient would miss what went
+    through them, so it is an error, and not a number."""
+    f, args = _call(name)
+    first = torch.autograd.grad(f(*args).square().sum(), args, create_graph=True)
+    assert all(torch.isfinite(x).all() for x in first)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (args[0].square().sum() + sum(x.square().sum() for x in first)).backward()  # (a penalty beside a plain term)
