@@ -44,7 +44,8 @@ __device__ __forceinline__ float act_value(float x) {
   }
 }
 // f'(x): Phi(x) + x phi(x), or s (1 + 1.702 x (1 - s)) with s = sigma(1.702 x).
-// Far on the negative side s is 0 and x (1 - s) finite: the product is 0.
+// Far on the negative side s is 0, and x s with it: no product there leaves fp32's
+// range, as 1.702 x would below -2e38.
 template <int ACT>
 __device__ __forceinline__ float act_slope(float x) {
   if constexpr (ACT == kActGelu) {
@@ -53,7 +54,7 @@ __device__ __forceinline__ float act_slope(float x) {
     return fmaf(x * 0.39894228040143268f, E, x > 0.f ? 1.f - q : q);
   } else {
     const float s = __builtin_amdgcn_rcpf(1.f + exp2_hw(-1.702f * kLog2e * x));
-    return s * (1.f + 1.702f * x * (1.f - s));
+    return fmaf(1.702f * (1.f - s), x * s, s);
   }
 }
 

@@ -80,6 +80,25 @@ def test_activation(n, d, dtype, act):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("act", ["gelu", "quick_gelu"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_activation_at_the_ends_of_the_range(dtype, act):
+    """From far below zero to far above: the slope is 0 and 1 there, the value 0
+    and x, up to the largest entries (each in a group of its own)."""
+    ends = [-3.38e38, -2.5e38, -2e38, -1e38, -1e30, -1e4, -60.0, 60.0, 1e4, 1e30, 1e38, 3.38e38]  # (bf16 ends at 3.3895e38)
+    x = torch.zeros((len(ends), 32))
+    x[:, 5] = torch.tensor(ends)
+    x = x.to(DT[dtype])
+    dy = torch.full_like(x, -1.5)
+    out, kept = infcl.ckpt8_act_fwd(x.cuda(), act)
+    dx = infcl.ckpt8_act_bwd(dy.cuda(), kept, act).cpu()
+    assert torch.equal(out.cpu()[:, 5], torch.where(x[:, 5] < 0, torch.zeros_like(x[:, 5]), x[:, 5]))
+    assert torch.equal(dx[:, 5], torch.where(x[:, 5] < 0, 0.0, -1.5).to(DT[dtype]))
+    # at 0 the slope is 1/2, by the bounds of test_activation
+    assert ((dx[:, :5].double() + 0.75).abs() <= HALF[dtype] * 0.75 + 8 * 2.0 ** -24 * 1.5).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("n,d,m,dtype,act,grad", [
     (1, 8, 8, "bf16", "none", "f32"), (31, 40, 72, "f16", "none", "f32"), (32, 128, 128, "bf16", "none", "bf16"),
     (33, 136, 120, "bf16", "gelu", "f32"), (500, 264, 520, "f16", "quick_gelu", "f16"), (2000, 256, 256, "bf16", "none", "f32"),
