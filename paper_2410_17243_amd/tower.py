@@ -454,6 +454,20 @@ def ckpt8_wgrad(dy, kept: Ckpt8, act: str = "none", grad_dtype=None):
     return dw
 
 
+def _check_learning(name, x, *weights):
+    """What the weight gradients will ask for, asked before the forward's work."""
+    if not torch.is_grad_enabled():
+        return
+    dtype = torch.get_autocast_dtype("cuda") if torch.is_autocast_enabled("cuda") else x.dtype
+    for w in weights:
+        if not w.requires_grad:
+            continue
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError(f"{name}: a layer learns from products in bfloat16 or float16, got {dtype}")
+        if w.shape[0] % 8:
+            raise ValueError(f"{name}: a layer that learns has a multiple of 8 outputs, got {w.shape[0]}")
+
+
 class _Linear8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, b):
@@ -476,7 +490,8 @@ class _Linear8(torch.autograd.Function):
 def linear8(x, w, b=None):
     """x w^T + b with x kept for the backward pass in 8 bits.  x, w (and b) of one
     16-bit dtype; the plain products are torch's, the weight gradient is
-    ckpt8_wgrad's."""
+    ckpt8_wgrad's (a multiple of 8 outputs)."""
+    _check_learning("linear8", x, w)
     return _Linear8.apply(x, w, b)
 
 
@@ -506,6 +521,8 @@ class _Mlp8(torch.autograd.Function):
 
 def mlp8(x, w1, b1, w2, b2, act: str = "gelu"):
     """f(x w1^T + b1) w2^T + b2, which keeps x and the first product in 8 bits for
-    the backward pass and nothing else (f of it is taken again from there)."""
+    the backward pass and nothing else (f of it is taken again from there).  Types
+    and widths as for linear8."""
     _act(act)
+    _check_learning("mlp8", x, w1, w2)
     return _Mlp8.apply(x, w1, b1, w2, b2, act)

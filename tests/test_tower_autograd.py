@@ -47,7 +47,7 @@ def plain_kernels(monkeypatch):
 def _call(name):
     """(the function of its differentiable arguments, those arguments)."""
     g = torch.Generator().manual_seed(3)
-    r = lambda *s: (torch.randn(s, generator=g) / math.sqrt(s[-1])).requires_grad_()  # noqa: E731
+    r = lambda *s: (torch.randn(s, generator=g) / math.sqrt(s[-1])).bfloat16().requires_grad_()  # noqa: E731
     cu = torch.tensor([0, 4, 6], dtype=torch.int32)
     return {
         "embed": (lambda w: infcl.embed(torch.tensor([1, 0, 3]), w, 2.0), [r(5, 8)]),
@@ -70,3 +70,39 @@ def test_second_derivatives_are_refused(plain_kernels, name):
     assert all(torch.isfinite(x).all() for x in first)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         (args[0].square().sum() + sum(x.square().sum() for x in first)).backward()  # (a penalty beside a plain term)
+
+
+def _layers():
+    r = lambda *s: torch.randn(s, generator=torch.Generator().manual_seed(5)).bfloat16().requires_grad_()  # noqa: E731
+    f32 = lambda *s: r(*s).detach().float().requires_grad_()  # noqa: E731
+    mlp = lambda *a: infcl.mlp8(*a, act="gelu")  # noqa: E731
+    return {
+        "linear8, 12 outputs": (infcl.linear8, (r(6, 8), r(12, 8), None), ValueError),
+        "linear8, fp32": (infcl.linear8, (f32(6, 8), f32(16, 8), None), TypeError),
+        "mlp8, 12 outputs": (mlp, (r(6, 8), r(16, 8), None, r(12, 16), None), ValueError),
+        "mlp8, 12 inside": (mlp, (r(6, 8), r(12, 8), None, r(8, 12).detach(), None), ValueError),
+        "mlp8, fp32": (mlp, (f32(6, 8), f32(16, 8), f32(16), f32(8, 16), f32(8)), TypeError),
+        "mlp8, fp32, one layer learns": (mlp, (f32(6, 8), f32(16, 8).detach(), None, f32(8, 16), None), TypeError),
+    }
+
+
+@pytest.mark.parametrize("name", list(_layers()))
+def test_layers_refuse_in_the_forward_what_the_backward_cannot_do(name):
+    """Widths that are no multiple of 8, and fp32 products, where a weight gradient is to come."""
+    f, args, error = _layers()[name]
+    with pytest.raises(error, match="layer"):
+        f(*args)
+
+
+@pytest.mark.parametrize("name", ["linear8", "mlp8"])
+def test_layers_with_frozen_weights_need_no_weight_gradient(plain_kernels, name):
+    """What only the weight gradient asks for is not asked for without one: fp32, and
+    12 outputs."""
+    g = torch.Generator().manual_seed(3)
+    x, w1, w2 = torch.randn((6, 8), generator=g).requires_grad_(), torch.randn((16, 8), generator=g), torch.randn((12, 16), generator=g)
+    y = infcl.linear8(x, w2[:, :8]) if name == "linear8" else infcl.mlp8(x, w1, None, w2, None)
+    y.sum().backward()
+    assert torch.isfinite(x.grad).all()
+    with torch.no_grad():
+        same = infcl.linear8(x, w2[:, :8].requires_grad_()) if name == "linear8" else infcl.mlp8(x, w1, None, w2.requires_grad_(), None)
+    assert torch.equal(same, y)
