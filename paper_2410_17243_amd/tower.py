@@ -32,6 +32,7 @@ import ctypes
 import functools
 
 import torch
+from torch.amp import custom_bwd, custom_fwd
 from torch.autograd.function import once_differentiable
 
 from . import INFCL_BF16, INFCL_F16, INFCL_F32, _check, _ptr, _raw_stream, load_library
@@ -470,6 +471,7 @@ def _check_learning(name, x, *weights):
 
 class _Linear8(torch.autograd.Function):
     @staticmethod
+    @custom_fwd(device_type="cuda")
     def forward(ctx, x, w, b):
         kept = ckpt8_pack(x)
         ctx.save_for_backward(kept.q, kept.exps, w)
@@ -478,6 +480,7 @@ class _Linear8(torch.autograd.Function):
 
     @staticmethod
     @once_differentiable
+    @custom_bwd(device_type="cuda")  # (the plain products as the forward's, under autocast too)
     def backward(ctx, dy):
         q, exps, w = ctx.saved_tensors
         dy = dy.contiguous()
@@ -489,14 +492,15 @@ class _Linear8(torch.autograd.Function):
 
 def linear8(x, w, b=None):
     """x w^T + b with x kept for the backward pass in 8 bits.  x, w (and b) of one
-    16-bit dtype; the plain products are torch's, the weight gradient is
-    ckpt8_wgrad's (a multiple of 8 outputs)."""
+    16-bit dtype, or of any under autocast; the plain products are torch's, the
+    weight gradient is ckpt8_wgrad's (a multiple of 8 outputs)."""
     _check_learning("linear8", x, w)
     return _Linear8.apply(x, w, b)
 
 
 class _Mlp8(torch.autograd.Function):
     @staticmethod
+    @custom_fwd(device_type="cuda")
     def forward(ctx, x, w1, b1, w2, b2, act):
         kx = ckpt8_pack(x)
         a, kh = ckpt8_act_fwd(torch.nn.functional.linear(x, w1, b1), act)
@@ -506,6 +510,7 @@ class _Mlp8(torch.autograd.Function):
 
     @staticmethod
     @once_differentiable
+    @custom_bwd(device_type="cuda")  # (the plain products as the forward's, under autocast too)
     def backward(ctx, dy):
         xq, xe, hq, he, w1, w2 = ctx.saved_tensors
         dy = dy.contiguous()

@@ -106,3 +106,26 @@ def test_layers_with_frozen_weights_need_no_weight_gradient(plain_kernels, name)
     with torch.no_grad():
         same = infcl.linear8(x, w2[:, :8].requires_grad_()) if name == "linear8" else infcl.mlp8(x, w1, None, w2.requires_grad_(), None)
     assert torch.equal(same, y)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["linear8", "mlp8"])
+def test_fp32_weights_under_autocast(name):
+    """fp32 weights and inputs under autocast: what the same layer gives for their
+    bf16 roundings, gradients included, with the backward pass outside of autocast."""
+    g = torch.Generator().manual_seed(3)
+    r = lambda *s: torch.randn(s, generator=g).cuda()  # noqa: E731
+    args = [r(40, 64), r(48, 64), r(48)] + ([r(16, 48), r(16)] if name == "mlp8" else [])
+    f = infcl.linear8 if name == "linear8" else (lambda *a: infcl.mlp8(*a, act="gelu"))
+    dy = r(40, 48 if name == "linear8" else 16).bfloat16()
+    low = [a.bfloat16().requires_grad_() for a in args]
+    y = f(*low)
+    y.backward(dy)
+    wide = [a.bfloat16().float().requires_grad_() for a in args]
+    with torch.autocast("cuda", torch.bfloat16):
+        z = f(*wide)
+    z.backward(dy)
+    assert z.dtype == torch.bfloat16 and torch.equal(z, y)
+    for a, b in zip(wide, low):
+        # (a bias's gradient is an fp32 sum under autocast)
+        assert a.grad.dtype == torch.float32 and torch.equal(a.grad.bfloat16(), b.grad)
