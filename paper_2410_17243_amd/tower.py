@@ -178,7 +178,10 @@ class _Embed(torch.autograd.Function):
 
 
 def embed(tokens, table, scale: float = 1.0):
-    """scale * table[tokens]; differentiable with respect to the table."""
+    """scale * table[tokens]; differentiable with respect to the table (up to 2^26
+    tokens)."""
+    if table.requires_grad and torch.is_grad_enabled() and table.dim() == 2:  # (the gradient's limits, before the work)
+        _workspace_bytes("infcl_embed_bwd_workspace", tokens.numel(), *table.shape)
     return _Embed.apply(tokens, table, float(scale))
 
 

@@ -129,3 +129,14 @@ def test_fp32_weights_under_autocast(name):
     for a, b in zip(wide, low):
         # (a bias's gradient is an fp32 sum under autocast)
         assert a.grad.dtype == torch.float32 and torch.equal(a.grad.bfloat16(), b.grad)
+
+
+def test_a_table_that_learns_takes_as_many_tokens_as_its_gradient():
+    """The gradient sorts up to 2^26 tokens; more are refused before the forward's work."""
+    table, n = torch.empty((100, 8), device="meta", requires_grad=True), 1 << 26
+    for tokens, status in ((n + 1, infcl.INFCL_ERR_UNSUPPORTED), (n, None)):
+        with pytest.raises((infcl.InfclError, ValueError)) as e:
+            infcl.embed(torch.empty(tokens, dtype=torch.int32, device="meta"), table)
+        assert getattr(e.value, "status", None) == status  # (n of them get as far as the device's check)
+    with torch.no_grad(), pytest.raises(ValueError, match="device"):
+        infcl.embed(torch.empty(n + 1, dtype=torch.int32, device="meta"), table)
