@@ -264,6 +264,17 @@ __device__ __forceinline__ void attn_store(uint16_t* row, const f32x16 (&acc)[FB
     }
 }
 
+// ---- Masked rows that hold infinities or NaN.  A masked weight is zero, but zero
+// times such an entry is NaN, and a product's swept rows are common to own rows
+// that see them and own rows that do not.  Only the tiles that a causal mask cuts
+// have rows of both kinds (past a sequence's end the copies leave zeros), and they
+// are a sweep's last ones.  A wave whose sums are not finite looks at the rows of
+// these tiles; where those are all finite its results stand.  Else its workgroup
+// sweeps again without them (CUT), and then takes them one by one on the vector
+// unit, in fp32, from memory, each for the own rows that see it: two tiles' rows
+// and a wave's 32 at most (times the heads of a group for keys), whatever the
+// length and whoever sees them.
+
 // Whether an accumulator holds a NaN (x 0 is NaN for infinities too).
 template <int FB>
 __device__ __forceinline__ bool attn_bad(const f32x16 (&acc)[FB]) {
@@ -274,15 +285,45 @@ __device__ __forceinline__ bool attn_bad(const f32x16 (&acc)[FB]) {
     for (int r = 0; r < 16; ++r) t = fmaf(acc[fb][r], 0.f, t);
   return !(t == 0.f);
 }
+// Whether rows [0, n) of x hold an entry that is not finite (the wave together).
+// Adding the exponent's last bit to |x| carries into the sign's place from the
+// exponent of all ones on.
+template <bool F16>
+__device__ __forceinline__ bool attn_odd(const uint16_t* x, int n, int64_t stride, int hd, int lane) {
+  uint32_t odd = 0;
+#pragma unroll 1
+  for (int r = lane >> 4; r < n; r += 4)
+    if (8 * (lane & 15) < hd) {
+      const u32x4 w = *(const u32x4*)(x + r * stride + 8 * (lane & 15));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) odd |= (w[i] & 0x7FFF7FFFu) + (F16 ? 0x04000400u : 0x00800080u);
+    }
+  return wave_any((odd & 0x80008000u) != 0);
+}
+// ... the keys x of sequence sq's key head in the tiles that the mask of a wave's
+// rows [rw, rw + 32) of (query, head of the group) cuts.
+template <bool F16>
+__device__ __forceinline__ bool attn_odd_keys(const uint16_t* x, int64_t stride, int hd, const AttnSeq& sq, int group,
+                                              uint32_t rw, uint32_t rows, int tile) {
+  const uint32_t rv = rw + 31 < rows ? rw + 31 : rows - 1;
+  int lo = (int)(rw / (uint32_t)group) + sq.n - sq.m + 1, hi = (int)(rv / (uint32_t)group) + sq.n - sq.m + 1 + tile;
+  lo = lo < 0 ? 0 : lo, hi = hi < sq.n ? hi : sq.n;
+  return attn_odd<F16>(x + lo * stride, hi - lo, stride, hd, (int)threadIdx.x & 63);
+}
+// Whether one of the workgroup's waves says so; `flags`: NW words that were not read
+// since the last barrier.
+template <int NW>
+__device__ __forceinline__ bool attn_vote(bool x, INFCL_LDS int* flags, int wave) {
+  if constexpr (NW == 1) return x;
+  flags[wave] = x;
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  int any = 0;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) any |= flags[i];
+  return __builtin_amdgcn_readfirstlane(any) != 0;
+}
 
-// ---- The row-by-row form.  A masked weight is zero, but zero times an infinity
-// or a NaN of a masked row would reach the product.  A wave whose sums are not
-// finite therefore takes its rows again on the vector unit, in fp32, from
-// memory, without reading any row that is masked.  Only such rows take the time
-// (a thousand times a sweep's).  The functions are calls, not inlined, with few
-// registers, so that the sweeps keep theirs: they go through the features 8 at a
-// time, with all weights anew.  Lanes L and L ^ 32 share an own row and take
-// every other 8 features of it.
+// Lanes L and L ^ 32 share an own row and take every other 8 features of it.
 
 // <x, y>, over both lanes' features.
 template <bool F16>
@@ -296,13 +337,24 @@ __device__ __forceinline__ float attn_dot(const uint16_t* x, const uint16_t* y, 
   }
   return attn_sum2(s);
 }
-// acc += w x[0 .. 7]
-template <bool F16>
-__device__ __forceinline__ void attn_axpy8(float (&acc)[8], float w, const uint16_t* x) {
-  const bf16x8 a = *(const bf16x8*)x;
+// acc += w x, acc as the products leave it.
+template <bool F16, int FB>
+__device__ __forceinline__ void attn_axpy(f32x16 (&acc)[FB], float w, const uint16_t* x, int h, int hd) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) acc[e] = fmaf(w, from16<F16>(a[e]), acc[e]);
+  for (int fb = 0; fb < FB; ++fb)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int d = 32 * fb + 8 * j + 4 * h;
+      if (d >= hd) continue;
+      const u32x2 a = *(const u32x2*)(x + d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint16_t b = (uint16_t)(a[e >> 1] >> (16 * (e & 1)));
+        acc[fb][4 * j + e] = fmaf(w, from16<F16>(__builtin_bit_cast(__bf16, b)), acc[fb][4 * j + e]);
+      }
+    }
 }
+// 8 sums times f as 16-bit elements.
 template <bool F16>
 __device__ __forceinline__ void attn_store8(uint16_t* x, const float (&acc)[8], float f) {
   bf16x8 a;
@@ -314,6 +366,16 @@ __device__ __forceinline__ void attn_store8(uint16_t* x, const float (&acc)[8], 
 // Barrier of the workgroup after all of this wave's copies and LDS reads.
 __device__ __forceinline__ void attn_barrier() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// A kernel's arguments (all of them, as a struct) read again: code after a sweep
+// that is seldom run then does not hold them in registers through the sweep.
+template <typename Args>
+__device__ __forceinline__ Args attn_reload() {
+  typedef const __attribute__((address_space(4))) char Kernarg;
+  Kernarg* p = (Kernarg*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm("" : "+s"(p));
+  return *(const Args*)p;
 }
 
 }  // namespace infcl

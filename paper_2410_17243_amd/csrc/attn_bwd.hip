@@ -47,100 +47,20 @@ struct AttnGrads {
   int64_t dqs, dqh, dks, dkh, dvs, dvh;
 };
 
-// Row by row (attn.hpp): dq of the lane's row from keys [0, lim).  own_d: D is
-// the sum of p dp.  Returns D.
-template <bool F16>
-__device__ __attribute__((noinline)) float attn_dq_rows(const uint16_t* q, const uint16_t* dout,
-                                                        const uint16_t* out, const uint16_t* k, const uint16_t* v,
-                                                        int64_t ks, int64_t vs, int lim, float scale, float lse,
-                                                        bool own_d, int hd, int h, uint16_t* dq) {
-  const float sl2 = scale * kLog2e, lse2 = lse == -__builtin_inff() ? 0.f : lse * kLog2e;
-  float D = 0.f;
-  if (lse != -__builtin_inff() && !own_d) D = attn_dot<F16>(dout, out, h, hd);
-  if (own_d) {
-#pragma unroll 1
-    for (int j = 0; j < lim; ++j) {
-      const float p = exp2_hw(fmaf(attn_dot<F16>(q, k + j * ks, h, hd), sl2, -lse2));
-      D = fmaf(p, attn_dot<F16>(dout, v + j * vs, h, hd), D);
-    }
-  }
-#pragma unroll 1
-  for (int d = 0; d < hd; d += 16) {
-    float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    const int at = d + 8 * h;
-#pragma unroll 1
-    for (int j = 0; j < lim; ++j) {
-      const float p = exp2_hw(fmaf(attn_dot<F16>(q, k + j * ks, h, hd), sl2, -lse2));
-      const float ds = p * (attn_dot<F16>(dout, v + j * vs, h, hd) - D);
-      if (at < hd) attn_axpy8<F16>(acc, ds, k + j * ks + at);
-    }
-    if (at < hd) attn_store8<F16>(dq + at, acc, scale);
-  }
-  return D;
-}
+// Whether dk's and dv's sweeps keep the own values in LDS (below).
+constexpr bool attn_own_in_lds(int dp, int nw) { return dp == 128 && nw > 1; }  // (a lone wave's tiles leave it a SIMD's registers)
 
-// ... dk and dv of the lane's key from queries [first, m) of the group's heads.
-template <bool F16>
-__device__ __attribute__((noinline)) void attn_dkv_rows(const uint16_t* k, const uint16_t* v, const uint16_t* q,
-                                                        const uint16_t* dout, int64_t qs, int64_t qh, int64_t ds_,
-                                                        int64_t dh, const float* stat, int64_t trow, int first, int m, int group, float scale, int hd, int h,
-                                                        uint16_t* dk, uint16_t* dv) {
-  const float sl2 = scale * kLog2e;
-#pragma unroll 1
-  for (int d = 0; d < hd; d += 16) {
-    float ak[8] = {0, 0, 0, 0, 0, 0, 0, 0}, av[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    const int at = d + 8 * h;
-#pragma unroll 1
-    for (int g = 0; g < group; ++g)
-#pragma unroll 1
-      for (int i = first < 0 ? 0 : first; i < m; ++i) {
-        const uint16_t* qr = q + g * qh + i * qs;
-        const uint16_t* dr = dout + g * dh + i * ds_;
-        const float p = exp2_hw(fmaf(attn_dot<F16>(k, qr, h, hd), sl2, -stat[(g * trow + i) * 2]));
-        const float ds = p * (attn_dot<F16>(v, dr, h, hd) - stat[(g * trow + i) * 2 + 1]);
-        if (at >= hd) continue;
-        attn_axpy8<F16>(av, p, dr + at);
-        attn_axpy8<F16>(ak, ds, qr + at);
-      }
-    if (at < hd) attn_store8<F16>(dk + at, ak, scale), attn_store8<F16>(dv + at, av, 1.f);
-  }
-}
-
-// The lane's row r of a sequence's key head, row by row.
-template <int KT, bool F16>
-__device__ __forceinline__ void attn_dq_again(const AttnArgs& a, const AttnGrads& w, const AttnSeq& sq, int kv,
-                                              uint32_t r) {
-  const int pos = (int)(r / (uint32_t)a.group), head = kv * a.group + (int)(r % (uint32_t)a.group);
-  const int64_t token = sq.q0 + pos;
-  const int lim = pos + sq.n - sq.m + 1;
-  const float D = attn_dq_rows<F16>(
-      a.q + token * a.qs + head * a.qh, w.dout + token * w.dos + head * w.doh, w.out + token * w.os + head * w.oh,
-      a.k + sq.k0 * a.ks + kv * a.kh, a.v + sq.k0 * a.vs + kv * a.vh, a.ks, a.vs, lim < sq.n ? lim : sq.n, a.scale,
-      w.lse[(int64_t)head * a.tq + token], lim <= KT, a.hd, (threadIdx.x >> 5) & 1,
-      w.dq + token * w.dqs + head * w.dqh);
-  if (threadIdx.x & 32) w.stat[((int64_t)head * w.trow + token) * 2 + 1] = D;
-}
-
-// Owns rows (query, head of the group); sweeps the keys they see.  SPLIT: one of
-// several parts of the keys, whose sums are left in fp32 for attn_dq_join.
-template <int DP, int NW, int KT, bool F16, bool SPLIT>
-__global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGrads w, int tiles, int parts) {
+// Rows [32 NW t, +32 NW) of (query, head of the group kv); sweeps the keys they see.
+// SPLIT: one of several parts of the keys, whose sums are left in fp32 for
+// attn_dq_join.  again: LDS is in use.  CUT: keys of the tiles that a mask cuts one
+// by one (attn.hpp).  Returns whether the wave's sums were not finite.
+template <int DP, int NW, int KT, bool F16, bool SPLIT, bool CUT>
+__device__ __forceinline__ bool attn_dq_tile(const AttnArgs& a, const AttnGrads& w, const AttnSeq& sq, int kv, int parts,
+                                             int part, uint32_t t, uint32_t rows, INFCL_LDS char* lds, bool again) {
   constexpr int kFb = DP / 32, kI = DP / 16, kKb = KT / 32;
   typedef AttnTile<DP, NW, KT> Tile;
-  __shared__ __attribute__((aligned(1024))) char lds_[4 * Tile::kBytes];
-  INFCL_LDS char* lds = (INFCL_LDS char*)lds_;
   const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int h = lane >> 5;
-  const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
-  const AttnPlace at = attn_place(blockIdx.x, (uint32_t)(tiles * parts), groups);
-  const int t0 = tiles - 1 - (int)at.t / (SPLIT ? parts : 1), part = SPLIT ? (int)at.t % parts : 0;
-  const int z = (int)(at.g / (uint32_t)a.kvh), kv = (int)(at.g % (uint32_t)a.kvh);
-  AttnSeq sq = attn_seq(a, z);
-  if (z == a.nseq) sq.n = 0;
-  const int64_t rows64 = (int64_t)sq.m * a.group;
-  const uint32_t rows = rows64 > 0x7FFFFFFF ? 0x7FFFFFFFu : (uint32_t)rows64;
-  if ((int64_t)t0 * (32 * NW) >= rows) return;
-
   AttnLanes<DP> ln;
   ln.init(lane);
   const uint32_t kst = (uint32_t)(a.ks * 2), vst = (uint32_t)(a.vs * 2);
@@ -150,148 +70,203 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnArgs a, AttnGra
   const uint16_t* kb = a.k + sq.k0 * a.ks + kv * a.kh;
   const uint16_t* vb = a.v + sq.k0 * a.vs + kv * a.vh;
 
-  bool bad = false;  // this wave's sums may hold what masked rows hold
-  for (uint32_t t = (uint32_t)t0; t * (uint64_t)(32 * NW) < rows; t += (uint32_t)tiles) {
-    const uint32_t r = t * (32 * NW) + wave * 32 + (lane & 31);
-    const bool live = r < rows;
-    const int pos = live ? (int)(r / (uint32_t)a.group) : 0, g = live ? (int)(r % (uint32_t)a.group) : 0;
-    const int head = kv * a.group + g;
-    const int64_t token = sq.q0 + pos;
-    const int shift = sq.n - sq.m + 1;
-    int lim = a.causal ? pos + shift : sq.n;
-    lim = lim < 0 ? 0 : lim;
-    if (!live) lim = 0;
-    const uint32_t rl = t * (uint64_t)(32 * NW) + 32 * NW < rows ? t * (32 * NW) + 32 * NW - 1 : rows - 1;
-    int kend = a.causal ? (int)(rl / (uint32_t)a.group) + shift : sq.n;
-    kend = kend < sq.n ? kend : sq.n;
-    int kbeg = 0;
-    if (SPLIT) {  // shares of the keys that this tile sees
-      const int share = ((kend > 0 ? kend : 0) + parts * KT - 1) / (parts * KT) * KT;
-      kbeg = share * part;
-      kend = kbeg + share < kend ? kbeg + share : kend;
-    }
-    const uint32_t rw = t * (32 * NW) + wave * 32;
-    const uint32_t rv = rw + 31 < rows ? rw + 31 : rows - 1;
-    const int wmin = rw >= rows ? 0 : a.causal ? (int)(rw / (uint32_t)a.group) + shift : sq.n;
-    const int wmax = rw >= rows ? 0 : a.causal ? (int)(rv / (uint32_t)a.group) + shift : sq.n;
+  const uint32_t r = t * (32 * NW) + wave * 32 + (lane & 31);
+  const bool live = r < rows;
+  const int pos = live ? (int)(r / (uint32_t)a.group) : 0, g = live ? (int)(r % (uint32_t)a.group) : 0;
+  const int head = kv * a.group + g;
+  const int64_t token = sq.q0 + pos;
+  const int shift = sq.n - sq.m + 1;
+  int lim = a.causal ? pos + shift : sq.n;
+  lim = lim < 0 ? 0 : lim;
+  if (!live) lim = 0;
+  const uint32_t rl = t * (uint64_t)(32 * NW) + 32 * NW < rows ? t * (32 * NW) + 32 * NW - 1 : rows - 1;
+  int kend = a.causal ? (int)(rl / (uint32_t)a.group) + shift : sq.n;
+  kend = kend < sq.n ? kend : sq.n;
+  int kbeg = 0;
+  if (SPLIT) {  // shares of the keys that this tile sees
+    const int share = ((kend > 0 ? kend : 0) + parts * KT - 1) / (parts * KT) * KT;
+    kbeg = share * part;
+    kend = kbeg + share < kend ? kbeg + share : kend;
+  }
+  const uint32_t rw = t * (32 * NW) + wave * 32;
+  const uint32_t rv = rw + 31 < rows ? rw + 31 : rows - 1;
+  const int wmin = rw >= rows ? 0 : a.causal ? (int)(rw / (uint32_t)a.group) + shift : sq.n;
+  const int wmax = rw >= rows ? 0 : a.causal ? (int)(rv / (uint32_t)a.group) + shift : sq.n;
 
-    if (t != (uint32_t)t0) attn_barrier();
-    if (kbeg < kend) {
-      Tile::issue(kb + (int64_t)kbeg * a.ks, sq.n - kbeg, kst, a.hd, lds, koff, wave);
-      Tile::issue(vb + (int64_t)kbeg * a.vs, sq.n - kbeg, vst, a.hd, lds + Tile::kBytes, voff, wave);
-    }
-    bf16x8 qf[kI], df[kI];
-    float D = 0.f;
+  if (again) attn_barrier();
+  if (kbeg < kend) {
+    Tile::issue(kb + (int64_t)kbeg * a.ks, sq.n - kbeg, kst, a.hd, lds, koff, wave);
+    Tile::issue(vb + (int64_t)kbeg * a.vs, sq.n - kbeg, vst, a.hd, lds + Tile::kBytes, voff, wave);
+  }
+  bf16x8 qf[kI], df[kI];
+  float D = 0.f;
+#pragma unroll
+  for (int i = 0; i < kI; ++i) {
+    qf[i] = attn_own(a.q + token * a.qs + head * a.qh, i, h, a.hd, live);
+    df[i] = attn_own(w.dout + token * w.dos + head * w.doh, i, h, a.hd, live);
+  }
+  if (wmax > KT) {
 #pragma unroll
     for (int i = 0; i < kI; ++i) {
-      qf[i] = attn_own(a.q + token * a.qs + head * a.qh, i, h, a.hd, live);
-      df[i] = attn_own(w.dout + token * w.dos + head * w.doh, i, h, a.hd, live);
+      const bf16x8 of = attn_own(w.out + token * w.os + head * w.oh, i, h, a.hd, live);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) D = fmaf(from16<F16>(df[i][e]), from16<F16>(of[e]), D);
     }
-    if (wmax > KT) {
+    D = attn_sum2(D);
+  }
+  float lse2 = 0.f;
+  if (live) lse2 = w.lse[(int64_t)head * a.tq + token] * kLog2e;
+  if (lse2 == -__builtin_inff()) lse2 = 0.f, D = 0.f;
+  attn_settle(qf);
+  attn_settle(df);
+  asm volatile("" : "+v"(lse2));
+  f32x16 acc[kFb];
 #pragma unroll
-      for (int i = 0; i < kI; ++i) {
-        const bf16x8 of = attn_own(w.out + token * w.os + head * w.oh, i, h, a.hd, live);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) D = fmaf(from16<F16>(df[i][e]), from16<F16>(of[e]), D);
+  for (int fb = 0; fb < kFb; ++fb) acc[fb] = f32x16_zero();
+  const int kcut = kbeg + (wmin > kbeg ? (wmin - kbeg) / KT * KT : 0), wend = CUT ? kcut : wmax;
+  {
+    int buf = 0;
+    for (int k = kbeg; k < kend; k += KT, buf ^= 1) {
+      attn_barrier();
+      if (k + KT < kend) {
+        INFCL_LDS char* nx = lds + (buf ^ 1) * 2 * Tile::kBytes;
+        Tile::issue(kb + (int64_t)(k + KT) * a.ks, sq.n - k - KT, kst, a.hd, nx, koff, wave);
+        Tile::issue(vb + (int64_t)(k + KT) * a.vs, sq.n - k - KT, vst, a.hd, nx + Tile::kBytes, voff, wave);
       }
-      D = attn_sum2(D);
-    }
-    float lse2 = 0.f;
-    if (live) lse2 = w.lse[(int64_t)head * a.tq + token] * kLog2e;
-    if (lse2 == -__builtin_inff()) lse2 = 0.f, D = 0.f;
-    attn_settle(qf);
-    attn_settle(df);
-    asm volatile("" : "+v"(lse2));
-    f32x16 acc[kFb];
+      if (k >= wend) continue;
+      const INFCL_LDS char* kt = lds + buf * 2 * Tile::kBytes;
+      const INFCL_LDS char* vt = kt + Tile::kBytes;
+      f32x16 p[kKb], dp[kKb];
 #pragma unroll
-    for (int fb = 0; fb < kFb; ++fb) acc[fb] = f32x16_zero();
-    {
-      int buf = 0;
-      for (int k = kbeg; k < kend; k += KT, buf ^= 1) {
-        attn_barrier();
-        if (k + KT < kend) {
-          INFCL_LDS char* nx = lds + (buf ^ 1) * 2 * Tile::kBytes;
-          Tile::issue(kb + (int64_t)(k + KT) * a.ks, sq.n - k - KT, kst, a.hd, nx, koff, wave);
-          Tile::issue(vb + (int64_t)(k + KT) * a.vs, sq.n - k - KT, vst, a.hd, nx + Tile::kBytes, voff, wave);
+      for (int b = 0; b < kKb; ++b) {
+        p[b] = f32x16_zero(), dp[b] = f32x16_zero();
+#pragma unroll
+        for (int i = 0; i < kI; ++i) {
+          p[b] = mfma16<F16>(attn_row(kt + b * 32 * Tile::kRow + ln.row[i]), qf[i], p[b]);
+          dp[b] = mfma16<F16>(attn_row(vt + b * 32 * Tile::kRow + ln.row[i]), df[i], dp[b]);
         }
-        if (k >= wmax) continue;
-        const INFCL_LDS char* kt = lds + buf * 2 * Tile::kBytes;
-        const INFCL_LDS char* vt = kt + Tile::kBytes;
-        f32x16 p[kKb], dp[kKb];
+      }
 #pragma unroll
-        for (int b = 0; b < kKb; ++b) {
-          p[b] = f32x16_zero(), dp[b] = f32x16_zero();
+      for (int b = 0; b < kKb; ++b)
 #pragma unroll
-          for (int i = 0; i < kI; ++i) {
-            p[b] = mfma16<F16>(attn_row(kt + b * 32 * Tile::kRow + ln.row[i]), qf[i], p[b]);
-            dp[b] = mfma16<F16>(attn_row(vt + b * 32 * Tile::kRow + ln.row[i]), df[i], dp[b]);
-          }
-        }
+        for (int x = 0; x < 16; ++x) p[b][x] = exp2_hw(fmaf(p[b][x], a.sl2, -lse2));
+      if (k + KT > wmin) {
+        const int left = attn_opaque(lim - k - 4 * h);
 #pragma unroll
         for (int b = 0; b < kKb; ++b)
 #pragma unroll
-          for (int x = 0; x < 16; ++x) p[b][x] = exp2_hw(fmaf(p[b][x], a.sl2, -lse2));
-        if (k + KT > wmin) {
-          const int left = attn_opaque(lim - k - 4 * h);
-#pragma unroll
-          for (int b = 0; b < kKb; ++b)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-              const bool seen = 32 * b + attn_reg_row(x, 0) < left;
-              p[b][x] = seen ? p[b][x] : 0.f;
-              dp[b][x] = seen ? dp[b][x] : 0.f;
-            }
-        }
-        if (wmax <= KT) {
-          float s = 0.f;
-#pragma unroll
-          for (int b = 0; b < kKb; ++b)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) s = fmaf(p[b][x], dp[b][x], s);
-          D = attn_sum2(s);
-        }
-#pragma unroll
-        for (int b = 0; b < kKb; ++b) {
-#pragma unroll
-          for (int x = 0; x < 16; ++x) p[b][x] *= dp[b][x] - D;
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const bf16x8 ds = attn_pack<F16>(p[b], u);
-            const int ro = (32 * b + 16 * u) * Tile::kRow;
-#pragma unroll
-            for (int fb = 0; fb < kFb; ++fb)
-              acc[fb] = mfma16<F16>(attn_tr(kt + ro + ln.tr[0][fb], kt + ro + ln.tr[1][fb]), ds, acc[fb]);
+          for (int x = 0; x < 16; ++x) {
+            const bool seen = 32 * b + attn_reg_row(x, 0) < left;
+            p[b][x] = seen ? p[b][x] : 0.f;
+            dp[b][x] = seen ? dp[b][x] : 0.f;
           }
+      }
+      if (wmax <= KT) {
+        float s = 0.f;
+#pragma unroll
+        for (int b = 0; b < kKb; ++b)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) s = fmaf(p[b][x], dp[b][x], s);
+        D = attn_sum2(s);
+      }
+#pragma unroll
+      for (int b = 0; b < kKb; ++b) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) p[b][x] *= dp[b][x] - D;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const bf16x8 ds = attn_pack<F16>(p[b], u);
+          const int ro = (32 * b + 16 * u) * Tile::kRow;
+#pragma unroll
+          for (int fb = 0; fb < kFb; ++fb)
+            acc[fb] = mfma16<F16>(attn_tr(kt + ro + ln.tr[0][fb], kt + ro + ln.tr[1][fb]), ds, acc[fb]);
         }
       }
     }
-    if (!SPLIT) bad |= a.causal && wave_any(live && attn_bad(acc));
-    if (!live) continue;
-    if (!SPLIT || part == 0) w.stat[((int64_t)head * w.trow + token) * 2 + h] = h ? D : lse2;
-    if constexpr (SPLIT) {
-      float* po = w.part_q + (((int64_t)part * a.tq + token) * a.heads + head) * a.hd;
-#pragma unroll
-      for (int fb = 0; fb < kFb; ++fb)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int d = 32 * fb + 8 * j + 4 * h;
-          if (d < a.hd)
-            *(f32x4*)(po + d) = f32x4{acc[fb][4 * j], acc[fb][4 * j + 1], acc[fb][4 * j + 2], acc[fb][4 * j + 3]};
-        }
-    } else {
-      attn_store<F16>(w.dq + token * w.dqs + head * w.dqh, acc, a.scale, h, a.hd);
+  }
+  const bool bad = !CUT && a.causal && wave_any(live && attn_bad(acc));
+  // (the row's place made here again, not kept through the sweep)
+  const int own_lane = attn_opaque(threadIdx.x & 63), oh = own_lane >> 5;
+  const uint32_t own = rw + (own_lane & 31);
+  if (own >= rows) return bad;
+  const int own_pos = (int)(own / (uint32_t)a.group), own_head = kv * a.group + (int)(own % (uint32_t)a.group);
+  const int64_t at = sq.q0 + own_pos;
+  if (CUT) {
+    const uint16_t *q = a.q + at * a.qs + own_head * a.qh, *dr = w.dout + at * w.dos + own_head * w.doh;
+    const int lim = own_pos + shift, stop = lim < kend ? lim : kend;
+    if (wmax <= KT) {
+#pragma unroll 1
+      for (int k = 0; k < stop; ++k)
+        D = fmaf(exp2_hw(fmaf(attn_dot<F16>(q, kb + k * a.ks, oh, a.hd), a.sl2, -lse2)),
+                 attn_dot<F16>(dr, vb + k * a.vs, oh, a.hd), D);
+    }
+#pragma unroll 1
+    for (int k = kcut; k < stop; ++k) {
+      const float p = exp2_hw(fmaf(attn_dot<F16>(q, kb + k * a.ks, oh, a.hd), a.sl2, -lse2));
+      attn_axpy<F16>(acc, p * (attn_dot<F16>(dr, vb + k * a.vs, oh, a.hd) - D), kb + k * a.ks, oh, a.hd);
     }
   }
-  if (!bad) return;
-  wait_dma();  // (the stores of these rows are done: other lanes write them again)
-  for (uint64_t r = (uint64_t)t0 * (32 * NW) + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31); r < rows;
-       r += (uint64_t)tiles * (32 * NW))
-    attn_dq_again<KT, F16>(a, w, sq, kv, (uint32_t)r);
+  if (!SPLIT || part == 0) w.stat[((int64_t)own_head * w.trow + at) * 2 + oh] = oh ? D : lse2;
+  if constexpr (SPLIT) {
+    float* po = w.part_q + (((int64_t)part * a.tq + at) * a.heads + own_head) * a.hd;
+#pragma unroll
+    for (int fb = 0; fb < kFb; ++fb)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int d = 32 * fb + 8 * j + 4 * oh;
+        if (d < a.hd)
+          *(f32x4*)(po + d) = f32x4{acc[fb][4 * j], acc[fb][4 * j + 1], acc[fb][4 * j + 2], acc[fb][4 * j + 3]};
+      }
+  } else {
+    attn_store<F16>(w.dq + at * w.dqs + own_head * w.dqh, acc, a.scale, oh, a.hd);
+  }
+  return bad;
+}
+
+struct AttnBwdArgs {
+  AttnArgs a;
+  AttnGrads w;
+  int tiles, parts;
+};
+
+template <int DP, int NW, int KT, bool F16, bool SPLIT>
+__global__ void __launch_bounds__(64 * NW, 2) attn_dq_kernel(AttnBwdArgs c) {
+  const AttnArgs& a = c.a;
+  const AttnGrads& w = c.w;
+  const int tiles = c.tiles, parts = c.parts;
+  __shared__ __attribute__((aligned(1024))) char lds_[4 * AttnTile<DP, NW, KT>::kBytes];
+  __shared__ int flags[NW];
+  INFCL_LDS char* lds = (INFCL_LDS char*)lds_;
+  const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
+  const AttnPlace at = attn_place(blockIdx.x, (uint32_t)(tiles * parts), groups);
+  const int t0 = tiles - 1 - (int)at.t / (SPLIT ? parts : 1), part = SPLIT ? (int)at.t % parts : 0;
+  const int z = (int)(at.g / (uint32_t)a.kvh), kv = (int)(at.g % (uint32_t)a.kvh);
+  AttnSeq sq = attn_seq(a, z);
+  if (z == a.nseq) sq.n = 0;
+  const int64_t rows64 = (int64_t)sq.m * a.group;
+  const uint32_t rows = rows64 > 0x7FFFFFFF ? 0x7FFFFFFFu : (uint32_t)rows64;
+  if ((int64_t)t0 * (32 * NW) >= rows) return;
+  bool bad = false;
+  for (uint32_t t = (uint32_t)t0; t * (uint64_t)(32 * NW) < rows; t += (uint32_t)tiles)
+    bad |= attn_dq_tile<DP, NW, KT, F16, SPLIT, false>(a, w, sq, kv, parts, part, t, rows, lds, t != (uint32_t)t0);
+  if (!a.causal) return;
+  const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  bool odd = false;  // keys of the tiles that a mask cuts
+  if (bad) {
+    const AttnBwdArgs r = attn_reload<AttnBwdArgs>();
+    for (uint32_t t = (uint32_t)t0; t * (uint64_t)(32 * NW) + 32 * wave < rows; t += (uint32_t)tiles)
+      odd |= attn_odd_keys<F16>(r.a.k + sq.k0 * r.a.ks + kv * r.a.kh, r.a.ks, r.a.hd, sq, r.a.group,
+                                t * (32 * NW) + 32 * wave, rows, KT);
+  }
+  if (!attn_vote<NW>(odd, (INFCL_LDS int*)flags, wave)) return;
+  const AttnBwdArgs r = attn_reload<AttnBwdArgs>();
+  for (uint32_t t = (uint32_t)t0; t * (uint64_t)(32 * NW) < rows; t += (uint32_t)tiles)
+    attn_dq_tile<DP, NW, KT, F16, SPLIT, true>(r.a, r.w, sq, kv, r.parts, part, t, rows, lds, true);
 }
 
 // The parts' dq, in order.  A wave takes 8 rows of a sequence's key head, 16 lanes to
-// a row; if one of them is not finite, all again row by row.
-template <int KT, bool F16>
+// a row.
+template <bool F16>
 __global__ void __launch_bounds__(256) attn_dq_join(AttnArgs a, AttnGrads w, int tiles, int parts) {
   const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
   const uint32_t gz = blockIdx.x % groups;
@@ -301,7 +276,6 @@ __global__ void __launch_bounds__(256) attn_dq_join(AttnArgs a, AttnGrads w, int
   const int64_t rows = (int64_t)sq.m * a.group, step = a.tq * a.heads * a.hd;
   const int lane = threadIdx.x & 63, d = 8 * (lane & 15);
   for (int64_t r0 = (int64_t)(blockIdx.x / groups) * 32 + (threadIdx.x >> 6) * 8; r0 < rows; r0 += (int64_t)tiles * 32) {
-    float sum = 0.f;
 #pragma unroll
     for (int i = lane >> 4; i < 8; i += 4) {
       if (r0 + i >= rows || d >= a.hd) continue;
@@ -318,13 +292,7 @@ __global__ void __launch_bounds__(256) attn_dq_join(AttnArgs a, AttnGrads w, int
         for (int e = 0; e < 4; ++e) acc[e] += x0[e], acc[4 + e] += x1[e];
       }
       attn_store8<F16>(w.dq + token * w.dqs + head * w.dqh + d, acc, a.scale);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum = fmaf(acc[e], 0.f, sum);
     }
-    if (!a.causal || !wave_any(!(sum == 0.f))) continue;
-    wait_dma();  // (the stores of these rows are done: other lanes write them again)
-    const int64_t r = r0 + (lane & 31);
-    if ((lane & 31) < 8 && r < rows) attn_dq_again<KT, F16>(a, w, sq, kv, (uint32_t)r);
   }
 }
 
@@ -338,17 +306,180 @@ __global__ void __launch_bounds__(256) attn_dq_join(AttnArgs a, AttnGrads w, int
 // (its reload waits for the tile copies in flight).
 // SPLIT: a workgroup takes one of several parts of the tiles and leaves its sums in
 // fp32 for attn_dkv_join.
-template <int DP, int NW, bool F16, bool SPLIT>
-__global__ void __launch_bounds__(64 * NW, 2) attn_dkv_kernel(AttnArgs a, AttnGrads w, int tiles, int parts) {
+// again: LDS is in use.  CUT: queries of the tiles that a mask cuts one by one
+// (attn.hpp).  Returns whether the wave's sums were not finite.
+template <int DP, int NW, bool F16, bool SPLIT, bool CUT>
+__device__ __forceinline__ bool attn_dkv_tile(const AttnArgs& a, const AttnGrads& w, const AttnSeq& sq, int kv, int parts,
+                                              int part, int64_t t, INFCL_LDS char* lds, INFCL_LDS float* stat, bool again) {
   constexpr int kFb = DP / 32, kI = DP / 16, QT = 32;
-  constexpr bool kVLds = DP == 128 && NW > 1;  // (a lone wave's tiles leave it a SIMD's registers)
+  constexpr bool kVLds = attn_own_in_lds(DP, NW);
   typedef AttnTile<DP, NW, QT> Tile;
   typedef AttnTile<DP, NW, 32 * NW> Own;
-  __shared__ __attribute__((aligned(1024))) char lds_[4 * Tile::kBytes + (kVLds ? Own::kBytes : 0)];
-  __shared__ __attribute__((aligned(16))) float stat_[NW][64];  // a tile's pairs of lse log2(e) and D
-  INFCL_LDS char* lds = (INFCL_LDS char*)lds_;
   const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int h = lane >> 5;
+  AttnLanes<DP> ln;
+  ln.init(lane);
+  const uint32_t qst = (uint32_t)(a.qs * 2), dst = (uint32_t)(w.dos * 2);
+  uint32_t qoff[Tile::kVar], doff[Tile::kVar];
+  Tile::offsets(qoff, wave, lane, qst, a.hd);
+  Tile::offsets(doff, wave, lane, dst, a.hd);
+
+  const int key0 = (int)(t * (32 * NW)), kw = key0 + 32 * wave;
+  bf16x8 kf[kI], vf[kVLds ? 1 : kI];
+  const int shift = sq.n - sq.m;
+  const int first = a.causal ? kw + (lane & 31) - shift : 0;  // queries from here on see this lane's key
+  {
+    const int key = kw + (lane & 31);
+    const bool live = key < sq.n;
+    const int64_t token = sq.k0 + (live ? key : 0);
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+      kf[i] = attn_own(a.k + token * a.ks + kv * a.kh, i, h, a.hd, live);
+      if constexpr (!kVLds) vf[i] = attn_own(a.v + token * a.vs + kv * a.vh, i, h, a.hd, live);
+    }
+  }
+  // from wall on all the wave's keys; none before qbeg sees one of the workgroup's
+  const int wall = a.causal ? kw + 31 - shift : 0, wany = a.causal ? kw - shift : 0;
+  int qbeg = a.causal ? key0 - shift : 0;
+  qbeg = qbeg < 0 ? 0 : qbeg / QT * QT;
+
+  f32x16 dk[kFb], dv[kFb];
+  if (again) attn_barrier();
+  const INFCL_LDS char* vown = lds + 4 * Tile::kBytes + wave * 32 * Tile::kRow;
+  if constexpr (kVLds) {
+    uint32_t off[Own::kVar];
+    Own::offsets(off, wave, lane, (uint32_t)(a.vs * 2), a.hd);
+    Own::issue(a.v + (sq.k0 + key0) * a.vs + kv * a.vh, sq.n - key0, (uint32_t)(a.vs * 2), a.hd,
+               lds + 4 * Tile::kBytes, off, wave);
+  }
+#pragma unroll
+  for (int fb = 0; fb < kFb; ++fb) dk[fb] = f32x16_zero(), dv[fb] = f32x16_zero();
+  // this part's tiles [c0, c1): tile c is head c % group of queries qbeg + QT (per - 1 - c / group) on
+  const int per = sq.m > qbeg ? (sq.m - qbeg + QT - 1) / QT : 0;
+  int64_t c0 = 0, c1 = (int64_t)per * a.group;
+  if (SPLIT) {
+    const int64_t share = (c1 + parts - 1) / parts;
+    c0 = share * part < c1 ? share * part : c1;
+    c1 = c0 + share < c1 ? c0 + share : c1;
+  }
+  // the lanes fetch a tile's 32 pairs a tile ahead
+  const float* row = w.stat + sq.q0 * 2;
+  float ahead = 0.f;
+  int g = (int)(c0 % a.group), i0 = qbeg + QT * (per - 1 - (int)(c0 / a.group));  // the tile in hand, then the next
+  auto issue = [&](int b) {
+    const int head = kv * a.group + g;
+    INFCL_LDS char* to = lds + b * 2 * Tile::kBytes;
+    Tile::issue(a.q + (sq.q0 + i0) * a.qs + head * a.qh, sq.m - i0, qst, a.hd, to, qoff, wave);
+    Tile::issue(w.dout + (sq.q0 + i0) * w.dos + head * w.doh, sq.m - i0, dst, a.hd, to + Tile::kBytes, doff, wave);
+    ahead = row[((int64_t)head * w.trow + i0) * 2 + lane];
+  };
+  if (c0 < c1) issue(0);
+  // the first `cut` tiles of queries are seen by some of the wave's keys and not by others
+  int cut = a.causal && wall > qbeg ? (wall - qbeg + QT - 1) / QT : 0;
+  cut = cut < per ? cut : per;
+  const int wend = CUT ? qbeg + cut * QT : wany;
+  int buf = 0;
+  for (int64_t c = c0; c < c1; ++c, buf ^= 1) {
+    const int i1 = i0;
+    const bool none = i1 + QT <= wend || kw >= sq.n;  // (no query of the tile sees a key of this wave)
+    stat[lane] = ahead;
+    if (++g == a.group) g = 0, i0 -= QT;
+    attn_barrier();
+    if (c + 1 < c1) issue(buf ^ 1);
+    if (none) continue;
+    const INFCL_LDS char* qt = lds + buf * 2 * Tile::kBytes;
+    const INFCL_LDS char* dt = qt + Tile::kBytes;
+    f32x16 p = f32x16_zero(), dp = f32x16_zero();
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+      p = mfma16<F16>(attn_row(qt + ln.row[i]), kf[i], p);
+      dp = mfma16<F16>(attn_row(dt + ln.row[i]), kVLds ? attn_row(vown + ln.row[i]) : vf[kVLds ? 0 : i], dp);
+    }
+#pragma unroll
+    for (int x4 = 0; x4 < 4; ++x4) {
+      const f32x4 lo = *(const INFCL_LDS f32x4*)(stat + 2 * attn_reg_row(4 * x4, h));
+      const f32x4 hi = *(const INFCL_LDS f32x4*)(stat + 2 * attn_reg_row(4 * x4, h) + 4);
+      const float L[4] = {lo[0], lo[2], hi[0], hi[2]}, D[4] = {lo[1], lo[3], hi[1], hi[3]};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int x = 4 * x4 + e;
+        p[x] = exp2_hw(fmaf(p[x], a.sl2, -L[e]));
+        dp[x] = p[x] * (dp[x] - D[e]);
+      }
+    }
+    if (i1 < wall || i1 + QT > sq.m) {
+      const int lo = attn_opaque(first - i1 - 4 * h), hi = attn_opaque(sq.m - i1 - 4 * h);
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const bool seen = attn_reg_row(x, 0) >= lo && attn_reg_row(x, 0) < hi;
+        p[x] = seen ? p[x] : 0.f;
+        dp[x] = seen ? dp[x] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const bf16x8 pw = attn_pack<F16>(p, u), ds = attn_pack<F16>(dp, u);
+      const int ro = 16 * u * Tile::kRow;
+#pragma unroll
+      for (int fb = 0; fb < kFb; ++fb) {
+        dv[fb] = mfma16<F16>(attn_tr(dt + ro + ln.tr[0][fb], dt + ro + ln.tr[1][fb]), pw, dv[fb]);
+        dk[fb] = mfma16<F16>(attn_tr(qt + ro + ln.tr[0][fb], qt + ro + ln.tr[1][fb]), ds, dk[fb]);
+      }
+    }
+  }
+  int own_lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(own_lane));  // (addresses made here, not kept through the sweep)
+  const int own_key = kw + (own_lane & 31);
+  const bool mine = own_key < sq.n;
+  const int64_t at = sq.k0 + own_key;
+  if (CUT && mine) {
+    const int64_t from = (int64_t)(per - cut) * a.group;
+    const int see = own_key - shift, oh = own_lane >> 5;
+    const uint16_t *kr = a.k + at * a.ks + kv * a.kh, *vr = a.v + at * a.vs + kv * a.vh;
+#pragma unroll 1
+    for (int64_t c = c0 > from ? c0 : from; c < c1; ++c) {
+      const int head = kv * a.group + (int)(c % a.group);
+      const int beg = qbeg + QT * (per - 1 - (int)(c / a.group)), end = beg + QT < sq.m ? beg + QT : sq.m;
+#pragma unroll 1
+      for (int i = beg > see ? beg : see; i < end; ++i) {
+        const uint16_t* qr = a.q + (sq.q0 + i) * a.qs + head * a.qh;
+        const uint16_t* dr = w.dout + (sq.q0 + i) * w.dos + head * w.doh;
+        const float* st = w.stat + ((int64_t)head * w.trow + sq.q0 + i) * 2;
+        const float p = exp2_hw(fmaf(attn_dot<F16>(kr, qr, oh, a.hd), a.sl2, -st[0]));
+        attn_axpy<F16>(dk, p * (attn_dot<F16>(vr, dr, oh, a.hd) - st[1]), qr, oh, a.hd);
+        attn_axpy<F16>(dv, p, dr, oh, a.hd);
+      }
+    }
+  }
+  const bool bad = !CUT && a.causal && wave_any(mine && (attn_bad(dk) || attn_bad(dv)));
+  if (!mine) return bad;
+  if constexpr (SPLIT) {
+    const int64_t rows = a.tk * a.kvh;
+    float* pk = w.part + ((int64_t)part * 2 * rows + at * a.kvh + kv) * a.hd;
+#pragma unroll
+    for (int fb = 0; fb < kFb; ++fb)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int d = 32 * fb + 8 * j + 4 * (own_lane >> 5);
+        if (d >= a.hd) continue;
+        *(f32x4*)(pk + d) = f32x4{dk[fb][4 * j], dk[fb][4 * j + 1], dk[fb][4 * j + 2], dk[fb][4 * j + 3]};
+        *(f32x4*)(pk + rows * a.hd + d) = f32x4{dv[fb][4 * j], dv[fb][4 * j + 1], dv[fb][4 * j + 2], dv[fb][4 * j + 3]};
+      }
+  } else {
+    attn_store<F16>(w.dk + at * w.dks + kv * w.dkh, dk, a.scale, own_lane >> 5, a.hd);
+    attn_store<F16>(w.dv + at * w.dvs + kv * w.dvh, dv, 1.f, own_lane >> 5, a.hd);
+  }
+  return bad;
+}
+
+template <int DP, int NW, bool F16, bool SPLIT>
+__global__ void __launch_bounds__(64 * NW, 2) attn_dkv_kernel(AttnArgs a, AttnGrads w, int tiles, int parts) {
+  __shared__ __attribute__((aligned(1024))) char lds_[4 * AttnTile<DP, NW, 32>::kBytes +
+                                                      (attn_own_in_lds(DP, NW) ? AttnTile<DP, NW, 32 * NW>::kBytes : 0)];
+  __shared__ __attribute__((aligned(16))) float stat_[NW][64];  // a tile's pairs of lse log2(e) and D
+  __shared__ int flags[NW];
+  INFCL_LDS char* lds = (INFCL_LDS char*)lds_;
+  const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   INFCL_LDS float* stat = (INFCL_LDS float*)stat_[wave];
   const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
   // (longest sweeps first: the first keys' parts)
@@ -359,155 +490,29 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_dkv_kernel(AttnArgs a, AttnGr
   if (z == a.nseq) sq.m = 0;
   if ((int64_t)t0 * (32 * NW) >= sq.n) return;
 
-  AttnLanes<DP> ln;
-  ln.init(lane);
-  const uint32_t qst = (uint32_t)(a.qs * 2), dst = (uint32_t)(w.dos * 2);
-  uint32_t qoff[Tile::kVar], doff[Tile::kVar];
-  Tile::offsets(qoff, wave, lane, qst, a.hd);
-  Tile::offsets(doff, wave, lane, dst, a.hd);
-
-  bool bad = false;  // this wave's sums may hold what masked rows hold
-  for (int64_t t = t0; t * (32 * NW) < sq.n; t += tiles) {
-    const int key0 = (int)(t * (32 * NW)), kw = key0 + 32 * wave;
-    bf16x8 kf[kI], vf[kVLds ? 1 : kI];
-    const int shift = sq.n - sq.m;
-    const int first = a.causal ? kw + (lane & 31) - shift : 0;  // queries from here on see this lane's key
-    {
-      const int key = kw + (lane & 31);
-      const bool live = key < sq.n;
-      const int64_t token = sq.k0 + (live ? key : 0);
-#pragma unroll
-      for (int i = 0; i < kI; ++i) {
-        kf[i] = attn_own(a.k + token * a.ks + kv * a.kh, i, h, a.hd, live);
-        if constexpr (!kVLds) vf[i] = attn_own(a.v + token * a.vs + kv * a.vh, i, h, a.hd, live);
+  bool bad = false;
+  for (int64_t t = t0; t * (32 * NW) < sq.n; t += tiles)
+    bad |= attn_dkv_tile<DP, NW, F16, SPLIT, false>(a, w, sq, kv, parts, part, t, lds, stat, t != t0);
+  if (!a.causal) return;
+  bool odd = false;  // queries and dout of the tiles that a mask cuts
+  if (bad) {
+    for (int64_t t = t0; t * (32 * NW) + 32 * wave < sq.n; t += tiles) {
+      int lo = (int)t * (32 * NW) + 32 * wave - (sq.n - sq.m), hi = lo + 31 < sq.m ? lo + 31 : sq.m;
+      lo = lo < 32 ? 0 : lo - 31;  // (the tile of the first query that sees one of the wave's keys)
+      for (int g = 0; g < a.group; ++g) {
+        const int head = kv * a.group + g;
+        odd |= attn_odd<F16>(a.q + (sq.q0 + lo) * a.qs + head * a.qh, hi - lo, a.qs, a.hd, threadIdx.x & 63) ||
+               attn_odd<F16>(w.dout + (sq.q0 + lo) * w.dos + head * w.doh, hi - lo, w.dos, a.hd, threadIdx.x & 63);
       }
-    }
-    // from wall on all the wave's keys; none before qbeg sees one of the workgroup's
-    const int wall = a.causal ? kw + 31 - shift : 0, wany = a.causal ? kw - shift : 0;
-    int qbeg = a.causal ? key0 - shift : 0;
-    qbeg = qbeg < 0 ? 0 : qbeg / QT * QT;
-
-    f32x16 dk[kFb], dv[kFb];
-    if (t != t0) attn_barrier();
-    const INFCL_LDS char* vown = lds + 4 * Tile::kBytes + wave * 32 * Tile::kRow;
-    if constexpr (kVLds) {
-      uint32_t off[Own::kVar];
-      Own::offsets(off, wave, lane, (uint32_t)(a.vs * 2), a.hd);
-      Own::issue(a.v + (sq.k0 + key0) * a.vs + kv * a.vh, sq.n - key0, (uint32_t)(a.vs * 2), a.hd,
-                 lds + 4 * Tile::kBytes, off, wave);
-    }
-#pragma unroll
-    for (int fb = 0; fb < kFb; ++fb) dk[fb] = f32x16_zero(), dv[fb] = f32x16_zero();
-    // this part's tiles [c0, c1): tile c is head c % group of queries qbeg + QT (per - 1 - c / group) on
-    const int per = sq.m > qbeg ? (sq.m - qbeg + QT - 1) / QT : 0;
-    int64_t c0 = 0, c1 = (int64_t)per * a.group;
-    if (SPLIT) {
-      const int64_t share = (c1 + parts - 1) / parts;
-      c0 = share * part < c1 ? share * part : c1;
-      c1 = c0 + share < c1 ? c0 + share : c1;
-    }
-    // the lanes fetch a tile's 32 pairs a tile ahead
-    const float* row = w.stat + sq.q0 * 2;
-    float ahead = 0.f;
-    int g = (int)(c0 % a.group), i0 = qbeg + QT * (per - 1 - (int)(c0 / a.group));  // the tile in hand, then the next
-    auto issue = [&](int b) {
-      const int head = kv * a.group + g;
-      INFCL_LDS char* to = lds + b * 2 * Tile::kBytes;
-      Tile::issue(a.q + (sq.q0 + i0) * a.qs + head * a.qh, sq.m - i0, qst, a.hd, to, qoff, wave);
-      Tile::issue(w.dout + (sq.q0 + i0) * w.dos + head * w.doh, sq.m - i0, dst, a.hd, to + Tile::kBytes, doff, wave);
-      ahead = row[((int64_t)head * w.trow + i0) * 2 + lane];
-    };
-    if (c0 < c1) issue(0);
-    int buf = 0;
-    for (int64_t c = c0; c < c1; ++c, buf ^= 1) {
-      const int i1 = i0;
-      const bool none = i1 + QT <= wany || kw >= sq.n;  // (no query of the tile sees a key of this wave)
-      stat[lane] = ahead;
-      if (++g == a.group) g = 0, i0 -= QT;
-      attn_barrier();
-      if (c + 1 < c1) issue(buf ^ 1);
-      if (none) continue;
-      const INFCL_LDS char* qt = lds + buf * 2 * Tile::kBytes;
-      const INFCL_LDS char* dt = qt + Tile::kBytes;
-      f32x16 p = f32x16_zero(), dp = f32x16_zero();
-#pragma unroll
-      for (int i = 0; i < kI; ++i) {
-        p = mfma16<F16>(attn_row(qt + ln.row[i]), kf[i], p);
-        dp = mfma16<F16>(attn_row(dt + ln.row[i]), kVLds ? attn_row(vown + ln.row[i]) : vf[kVLds ? 0 : i], dp);
-      }
-#pragma unroll
-      for (int x4 = 0; x4 < 4; ++x4) {
-        const f32x4 lo = *(const INFCL_LDS f32x4*)(stat + 2 * attn_reg_row(4 * x4, h));
-        const f32x4 hi = *(const INFCL_LDS f32x4*)(stat + 2 * attn_reg_row(4 * x4, h) + 4);
-        const float L[4] = {lo[0], lo[2], hi[0], hi[2]}, D[4] = {lo[1], lo[3], hi[1], hi[3]};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int x = 4 * x4 + e;
-          p[x] = exp2_hw(fmaf(p[x], a.sl2, -L[e]));
-          dp[x] = p[x] * (dp[x] - D[e]);
-        }
-      }
-      if (i1 < wall || i1 + QT > sq.m) {
-        const int lo = attn_opaque(first - i1 - 4 * h), hi = attn_opaque(sq.m - i1 - 4 * h);
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const bool seen = attn_reg_row(x, 0) >= lo && attn_reg_row(x, 0) < hi;
-          p[x] = seen ? p[x] : 0.f;
-          dp[x] = seen ? dp[x] : 0.f;
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const bf16x8 pw = attn_pack<F16>(p, u), ds = attn_pack<F16>(dp, u);
-        const int ro = 16 * u * Tile::kRow;
-#pragma unroll
-        for (int fb = 0; fb < kFb; ++fb) {
-          dv[fb] = mfma16<F16>(attn_tr(dt + ro + ln.tr[0][fb], dt + ro + ln.tr[1][fb]), pw, dv[fb]);
-          dk[fb] = mfma16<F16>(attn_tr(qt + ro + ln.tr[0][fb], qt + ro + ln.tr[1][fb]), ds, dk[fb]);
-        }
-      }
-    }
-    int own_lane = threadIdx.x & 63;
-    asm volatile("" : "+v"(own_lane));  // (addresses made here, not kept through the sweep)
-    const int own_key = kw + (own_lane & 31);
-    const bool mine = own_key < sq.n;
-    const int64_t at = sq.k0 + own_key;
-    if constexpr (SPLIT) {
-      if (!mine) continue;
-      const int64_t rows = a.tk * a.kvh;
-      float* pk = w.part + ((int64_t)part * 2 * rows + at * a.kvh + kv) * a.hd;
-#pragma unroll
-      for (int fb = 0; fb < kFb; ++fb)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int d = 32 * fb + 8 * j + 4 * (own_lane >> 5);
-          if (d >= a.hd) continue;
-          *(f32x4*)(pk + d) = f32x4{dk[fb][4 * j], dk[fb][4 * j + 1], dk[fb][4 * j + 2], dk[fb][4 * j + 3]};
-          *(f32x4*)(pk + rows * a.hd + d) = f32x4{dv[fb][4 * j], dv[fb][4 * j + 1], dv[fb][4 * j + 2], dv[fb][4 * j + 3]};
-        }
-    } else {
-      bad |= a.causal && wave_any(mine && (attn_bad(dk) || attn_bad(dv)));
-      if (!mine) continue;
-      attn_store<F16>(w.dk + at * w.dks + kv * w.dkh, dk, a.scale, own_lane >> 5, a.hd);
-      attn_store<F16>(w.dv + at * w.dvs + kv * w.dvh, dv, 1.f, own_lane >> 5, a.hd);
     }
   }
-  if (!bad) return;
-  wait_dma();  // (the stores of these rows are done: other lanes write them again)
-  const int h0 = kv * a.group;
-  for (int64_t key = (int64_t)t0 * (32 * NW) + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31); key < sq.n;
-       key += (int64_t)tiles * (32 * NW)) {
-    const int64_t token = sq.k0 + key;
-    attn_dkv_rows<F16>(a.k + token * a.ks + kv * a.kh, a.v + token * a.vs + kv * a.vh, a.q + sq.q0 * a.qs + h0 * a.qh,
-                       w.dout + sq.q0 * w.dos + h0 * w.doh, a.qs, a.qh, w.dos, w.doh,
-                       w.stat + (h0 * w.trow + sq.q0) * 2, w.trow, (int)key - (sq.n - sq.m), sq.m, a.group, a.scale,
-                       a.hd, (threadIdx.x >> 5) & 1, w.dk + token * w.dks + kv * w.dkh,
-                       w.dv + token * w.dvs + kv * w.dvh);
-  }
+  if (!attn_vote<NW>(odd, (INFCL_LDS int*)flags, wave)) return;
+  for (int64_t t = t0; t * (32 * NW) < sq.n; t += tiles)
+    attn_dkv_tile<DP, NW, F16, SPLIT, true>(a, w, sq, kv, parts, part, t, lds, stat, true);
 }
 
 // The parts' dk and dv, in order.  A wave takes 8 rows of one sequence's key head,
-// 16 lanes to a row; if one of them is not finite, all again row by row.
+// 16 lanes to a row.
 template <bool F16>
 __global__ void __launch_bounds__(256) attn_dkv_join(AttnArgs a, AttnGrads w, int tiles, int parts) {
   const uint32_t groups = (uint32_t)(a.nseq + 1) * (uint32_t)a.kvh;
@@ -519,7 +524,6 @@ __global__ void __launch_bounds__(256) attn_dkv_join(AttnArgs a, AttnGrads w, in
   const int64_t step = a.tk * a.kvh * a.hd;  // from dk to dv of a part, and on to the next part's dk
   for (int64_t key0 = (int64_t)(blockIdx.x / groups) * 32 + (threadIdx.x >> 6) * 8; key0 < sq.n;
        key0 += (int64_t)tiles * 32) {
-    float sum = 0.f;
 #pragma unroll
     for (int r = lane >> 4; r < 8; r += 4) {
       const int64_t token = sq.k0 + key0 + r;
@@ -535,18 +539,7 @@ __global__ void __launch_bounds__(256) attn_dkv_join(AttnArgs a, AttnGrads w, in
       }
       attn_store8<F16>(w.dk + token * w.dks + kv * w.dkh + d, ak, a.scale);
       attn_store8<F16>(w.dv + token * w.dvs + kv * w.dvh + d, av, 1.f);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum = fmaf(ak[e], 0.f, fmaf(av[e], 0.f, sum));
     }
-    if (!a.causal || !wave_any(!(sum == 0.f))) continue;
-    wait_dma();  // (the stores of these rows are done: other lanes write them again)
-    const int64_t key = key0 + (lane & 31), token = sq.k0 + key;
-    const int h0 = kv * a.group;
-    if ((lane & 31) < 8 && key < sq.n)
-      attn_dkv_rows<F16>(a.k + token * a.ks + kv * a.kh, a.v + token * a.vs + kv * a.vh, a.q + sq.q0 * a.qs + h0 * a.qh,
-                         w.dout + sq.q0 * w.dos + h0 * w.doh, a.qs, a.qh, w.dos, w.doh,
-                         w.stat + (h0 * w.trow + sq.q0) * 2, w.trow, (int)key - (sq.n - sq.m), sq.m, a.group, a.scale,
-                         a.hd, lane >> 5, w.dk + token * w.dks + kv * w.dkh, w.dv + token * w.dvs + kv * w.dvh);
   }
 }
 
@@ -558,10 +551,12 @@ void launch_both(const AttnArgs& a, const AttnGrads& w, const AttnBwdPlan& p, in
   const int64_t tk = ((max_k < 1 ? 1 : max_k) + 32 * NW - 1) / (32 * NW);
   const dim3 qgrid((unsigned)(tq * groups * p.parts_q));
   if (p.parts_q == 1) {
-    hipLaunchKernelGGL((attn_dq_kernel<DP, NW, KT, F16, false>), qgrid, dim3(64 * NW), 0, st, a, w, (int)tq, 1);
+    hipLaunchKernelGGL((attn_dq_kernel<DP, NW, KT, F16, false>), qgrid, dim3(64 * NW), 0, st,
+                       AttnBwdArgs{a, w, (int)tq, 1});
   } else if constexpr (NW > 1) {
-    hipLaunchKernelGGL((attn_dq_kernel<DP, NW, KT, F16, true>), qgrid, dim3(64 * NW), 0, st, a, w, (int)tq, p.parts_q);
-    hipLaunchKernelGGL((attn_dq_join<KT, F16>), dim3((unsigned)(NW * tq * groups)), dim3(256), 0, st, a, w,
+    hipLaunchKernelGGL((attn_dq_kernel<DP, NW, KT, F16, true>), qgrid, dim3(64 * NW), 0, st,
+                       AttnBwdArgs{a, w, (int)tq, p.parts_q});
+    hipLaunchKernelGGL((attn_dq_join<F16>), dim3((unsigned)(NW * tq * groups)), dim3(256), 0, st, a, w,
                        (int)(NW * tq), p.parts_q);
   }
   const dim3 grid((unsigned)(tk * groups * p.parts));

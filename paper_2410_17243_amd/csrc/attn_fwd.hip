@@ -38,48 +38,10 @@ struct AttnParts {
   int64_t rows;
 };
 
-// Row by row (attn.hpp): keys [kbeg, kstop) of the lane's row q, results as the
-// sweep leaves them.
-template <bool F16>
-__device__ __attribute__((noinline)) void attn_fwd_rows(const uint16_t* q, const uint16_t* k, const uint16_t* v,
-                                                        int64_t ks, int64_t vs, int kbeg, int kstop, float scale, int hd,
-                                                        int h, float* po, float* ml, uint16_t* out, float* lse) {
-  const float sl2 = scale * kLog2e;
-  float M = -__builtin_inff(), l = 0.f;
-#pragma unroll 1
-  for (int j = kbeg; j < kstop; ++j) M = fmaxf(M, attn_dot<F16>(q, k + j * ks, h, hd));
-  const float ref = M == -__builtin_inff() ? 0.f : M * sl2;
-#pragma unroll 1
-  for (int j = kbeg; j < kstop; ++j) l += exp2_hw(fmaf(attn_dot<F16>(q, k + j * ks, h, hd), sl2, -ref));
-  const float inv = po ? 1.f : l == 0.f ? 0.f : 1.f / l;
-#pragma unroll 1
-  for (int d = 0; d < hd; d += 16) {
-    float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    const int at = d + 8 * h;
-#pragma unroll 1
-    for (int j = kbeg; j < kstop; ++j) {
-      const float p = exp2_hw(fmaf(attn_dot<F16>(q, k + j * ks, h, hd), sl2, -ref));
-      if (at < hd) attn_axpy8<F16>(acc, p, v + j * vs + at);
-    }
-    if (at >= hd) continue;
-    if (po) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) po[at + e] = acc[e];
-    } else {
-      attn_store8<F16>(out + at, acc, inv);
-    }
-  }
-  if (h) return;
-  if (po)
-    ml[0] = l > 0.f || l != l ? ref : -__builtin_inff(), ml[1] = l;
-  else if (lse)
-    *lse = l == 0.f ? -__builtin_inff() : fmaf(M, scale, logf(l));
-}
-
 // One workgroup's tile t of sequence sq's rows (query, head of the group kv), over
-// its part of the keys.  again: LDS is in use.  Returns whether the wave's sums were not finite: they
-// may hold what masked rows hold, and its rows are to be taken row by row.
-template <int DP, int NW, int KT, bool F16, bool SPLIT>
+// its part of the keys.  again: LDS is in use.  CUT: keys of the tiles that a mask
+// cuts one by one (attn.hpp).  Returns whether the wave's sums were not finite.
+template <int DP, int NW, int KT, bool F16, bool SPLIT, bool CUT>
 __device__ __forceinline__ bool attn_fwd_tile(const AttnArgs& a, uint16_t* __restrict__ out, int64_t os, int64_t oh,
                                               float* __restrict__ lse, int parts, const AttnParts& pw,
                                               const AttnSeq& sq, int kv, int part, uint32_t t, uint32_t rows,
@@ -135,6 +97,7 @@ __device__ __forceinline__ bool attn_fwd_tile(const AttnArgs& a, uint16_t* __res
   for (int i = 0; i < kI; ++i) qf[i] = attn_own(a.q + token * a.qs + head * a.qh, i, h, a.hd, live);
   attn_settle(qf);
   int buf = 0;
+  const int kcut = kbeg + (wmin > kbeg ? (wmin - kbeg) / KT * KT : 0), wend = CUT ? kcut : wmax;
   for (int k = kbeg; k < kend; k += KT, buf ^= 1) {
     attn_barrier();
     if (k + KT < kend) {
@@ -142,7 +105,7 @@ __device__ __forceinline__ bool attn_fwd_tile(const AttnArgs& a, uint16_t* __res
       Tile::issue(kb + (int64_t)(k + KT) * a.ks, sq.n - k - KT, kst, a.hd, nx, koff, wave);
       Tile::issue(vb + (int64_t)(k + KT) * a.vs, sq.n - k - KT, vst, a.hd, nx + Tile::kBytes, voff, wave);
     }
-    if (k >= wmax) continue;
+    if (k >= wend) continue;
     const INFCL_LDS char* kt = lds + buf * 2 * Tile::kBytes;
     const INFCL_LDS char* vt = kt + Tile::kBytes;
     // All row fragments first, then the products, and the transposed fragments of
@@ -214,11 +177,32 @@ __device__ __forceinline__ bool attn_fwd_tile(const AttnArgs& a, uint16_t* __res
         for (int fb = 0; fb < kFb; ++fb) acc[fb] = mfma16<F16>(vf[b][u][fb], p, acc[fb]);
       }
   }
+  if (CUT && live) {
+    const uint16_t* q = a.q + token * a.qs + head * a.qh;
+    const int stop = lim < kstop ? lim : kstop;
+    float top = M;
+#pragma unroll 1
+    for (int k = kcut; k < stop; ++k) top = fmaxf(top, attn_dot<F16>(q, kb + k * a.ks, h, a.hd));
+    const float f = M == -__builtin_inff() ? 1.f : exp2_hw((M - top) * a.sl2);  // (nothing summed yet: 0)
+    M = top;
+    l *= f;
+#pragma unroll
+    for (int fb = 0; fb < kFb; ++fb)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) acc[fb][x] *= f;
+    const float ref = M == -__builtin_inff() ? 0.f : M * a.sl2;
+#pragma unroll 1
+    for (int k = kcut; k < stop; ++k) {
+      const float p = exp2_hw(fmaf(attn_dot<F16>(q, kb + k * a.ks, h, a.hd), a.sl2, -ref));
+      l += h ? 0.f : p;
+      attn_axpy<F16>(acc, p, vb + k * a.vs, h, a.hd);
+    }
+  }
   l = attn_sum2(l);
   const int64_t id = token * a.heads + head;
   float* po = SPLIT ? pw.o + ((int64_t)part * pw.rows + id) * a.hd : nullptr;
   float* ml = SPLIT ? pw.ml + ((int64_t)part * pw.rows + id) * 2 : nullptr;
-  const bool bad = a.causal && wave_any(live && attn_bad(acc));
+  const bool bad = !CUT && a.causal && wave_any(live && attn_bad(acc));
   if (!live) return bad;
   if constexpr (SPLIT) {
 #pragma unroll
@@ -238,14 +222,25 @@ __device__ __forceinline__ bool attn_fwd_tile(const AttnArgs& a, uint16_t* __res
   return bad;
 }
 
+struct AttnFwdArgs {
+  AttnArgs a;
+  uint16_t* out;
+  int64_t os, oh;
+  float* lse;
+  int tiles, parts;
+  AttnParts pw;
+};
+
 // Workgroup idx takes rows [32 NW t, +32 NW) of sequence z's group of heads kv,
 // t descending (with causal masks the last rows see most keys), and part
 // `part` of its keys.
 template <int DP, int NW, int KT, bool F16, bool SPLIT>
 __global__ void __launch_bounds__(64 * NW, 2)
-    attn_fwd_kernel(AttnArgs a, uint16_t* __restrict__ out, int64_t os, int64_t oh, float* __restrict__ lse, int tiles,
-                    int parts, AttnParts pw) {
+    attn_fwd_kernel(AttnFwdArgs c) {
+  const AttnArgs& a = c.a;
+  const int tiles = c.tiles, parts = c.parts;
   __shared__ __attribute__((aligned(1024))) char lds[4 * AttnTile<DP, NW, KT>::kBytes];
+  __shared__ int flags[NW];
   uint32_t idx = blockIdx.x;
   const int part = SPLIT ? (int)(idx % (uint32_t)parts) : 0;
   if (SPLIT) idx /= (uint32_t)parts;
@@ -260,23 +255,22 @@ __global__ void __launch_bounds__(64 * NW, 2)
   // (one tile, unless sequences are longer than the caller said)
   bool bad = false;
   for (uint32_t t = (uint32_t)t0; t * (uint64_t)(32 * NW) < rows; t += (uint32_t)tiles)
-    bad |= attn_fwd_tile<DP, NW, KT, F16, SPLIT>(a, out, os, oh, lse, parts, pw, sq, kv, part, t, rows,
-                                                 (INFCL_LDS char*)lds, t != (uint32_t)t0);
-  if (!bad) return;
-  wait_dma();  // (the stores of these rows are done: other lanes write them again)
-  const int h = (threadIdx.x >> 5) & 1;
-  const int per = SPLIT ? ((sq.n + parts - 1) / parts + KT - 1) / KT * KT : sq.n;
-  for (uint64_t r = (uint64_t)t0 * (32 * NW) + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31); r < rows;
-       r += (uint64_t)tiles * (32 * NW)) {
-    const int pos = (int)((uint32_t)r / (uint32_t)a.group), head = kv * a.group + (int)((uint32_t)r % (uint32_t)a.group);
-    const int64_t token = sq.q0 + pos, id = token * a.heads + head;
-    const int lim = pos + sq.n - sq.m + 1, kbeg = part * per, kend = kbeg + per < sq.n ? kbeg + per : sq.n;
-    attn_fwd_rows<F16>(a.q + token * a.qs + head * a.qh, a.k + sq.k0 * a.ks + kv * a.kh, a.v + sq.k0 * a.vs + kv * a.vh,
-                       a.ks, a.vs, kbeg, lim < kend ? lim : kend, a.scale, a.hd, h,
-                       SPLIT ? pw.o + ((int64_t)part * pw.rows + id) * a.hd : nullptr,
-                       SPLIT ? pw.ml + ((int64_t)part * pw.rows + id) * 2 : nullptr, out + token * os + head * oh,
-                       lse ? lse + (int64_t)head * a.tq + token : nullptr);
+    bad |= attn_fwd_tile<DP, NW, KT, F16, SPLIT, false>(a, c.out, c.os, c.oh, c.lse, parts, c.pw, sq, kv, part, t, rows,
+                                                        (INFCL_LDS char*)lds, t != (uint32_t)t0);
+  if (!a.causal) return;
+  const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  bool odd = false;  // values of the tiles that a mask cuts
+  if (bad) {
+    const AttnArgs r = attn_reload<AttnFwdArgs>().a;
+    for (uint32_t t = (uint32_t)t0; t * (uint64_t)(32 * NW) + 32 * wave < rows; t += (uint32_t)tiles)
+      odd |= attn_odd_keys<F16>(r.v + sq.k0 * r.vs + kv * r.vh, r.vs, r.hd, sq, r.group, t * (32 * NW) + 32 * wave, rows,
+                                KT);
   }
+  if (!attn_vote<NW>(odd, (INFCL_LDS int*)flags, wave)) return;
+  const AttnFwdArgs r = attn_reload<AttnFwdArgs>();
+  for (uint32_t t = (uint32_t)t0; t * (uint64_t)(32 * NW) < rows; t += (uint32_t)tiles)
+    attn_fwd_tile<DP, NW, KT, F16, SPLIT, true>(r.a, r.out, r.os, r.oh, r.lse, r.parts, r.pw, sq, kv, part, t, rows,
+                                                (INFCL_LDS char*)lds, true);
 }
 
 // Joins the parts of every row: M the largest, l and o the rescaled sums.  A
@@ -320,12 +314,11 @@ void launch_one(const AttnArgs& a, const AttnFwdPlan& p, uint16_t* out, int64_t 
                 hipStream_t st) {
   AttnParts pw{(float*)(ws + p.o), (float*)(ws + p.ml), a.tq * a.heads};
   const dim3 grid((unsigned)((int64_t)p.tiles * (a.nseq + 1) * a.kvh * p.parts));
+  const AttnFwdArgs c{a, out, os, oh, lse, p.tiles, p.parts, pw};
   if (p.parts > 1)
-    hipLaunchKernelGGL((attn_fwd_kernel<DP, NW, KT, F16, true>), grid, dim3(64 * NW), 0, st, a, out, os, oh, lse,
-                       p.tiles, p.parts, pw);
+    hipLaunchKernelGGL((attn_fwd_kernel<DP, NW, KT, F16, true>), grid, dim3(64 * NW), 0, st, c);
   else
-    hipLaunchKernelGGL((attn_fwd_kernel<DP, NW, KT, F16, false>), grid, dim3(64 * NW), 0, st, a, out, os, oh, lse,
-                       p.tiles, 1, pw);
+    hipLaunchKernelGGL((attn_fwd_kernel<DP, NW, KT, F16, false>), grid, dim3(64 * NW), 0, st, c);
 }
 
 }  // namespace
