@@ -48,6 +48,17 @@ struct AttnBwdPlan {
   size_t stat, part, part_q, total;
 };
 
+// A launch has less than 2^32 work-items (past that its grid would wrap, without an
+// error).  So many of `tiles` tiles for each of `others` workgroups at once: the
+// kernels go on to the rest in steps of that number.
+constexpr int64_t kAttnItems = ((int64_t)1 << 32) - 1;
+inline int64_t attn_at_once(int64_t tiles, int64_t others, int threads) {
+  const int64_t most = kAttnItems / threads / others;
+  return tiles < most ? tiles : most < 1 ? 1 : most;
+}
+// Pairs of sequence (and the rows past the last one) and key head.
+inline int64_t attn_groups(const AttnArgs& a) { return ((int64_t)a.nseq + 1) * a.kvh; }
+
 // Tiles of nseq sequences, of which none has more than `most` and all together
 // about `sum`.
 inline int64_t attn_tiles(int64_t nseq, int64_t most, int64_t sum) {

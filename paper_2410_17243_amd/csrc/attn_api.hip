@@ -31,11 +31,9 @@ infcl_status shape_status(const infcl_attn_shape* s) {
   if (s->dtype == INFCL_F32 || s->head_dim % 8 != 0 || s->head_dim > 128 || s->total_q > kMaxTokens ||
       s->total_k > kMaxTokens || s->heads > 4096 || s->nseq > (1 << 24))
     return INFCL_ERR_UNSUPPORTED;
-  // workgroups of the largest grid, and rows of a sequence, in 31 bits
-  const int64_t group = s->heads / s->kv_heads, mq = s->max_q < s->total_q ? s->max_q : s->total_q,
-                mk = s->max_k < s->total_k ? s->max_k : s->total_k;
-  const int64_t tiles = mq * group > mk ? mq * group / 32 + 1 : mk / 32 + 1;
-  if (mq * group > kMaxTokens || (double)tiles * ((double)s->nseq + 1) * s->kv_heads > 2e9) return INFCL_ERR_UNSUPPORTED;
+  // rows of a sequence in 31 bits; a wave for each sequence and key head in one launch
+  const int64_t group = s->heads / s->kv_heads, mq = s->max_q < s->total_q ? s->max_q : s->total_q;
+  if (mq * group > kMaxTokens || ((int64_t)s->nseq + 1) * s->kv_heads > kAttnItems / 64) return INFCL_ERR_UNSUPPORTED;
   return INFCL_OK;
 }
 

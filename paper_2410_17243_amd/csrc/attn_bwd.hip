@@ -546,26 +546,26 @@ __global__ void __launch_bounds__(256) attn_dkv_join(AttnArgs a, AttnGrads w, in
 template <int DP, bool F16, int NW, int KT>
 void launch_both(const AttnArgs& a, const AttnGrads& w, const AttnBwdPlan& p, int64_t max_q, int64_t max_k,
                  hipStream_t st) {
-  const int64_t groups = (int64_t)(a.nseq + 1) * a.kvh;
-  const int64_t tq = ((max_q < 1 ? 1 : max_q) * a.group + 32 * NW - 1) / (32 * NW);
-  const int64_t tk = ((max_k < 1 ? 1 : max_k) + 32 * NW - 1) / (32 * NW);
+  const int64_t groups = attn_groups(a);
+  const int64_t tq = attn_at_once(((max_q < 1 ? 1 : max_q) * a.group + 32 * NW - 1) / (32 * NW), groups * p.parts_q, 64 * NW);
+  const int64_t tk = attn_at_once(((max_k < 1 ? 1 : max_k) + 32 * NW - 1) / (32 * NW), groups * p.parts, 64 * NW);
   const dim3 qgrid((unsigned)(tq * groups * p.parts_q));
   if (p.parts_q == 1) {
     hipLaunchKernelGGL((attn_dq_kernel<DP, NW, KT, F16, false>), qgrid, dim3(64 * NW), 0, st,
                        AttnBwdArgs{a, w, (int)tq, 1});
   } else if constexpr (NW > 1) {
+    const int64_t tj = attn_at_once(NW * tq, groups, 256);
     hipLaunchKernelGGL((attn_dq_kernel<DP, NW, KT, F16, true>), qgrid, dim3(64 * NW), 0, st,
                        AttnBwdArgs{a, w, (int)tq, p.parts_q});
-    hipLaunchKernelGGL((attn_dq_join<F16>), dim3((unsigned)(NW * tq * groups)), dim3(256), 0, st, a, w,
-                       (int)(NW * tq), p.parts_q);
+    hipLaunchKernelGGL((attn_dq_join<F16>), dim3((unsigned)(tj * groups)), dim3(256), 0, st, a, w, (int)tj, p.parts_q);
   }
   const dim3 grid((unsigned)(tk * groups * p.parts));
   if (p.parts == 1) {
     hipLaunchKernelGGL((attn_dkv_kernel<DP, NW, F16, false>), grid, dim3(64 * NW), 0, st, a, w, (int)tk, 1);
   } else if constexpr (NW > 1) {
+    const int64_t tj = attn_at_once(4 * tk, groups, 256);
     hipLaunchKernelGGL((attn_dkv_kernel<DP, NW, F16, true>), grid, dim3(64 * NW), 0, st, a, w, (int)tk, p.parts);
-    hipLaunchKernelGGL((attn_dkv_join<F16>), dim3((unsigned)(4 * tk * groups)), dim3(256), 0, st, a, w, (int)(4 * tk),
-                       p.parts);
+    hipLaunchKernelGGL((attn_dkv_join<F16>), dim3((unsigned)(tj * groups)), dim3(256), 0, st, a, w, (int)tj, p.parts);
   }
 }
 
@@ -593,7 +593,7 @@ void launch_t(const AttnArgs& a, const AttnGrads& w, const AttnBwdPlan& p, int64
 // of the other side), and one long sweep would be waited for.
 AttnBwdPlan attn_bwd_plan(const AttnArgs& a, int64_t max_q, int64_t max_k) {
   AttnBwdPlan p;
-  p.few = max_q * a.group <= 128 && max_k <= 128;
+  p.few = (max_q * a.group <= 128 && max_k <= 128) || attn_groups(a) > kAttnItems / 256;  // (as in the forward)
   p.parts = p.parts_q = 1;
   if (!p.few) {
     const int64_t tiles = max_k > 0 ? attn_tiles(a.nseq, (max_k + 127) / 128, a.tk / 128) * a.kvh : 0;

@@ -279,41 +279,41 @@ template <bool F16>
 __global__ void __launch_bounds__(256) attn_join(AttnParts pw, int parts, int heads, int hd, int64_t tq,
                                                  uint16_t* __restrict__ out, int64_t os, int64_t oh,
                                                  float* __restrict__ lse) {
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 5;
   const int d = 4 * (threadIdx.x & 31);
-  if (i >= pw.rows) return;
-  float M = -__builtin_inff();
-  for (int p = 0; p < parts; ++p) M = fmaxf(M, pw.ml[((int64_t)p * pw.rows + i) * 2]);
-  float l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 5; i < pw.rows; i += (int64_t)gridDim.x * 8) {
+    float M = -__builtin_inff();
+    for (int p = 0; p < parts; ++p) M = fmaxf(M, pw.ml[((int64_t)p * pw.rows + i) * 2]);
+    float l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int p = 0; p < parts; ++p) {
-    const float* ml = pw.ml + ((int64_t)p * pw.rows + i) * 2;
-    if (ml[1] == 0.f) continue;  // (sees nothing of this part)
-    const float f = exp2_hw(ml[0] - M);
-    l = fmaf(ml[1], f, l);
-    if (d < hd) {
-      const f32x4 x = *(const f32x4*)(pw.o + ((int64_t)p * pw.rows + i) * hd + d);
+    for (int p = 0; p < parts; ++p) {
+      const float* ml = pw.ml + ((int64_t)p * pw.rows + i) * 2;
+      if (ml[1] == 0.f) continue;  // (sees nothing of this part)
+      const float f = exp2_hw(ml[0] - M);
+      l = fmaf(ml[1], f, l);
+      if (d < hd) {
+        const f32x4 x = *(const f32x4*)(pw.o + ((int64_t)p * pw.rows + i) * hd + d);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = fmaf(x[e], f, o[e]);
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(x[e], f, o[e]);
+      }
     }
-  }
-  const int64_t token = i / heads;
-  const int head = (int)(i % heads);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  if (d < hd) {
-    uint16_t* po = out + token * os + head * oh + d;
+    const int64_t token = i / heads;
+    const int head = (int)(i % heads);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (d < hd) {
+      uint16_t* po = out + token * os + head * oh + d;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) po[e] = __builtin_bit_cast(uint16_t, to16<F16>(o[e] * inv));
+      for (int e = 0; e < 4; ++e) po[e] = __builtin_bit_cast(uint16_t, to16<F16>(o[e] * inv));
+    }
+    if (lse && d == 0) lse[(int64_t)head * tq + token] = l == 0.f ? -__builtin_inff() : kLn2 * M + logf(l);
   }
-  if (lse && d == 0) lse[(int64_t)head * tq + token] = l == 0.f ? -__builtin_inff() : kLn2 * M + logf(l);
 }
 
 template <int DP, bool F16, int NW, int KT>
 void launch_one(const AttnArgs& a, const AttnFwdPlan& p, uint16_t* out, int64_t os, int64_t oh, float* lse, char* ws,
                 hipStream_t st) {
   AttnParts pw{(float*)(ws + p.o), (float*)(ws + p.ml), a.tq * a.heads};
-  const dim3 grid((unsigned)((int64_t)p.tiles * (a.nseq + 1) * a.kvh * p.parts));
+  const dim3 grid((unsigned)(p.tiles * attn_groups(a) * p.parts));
   const AttnFwdArgs c{a, out, os, oh, lse, p.tiles, p.parts, pw};
   if (p.parts > 1)
     hipLaunchKernelGGL((attn_fwd_kernel<DP, NW, KT, F16, true>), grid, dim3(64 * NW), 0, st, c);
@@ -334,7 +334,7 @@ void launch_one(const AttnArgs& a, const AttnFwdPlan& p, uint16_t* out, int64_t 
 AttnFwdPlan attn_fwd_plan(const AttnArgs& a, int64_t max_q, int64_t max_k) {
   AttnFwdPlan p;
   const int64_t rows = (max_q < 1 ? 1 : max_q) * a.group;
-  p.nw = rows <= 128 ? 1 : 4;
+  p.nw = rows <= 128 || attn_groups(a) > kAttnItems / 256 ? 1 : 4;  // (so many pairs: one wave each fits a launch)
   p.tiles = (int)((rows + 32 * p.nw - 1) / (32 * p.nw));
   const int64_t wgs = (int64_t)p.tiles * (a.nseq > 1 ? a.nseq : 1) * a.kvh, want = p.nw == 1 ? 2048 : 512;
   int64_t parts = 1;
@@ -345,6 +345,7 @@ AttnFwdPlan attn_fwd_plan(const AttnArgs& a, int64_t max_q, int64_t max_k) {
     if (parts < 1) parts = 1;
   }
   p.parts = (int)parts;
+  p.tiles = (int)attn_at_once(p.tiles, attn_groups(a) * parts, 64 * p.nw);
   const size_t r = (size_t)a.tq * (size_t)a.heads;
   size_t off = 0;
   p.o = off, off = (off + (parts > 1 ? r * a.hd * 4 * parts : 0) + 255) & ~(size_t)255;
@@ -370,7 +371,7 @@ static int attn_fwd_t(const AttnArgs& a, const AttnFwdPlan& p, uint16_t* out, in
   if (hipGetLastError() != hipSuccess) return INFCL_ERR_HIP;
   if (p.parts > 1) {
     AttnParts pw{(float*)(ws + p.o), (float*)(ws + p.ml), a.tq * a.heads};
-    const dim3 grid((unsigned)((pw.rows + 7) / 8));
+    const dim3 grid((unsigned)attn_at_once((pw.rows + 7) / 8, 1, 256));
     hipLaunchKernelGGL((attn_join<F16>), grid, dim3(256), 0, st, pw, p.parts, a.heads, a.hd, a.tq, out, os, oh, lse);
     if (hipGetLastError() != hipSuccess) return INFCL_ERR_HIP;
   }

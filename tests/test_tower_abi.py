@@ -124,3 +124,15 @@ def test_token_counts_that_the_sort_would_take_too_long_for(lib):
     n = ctypes.c_size_t(0)
     assert lib.infcl_embed_bwd_workspace(1 << 26, 100, 8, ctypes.byref(n)) == OK
     assert lib.infcl_embed_bwd_workspace((1 << 26) + 1, 100, 8, ctypes.byref(n)) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("kw,want", [
+    # a launch has at most 2^32 - 1 work-items: 64 for each sequence (and the rows past them) and key head
+    (dict(nseq=(1 << 25) // 16 * 2 - 1, heads=16, kv=16), UNSUPPORTED), (dict(nseq=(1 << 25) // 16 * 2 - 2, heads=16, kv=16), OK),
+    (dict(nseq=1 << 14, heads=4096, kv=4096), UNSUPPORTED), (dict(nseq=(1 << 14) - 2, heads=4096, kv=4096), OK),
+    # many short sequences and a long one: no more tiles at once than that, not a refusal
+    (dict(nseq=1 << 20, tq=1 << 24, tk=1 << 24, mq=1 << 20, mk=1 << 20, heads=16, kv=16), OK),
+])
+def test_launches_stay_within_the_work_items_there_are(lib, kw, want):
+    f, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    assert lib.infcl_attn_workspace(ctypes.byref(_shape(kw)), ctypes.byref(f), ctypes.byref(b)) == want

@@ -358,3 +358,25 @@ def test_far_rows():
     dq, dk, dv = infcl.packed_attn_bwd(*a, out, lse, _dev(do), *off)
     _check_bwd((dq, dk[far:], dv[far:]), r, "bf16")
     assert int(dk[:far].count_nonzero()) == 0 and int(dv[:far].count_nonzero()) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("short,length", [(140_000, 1024), (1_060_000, 300)])
+def test_many_sequences_and_a_long_one(short, length):
+    """More tiles of the longest length, or more sequences alone, than a launch of 256
+    work-items each takes.  A lone token's out is its value, its dv dout and its
+    dq and dk zero."""
+    heads, hd, t = 16, 8, short + length
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, k, v, do = [torch.randn((t, heads, hd), generator=g, device="cuda").bfloat16() for _ in range(4)]
+    cu = torch.cat([torch.arange(short + 1), torch.tensor([t])]).int().cuda()
+    out, lse = infcl.packed_attn_fwd(q, k, v, cu, length)
+    assert torch.equal(out[:short], v[:short])
+    dq, dk, dv = infcl.packed_attn_bwd(q, k, v, out, lse, do, cu, length)
+    assert torch.equal(dv[:short], do[:short])
+    # (D is the sum of p dp, p is 1 up to fp32 roundings of lse: ds below 2^-20 |do| |v|)
+    assert float(dq[:short].abs().max()) < 2.0 ** -10 and float(dk[:short].abs().max()) < 2.0 ** -10
+    last = [x[short:].cpu() for x in (q, k, v)]
+    r = tower.attention(*last, [0, length], [0, length], True, hd ** -0.5, do[short:].cpu())
+    _check_fwd(out[short:], lse[:, short:], r, "bf16")
+    _check_bwd([x[short:] for x in (dq, dk, dv)], r, "bf16")
