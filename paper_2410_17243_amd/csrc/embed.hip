@@ -342,18 +342,21 @@ __global__ void __launch_bounds__(256) embed_sum(Runs r, int64_t n, const u32x4*
   const uint32_t per = 256u >> ls;
   float s[N];
   if (blockIdx.x < row_blocks) {
-    uint32_t v = blockIdx.x * per + (threadIdx.x >> ls), a, b;
-    if (r.run) {  // a run by its first position
-      if (v >= n) return;
-      a = r.run[v].x, b = r.run[v].y;
-      if (a != v) return;
-      v = r.sorted[v].x;
+    const int64_t rows = r.run ? n : (int64_t)vocab, step = (int64_t)row_blocks * per;
+    for (int64_t at = (int64_t)blockIdx.x * per + (threadIdx.x >> ls); at < rows; at += step) {
+      uint32_t v = (uint32_t)at, a, b;
+      if (r.run) {  // a run by its first position
+        a = r.run[at].x, b = r.run[at].y;
+        if (a != v) continue;
+        v = r.sorted[at].x;
+        if (v >= vocab) continue;
+      } else {
+        a = r.start[v], b = r.start[v + 1];
+      }
+      if (b - a > 1u << r.lg) continue;
+      sum_rows<T>(r.sorted, dout, c, i, gl, ls, a, b, s);
+      if (i < c) put_row<T, G>(dtable, v, c, i, s, scale);
     }
-    if (v >= vocab) return;
-    if (!r.run) a = r.start[v], b = r.start[v + 1];
-    if (b - a > 1u << r.lg) return;
-    sum_rows<T>(r.sorted, dout, c, i, gl, ls, a, b, s);
-    if (i < c) put_row<T, G>(dtable, v, c, i, s, scale);
     return;
   }
   const int64_t p = (int64_t)(blockIdx.x - row_blocks) * per + (threadIdx.x >> ls);
@@ -577,7 +580,9 @@ int embed_bwd_t(const void* tokens, int tb, int64_t n, const void* dout, int64_t
   if (rc != INFCL_OK) return rc;
   const int ls = row_lanes_log2(c, 1);
   const int64_t per = 256 >> ls, rows = s.few ? n : vocab, parts = (n + (1 << s.lg) - 1) >> s.lg;
-  const int64_t rb = (rows + per - 1) / per, pb = n > 1 << s.lg ? (parts + per - 1) / per : 0;
+  // (a launch has less than 2^32 work-items: 2^23 blocks of rows, which go on in steps, and at most 2^18 of parts)
+  const int64_t all = (rows + per - 1) / per, rb = all < (1 << 23) ? all : 1 << 23;
+  const int64_t pb = n > 1 << s.lg ? (parts + per - 1) / per : 0;
   const unsigned slices = (unsigned)((c + (1 << ls) - 1) >> ls);
   hipLaunchKernelGGL((embed_sum<T, G>), dim3((unsigned)(rb + pb), slices), dim3(256), 0, st, r, n, (const u32x4*)dout,
                      (uint32_t)vocab, (int)c, ls, scale, dtable, (float*)(ws + s.part), (uint32_t)rb);

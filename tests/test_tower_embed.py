@@ -105,3 +105,27 @@ def test_refusals():
         infcl.embed_bwd(t, w[:4], 6, grad_dtype=torch.float16)
     with pytest.raises(infcl.InfclError):
         infcl.embed_fwd(t, torch.zeros((6, 6), device="cuda"))  # rows of 24 bytes
+
+
+@pytest.mark.gpu
+def test_gradient_of_more_rows_than_a_launch_has_groups():
+    """2^26 rows of 64 lanes each: as many work-items as a launch cannot have."""
+    vocab, d, n = 1 << 26, 264, 5000
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 80 GB of device memory")
+    g = torch.Generator().manual_seed(1)
+    tok = torch.randint(0, vocab, (n,), generator=g)
+    tok[:4], tok[4:4000:2] = torch.tensor([0, vocab - 1, vocab - 2, 1 << 25]), vocab - 1
+    dout = torch.randn((n, d), generator=g).bfloat16()
+    dw = infcl.embed_bwd(tok.cuda(), dout.cuda(), vocab, 0.5, grad_dtype=torch.bfloat16)
+    rows, inv, count = torch.unique(tok, return_inverse=True, return_counts=True)
+    ref, size = torch.zeros((2, len(rows), d), dtype=torch.float64)
+    ref.index_add_(0, inv, 0.5 * dout.double())
+    size.index_add_(0, inv, 0.5 * dout.double().abs())
+    got = dw[rows.cuda()].cpu().double()
+    assert ((got - ref).abs() <= (count[:, None] + 2) * 2.0 ** -23 * size + EPS["bf16"] * ref.abs()).all()
+    for a, b in ((1, 4096), (vocab - 70000, vocab - 2), ((1 << 25) + 1, (1 << 25) + 4096)):  # rows of no token but these
+        mine = rows[(rows >= a) & (rows < b)] - a
+        part = dw[a:b].clone()
+        part[mine.cuda()] = 0
+        assert int(part.count_nonzero()) == 0
