@@ -129,3 +129,30 @@ def test_gradient_of_more_rows_than_a_launch_has_groups():
         part = dw[a:b].clone()
         part[mine.cuda()] = 0
         assert int(part.count_nonzero()) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lo,hi", [(0, 100), ((1 << 22) - 100, 1 << 22), (1 << 21, (1 << 21) + 1), (1 << 30, 1 << 31)])
+def test_ids_from_a_part_of_the_table(lo, hi):
+    """Tokens of the first hundred rows of a large table, of the last, of a single one
+    in between, of none: right, and no slower than tokens from all over it (a run of
+    absent rows is not one lane's work; measured up to twice as long, the bound is 5)."""
+    vocab, d, n = 1 << 22, 8, 10000
+    g = torch.Generator().manual_seed(2)
+    tok, dout = torch.randint(lo, hi, (n,), generator=g), torch.randn((n, d), generator=g)
+    dw = infcl.embed_bwd(tok.cuda(), dout.cuda(), vocab).cpu()
+    ref, size, count = tower.embedding_grad(tok, dout, vocab, 1.0)
+    assert ((dw.double() - ref).abs() <= (count[:, None] + 2) * 2.0 ** -24 * size).all()
+
+    def time(t):
+        t, x, took = t.cuda(), dout.cuda(), []
+        for _ in range(6):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            infcl.embed_bwd(t, x, vocab)
+            b.record()
+            torch.cuda.synchronize()
+            took.append(a.elapsed_time(b))
+        return min(took)
+
+    assert time(tok) < 5 * time(torch.randint(0, vocab, (n,), generator=g))
