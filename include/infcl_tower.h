@@ -95,7 +95,9 @@ infcl_status infcl_attn_fwd(const infcl_attn_shape* shape, infcl_attn_view q, in
                             const int32_t* cu_q, const int32_t* cu_k, const int32_t* len_k, infcl_attn_view out,
                             float* lse, void* workspace, size_t ws_bytes, void* stream);
 
-/* dq, dk, dv of dtype; out and lse as infcl_attn_fwd left them. */
+/* dq, dk, dv of dtype; out and lse as infcl_attn_fwd left them without len_k: the
+ * backward pass is that of all keys cu_k[z] .. cu_k[z+1] (after a call with len_k it
+ * would count the unused rows as seen). */
 infcl_status infcl_attn_bwd(const infcl_attn_shape* shape, infcl_attn_view q, infcl_attn_view k, infcl_attn_view v,
                             const int32_t* cu_q, const int32_t* cu_k, infcl_attn_view out, const float* lse,
                             infcl_attn_view dout, infcl_attn_view dq, infcl_attn_view dk, infcl_attn_view dv,

@@ -265,7 +265,8 @@ def packed_attn_fwd(q, k, v, cu_q, max_q: int, cu_k=None, max_k=None, causal: bo
 
 def packed_attn_bwd(q, k, v, out, lse, dout, cu_q, max_q: int, cu_k=None, max_k=None, causal: bool = True, scale=None,
                     grads=None):
-    """dq, dk, dv of packed_attn_fwd; written into grads = (dq, dk, dv) where given."""
+    """dq, dk, dv of packed_attn_fwd without len_k (every key between cu_k's offsets counts
+    as in use); written into grads = (dq, dk, dv) where given."""
     dev, (sh, _, n), vq, vk, vv, cu_k = _attn_call(q, k, v, cu_q, max_q, cu_k, max_k, causal, scale)
     _device(("q", q), ("out", out), ("lse", lse), ("dout", dout))
     if out.shape != q.shape or dout.shape != q.shape:
