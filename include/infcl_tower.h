@@ -107,11 +107,14 @@ infcl_status infcl_attn_bwd(const infcl_attn_shape* shape, infcl_attn_view q, in
  * x [n, d] is kept as q [n, d] (int8, 16-byte aligned) and exps [n, ceil(d/32)]
  * (one byte): 32 consecutive features of a row share the least e >= -126 with
  * rint(max|x| 2^-e) <= 127, q = rint(x 2^-e) (ties to even), exps = e + 127, and
- * x^ = q 2^e stands for x: within 2^(e-1) <= max|x| / 127 of it.  A group that
- * holds an infinity or a NaN has exponent byte 255 and reads back as NaN; a
- * maximum that would round to 2^128 is kept as 127 2^121.  d a multiple of 8;
- * x_stride, dy_stride: elements from row to row (a multiple of 8, >= d); the
- * other arrays are contiguous.  Entries of fp16 results are limited to 65504. */
+ * x^ = q 2^e stands for x: within 2^(e-1) of it, which is at most max|x| / 127 for
+ * e > -126 (groups below 2^-119 or so are kept with e = -126, to 2^-127).  A maximum
+ * that would round to 2^128 is kept as 127 2^121, entries of its group within 2^121.
+ * A group that holds an infinity or a NaN has exponent byte 255 and reads back as
+ * NaN.  d a multiple of 8; x_stride, dy_stride: elements from row to row (a multiple
+ * of 8, >= d); the other arrays are contiguous.  In fp16, x^ and f(x^) are limited to
+ * 65504 (an entry next to it rounds to 65536 in 8 bits); dx is not, as no product is.
+ */
 typedef enum {
   INFCL_ACT_NONE = 0,
   INFCL_ACT_GELU = 1,       /* x Phi(x), Phi by erf        */

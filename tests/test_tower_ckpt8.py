@@ -182,3 +182,22 @@ def test_refusals():
         infcl.ckpt8_wgrad(x, kept, grad_dtype=torch.float16)
     with pytest.raises(ValueError):
         infcl.ckpt8_unpack(infcl.Ckpt8(kept.q, kept.exps[:, :1], x.dtype))
+
+
+def test_how_far_a_kept_entry_may_be_off():
+    """The bounds of include/infcl_tower.h, by the oracle: half a step, at most max / 127
+    of it above e = -126; 2^-127 there; 2^121 next to the largest float."""
+    g = torch.Generator().manual_seed(8)
+    top = torch.cat([torch.exp2(torch.linspace(-145, 127.99, 150, dtype=torch.float64)), torch.tensor([127.5 * 2.0 ** -126,
+                     127.5 * 2.0 ** 120, 127.49 * 2.0 ** 120, 127.5 * 2.0 ** 121, 3.4028234663852886e38], dtype=torch.float64)])
+    x = (torch.rand((len(top), 32), generator=g, dtype=torch.float64) * 2 - 1) * top[:, None]
+    x[:, 0] = top
+    x = x.float()
+    q, e = tower.kept(x)
+    most, off, e = x.double().abs().max(1).values, (tower.unkept(q, e) - x.double()).abs().max(1).values, e[:, 0].double() - 127
+    kept_at_the_end = most >= 127.5 * 2.0 ** 121
+    plain = (e > -126) & ~kept_at_the_end
+    assert plain.any() and kept_at_the_end.any() and (e == -126).any()
+    assert (off[~kept_at_the_end] <= torch.exp2(e - 1)[~kept_at_the_end]).all()
+    assert (torch.exp2(e - 1)[plain] <= most[plain] / 127).all()
+    assert (off[kept_at_the_end] <= 2.0 ** 121).all() and (off[kept_at_the_end] > most[kept_at_the_end] / 136).any()
