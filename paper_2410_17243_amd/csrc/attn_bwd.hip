@@ -12,26 +12,30 @@
 // lse log2(e), rows with no keys as 0, for the second.
 //
 // p and ds are rounded to 16 bits for the second products, as the inputs are.
-// D comes from o as stored, except for rows that see the first tile of keys only:
-// there it is the sum of p dp in the registers, which no rounding of o touches.
-// (The error of D from o's rounding, beside that of rounding ds, is the sum of
-// p^2 over a row in the mean square: near 1 for a row that sees few keys, 3 / n
-// over n keys of similar scores.)  ds is rounded as it stands: in fp16 its range is
-// that of the gradients times 1 / scale, which loss scaling has to respect.
+// D comes from o as stored, except in waves none of whose rows sees past the first
+// tile of keys (32 or 64): there it is the sum of p dp in the registers, which no
+// rounding of o touches.  (The error of D from o's rounding, beside that of rounding
+// ds, is the sum of p^2 over a row in the mean square: near 1 for a row that sees
+// few keys, 3 / n over n keys of similar scores.  Which of the two a row of few keys
+// gets depends on the rows beside it.)  ds is rounded as it stands: in fp16 its
+// range is that of dout's products with v times p, about 1 / n over n keys of
+// similar scores, so that long rows leave the normal numbers long before dout
+// does, which loss scaling has to respect.
 //
-// 4 sequences of up to 4096 tokens, 16 heads of 128 over 4: dq 229 us (910 TFLOP/s),
-// dk and dv 335 us (825) and 25 us to join their parts; bound by the latency of
-// each tile's chain (products, weights, products) at two waves per SIMD, which is
-// what 128 features' accumulators leave.  1024 captions of about 17 tokens, 8
-// heads of 64: 30 and 32 us; a wave's chain of loads for one tile of work.
+// 4 sequences of up to 4096 tokens, 16 heads of 128 over 4: dq 231 us (900 TFLOP/s,
+// MFMAs busy 42% of the time), dk and dv 338 us (820, 39%) and 23 us to join their
+// parts; bound by the latency of each tile's chain (products, weights, products) at
+// two waves per SIMD, which is what 128 features' accumulators leave.  1024 captions
+// of about 17 tokens, 8 heads of 64: 28 and 32 us; a wave's chain of loads for one tile
+// of work, five waves to a compute unit.
 #include "attn.hpp"
 
 namespace infcl {
 namespace {
 
 // Workgroups that the sweeps over queries, and over keys, are cut into, about (4
-// sequences of up to 4096 tokens, 4 key heads: dk and dv with their join 560 us
-// uncut, 511, 413, 422 and 425 at 512, 768, 1024 and 1536; 3 of up to 3371 tokens, one
+// sequences of up to 4096 tokens, 4 key heads: dk and dv with their join 819 us
+// uncut, 475, 362, 372 and 370 at 512, 768, 1024 and 1536; 3 of up to 3371 tokens, one
 // key head: dq 115 us uncut, 81 so).
 constexpr int64_t kBwdGroups = 768, kBwdRowGroups = 384;
 
@@ -302,8 +306,8 @@ __global__ void __launch_bounds__(256) attn_dq_join(AttnArgs a, AttnGrads w, int
 // through them together, so that the copies find them in L2.
 // At 128 features the own rows, the two sums and a tile's weights are more than
 // the registers of two waves per SIMD: the own values stay in LDS there (a fifth
-// of the sweep's LDS reads), for a register spilled in the sweep costs far more
-// (its reload waits for the tile copies in flight).
+// of the sweep's LDS reads), for a register spilled in the sweep costs more
+// (its reload waits for the tile copies in flight); none is.
 // SPLIT: a workgroup takes one of several parts of the tiles and leaves its sums in
 // fp32 for attn_dkv_join.
 // again: LDS is in use.  CUT: queries of the tiles that a mask cuts one by one

@@ -16,12 +16,12 @@
 // and keys many the keys are cut into parts; each part leaves its M, l and
 // unnormalised sums in fp32, and a second launch joins them in order.
 //
-// 64 features, causal, 2 x 8192 tokens, 8 heads: 169 us, 815 TFLOP/s of the visible
-// pairs; 128 features, up to 4096 tokens, 16 heads over 4: 166 us, 840 TFLOP/s.
-// Bound there by the exponentials and the other vector work of the weights (per
+// 64 features, causal, 2 x 8192 tokens, 8 heads: 168 us, 818 TFLOP/s of the visible
+// pairs; 128 features, up to 4096 tokens, 16 heads over 4: 168 us, 830 TFLOP/s, MFMAs
+// busy 39% of the time.  Bound there by the exponentials and the other vector work of the weights (per
 // 64 keys and 32 rows 130 instructions and 32 exponentials beside 16 or 32
 // products), of which half runs beside the products of another wave.  256 x 257
-// tokens, 16 heads of 64: 201 us, 543 MB at 2.7 TB/s: the 257th row and key cost a
+// tokens, 16 heads of 64: 204 us, 543 MB at 2.7 TB/s: the 257th row and key cost a
 // third row tile and a fifth key tile.  One token each of 64 sequences over up to
 // 8192 keys, 32 heads of 128 over 8: 224 us, 4.9 TB/s, the rate of a large copy.
 #include "attn.hpp"
@@ -326,7 +326,11 @@ void launch_one(const AttnArgs& a, const AttnFwdPlan& p, uint16_t* out, int64_t 
 // Rows of a sequence's group of heads, the waves of a workgroup, and the parts of
 // the keys.  Sequences of at most 128 rows run one wave to a workgroup: their
 // waves need not wait for one another, and short ones leave no wave idle (1024
-// captions of up to 77 tokens, 8 heads of 64: 24 us, four waves 42).  Keys are cut
+// captions of up to 77 tokens, 8 heads of 64: 25 us, four waves 42).  Near the edge
+// it is the rows in the last tile that decide (32768 tokens in equal lengths, 8 heads
+// of 64, causal, forward and backward, one wave | four: 64 rows 32 + 95 | 34 + 95 us,
+// 96 rows 31 + 92 | 34 + 101, 128 rows 36 + 105 | 32 + 100, 160 rows 33 + 99 | 38 + 138,
+// 256 rows 41 + 117 | 36 + 118).  Keys are cut
 // where there are fewer workgroups than two waves for every SIMD (one token over
 // 777 keys, 8 heads of 64: 12 us with the join, 18 uncut; 64 over up to 8192, 8 key
 // heads of 128: 219 and 264).  Tiles of 64 keys for four waves: 2 x 8192 tokens,

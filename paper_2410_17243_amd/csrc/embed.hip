@@ -13,7 +13,7 @@
 // or 64 sorted positions, joined in order.
 //
 // 524288 tokens, 512 features of bf16, vocabulary 50000: forward 147 us (4.0 TB/s of
-// the 588 MB), sort 53 us in five launches, sums 140 us (638 MB at 4.6 TB/s), joins 15
+// the 588 MB), sort 54 us in five launches, sums 140 us (638 MB at 4.6 TB/s), joins 15
 // us (the parts of the two tokens that every caption has are a chain each).  2001
 // tokens, 512 features of fp32, vocabulary 8192: 4 + 11 + 8 + 4 us, launches and the
 // latency of dependent reads.
