@@ -62,7 +62,8 @@ infcl_status infcl_embed_bwd(const void* tokens, int token_bytes, int64_t n, con
  * from cu_q[nseq] (cu_k[nseq]) to the end of the arrays count as such queries
  * (keys that no one sees): their outputs and gradients are zeros.  What a masked
  * key, value, query or dout row holds reaches no one, infinities and NaN included;
- * those that are seen propagate.
+ * those that are seen propagate (a query whose scores are all -infinity has no
+ * weights: out and lse are NaN).
  * dtype is INFCL_BF16 or INFCL_F16 (MFMA products accumulated in fp32, softmax in
  * fp32, its weights rounded to dtype for the products with v, dout, q and k);
  * head_dim is a multiple of 8 up to 128 (built for 64 and 128), scale > 0.

@@ -34,7 +34,7 @@ constexpr float kSlack = 8.f;  // log2 of how far scores may pass the running ma
 // What a part of the keys leaves, for row id token * heads + head.
 struct AttnParts {
   float* o;   // [parts][rows][hd]
-  float* ml;  // [parts][rows][2]: M scale log2(e), l
+  float* ml;  // [parts][rows][2]: M scale log2(e), l (-1: sees keys, all of score -infinity)
   int64_t rows;
 };
 
@@ -213,8 +213,12 @@ __device__ __forceinline__ bool attn_fwd_tile(const AttnArgs& a, uint16_t* __res
         if (d < a.hd)
           *(f32x4*)(po + d) = f32x4{acc[fb][4 * j], acc[fb][4 * j + 1], acc[fb][4 * j + 2], acc[fb][4 * j + 3]};
       }
-    if (h == 0) ml[0] = l > 0.f || l != l ? M * a.sl2 : -__builtin_inff(), ml[1] = l;
+    if (h == 0) {
+      ml[0] = l > 0.f || l != l ? M * a.sl2 : -__builtin_inff();
+      ml[1] = l == 0.f && lim > kbeg && kstop > kbeg ? -1.f : l;
+    }
   } else {
+    if (l == 0.f && lim > 0) l = __builtin_nanf("");  // (scores of -infinity only: no weights)
     const float inv = l == 0.f ? 0.f : 1.f / l;
     attn_store<F16>(out + token * os + head * oh, acc, inv, h, a.hd);
     if (lse && h == 0) lse[(int64_t)head * a.tq + token] = l == 0.f ? -__builtin_inff() : fmaf(M, a.scale, logf(l));
@@ -284,11 +288,13 @@ __global__ void __launch_bounds__(256) attn_join(AttnParts pw, int parts, int he
     float M = -__builtin_inff();
     for (int p = 0; p < parts; ++p) M = fmaxf(M, pw.ml[((int64_t)p * pw.rows + i) * 2]);
     float l = 0.f;
+    bool none = true;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int p = 0; p < parts; ++p) {
       const float* ml = pw.ml + ((int64_t)p * pw.rows + i) * 2;
-      if (ml[1] == 0.f) continue;  // (sees nothing of this part)
+      none = none && ml[1] == 0.f;  // (sees nothing of this part)
+      if (ml[1] <= 0.f) continue;
       const float f = exp2_hw(ml[0] - M);
       l = fmaf(ml[1], f, l);
       if (d < hd) {
@@ -297,6 +303,7 @@ __global__ void __launch_bounds__(256) attn_join(AttnParts pw, int parts, int he
         for (int e = 0; e < 4; ++e) o[e] = fmaf(x[e], f, o[e]);
       }
     }
+    if (l == 0.f && !none) l = __builtin_nanf("");
     const int64_t token = i / heads;
     const int head = (int)(i % heads);
     const float inv = l == 0.f ? 0.f : 1.f / l;

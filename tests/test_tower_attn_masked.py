@@ -182,3 +182,29 @@ def test_a_step_that_overflowed_takes_about_as_long():
     clean, one = time(do), do.clone()
     one[length // 2] = math.inf
     assert time(one) < 100 * clean and time(torch.full_like(do, math.nan)) < 100 * clean
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,heads,kv,hd", [(5, 2, 1, 64), (200, 2, 2, 128), (3000, 4, 1, 64)])
+def test_scores_of_minus_infinity(n, heads, kv, hd):
+    """Keys whose scores are all -infinity weigh nothing beside others; a query that
+    sees no others has no weights at all: NaN, not the zeros of a query that sees no
+    key."""
+    g = torch.Generator().manual_seed(n)
+    q, k, v = (torch.rand((n, h, hd), generator=g).bfloat16() + 0.5 for h in (heads, kv, kv))
+    k[:n // 3] = -math.inf  # (q is positive)
+    a, cu = [x.cuda() for x in (q, k, v)], _dev([0, n])
+    first = n // 3
+    out, lse = infcl.packed_attn_fwd(*a, cu, n)
+    assert torch.isnan(out[:first]).all() and torch.isnan(lse[:, :first]).all()
+    r = tower.attention(q[first:], k[first:], v[first:], [0, n - first], [0, n - first], True, hd ** -0.5)
+    _near(out[first:], r["out"], _tol(r, "out", EPS["bf16"], "bf16"), "out")
+    # one query over all the keys (in parts where there are many), over the first third, over none
+    for keys, want in ((n, 0), (first, math.nan), (0, 0)):
+        one, lse = infcl.packed_attn_fwd(a[0][-1:], a[1], a[2], _dev([0, 1]), 1, _dev([0, keys]), keys)
+        if want != want:
+            assert torch.isnan(one).all() and torch.isnan(lse).all()
+        elif keys:
+            assert (one[0].double() - out[-1].double()).abs().max() <= 4 * EPS["bf16"] * 1.5
+        else:
+            assert (one == 0).all() and (lse == -math.inf).all()
