@@ -350,14 +350,6 @@ __device__ __forceinline__ bool attn_dkv_tile(const AttnArgs& a, const AttnGrads
   f32x16 dk[kFb], dv[kFb];
   if (again) attn_barrier();
   const INFCL_LDS char* vown = lds + 4 * Tile::kBytes + wave * 32 * Tile::kRow;
-  if constexpr (kVLds) {
-    uint32_t off[Own::kVar];
-    Own::offsets(off, wave, lane, (uint32_t)(a.vs * 2), a.hd);
-    Own::issue(a.v + (sq.k0 + key0) * a.vs + kv * a.vh, sq.n - key0, (uint32_t)(a.vs * 2), a.hd,
-               lds + 4 * Tile::kBytes, off, wave);
-  }
-#pragma unroll
-  for (int fb = 0; fb < kFb; ++fb) dk[fb] = f32x16_zero(), dv[fb] = f32x16_zero();
   // this part's tiles [c0, c1): tile c is head c % group of queries qbeg + QT (per - 1 - c / group) on
   const int per = sq.m > qbeg ? (sq.m - qbeg + QT - 1) / QT : 0;
   int64_t c0 = 0, c1 = (int64_t)per * a.group;
@@ -366,6 +358,15 @@ __device__ __forceinline__ bool attn_dkv_tile(const AttnArgs& a, const AttnGrads
     c0 = share * part < c1 ? share * part : c1;
     c1 = c0 + share < c1 ? c0 + share : c1;
   }
+  if constexpr (kVLds) {
+    uint32_t off[Own::kVar];
+    Own::offsets(off, wave, lane, (uint32_t)(a.vs * 2), a.hd);
+    if (c0 < c1)  // (the first tile's barrier waits for them)
+      Own::issue(a.v + (sq.k0 + key0) * a.vs + kv * a.vh, sq.n - key0, (uint32_t)(a.vs * 2), a.hd,
+                 lds + 4 * Tile::kBytes, off, wave);
+  }
+#pragma unroll
+  for (int fb = 0; fb < kFb; ++fb) dk[fb] = f32x16_zero(), dv[fb] = f32x16_zero();
   // the lanes fetch a tile's 32 pairs a tile ahead
   const float* row = w.stat + sq.q0 * 2;
   float ahead = 0.f;

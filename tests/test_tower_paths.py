@@ -128,3 +128,12 @@ def test_weight_gradient_with_large_tiles(n, d, m, dtype, act, grad, parts):
     assert dw.dtype == DT[grad] and ((dw.cpu().double() - ref).abs() <= tol).all()
     again = infcl.ckpt8_wgrad(dy.cuda(), kept, act, DT[grad])
     assert torch.equal(dw, again)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens_q,lens_k", [([0, 200, 0, 150], [300, 200, 129, 150]), ([10, 0, 700], [700, 900, 700])])
+def test_keys_that_no_query_sweeps(lens_q, lens_k, causal):
+    """Heads of 128 features whose own values are copied to LDS: sequences of keys alone,
+    and parts that get no tile, copy nothing that is waited for by no one."""
+    _attention(lens_q, lens_k, 4, 2, 128, "bf16", causal, (max(lens_q), max(lens_k)))
