@@ -28,6 +28,7 @@ LIB_PATH = os.path.join(_PKG, "libinfcl.so")
 HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "infcl.h")
 ABLATION_HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "infcl_ablation.h")
 TOWER_HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "infcl_tower.h")
+BLOCK_HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "infcl_block.h")
 
 INFCL_OK, INFCL_ERR_INVALID, INFCL_ERR_UNSUPPORTED, INFCL_ERR_WORKSPACE, INFCL_ERR_HIP = range(5)
 INFCL_BF16, INFCL_F32, INFCL_F16 = 0, 1, 2
@@ -354,10 +355,19 @@ def clip_loss(img, txt, scale):
 _TOWER = ("embed", "embed_fwd", "embed_bwd", "Ckpt8", "ckpt8_pack", "ckpt8_unpack", "ckpt8_act_fwd", "ckpt8_act_bwd",
           "ckpt8_wgrad", "linear8", "mlp8", "packed_attn", "packed_attn_qkv", "packed_attn_fwd", "packed_attn_bwd")
 
+# And those around a block's attention (block.py).
+_BLOCK = ("rotary", "rotary_fwd", "rotary_bwd", "rotary_freqs", "dropout", "dropout_fwd", "dropout_bwd", "add_norm",
+          "add_norm_fwd", "add_norm_bwd", "AddNormKept", "Fp8", "fp8_pack", "fp8_pack_both", "fp8_unpack", "fp8_matmul",
+          "linear_fp8", "linear_fp8_fwd", "linear_fp8_bwd")
+
 
 def __getattr__(name):
     if name in _TOWER:
         from . import tower
 
         return getattr(tower, name)
+    if name in _BLOCK:
+        from . import block
+
+        return getattr(block, name)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

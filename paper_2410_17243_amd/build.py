@@ -24,7 +24,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libinfcl.so")
 SOURCES = ["api.hip", "fwd.hip", "fwd2.hip", "bwd.hip", "bwd_wide.hip", "bwd_f32.hip", "ablation.hip",
-           "embed.hip", "ckpt8.hip", "wgrad.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_api.hip"]
+           "embed.hip", "ckpt8.hip", "wgrad.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_api.hip",
+           "rotary.hip", "dropout.hip", "add_norm.hip", "fp8.hip", "fp8_gemm.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

@@ -1,0 +1,479 @@
+// A block's output normed, dropped out, gated and added to the residual rows, and
+// the norm of the sum:
+//   t = gate D(N(y) post_w + post_b),  h = alpha x + t,  z = N(h) pre_w + pre_b
+// and all gradients in one pass over x, y, dh and dz.
+//
+// With v = N(y), r1 its factor, k = N(h), r2 its factor, D = 0 or 1 / (1 - p), and for
+// a norm's rows <.> the mean over features (second terms: layer norms only):
+//   g = dz pre_w,  e = dh + r2 (g - k <g k> - <g>)
+//   dx = alpha e,  s = e gate D,  q = s post_w,  dy = r1 (q - v <q v> - <q>)
+//   dpre_w = sum dz k, dpre_b = sum dz, dgate = sum e D (v post_w + post_b),
+//   dpost_w = sum s v, dpost_b = sum s
+//
+// A row is 8 features in each of up to 1024 lanes: a group of 8 to 64 lanes of one
+// wave, or several waves.  It stays in registers from its load to its last use, so the
+// variance is that of the centred row and the backward reads each input once; h is
+// taken again from x and y there (as many bytes as reading it back, and not rounded).
+// What a lane adds up for its features over all its rows are 40 registers at most, then
+// one row of partial sums for each workgroup, joined in order by a second launch.
+// Bound by the rows' bytes.
+#include "block.hpp"
+
+namespace infcl {
+namespace {
+
+struct NormArgs {
+  const void *x, *y, *gate, *post_w, *post_b, *pre_w, *pre_b, *dh, *dz;
+  void *h, *z, *dx, *dy;
+  float4* stats;
+  float* part;  // [workgroups][sums][d]
+  int64_t n, xs, ys, dhs, dzs;
+  int c, ls;  // chunks of a row; log2 of the lanes of a row within a wave
+  int rms, wf32;
+  int want_gate, want_post, want_post_b, want_pre, want_pre_b;  // sums that are taken, in this order
+  float eps, alpha, by_d;
+  Drop drop;
+};
+
+// Sums over a row of K values of each lane: over its group of lanes, or over all waves
+// of the workgroup (WAVES > 0) through one of two buffers in turn, so that one barrier
+// does for each.
+template <int WIDE, int K>
+__device__ __forceinline__ void row_sums(float (&s)[K], int ls, float (*buf)[16][2], int& turn) {
+#pragma unroll
+  for (int i = 0; i < K; ++i) s[i] = group_sum(s[i], ls);
+  if constexpr (WIDE) {
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int i = 0; i < K; ++i) buf[turn][wave][i] = s[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < K; ++i) s[i] = 0.f;
+    for (int w = 0; w < waves; ++w)
+#pragma unroll
+      for (int i = 0; i < K; ++i) s[i] += buf[turn][w][i];
+    turn ^= 1;
+  }
+}
+
+// N(t): the mean and factor of the row, t becomes the normed row.  Lanes past the row
+// (`in` false) hold zeros before and after.
+template <int WIDE>
+__device__ __forceinline__ void norm_row(float (&t)[8], bool in, const NormArgs& a, float& mean, float& r,
+                                         float (*buf)[16][2], int& turn) {
+  mean = 0.f;
+  if (!a.rms) {
+    float s[1] = {0.f};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[0] += t[e];
+    row_sums<WIDE, 1>(s, a.ls, buf, turn);
+    mean = s[0] * a.by_d;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] = in ? t[e] - mean : 0.f;
+  }
+  float s[1] = {0.f};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s[0] += t[e] * t[e];
+  row_sums<WIDE, 1>(s, a.ls, buf, turn);
+  r = 1.f / sqrtf(s[0] * a.by_d + a.eps);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) t[e] *= r;
+}
+
+// A lane's place: its row of the launch's first sweep, the step between rows, its chunk.
+template <int WIDE>
+__device__ __forceinline__ void place(const NormArgs& a, int64_t& row, int64_t& step, int& chunk) {
+  if constexpr (WIDE) {
+    row = blockIdx.x, step = gridDim.x, chunk = threadIdx.x;
+  } else {
+    const int g = threadIdx.x >> a.ls, groups = (int)blockDim.x >> a.ls;
+    row = (int64_t)blockIdx.x * groups + g, step = (int64_t)gridDim.x * groups;
+    chunk = threadIdx.x & ((1 << a.ls) - 1);
+  }
+}
+
+template <int T, int WIDE>
+__global__ void __launch_bounds__(WIDE ? 1024 : 256) norm_fwd(const NormArgs a) {
+  __shared__ float buf[2][16][2];
+  int64_t row, step;
+  int chunk, turn = 0;
+  place<WIDE>(a, row, step, chunk);
+  const bool in = chunk < a.c;
+  const int64_t col = 8 * (int64_t)chunk;
+  float gate[8], w1[8], b1[8], w2[8], b2[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) gate[e] = w1[e] = w2[e] = 1.f, b1[e] = b2[e] = 0.f;
+  if (in) {
+    if (a.gate) load8_or_f32<T>(a.gate, col, a.wf32, gate);
+    if (a.post_w) load8_or_f32<T>(a.post_w, col, a.wf32, w1);
+    if (a.post_b) load8_or_f32<T>(a.post_b, col, a.wf32, b1);
+    if (a.pre_w) load8_or_f32<T>(a.pre_w, col, a.wf32, w2);
+    if (a.pre_b) load8_or_f32<T>(a.pre_b, col, a.wf32, b2);
+  }
+  const uint64_t seed = a.drop.cut ? a.drop.the_seed() : 0;
+  for (; row < a.n; row += step) {
+    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, t[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (in) load8<T>(a.x, row * a.xs + col, x);
+    float m1 = 0.f, r1 = 0.f, m2 = 0.f, r2 = 0.f;
+    if (a.y) {
+      if (in) load8<T>(a.y, row * a.ys + col, t);
+      if (a.post_w) {
+        norm_row<WIDE>(t, in, a, m1, r1, buf, turn);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = fmaf(t[e], w1[e], b1[e]);
+      }
+      if (a.drop.cut) {
+        const Random128 u = philox(a.drop.first + (uint64_t)row * a.c + chunk, a.drop.site, seed);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = u.bits16(e) >= a.drop.cut ? t[e] * a.drop.unit : 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = fmaf(a.alpha, x[e], gate[e] * t[e]);
+      if (in) store8<T>(a.h, row * (8 * (int64_t)a.c) + col, x);
+    }
+    if (a.pre_w) {
+      if (!in)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.f;
+      norm_row<WIDE>(x, in, a, m2, r2, buf, turn);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], w2[e], b2[e]);
+      if (in) store8<T>(a.z, row * (8 * (int64_t)a.c) + col, x);
+    }
+    if (a.stats && chunk == 0) a.stats[row] = make_float4(m1, r1, m2, r2);
+  }
+}
+
+template <int T, int WIDE>
+__global__ void __launch_bounds__(WIDE ? 1024 : 256) norm_bwd(const NormArgs a) {
+  __shared__ float buf[2][16][2];
+  __shared__ float joined[WIDE ? 1 : 4][WIDE ? 1 : 512];
+  int64_t row, step;
+  int chunk, turn = 0;
+  place<WIDE>(a, row, step, chunk);
+  const bool in = chunk < a.c;
+  const int64_t col = 8 * (int64_t)chunk;
+  float gate[8], w1[8], b1[8], w2[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) gate[e] = w1[e] = w2[e] = 1.f, b1[e] = 0.f;
+  if (in) {
+    if (a.gate) load8_or_f32<T>(a.gate, col, a.wf32, gate);
+    if (a.post_w) load8_or_f32<T>(a.post_w, col, a.wf32, w1);
+    if (a.post_b) load8_or_f32<T>(a.post_b, col, a.wf32, b1);
+    if (a.pre_w) load8_or_f32<T>(a.pre_w, col, a.wf32, w2);
+  }
+  float sg[8], sw1[8], sb1[8], sw2[8], sb2[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sg[e] = sw1[e] = sb1[e] = sw2[e] = sb2[e] = 0.f;
+  const uint64_t seed = a.drop.cut ? a.drop.the_seed() : 0;
+  for (; row < a.n; row += step) {
+    float h[8] = {0, 0, 0, 0, 0, 0, 0, 0}, v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, e8[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    float g[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const float4 st = a.stats[row];
+    if (in) {
+      load8<T>(a.x, row * a.xs + col, h);
+      if (a.y) load8<T>(a.y, row * a.ys + col, v);
+      if (a.dh) load8<T>(a.dh, row * a.dhs + col, e8);
+      if (a.dz) load8<T>(a.dz, row * a.dzs + col, g);
+    }
+    Random128 u;
+    if (a.drop.cut) u = philox(a.drop.first + (uint64_t)row * a.c + chunk, a.drop.site, seed);
+    float t[8];  // what the gate took
+    if (a.y) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        t[e] = v[e];
+        if (a.post_w) {
+          v[e] = in ? (v[e] - st.x) * st.y : 0.f;
+          t[e] = fmaf(v[e], w1[e], b1[e]);
+        }
+        if (a.drop.cut) t[e] = u.bits16(e) >= a.drop.cut ? t[e] * a.drop.unit : 0.f;
+        h[e] = fmaf(a.alpha, h[e], gate[e] * t[e]);
+      }
+    }
+    if (a.pre_w) {
+      float s[2] = {0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        h[e] = in ? (h[e] - st.z) * st.w : 0.f;
+        sw2[e] = fmaf(g[e], h[e], sw2[e]);
+        sb2[e] += g[e];
+        g[e] *= w2[e];
+        s[0] += g[e], s[1] = fmaf(g[e], h[e], s[1]);
+      }
+      row_sums<WIDE, 2>(s, a.ls, buf, turn);
+      const float m = a.rms ? 0.f : s[0] * a.by_d, k = s[1] * a.by_d;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) e8[e] += in ? st.w * (g[e] - m - h[e] * k) : 0.f;
+    }
+    if (a.dx && in) {
+      float o[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = a.alpha * e8[e];
+      store8<T>(a.dx, row * (8 * (int64_t)a.c) + col, o);
+    }
+    if (!a.y) continue;
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      sg[e] = fmaf(e8[e], t[e], sg[e]);
+      float q = e8[e] * gate[e];
+      if (a.drop.cut) q = u.bits16(e) >= a.drop.cut ? q * a.drop.unit : 0.f;
+      if (a.post_w) {
+        sw1[e] = fmaf(q, v[e], sw1[e]);
+        sb1[e] += q;
+        q *= w1[e];
+        s[0] += q, s[1] = fmaf(q, v[e], s[1]);
+      }
+      e8[e] = q;
+    }
+    if (a.post_w) {
+      row_sums<WIDE, 2>(s, a.ls, buf, turn);
+      const float m = a.rms ? 0.f : s[0] * a.by_d, k = s[1] * a.by_d;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) e8[e] = st.y * (e8[e] - m - v[e] * k);
+    }
+    if (a.dy && in) store8<T>(a.dy, row * (8 * (int64_t)a.c) + col, e8);
+  }
+
+  // One row of sums of the workgroup: groups of a wave, then waves, in order.
+  const int d = 8 * a.c;
+  float* part = a.part;
+  int k = 0;
+  const int sums = a.want_gate + a.want_post + a.want_post_b + a.want_pre + a.want_pre_b;
+  auto put = [&](float (&s)[8]) {
+    float* to = part + ((int64_t)blockIdx.x * sums + k++) * d;
+    if constexpr (WIDE) {
+      if (in) store8<kF32>(to, col, s);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float p, q;
+        if (a.ls < 4) s[e] += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(s[e]), 0x128, 0xF, 0xF, true));  // row_ror 8
+        if (a.ls < 5) both16(s[e], p, q), s[e] = p + q;
+        if (a.ls < 6) both32(s[e], p, q), s[e] = p + q;
+      }
+      const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+      __syncthreads();
+      if (lane < 1 << a.ls)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) joined[wave][64 * e + lane] = s[e];
+      __syncthreads();
+      for (int i = threadIdx.x; i < d; i += 256) {
+        const int at = 64 * (i & 7) + (i >> 3);
+        to[i] = joined[0][at] + joined[1][at] + joined[2][at] + joined[3][at];
+      }
+    }
+  };
+  if (a.want_gate) put(sg);
+  if (a.want_post) put(sw1);
+  if (a.want_post_b) put(sb1);
+  if (a.want_pre) put(sw2);
+  if (a.want_pre_b) put(sb2);
+}
+
+// Sums of parts [parts][sums][d] in a fixed order: 32 columns of one vector for each
+// workgroup, 16 slices of the parts, joined through LDS.
+template <int T>
+__global__ void __launch_bounds__(512) norm_join(const float* __restrict__ part, int parts, int sums, int d, int wf32,
+                                                 void* o0, void* o1, void* o2, void* o3, void* o4) {
+  __shared__ float lds[16][33];
+  const int cols = (d + 31) / 32, k = blockIdx.x / cols, col = (blockIdx.x - k * cols) * 32 + (threadIdx.x & 31);
+  const int slice = threadIdx.x >> 5;
+  float s = 0.f;
+  if (col < d) {
+    const float* p = part + (int64_t)k * d + col;
+    const int64_t row = (int64_t)sums * d;
+    int i = slice;
+    for (; i + 16 * 7 < parts; i += 16 * 8) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = p[(i + 16 * j) * row];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s += v[j];
+    }
+    for (; i < parts; i += 16) s += p[i * row];
+  }
+  lds[slice][threadIdx.x & 31] = s;
+  __syncthreads();
+  if (slice == 0 && col < d) {
+    float t = 0.f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) t += lds[j][threadIdx.x];
+    void* const to = k == 0 ? o0 : k == 1 ? o1 : k == 2 ? o2 : k == 3 ? o3 : o4;
+    if (T == kF32 || wf32)
+      ((float*)to)[col] = t;
+    else if constexpr (T == kF16)
+      ((_Float16*)to)[col] = (_Float16)t;
+    else
+      ((__bf16*)to)[col] = (__bf16)t;
+  }
+}
+
+struct Shape {
+  bool wide;
+  unsigned threads;
+  int ls;
+  int64_t groups;  // rows of a workgroup at a time
+};
+Shape shape_of(int64_t d) {
+  Shape s;
+  const int c = (int)(d / 8);
+  s.wide = c > 64;
+  s.threads = s.wide ? (unsigned)((c + 63) / 64 * 64) : 256;
+  s.ls = s.wide ? 6 : row_lanes_log2(c, 8);
+  s.groups = s.wide ? 1 : 256 >> s.ls;
+  return s;
+}
+// Workgroups: what covers the rows, at most some waves for each SIMD.
+unsigned grid_of(const Shape& s, int64_t n, int64_t waves) {
+  const int64_t need = (n + s.groups - 1) / s.groups, most = 1024 * waves / (s.threads / 64);
+  return (unsigned)(need < most ? need : most);
+}
+constexpr int kFwdWaves = 8, kBwdWaves = 4;
+
+infcl_status check(const infcl_add_norm* a) {
+  if (!a || a->n < 0 || a->d < 1 || !type_known(a->dtype) || !type_known(a->wdtype) ||
+      (a->norm != INFCL_NORM_LAYER && a->norm != INFCL_NORM_RMS) || !(a->eps >= 0.f) || a->eps > 3e38f ||
+      !(a->alpha >= -3e38f && a->alpha <= 3e38f) || !drop_ok(a->drop) || a->x_stride < a->d ||
+      (a->post_b && !a->post_w) || (a->pre_b && !a->pre_w))
+    return INFCL_ERR_INVALID;
+  if (a->d % 8 != 0 || a->d > 8192 || a->x_stride % 8 != 0 || a->n > ((int64_t)1 << 40) / a->d ||
+      a->x_stride > ((int64_t)1 << 32) || (a->wdtype != INFCL_F32 && a->wdtype != a->dtype) ||
+      a->drop.row0 > ((int64_t)1 << 62) / a->d)
+    return INFCL_ERR_UNSUPPORTED;
+  return INFCL_OK;
+}
+// The vectors and y of a call that has rows.
+infcl_status check_rows(const infcl_add_norm* a, const void* x, const void* y) {
+  const void* w[5] = {a->gate, a->post_w, a->post_b, a->pre_w, a->pre_b};
+  for (const void* p : w)
+    if (p && ((uintptr_t)p % 16) != 0) return INFCL_ERR_INVALID;
+  if (!y && (a->gate || a->post_w || a->drop.p > 0.f || a->alpha != 1.f || !a->pre_w)) return INFCL_ERR_INVALID;
+  if (y && a->y_stride < a->d) return INFCL_ERR_INVALID;
+  if (y && (a->y_stride % 8 != 0 || a->y_stride > ((int64_t)1 << 32))) return INFCL_ERR_UNSUPPORTED;
+  if (a->n > 0 && (!block_aligned(x, 16) || ((uintptr_t)y % 16) != 0)) return INFCL_ERR_INVALID;
+  return INFCL_OK;
+}
+NormArgs args_of(const infcl_add_norm* a, const Shape& s, const void* x, const void* y) {
+  NormArgs r = {};
+  r.x = x, r.y = y, r.gate = a->gate, r.post_w = a->post_w, r.post_b = a->post_b, r.pre_w = a->pre_w, r.pre_b = a->pre_b;
+  r.n = a->n, r.xs = a->x_stride, r.ys = a->y_stride, r.c = (int)(a->d / 8), r.ls = s.ls;
+  r.rms = a->norm == INFCL_NORM_RMS, r.wf32 = a->wdtype == INFCL_F32, r.eps = a->eps, r.alpha = a->alpha;
+  r.by_d = 1.f / (float)a->d;
+  r.drop = drop_of(a->drop, a->d);
+  return r;
+}
+
+template <int T>
+void fwd_t(const NormArgs& r, const Shape& s, hipStream_t st) {
+  const dim3 grid(grid_of(s, r.n, kFwdWaves)), block(s.threads);
+  if (s.wide)
+    hipLaunchKernelGGL((norm_fwd<T, 1>), grid, block, 0, st, r);
+  else
+    hipLaunchKernelGGL((norm_fwd<T, 0>), grid, block, 0, st, r);
+}
+template <int T>
+void bwd_t(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
+  if (s.wide)
+    hipLaunchKernelGGL((norm_bwd<T, 1>), dim3(wgs), dim3(s.threads), 0, st, r);
+  else
+    hipLaunchKernelGGL((norm_bwd<T, 0>), dim3(wgs), dim3(s.threads), 0, st, r);
+}
+template <int T>
+void join_t(const NormArgs& r, unsigned wgs, int sums, void* const* o, hipStream_t st) {
+  const int d = 8 * r.c;
+  hipLaunchKernelGGL((norm_join<T>), dim3((unsigned)(sums * ((d + 31) / 32))), dim3(512), 0, st, r.part, (int)wgs, sums, d,
+                     r.wf32, o[0], o[1], o[2], o[3], o[4]);
+}
+
+}  // namespace
+}  // namespace infcl
+
+using namespace infcl;
+
+extern "C" infcl_status infcl_add_norm_fwd(const infcl_add_norm* a, const void* x, const void* y, void* h, void* z,
+                                           float* stats, void* stream) {
+  infcl_status s = check(a);
+  if (s == INFCL_OK) s = check_rows(a, x, y);
+  if (s != INFCL_OK || a->n == 0) return s;
+  if ((y && !block_aligned(h, 16)) || (a->pre_w && !block_aligned(z, 16)) || ((uintptr_t)stats % 16) != 0)
+    return INFCL_ERR_INVALID;
+  const Shape sh = shape_of(a->d);
+  NormArgs r = args_of(a, sh, x, y);
+  r.h = h, r.z = z, r.stats = (float4*)stats;
+  hipStream_t st = (hipStream_t)stream;
+  if (a->dtype == INFCL_BF16)
+    fwd_t<kBF16>(r, sh, st);
+  else if (a->dtype == INFCL_F16)
+    fwd_t<kF16>(r, sh, st);
+  else
+    fwd_t<kF32>(r, sh, st);
+  return launch_status();
+}
+
+extern "C" infcl_status infcl_add_norm_bwd_workspace(const infcl_add_norm* a, size_t* bytes) {
+  const infcl_status s = check(a);
+  if (s != INFCL_OK) return s;
+  if (!bytes) return INFCL_ERR_INVALID;
+  const Shape sh = shape_of(a->d);
+  const size_t n = (size_t)grid_of(sh, a->n, kBwdWaves) * 5 * (size_t)a->d * 4;
+  *bytes = n < 256 ? 256 : (n + 255) & ~(size_t)255;
+  return INFCL_OK;
+}
+
+extern "C" infcl_status infcl_add_norm_bwd(const infcl_add_norm* a, const void* x, const void* y, const float* stats,
+                                           const infcl_add_norm_grads* g, void* workspace, size_t ws_bytes,
+                                           void* stream) {
+  infcl_status s = check(a);
+  if (s == INFCL_OK) s = check_rows(a, x, y);
+  if (s != INFCL_OK) return s;
+  if (!g || (g->dh && g->dh_stride < a->d) || (g->dz && (g->dz_stride < a->d || !a->pre_w)) || (g->dy && !y) ||
+      (g->dgate && !a->gate) || (g->dpost_w && !a->post_w) || (g->dpost_b && !a->post_b) || (g->dpre_w && !a->pre_w) ||
+      (g->dpre_b && !a->pre_b))
+    return INFCL_ERR_INVALID;
+  if ((g->dh && (g->dh_stride % 8 != 0 || g->dh_stride > ((int64_t)1 << 32))) ||
+      (g->dz && (g->dz_stride % 8 != 0 || g->dz_stride > ((int64_t)1 << 32))))
+    return INFCL_ERR_UNSUPPORTED;
+  const void* p[9] = {g->dh, g->dz, g->dx, g->dy, g->dgate, g->dpost_w, g->dpost_b, g->dpre_w, g->dpre_b};
+  for (const void* q : p)
+    if (((uintptr_t)q % 16) != 0) return INFCL_ERR_INVALID;
+  if (!block_aligned(workspace, 256) || (a->n > 0 && !block_aligned(stats, 16))) return INFCL_ERR_INVALID;
+  size_t need = 0;
+  s = infcl_add_norm_bwd_workspace(a, &need);
+  if (s != INFCL_OK) return s;
+  if (ws_bytes < need) return INFCL_ERR_WORKSPACE;
+  const Shape sh = shape_of(a->d);
+  NormArgs r = args_of(a, sh, x, y);
+  r.stats = (float4*)stats, r.part = (float*)workspace;
+  r.dh = g->dh, r.dz = g->dz, r.dhs = g->dh_stride, r.dzs = g->dz_stride, r.dx = g->dx, r.dy = g->dy;
+  r.want_gate = g->dgate != nullptr, r.want_post = g->dpost_w != nullptr, r.want_post_b = g->dpost_b != nullptr;
+  r.want_pre = g->dpre_w != nullptr, r.want_pre_b = g->dpre_b != nullptr;
+  void* outs[5] = {nullptr, nullptr, nullptr, nullptr, nullptr};
+  int sums = 0;
+  for (void* o : {g->dgate, g->dpost_w, g->dpost_b, g->dpre_w, g->dpre_b})
+    if (o) outs[sums++] = o;
+  hipStream_t st = (hipStream_t)stream;
+  const unsigned wgs = grid_of(sh, a->n, kBwdWaves);
+  if (wgs > 0) {
+    if (a->dtype == INFCL_BF16)
+      bwd_t<kBF16>(r, sh, wgs, st);
+    else if (a->dtype == INFCL_F16)
+      bwd_t<kF16>(r, sh, wgs, st);
+    else
+      bwd_t<kF32>(r, sh, wgs, st);
+    s = launch_status();
+    if (s != INFCL_OK) return s;
+  }
+  if (sums > 0) {  // (no rows: zeros)
+    if (a->dtype == INFCL_BF16)
+      join_t<kBF16>(r, wgs, sums, outs, st);
+    else if (a->dtype == INFCL_F16)
+      join_t<kF16>(r, wgs, sums, outs, st);
+    else
+      join_t<kF32>(r, wgs, sums, outs, st);
+    return launch_status();
+  }
+  return INFCL_OK;
+}
