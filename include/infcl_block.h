@@ -50,7 +50,7 @@ typedef struct {
   int64_t n;
   int32_t heads, turned, head_dim, dtype, paired, back, axes, pos_dtype;
   int32_t sections[4];
-  int64_t pos_stride; /* elements, >= axes */
+  int64_t pos_stride; /* elements; 0: one position for all */
 } infcl_rotary_shape;
 
 infcl_status infcl_rotary(const infcl_rotary_shape* shape, infcl_attn_view x, infcl_attn_view out, const void* pos,

@@ -151,9 +151,7 @@ def _turn(x, pos, freqs, sections, turned, paired, back, name):
     out = torch.empty((n, heads, hd), dtype=x.dtype, device=dev)
     if out.numel() == 0:
         return out
-    stride = pos.stride(0) if n > 1 else axes
-    if stride < axes:
-        raise ValueError(f"pos must have a row for each token, got strides {pos.stride()}")
+    stride = pos.stride(0) if n > 1 else 0
     shape = _Rotary(n, heads, turned, hd, code, PAIRED[paired], back, axes, int(pos.dtype == torch.float32),
                     (_i32 * 4)(*sections), stride)
     _call("infcl_rotary", dev, ctypes.byref(shape), view, _View(out.data_ptr(), heads * hd, hd), pos.data_ptr(),

@@ -350,10 +350,11 @@ infcl_status check_rows(const infcl_add_norm* a, const void* x, const void* y) {
   const void* w[5] = {a->gate, a->post_w, a->post_b, a->pre_w, a->pre_b};
   for (const void* p : w)
     if (p && ((uintptr_t)p % 16) != 0) return INFCL_ERR_INVALID;
+  if (a->n == 0) return INFCL_OK;  // (rows have no addresses then)
   if (!y && (a->gate || a->post_w || a->drop.p > 0.f || a->alpha != 1.f || !a->pre_w)) return INFCL_ERR_INVALID;
   if (y && a->y_stride < a->d) return INFCL_ERR_INVALID;
   if (y && (a->y_stride % 8 != 0 || a->y_stride > ((int64_t)1 << 32))) return INFCL_ERR_UNSUPPORTED;
-  if (a->n > 0 && (!block_aligned(x, 16) || ((uintptr_t)y % 16) != 0)) return INFCL_ERR_INVALID;
+  if (!block_aligned(x, 16) || ((uintptr_t)y % 16) != 0) return INFCL_ERR_INVALID;
   return INFCL_OK;
 }
 NormArgs args_of(const infcl_add_norm* a, const Shape& s, const void* x, const void* y) {
@@ -429,7 +430,7 @@ extern "C" infcl_status infcl_add_norm_bwd(const infcl_add_norm* a, const void* 
   infcl_status s = check(a);
   if (s == INFCL_OK) s = check_rows(a, x, y);
   if (s != INFCL_OK) return s;
-  if (!g || (g->dh && g->dh_stride < a->d) || (g->dz && (g->dz_stride < a->d || !a->pre_w)) || (g->dy && !y) ||
+  if (!g || (g->dh && g->dh_stride < a->d) || (g->dz && (g->dz_stride < a->d || !a->pre_w)) || (g->dy && !y && a->n > 0) ||
       (g->dgate && !a->gate) || (g->dpost_w && !a->post_w) || (g->dpost_b && !a->post_b) || (g->dpre_w && !a->pre_w) ||
       (g->dpre_b && !a->pre_b))
     return INFCL_ERR_INVALID;

@@ -151,7 +151,7 @@ extern "C" infcl_status infcl_rotary(const infcl_rotary_shape* s, infcl_attn_vie
   if (!s || s->n < 0 || s->heads < 1 || s->turned < 0 || s->turned > s->heads || s->head_dim < 1 ||
       !type_known(s->dtype) || (s->paired != INFCL_PAIRED_HALVES && s->paired != INFCL_PAIRED_NEIGHBOURS) ||
       (s->back != 0 && s->back != 1) || s->axes < 1 || s->axes > 4 || (s->pos_dtype != 0 && s->pos_dtype != 1) ||
-      s->pos_stride < s->axes)
+      s->pos_stride < 0)
     return INFCL_ERR_INVALID;
   int64_t pairs = 0, ends[4] = {0, 0, 0, 0};
   for (int i = 0; i < 4; ++i) {

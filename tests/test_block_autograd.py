@@ -1,0 +1,181 @@
+"""The block operators' autograd functions as the graph sees them, without a GPU (the
+kernels' places are taken by torch products that leave no graph), and captured into a
+HIP graph on one."""
+
+import pytest
+import torch
+
+import paper_2410_17243_amd as infcl
+from oracle import block as oracle
+from paper_2410_17243_amd import block
+
+
+@pytest.fixture
+def plain_kernels(monkeypatch):
+    """Stand-ins that compute on the CPU."""
+    def turn(x, pos, freqs, sections=None, turned=None, paired="halves", back=False):
+        y = oracle.turned(x.detach(), pos[:, None], freqs, (freqs.numel(),), x.shape[1] if turned is None else turned,
+                          paired == "neighbours", back)[0]
+        return y.to(x.dtype)
+
+    def norm_fwd(x, y=None, gate=None, post_w=None, post_b=None, pre_w=None, pre_b=None, norm="layer", eps=1e-5, alpha=1.0,
+                 p=0.0, seed=0, site=0, row0=0, need_grad=True):
+        v = (gate, post_w, post_b, pre_w, pre_b)
+        t = [None if a is None else a.detach() for a in (x, y, *v)]
+        r = oracle.add_norm(*t, rms=norm == "rms", eps=eps, alpha=alpha)
+        h, z = r.get("h"), r.get("z")
+        return (x if h is None else h.to(x.dtype), None if z is None else z.to(x.dtype),
+                infcl.AddNormKept(x, y, v, torch.zeros((x.numel() // x.shape[-1], 4)), (norm, eps, alpha, p, seed, site, row0)))
+
+    def norm_bwd(dh, dz, kept, need=(True,) * 7):
+        t = [None if a is None else a.detach() for a in (kept.x, kept.y, *kept.vectors, dh, dz)]
+        r = oracle.add_norm(*t[:7], rms=kept.options[0] == "rms", eps=kept.options[1], alpha=kept.options[2], dh=t[7], dz=t[8])
+        args = (kept.x, kept.y, *kept.vectors)
+        return tuple(None if a is None or not n else r["d" + k].to(a.dtype) for a, n, k in
+                     zip(args, need, ("x", "y", "gate", "post_w", "post_b", "pre_w", "pre_b")))
+
+    def lin_fwd(x, w, b=None, need_dx=True, need_dw=True):
+        pack = lambda t: infcl.Fp8(t.detach().clone(), torch.zeros(1), t.shape[1], t.dtype)  # noqa: E731
+        y = torch.nn.functional.linear(x.detach(), w.detach(), None if b is None else b.detach())
+        return y, (pack(x) if need_dw else None, pack(w) if need_dx else None, b is not None)
+
+    def lin_bwd(dy, kept, need=(True, True, True)):
+        x, w, has_b = kept
+        d = dy.detach()
+        return (d @ w.q if need[0] and w else None, d.t() @ x.q if need[1] and x else None, d.sum(0) if need[2] and has_b else None)
+
+    for name, fn in {
+        "rotary_fwd": turn, "rotary_bwd": lambda d, *a: turn(d, *a, back=True),
+        "dropout_fwd": lambda x, p, *a: x.detach() * oracle.kept(*x.shape, p, *a).to(x.dtype),
+        "dropout_bwd": lambda x, p, *a: x.detach() * oracle.kept(*x.shape, p, *a).to(x.dtype),
+        "add_norm_fwd": norm_fwd, "add_norm_bwd": norm_bwd, "linear_fp8_fwd": lin_fwd, "linear_fp8_bwd": lin_bwd,
+    }.items():
+        monkeypatch.setattr(block, name, fn)
+
+
+def _call(name):
+    """(the function of its differentiable arguments, those arguments)."""
+    g = torch.Generator().manual_seed(3)
+    r = lambda *s: torch.randn(s, generator=g, dtype=torch.float64).requires_grad_()  # noqa: E731
+    pos, freqs = torch.tensor([0, 5, 9]), torch.tensor([1.0, 0.3, 0.1])
+    both = lambda *a: torch.cat([t for t in infcl.add_norm(*a, alpha=0.5) if t is not None])  # noqa: E731
+    return {
+        "rotary": (lambda x: infcl.rotary(x, pos, freqs, turned=1), [r(3, 2, 8)]),
+        "dropout": (lambda x: infcl.dropout(x, 0.25, 7, 2), [r(6, 8)]),
+        "add_norm": (both, [r(6, 8), r(6, 8), r(8), r(8), r(8), r(8), r(8)]),
+        "add_norm, no z": (both, [r(6, 8), r(6, 8), r(8)]),
+        "add_norm, no y": (lambda x, w, b: infcl.add_norm(x, pre_w=w, pre_b=b, norm="rms")[1], [r(6, 8), r(8), r(8)]),
+        "linear_fp8": (infcl.linear_fp8, [r(6, 8), r(16, 8), r(16)]),
+    }[name]
+
+
+NAMES = ["rotary", "dropout", "add_norm", "add_norm, no z", "add_norm, no y", "linear_fp8"]
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_gradients_by_differences(plain_kernels, name):
+    f, args = _call(name)
+    d = torch.randn(f(*args).shape, generator=torch.Generator().manual_seed(1), dtype=torch.float64)
+    got = torch.autograd.grad((f(*args) * d).sum(), args)
+    for i, a in enumerate(args):
+        for at in range(0, a.numel(), 5):
+            e = torch.zeros_like(a).detach()
+            e.view(-1)[at] = 1e-6
+            hi, lo = (float((f(*[t.detach() + s * e if j == i else t.detach() for j, t in enumerate(args)]) * d).sum()) for s in (1, -1))
+            assert abs((hi - lo) / 2e-6 - float(got[i].reshape(-1)[at])) < 1e-6, (i, at)
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_second_derivatives_are_refused(plain_kernels, name):
+    f, args = _call(name)
+    first = torch.autograd.grad(f(*args).square().sum(), args, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (args[0].square().sum() + sum(x.square().sum() for x in first)).backward()
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_only_what_is_asked_for_has_a_gradient(plain_kernels, name):
+    f, args = _call(name)
+    full = torch.autograd.grad(f(*args).sum(), args)
+    for i in range(len(args)):
+        some = [a.detach().requires_grad_(j == i) for j, a in enumerate(args)]
+        f(*some).sum().backward()
+        assert torch.equal(some[i].grad, full[i]) and all(a.grad is None for j, a in enumerate(some) if j != i)
+
+
+@pytest.mark.gpu
+def test_a_block_captured_into_a_graph():
+    """Forward and backward of a run of all of them, captured once and replayed with new
+    inputs and seeds between eager work: every replay gives what the eager calls give."""
+    n, heads, hd, d, m = 300, 6, 32, 64, 192
+    dt = torch.bfloat16
+    r = lambda *s: torch.randn(s, device="cuda").to(dt)  # noqa: E731
+    x, w, b, o, dq = r(n, d), r(m, d) / 8, r(m), r(d, m) / 14, r(n, heads, hd)
+    gate, pw, dh, dz = r(d), r(d), r(n, d), r(n, d)
+    pos, freqs = torch.arange(n, dtype=torch.int32, device="cuda"), infcl.rotary_freqs(16)
+    seed = torch.tensor([5], device="cuda")
+
+    def step():
+        q, kept = infcl.linear_fp8_fwd(x, w, b)
+        q = infcl.rotary_fwd(q.view(n, heads, hd), pos, freqs, turned=4)
+        t, kept_o = infcl.linear_fp8_fwd(q.view(n, m), o)
+        h, z, kept_n = infcl.add_norm_fwd(x, t, gate=gate, post_w=pw, pre_w=pw, norm="rms", p=0.2, seed=seed, site=1)
+        z = infcl.dropout_fwd(z, 0.1, seed)
+        dx, dt_, *dn = infcl.add_norm_bwd(dh, infcl.dropout_bwd(dz, 0.1, seed), kept_n)
+        dt_, do, _ = infcl.linear_fp8_bwd(dt_, kept_o)
+        dt_ = infcl.rotary_bwd(dt_.view(n, heads, hd), pos, freqs, turned=4)
+        return [h, z, dx, *[t for t in dn if t is not None], do, *infcl.linear_fp8_bwd(dt_.view(n, m), kept)]
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step()
+    seen = []
+    for rep in range(4):
+        x.copy_(r(n, d))
+        seed.fill_(rep)
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(got, want)), rep
+        seen.append(got[0])
+    assert not torch.equal(seen[0], seen[1])
+
+
+@pytest.mark.gpu
+def test_on_a_stream_of_its_own():
+    """Calls on another stream than the default one follow that stream's work."""
+    x, w = torch.randn((2000, 512), device="cuda"), torch.randn(512, device="cuda")
+    want = infcl.add_norm_fwd(x * 3, x, pre_w=w)[1]
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        y = x.clone()
+        for _ in range(20):
+            y = y * 1.0
+        z = infcl.add_norm_fwd(y * 3, y, pre_w=w)[1]
+    s.synchronize()
+    assert torch.equal(z, want)
+
+
+@pytest.mark.gpu
+def test_runs_repeat_bit_for_bit():
+    x, y, w = torch.randn((3001, 264), device="cuda").bfloat16(), torch.randn((3001, 264), device="cuda").bfloat16(), torch.randn(264, device="cuda")
+    lw = torch.randn((520, 264), device="cuda").bfloat16()
+    dy = torch.randn((3001, 520), device="cuda").bfloat16()
+
+    def once():
+        h, z, kept = infcl.add_norm_fwd(x, y, gate=w, pre_w=w, p=0.1, seed=1)
+        o, k = infcl.linear_fp8_fwd(z, lw)
+        return [h, z, o, *infcl.add_norm_bwd(h, z, kept), *infcl.linear_fp8_bwd(dy, k)]
+
+    first = once()
+    for _ in range(3):
+        assert all(a is None or torch.equal(a, b) for a, b in zip(once(), first))
