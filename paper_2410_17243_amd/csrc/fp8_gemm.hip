@@ -40,7 +40,7 @@ struct Tile {
   static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
   static constexpr int kCopies = kRows / 16 / kWaves;  // 16 rows of 64 bytes each
   static constexpr int kStage = kRows * kStep;
-  static_assert(kRows % (16 * kWaves) == 0 && BM % 16 == 0, "layout");
+  static_assert(kRows % (16 * kWaves) == 0 && BM % (16 * kCopies) == 0, "layout");
 };
 
 struct MatmulArgs {
@@ -65,28 +65,24 @@ __global__ void __launch_bounds__(W::kThreads, 2) matmul_kernel(const MatmulArgs
   const int s0 = part * p.steps, ns = p.stages - s0 < p.steps ? p.stages - s0 : p.steps;
   const int rows_b = (int)(p.m - m0 < W::BM ? p.m - m0 : W::BM), rows_a = (int)(p.n - n0 < W::BN ? p.n - n0 : W::BN);
 
+  // A wave's copies are of one operand: 16 rows each, from row `first` of its tile on.
   const uint32_t kp = (uint32_t)p.kp;
-  const uint32_t voff = (uint32_t)(lane >> 2) * kp + 16 * ((lane & 3) ^ ((lane >> 4) & 3));
-  const uint64_t base_b = (uint64_t)(p.b + m0 * p.kp), base_a = (uint64_t)(p.a + n0 * p.kp);
+  const bool of_b = 16 * W::kCopies * wave < W::BM;
+  const int first = 16 * W::kCopies * wave - (of_b ? 0 : W::BM);
+  const uint32_t voff = (uint32_t)(first + (lane >> 2)) * kp + 16 * ((lane & 3) ^ ((lane >> 4) & 3));
+  const uint64_t base = (uint64_t)(of_b ? p.b + m0 * p.kp : p.a + n0 * p.kp) + (uint64_t)s0 * kStep;
+  const uint32_t limit = (uint32_t)((of_b ? rows_b : rows_a) - 1) * kp + kStep;
   auto issue = [&](int s) {  // stage s of this part; past its end: zeros
-    u32x4 rb, ra;
-    const uint64_t at = (uint64_t)(s0 + s) * kStep, ab = base_b + at, aa = base_a + at;
-    rb[0] = (uint32_t)ab, rb[1] = (uint32_t)(ab >> 32) & 0xFFFFu, rb[3] = 0x00020000u;
-    ra[0] = (uint32_t)aa, ra[1] = (uint32_t)(aa >> 32) & 0xFFFFu, ra[3] = 0x00020000u;
-    rb[2] = s < ns ? (uint32_t)(rows_b - 1) * kp + kStep : 0;
-    ra[2] = s < ns ? (uint32_t)(rows_a - 1) * kp + kStep : 0;
-    INFCL_LDS char* to = (INFCL_LDS char*)lds + (s % kStages) * W::kStage;
+    const uint64_t at = base + (uint64_t)s * kStep;
+    u32x4 r;
+    r[0] = (uint32_t)at, r[1] = (uint32_t)(at >> 32) & 0xFFFFu, r[2] = s < ns ? limit : 0, r[3] = 0x00020000u;
+    INFCL_LDS char* to = (INFCL_LDS char*)lds + (s % kStages) * W::kStage + 1024 * W::kCopies * wave;
 #pragma unroll
-    for (int i = 0; i < W::kCopies; ++i) {
-      const int c = W::kCopies * wave + i;
-      if (16 * c < W::BM)
-        dma16_asm(rb, to + 1024 * c, voff, (uint32_t)(16 * c) * kp);
-      else
-        dma16_asm(ra, to + 1024 * c, voff, (uint32_t)(16 * c - W::BM) * kp);
-    }
+    for (int i = 0; i < W::kCopies; ++i) dma16_asm(r, to + 1024 * i, voff, (uint32_t)(16 * i) * kp);
   };
   auto exponents = [&](int s) {  // of 64 stages from s (a multiple of 64) on
     const int64_t word0 = (int64_t)(s0 + s) / 8;
+#pragma unroll 1
     for (int i = threadIdx.x; i < kGroups * W::kRows; i += W::kThreads) {
       const int r = i % W::kRows, g = i / W::kRows;
       const bool isb = r < W::BM;
@@ -107,48 +103,62 @@ __global__ void __launch_bounds__(W::kThreads, 2) matmul_kernel(const MatmulArgs
   const int row = lane & 31, swz = (row >> 2) & 3;
   const int off0 = row * kStep + 16 * ((2 * h) ^ swz), off1 = row * kStep + 16 * ((2 * h + 1) ^ swz);
   const int bm = wm * W::FM * 32, bn = W::BM + wn * W::FN * 32;  // first rows of this wave's blocks
+  i32x8 b[W::FM], a0[W::FN], a1[W::FN];
+  auto frag = [&](int s, int first) {
+    const INFCL_LDS char* cur = (const INFCL_LDS char*)lds + (s % kStages) * W::kStage + first * kStep;
+    const i32x4 lo = *(const INFCL_LDS i32x4*)(cur + off0), hi = *(const INFCL_LDS i32x4*)(cur + off1);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
   uint32_t eb[W::FM], ea[W::FN];
+  auto words = [&](int s) {  // the exponents of eight stages from s on
+    const uint32_t* e = exps + (s / 8 % kGroups) * W::kRows + row;
 #pragma unroll
-  for (int s = 0; s < kStages - 1; ++s) issue(s);
-  for (int s = 0; s < ns; ++s) {
-    if (s % 64 == 0) {
-      if (s > 0) __syncthreads();
-      exponents(s);
-    }
-    // this wave's copies of stage s are done (those of two later ones may not be), and
-    // with the barrier every wave's; all reads of the stage before are done too
-    if constexpr (W::kCopies == 4)
-      asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    else
-      asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    static_assert(W::kCopies == 4 || W::kCopies == 2, "waits");
-    issue(s + kStages - 1);
-    if (s % 8 == 0) {
-      const uint32_t* e = exps + (s / 8 % kGroups) * W::kRows + row;
+    for (int i = 0; i < W::FM; ++i) eb[i] = e[bm + 32 * i];
 #pragma unroll
-      for (int i = 0; i < W::FM; ++i) eb[i] = e[bm + 32 * i];
+    for (int j = 0; j < W::FN; ++j) ea[j] = e[bn + 32 * j];
+  };
+  static_assert(W::kCopies == 4, "waits");
+  // One stage: its fragments are in registers, those of the next one are read beside its
+  // products, b's into the registers that a product has just read.  At the barrier this
+  // wave's copies of stage s + 1 are done (those of two later ones may not be) and with it
+  // every wave's; all reads of stage s are done too, so its place takes stage s + 4.
+  auto step = [&](int s, const i32x8 (&a)[W::FN], i32x8 (&next)[W::FN]) {
+    asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    issue(s + kStages);
 #pragma unroll
-      for (int j = 0; j < W::FN; ++j) ea[j] = e[bn + 32 * j];
-    }
-    const INFCL_LDS char* cur = (const INFCL_LDS char*)lds + (s % kStages) * W::kStage;
-    i32x8 b[W::FM], a[W::FN];
-    auto frag = [&](int first) {
-      const i32x4 lo = *(const INFCL_LDS i32x4*)(cur + first * kStep + off0);
-      const i32x4 hi = *(const INFCL_LDS i32x4*)(cur + first * kStep + off1);
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
+    for (int j = 0; j < W::FN; ++j) next[j] = frag(s + 1, bn + 32 * j);
 #pragma unroll
-    for (int i = 0; i < W::FM; ++i) b[i] = frag(bm + 32 * i);
-#pragma unroll
-    for (int j = 0; j < W::FN; ++j) a[j] = frag(bn + 32 * j);
-#pragma unroll
-    for (int i = 0; i < W::FM; ++i)
+    for (int i = 0; i < W::FM; ++i) {
 #pragma unroll
       for (int j = 0; j < W::FN; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b[i], a[j], acc[i][j], 0, 0, 0, (int)eb[i], 0, (int)ea[j]);
-    if (s & 1) {  // the next block's bytes
+      __builtin_amdgcn_sched_barrier(0);
+      b[i] = frag(s + 1, bm + 32 * i);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
 #pragma unroll
-      for (int i = 0; i < W::FM; ++i) eb[i] >>= 8;
+  for (int s = 0; s < kStages; ++s) issue(s);
+  exponents(0);
+  asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < W::FN; ++j) a0[j] = frag(0, bn + 32 * j);
+#pragma unroll
+  for (int i = 0; i < W::FM; ++i) b[i] = frag(0, bm + 32 * i);
+  for (int s = 0; s < ns;) {  // (128 entries at least: an even number of stages)
+    if (s > 0 && s % 64 == 0) {
+      __syncthreads();
+      exponents(s);
+      __syncthreads();
+    }
+    words(s);
+    const int end = s + 8 < ns ? s + 8 : ns;
+#pragma unroll 1
+    for (; s < end; s += 2) {
+      step(s, a0, a1);
+      step(s + 1, a1, a0);
+#pragma unroll
+      for (int i = 0; i < W::FM; ++i) eb[i] >>= 8;  // the next block's bytes
 #pragma unroll
       for (int j = 0; j < W::FN; ++j) ea[j] >>= 8;
     }
@@ -157,7 +167,62 @@ __global__ void __launch_bounds__(W::kThreads, 2) matmul_kernel(const MatmulArgs
   // landed before the workgroup's LDS is given away.
   wait_dma();
 
-  const bool quads = p.m % 4 == 0;
+  // Rows of a lane's own entries would be 8 bytes of 32 rows in one store.  Where rows are
+  // 16-byte aligned, a wave's block goes through its share of the LDS instead and comes out
+  // in whole rows of it: PARTS 32 rows of a at a time, in fp32, else all in 16 bits.
+  constexpr int kSize = PARTS ? 4 : 2, kAcross = W::FM * 32 * kSize / 16;  // chunks of a row
+  if (p.m % (16 / kSize) == 0) {
+    constexpr int kJ = PARTS ? 1 : W::FN, kRowsOut = 32 * kJ;
+    static_assert(kRowsOut * kAcross * 16 * W::kWaves <= kStages * W::kStage, "LDS of the output");
+    INFCL_LDS char* mine = (INFCL_LDS char*)lds + wave * (kRowsOut * kAcross * 16);
+    const int64_t c0 = m0 + bm, r0 = n0 + 32 * wn * W::FN;
+    __syncthreads();  // every wave's reads of the last stage are done
+#pragma unroll
+    for (int j0 = 0; j0 < W::FN; j0 += kJ) {
+#pragma unroll
+      for (int i = 0; i < W::FM; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int at = 32 * i + 8 * g + 4 * h;  // of this wave's entries along m
+          float bias[4] = {0.f, 0.f, 0.f, 0.f};
+          if (!PARTS && p.bias && c0 + at < p.m) {
+            typedef __attribute__((__vector_size__(8), __aligned__(2))) __bf16 quad;
+            const quad y = *(const quad*)((const __bf16*)p.bias + c0 + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bias[e] = from16<F16>(y[e]);
+          }
+#pragma unroll
+          for (int jj = 0; jj < kJ; ++jj) {
+            const int j = j0 + jj, r = 32 * jj + (lane & 31), c = at * kSize / 16;
+            INFCL_LDS char* to = mine + (r * kAcross + (c ^ (r & (kAcross - 1)))) * 16 + (at * kSize & 15);
+            f32x4v v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              v[e] = acc[i][j][4 * g + e] + bias[e];
+            }
+            if constexpr (PARTS) {
+              *(INFCL_LDS f32x4v*)to = v;
+            } else {
+              __bf16 y[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) y[e] = to16<F16>(v[e]);
+              *(INFCL_LDS uint64_t*)to = __builtin_bit_cast(uint64_t, y);
+            }
+          }
+        }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 4
+      for (int t = 0; t < kRowsOut * kAcross / 64; ++t) {
+        const int r = t * (64 / kAcross) + lane / kAcross, c = lane % kAcross;
+        const i32x4 v = *(const INFCL_LDS i32x4*)(mine + (r * kAcross + (c ^ (r & (kAcross - 1)))) * 16);
+        const int64_t row = r0 + 32 * j0 + r, col = c0 + c * (16 / kSize);
+        if (row < p.n && col < p.m)
+          *(i32x4*)((char*)(PARTS ? (void*)(p.part + part * p.nm) : p.out) + (row * p.m + col) * kSize) = v;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < W::FN; ++j) {
     const int64_t col = n0 + 32 * (wn * W::FN + j) + (lane & 31);
@@ -165,34 +230,13 @@ __global__ void __launch_bounds__(W::kThreads, 2) matmul_kernel(const MatmulArgs
 #pragma unroll
     for (int i = 0; i < W::FM; ++i)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int64_t r0 = m0 + bm + 32 * i + 8 * g + 4 * h;
-        if (r0 >= p.m) continue;
-        if constexpr (PARTS) {
-          float* to = p.part + part * p.nm + col * p.m + r0;
-          if (quads) {
-            *(f32x4v*)to = f32x4v{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (r0 + e < p.m) to[e] = acc[i][j][4 * g + e];
-          }
-        } else {
-          __bf16* to = (__bf16*)p.out + col * p.m + r0;
-          __bf16 y[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float bias = p.bias && r0 + e < p.m ? from16<F16>(((const __bf16*)p.bias)[r0 + e]) : 0.f;
-            y[e] = to16<F16>(acc[i][j][4 * g + e] + bias);
-          }
-          if (quads) {
-            *(uint64_t*)to = __builtin_bit_cast(uint64_t, y);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (r0 + e < p.m) to[e] = y[e];
-          }
-        }
+      for (int r = 0; r < 16; ++r) {
+        const int64_t at = m0 + bm + 32 * i + 8 * (r >> 2) + 4 * h + (r & 3);
+        if (at >= p.m) continue;
+        if constexpr (PARTS)
+          p.part[part * p.nm + col * p.m + at] = acc[i][j][r];
+        else
+          ((__bf16*)p.out)[col * p.m + at] = to16<F16>(acc[i][j][r] + (p.bias ? from16<F16>(((const __bf16*)p.bias)[at]) : 0.f));
       }
   }
 }
