@@ -93,43 +93,55 @@ __device__ __forceinline__ void place(const NormArgs& a, int64_t& row, int64_t& 
   }
 }
 
-template <int T, int WIDE>
-__global__ void __launch_bounds__(WIDE ? 1024 : 256) norm_fwd(const NormArgs a) {
+// The vectors of a call: a lane's entries, 1 and 0 where there are none.
+struct Vectors {
+  float gate[8], w1[8], b1[8], w2[8], b2[8];
+};
+template <int T, bool FULL, bool BIAS>
+__device__ __forceinline__ void load_vectors(const NormArgs& a, bool in, int64_t col, Vectors& w) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) w.gate[e] = w.w1[e] = w.w2[e] = 1.f, w.b1[e] = w.b2[e] = 0.f;
+  if (!in) return;
+  if (FULL && a.gate) load8_or_f32<T>(a.gate, col, a.wf32, w.gate);
+  if (FULL && a.post_w) load8_or_f32<T>(a.post_w, col, a.wf32, w.w1);
+  if (FULL && BIAS && a.post_b) load8_or_f32<T>(a.post_b, col, a.wf32, w.b1);
+  if (a.pre_w) load8_or_f32<T>(a.pre_w, col, a.wf32, w.w2);
+  if (BIAS && a.pre_b) load8_or_f32<T>(a.pre_b, col, a.wf32, w.b2);
+}
+
+// WIDE: 0, rows within a wave; else rows of up to that many lanes.  FULL: with a gate, a
+// norm of y or a dropout; without, the registers of their vectors and sums are free for
+// more waves.
+template <int T, int WIDE, bool FULL>
+__global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE == 1024 ? 4 : 2) norm_fwd(const NormArgs a) {
   __shared__ float buf[2][16][2];
   int64_t row, step;
   int chunk, turn = 0;
   place<WIDE>(a, row, step, chunk);
   const bool in = chunk < a.c;
   const int64_t col = 8 * (int64_t)chunk;
-  float gate[8], w1[8], b1[8], w2[8], b2[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) gate[e] = w1[e] = w2[e] = 1.f, b1[e] = b2[e] = 0.f;
-  if (in) {
-    if (a.gate) load8_or_f32<T>(a.gate, col, a.wf32, gate);
-    if (a.post_w) load8_or_f32<T>(a.post_w, col, a.wf32, w1);
-    if (a.post_b) load8_or_f32<T>(a.post_b, col, a.wf32, b1);
-    if (a.pre_w) load8_or_f32<T>(a.pre_w, col, a.wf32, w2);
-    if (a.pre_b) load8_or_f32<T>(a.pre_b, col, a.wf32, b2);
-  }
-  const uint64_t seed = a.drop.cut ? a.drop.the_seed() : 0;
+  Vectors w;
+  load_vectors<T, FULL, true>(a, in, col, w);
+  const bool drop = FULL && a.drop.cut;
+  const uint64_t seed = drop ? a.drop.the_seed() : 0;
   for (; row < a.n; row += step) {
     float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, t[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (in) load8<T>(a.x, row * a.xs + col, x);
     float m1 = 0.f, r1 = 0.f, m2 = 0.f, r2 = 0.f;
     if (a.y) {
       if (in) load8<T>(a.y, row * a.ys + col, t);
-      if (a.post_w) {
+      if (FULL && a.post_w) {
         norm_row<WIDE>(t, in, a, m1, r1, buf, turn);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] = fmaf(t[e], w1[e], b1[e]);
+        for (int e = 0; e < 8; ++e) t[e] = fmaf(t[e], w.w1[e], w.b1[e]);
       }
-      if (a.drop.cut) {
+      if (drop) {
         const Random128 u = philox(a.drop.first + (uint64_t)row * a.c + chunk, a.drop.site, seed);
 #pragma unroll
         for (int e = 0; e < 8; ++e) t[e] = u.bits16(e) >= a.drop.cut ? t[e] * a.drop.unit : 0.f;
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = fmaf(a.alpha, x[e], gate[e] * t[e]);
+      for (int e = 0; e < 8; ++e) x[e] = fmaf(a.alpha, x[e], FULL ? w.gate[e] * t[e] : t[e]);
       if (in) store8<T>(a.h, row * (8 * (int64_t)a.c) + col, x);
     }
     if (a.pre_w) {
@@ -138,15 +150,20 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256) norm_fwd(const NormArgs a) 
         for (int e = 0; e < 8; ++e) x[e] = 0.f;
       norm_row<WIDE>(x, in, a, m2, r2, buf, turn);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], w2[e], b2[e]);
+      for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], w.w2[e], w.b2[e]);
       if (in) store8<T>(a.z, row * (8 * (int64_t)a.c) + col, x);
     }
     if (a.stats && chunk == 0) a.stats[row] = make_float4(m1, r1, m2, r2);
   }
 }
 
-template <int T, int WIDE>
-__global__ void __launch_bounds__(WIDE ? 1024 : 256) norm_bwd(const NormArgs a) {
+// BIAS: with sums for biases.  With everything (FULL, BIAS) a lane takes 153 registers, three
+// waves on a SIMD.  Where the rows' waves do not divide those twelve, the biases' sums, the
+// first bias and the gate are in LDS, each lane its own 32 bytes of them, and 16 waves fit
+// (everything, us with registers and with LDS: 50001 x 1160 348 and 320, 8001 x 8192 457 and 294;
+// but 50001 x 768 174 and 205, 30001 x 2048 214 and 265).
+template <int T, int WIDE, bool FULL, bool BIAS>
+__global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE >= 512 || !BIAS ? 4 : 2) norm_bwd(const NormArgs a) {
   __shared__ float buf[2][16][2];
   __shared__ float joined[WIDE ? 1 : 4][WIDE ? 1 : 512];
   int64_t row, step;
@@ -154,58 +171,100 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256) norm_bwd(const NormArgs a) 
   place<WIDE>(a, row, step, chunk);
   const bool in = chunk < a.c;
   const int64_t col = 8 * (int64_t)chunk;
-  float gate[8], w1[8], b1[8], w2[8];
+  extern __shared__ f32x4 own[];  // kOwn: [sb2, sb1, b1, gate][halves][lanes]
+  constexpr bool kOwn = WIDE >= 512 && FULL && BIAS;
+  auto add_own = [&](int k, const float (&q)[8]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) gate[e] = w1[e] = w2[e] = 1.f, b1[e] = 0.f;
-  if (in) {
-    if (a.gate) load8_or_f32<T>(a.gate, col, a.wf32, gate);
-    if (a.post_w) load8_or_f32<T>(a.post_w, col, a.wf32, w1);
-    if (a.post_b) load8_or_f32<T>(a.post_b, col, a.wf32, b1);
-    if (a.pre_w) load8_or_f32<T>(a.pre_w, col, a.wf32, w2);
+    for (int i = 0; i < 2; ++i)
+      own[(2 * k + i) * blockDim.x + threadIdx.x] += f32x4{q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]};
+  };
+  auto get_own = [&](int k, float (&q)[8]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const f32x4 x = own[(2 * k + i) * blockDim.x + threadIdx.x];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q[4 * i + e] = x[e];
+    }
+  };
+  Vectors w;
+  load_vectors<T, FULL, BIAS>(a, in, col, w);
+  if constexpr (kOwn) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) own[i * blockDim.x + threadIdx.x] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
+  auto put_own = [&](int k, const float (&q)[8]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      own[(2 * k + i) * blockDim.x + threadIdx.x] = f32x4{q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]};
+  };
   float sg[8], sw1[8], sb1[8], sw2[8], sb2[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) sg[e] = sw1[e] = sb1[e] = sw2[e] = sb2[e] = 0.f;
-  const uint64_t seed = a.drop.cut ? a.drop.the_seed() : 0;
+  const bool drop = FULL && a.drop.cut;
+  const uint64_t seed = drop ? a.drop.the_seed() : 0;
+  // dropout's factor is the gate's, and that of the gate's sums
+  if (FULL)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w.gate[e] *= drop ? a.drop.unit : 1.f;
+  if (kOwn) put_own(2, w.b1), put_own(3, w.gate);
   for (; row < a.n; row += step) {
     float h[8] = {0, 0, 0, 0, 0, 0, 0, 0}, v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, e8[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     float g[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    const float4 st = a.stats[row];
+    float4 st = a.stats[row];
     if (in) {
       load8<T>(a.x, row * a.xs + col, h);
       if (a.y) load8<T>(a.y, row * a.ys + col, v);
       if (a.dh) load8<T>(a.dh, row * a.dhs + col, e8);
       if (a.dz) load8<T>(a.dz, row * a.dzs + col, g);
+    } else {
+      st.y = st.w = 0.f;  // (normed rows of lanes past the row are zeros)
     }
-    Random128 u;
-    if (a.drop.cut) u = philox(a.drop.first + (uint64_t)row * a.c + chunk, a.drop.site, seed);
-    float t[8];  // what the gate took
+    bool keep[8];
+    if (drop) {
+      const Random128 u = philox(a.drop.first + (uint64_t)row * a.c + chunk, a.drop.site, seed);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) keep[e] = u.bits16(e) >= a.drop.cut;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) keep[e] = true;
+    }
+    // what the gate took (without dropout's factor), from the normed y
+    auto taken = [&](int e, const float (&b)[8]) {
+      const float t = a.post_w ? (BIAS ? fmaf(v[e], w.w1[e], b[e]) : v[e] * w.w1[e]) : v[e];
+      return keep[e] ? t : 0.f;
+    };
+    float b1[8], gate[8];
+    auto get = [&]() {
+      if constexpr (kOwn) {
+        get_own(2, b1), get_own(3, gate);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b1[e] = w.b1[e], gate[e] = w.gate[e];
+      }
+    };
+    get();
     if (a.y) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        t[e] = v[e];
-        if (a.post_w) {
-          v[e] = in ? (v[e] - st.x) * st.y : 0.f;
-          t[e] = fmaf(v[e], w1[e], b1[e]);
-        }
-        if (a.drop.cut) t[e] = u.bits16(e) >= a.drop.cut ? t[e] * a.drop.unit : 0.f;
-        h[e] = fmaf(a.alpha, h[e], gate[e] * t[e]);
+        if (FULL && a.post_w) v[e] = (v[e] - st.x) * st.y;
+        h[e] = fmaf(a.alpha, h[e], FULL ? gate[e] * taken(e, b1) : v[e]);
       }
     }
     if (a.pre_w) {
+      if (kOwn && a.want_pre_b) add_own(0, g);
       float s[2] = {0.f, 0.f};
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        h[e] = in ? (h[e] - st.z) * st.w : 0.f;
+        h[e] = (h[e] - st.z) * st.w;
         sw2[e] = fmaf(g[e], h[e], sw2[e]);
-        sb2[e] += g[e];
-        g[e] *= w2[e];
+        if (BIAS && !kOwn) sb2[e] += g[e];
+        g[e] *= w.w2[e];
         s[0] += g[e], s[1] = fmaf(g[e], h[e], s[1]);
       }
       row_sums<WIDE, 2>(s, a.ls, buf, turn);
       const float m = a.rms ? 0.f : s[0] * a.by_d, k = s[1] * a.by_d;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) e8[e] += in ? st.w * (g[e] - m - h[e] * k) : 0.f;
+      for (int e = 0; e < 8; ++e) e8[e] = fmaf(st.w, g[e] - fmaf(h[e], k, m), e8[e]);
     }
     if (a.dx && in) {
       float o[8];
@@ -214,28 +273,37 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256) norm_bwd(const NormArgs a) 
       store8<T>(a.dx, row * (8 * (int64_t)a.c) + col, o);
     }
     if (!a.y) continue;
-    float s[2] = {0.f, 0.f};
+    if constexpr (FULL) {
+      get();
+      float s[2] = {0.f, 0.f}, qs[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      sg[e] = fmaf(e8[e], t[e], sg[e]);
-      float q = e8[e] * gate[e];
-      if (a.drop.cut) q = u.bits16(e) >= a.drop.cut ? q * a.drop.unit : 0.f;
-      if (a.post_w) {
-        sw1[e] = fmaf(q, v[e], sw1[e]);
-        sb1[e] += q;
-        q *= w1[e];
-        s[0] += q, s[1] = fmaf(q, v[e], s[1]);
+      for (int e = 0; e < 8; ++e) {
+        sg[e] = fmaf(e8[e], taken(e, b1), sg[e]);
+        float q = keep[e] ? e8[e] * gate[e] : 0.f;
+        if (a.post_w) {
+          sw1[e] = fmaf(q, v[e], sw1[e]);
+          if (BIAS && !kOwn) sb1[e] += q;
+          qs[e] = q;
+          q *= w.w1[e];
+          s[0] += q, s[1] = fmaf(q, v[e], s[1]);
+        }
+        e8[e] = q;
       }
-      e8[e] = q;
-    }
-    if (a.post_w) {
-      row_sums<WIDE, 2>(s, a.ls, buf, turn);
-      const float m = a.rms ? 0.f : s[0] * a.by_d, k = s[1] * a.by_d;
+      if (a.post_w) {
+        if (kOwn && a.want_post_b) add_own(1, qs);
+        row_sums<WIDE, 2>(s, a.ls, buf, turn);
+        const float m = a.rms ? 0.f : s[0] * a.by_d, k = s[1] * a.by_d;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) e8[e] = st.y * (e8[e] - m - v[e] * k);
+        for (int e = 0; e < 8; ++e) e8[e] = st.y * (e8[e] - fmaf(v[e], k, m));
+      }
     }
     if (a.dy && in) store8<T>(a.dy, row * (8 * (int64_t)a.c) + col, e8);
   }
+  if (FULL && drop)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sg[e] *= a.drop.unit;
+
+  if constexpr (kOwn) get_own(0, sb2), get_own(1, sb1);
 
   // One row of sums of the workgroup: groups of a wave, then waves, in order.
   const int d = 8 * a.c;
@@ -266,11 +334,11 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256) norm_bwd(const NormArgs a) 
       }
     }
   };
-  if (a.want_gate) put(sg);
-  if (a.want_post) put(sw1);
-  if (a.want_post_b) put(sb1);
+  if (FULL && a.want_gate) put(sg);
+  if (FULL && a.want_post) put(sw1);
+  if (FULL && BIAS && a.want_post_b) put(sb1);
   if (a.want_pre) put(sw2);
-  if (a.want_pre_b) put(sb2);
+  if (BIAS && a.want_pre_b) put(sb2);
 }
 
 // Sums of parts [parts][sums][d] in a fixed order: 32 columns of one vector for each
@@ -326,12 +394,18 @@ Shape shape_of(int64_t d) {
   s.groups = s.wide ? 1 : 256 >> s.ls;
   return s;
 }
-// Workgroups: what covers the rows, at most some waves for each SIMD.
-unsigned grid_of(const Shape& s, int64_t n, int64_t waves) {
-  const int64_t need = (n + s.groups - 1) / s.groups, most = 1024 * waves / (s.threads / 64);
+// Workgroups: what covers the rows, at most as many as are resident at once with
+// `waves` to a compute unit, so that all of them go through as many rows.
+unsigned grid_of(const Shape& s, int64_t n, int waves) {
+  const int64_t need = (n + s.groups - 1) / s.groups, each = waves / (int)(s.threads / 64), most = 256 * (each < 1 ? 1 : each);
   return (unsigned)(need < most ? need : most);
 }
-constexpr int kFwdWaves = 8, kBwdWaves = 4;
+// The forward starts more than that: nothing is left to be joined.  The backward's kernels
+// have registers for 16 or more waves, with everything and biases for 12 (17408 x 512: 37 us
+// with 12, 46 with 16; 30001 x 2048 without gate and norm of y: 144 us with 16, 151 with 20).
+constexpr int kFwdWaves = 32, kBwdWaves = 16, kBwdWavesAll = 12;
+
+bool all_in_registers(const Shape& s) { return s.wide && (s.threads == 128 || s.threads == 256); }
 
 infcl_status check(const infcl_add_norm* a) {
   if (!a || a->n < 0 || a->d < 1 || !type_known(a->dtype) || !type_known(a->wdtype) ||
@@ -367,20 +441,42 @@ NormArgs args_of(const infcl_add_norm* a, const Shape& s, const void* x, const v
   return r;
 }
 
-template <int T>
+template <int T, bool FULL>
 void fwd_t(const NormArgs& r, const Shape& s, hipStream_t st) {
   const dim3 grid(grid_of(s, r.n, kFwdWaves)), block(s.threads);
-  if (s.wide)
-    hipLaunchKernelGGL((norm_fwd<T, 1>), grid, block, 0, st, r);
+  if (s.threads > 512)
+    hipLaunchKernelGGL((norm_fwd<T, 1024, FULL>), grid, block, 0, st, r);
+  else if (s.wide)
+    hipLaunchKernelGGL((norm_fwd<T, 512, FULL>), grid, block, 0, st, r);
   else
-    hipLaunchKernelGGL((norm_fwd<T, 0>), grid, block, 0, st, r);
+    hipLaunchKernelGGL((norm_fwd<T, 0, FULL>), grid, block, 0, st, r);
+}
+template <int T, bool FULL, bool BIAS>
+void bwd_t(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
+  const dim3 grid(wgs), block(s.threads);
+  const size_t own = FULL && BIAS ? 8 * 16 * (size_t)s.threads : 0;
+  if (all_in_registers(s) && FULL && BIAS)
+    hipLaunchKernelGGL((norm_bwd<T, FULL && BIAS ? 256 : 512, FULL, BIAS>), grid, block, 0, st, r);
+  else if (s.threads > 512)
+    hipLaunchKernelGGL((norm_bwd<T, 1024, FULL, BIAS>), grid, block, own, st, r);
+  else if (s.wide)
+    hipLaunchKernelGGL((norm_bwd<T, 512, FULL, BIAS>), grid, block, own, st, r);
+  else
+    hipLaunchKernelGGL((norm_bwd<T, 0, FULL, BIAS>), grid, block, 0, st, r);
+}
+bool full(const NormArgs& r) { return r.gate || r.post_w || r.drop.cut; }
+template <int T>
+void fwd_any(const NormArgs& r, const Shape& s, hipStream_t st) {
+  full(r) ? fwd_t<T, true>(r, s, st) : fwd_t<T, false>(r, s, st);
 }
 template <int T>
-void bwd_t(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
-  if (s.wide)
-    hipLaunchKernelGGL((norm_bwd<T, 1>), dim3(wgs), dim3(s.threads), 0, st, r);
+void bwd_any(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
+  if (!full(r))
+    bwd_t<T, false, true>(r, s, wgs, st);
+  else if (r.post_b || r.pre_b)
+    bwd_t<T, true, true>(r, s, wgs, st);
   else
-    hipLaunchKernelGGL((norm_bwd<T, 0>), dim3(wgs), dim3(s.threads), 0, st, r);
+    bwd_t<T, true, false>(r, s, wgs, st);
 }
 template <int T>
 void join_t(const NormArgs& r, unsigned wgs, int sums, void* const* o, hipStream_t st) {
@@ -406,11 +502,11 @@ extern "C" infcl_status infcl_add_norm_fwd(const infcl_add_norm* a, const void* 
   r.h = h, r.z = z, r.stats = (float4*)stats;
   hipStream_t st = (hipStream_t)stream;
   if (a->dtype == INFCL_BF16)
-    fwd_t<kBF16>(r, sh, st);
+    fwd_any<kBF16>(r, sh, st);
   else if (a->dtype == INFCL_F16)
-    fwd_t<kF16>(r, sh, st);
+    fwd_any<kF16>(r, sh, st);
   else
-    fwd_t<kF32>(r, sh, st);
+    fwd_any<kF32>(r, sh, st);
   return launch_status();
 }
 
@@ -456,14 +552,14 @@ extern "C" infcl_status infcl_add_norm_bwd(const infcl_add_norm* a, const void* 
   for (void* o : {g->dgate, g->dpost_w, g->dpost_b, g->dpre_w, g->dpre_b})
     if (o) outs[sums++] = o;
   hipStream_t st = (hipStream_t)stream;
-  const unsigned wgs = grid_of(sh, a->n, kBwdWaves);
+  const unsigned wgs = grid_of(sh, a->n, full(r) && (r.post_b || r.pre_b) && (!sh.wide || all_in_registers(sh)) ? kBwdWavesAll : kBwdWaves);
   if (wgs > 0) {
     if (a->dtype == INFCL_BF16)
-      bwd_t<kBF16>(r, sh, wgs, st);
+      bwd_any<kBF16>(r, sh, wgs, st);
     else if (a->dtype == INFCL_F16)
-      bwd_t<kF16>(r, sh, wgs, st);
+      bwd_any<kF16>(r, sh, wgs, st);
     else
-      bwd_t<kF32>(r, sh, wgs, st);
+      bwd_any<kF32>(r, sh, wgs, st);
     s = launch_status();
     if (s != INFCL_OK) return s;
   }
