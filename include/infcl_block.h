@@ -120,11 +120,12 @@ infcl_status infcl_add_norm_bwd(const infcl_add_norm* a, const void* x, const vo
                                 const infcl_add_norm_grads* g, void* workspace, size_t ws_bytes, void* stream);
 
 /* ---- 8-bit floats with a power of two for each 128.
- * rows x k entries are q [rows][kp] bytes, kp = 128 ceil(k / 128), and exps [rows][ep]
- * bytes, ep = 4 ceil(kp / 512): block j of a row (entries 128 j and up) has the least
+ * rows x k entries are q [rows][kp] bytes, kp = 128 ceil(k / 128) and 128 more where that
+ * is a multiple of 16384 (never read), and exps [rows][ep] bytes, ep = 4 ceil(k / 512), 127
+ * where there is no block: block j of a row (entries 128 j and up) has the least
  * e >= -126 with max|x| 2^-e <= 448, q = x 2^-e to the nearest 8-bit float of 4 exponent
  * and 3 fraction bits (E4M3 without infinities, ties to even), exps[j] = e + 127.  Entries
- * past k are zeros.  A block that holds an infinity or a NaN is all NaN (0x7F, exps 255).
+ * past k are zeros up to the end of their block.  A block that holds an infinity or a NaN is all NaN (0x7F, exps 255).
  *
  * x [n, d] of dtype, d a multiple of 8 (x_stride: a multiple of 8, >= d).  q, exps: blocks
  * along its rows (d entries); qt, expst: those of its transpose, blocks along its columns
@@ -139,9 +140,10 @@ infcl_status infcl_fp8_unpack(const void* q, const void* exps, int64_t rows, int
                               void* stream);
 
 /* out [n, m] = a b^T + bias for packed a [n, k] and b [m, k]; out and bias [m] (may be
- * NULL; 2-byte aligned) of dtype, INFCL_BF16 or INFCL_F16, one rounding.  Products are
+ * NULL; 4-byte aligned) of dtype, INFCL_BF16 or INFCL_F16, one rounding.  Products are
  * exact; the matrix unit adds them in groups of eight, of each of which 13 bits below its
- * largest product's count, and the groups in fp32.  k up to 2^23, n and m up to 2^27. */
+ * largest product's count, and the groups in fp32.  k up to 2^23, n up to 2^27, m
+ * up to 2^24. */
 infcl_status infcl_fp8_matmul_workspace(int64_t n, int64_t m, int64_t k, size_t* bytes);
 infcl_status infcl_fp8_matmul(const void* aq, const void* aexps, int64_t n, const void* bq, const void* bexps,
                               int64_t m, int64_t k, const void* bias, int dtype, void* out, void* workspace,

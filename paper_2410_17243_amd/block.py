@@ -386,8 +386,8 @@ def add_norm(x, y=None, gate=None, post_w=None, post_b=None, pre_w=None, pre_b=N
 # ---------------------------------------------------------------- 8-bit floats
 
 class Fp8:
-    """Rows [rows, k] in 8-bit floats: q [rows, 128 ceil(k / 128)] uint8 (E4M3 bytes),
-    exps [rows, 4 ceil(k / 512)] uint8 (a power of two for 128 entries), and the dtype
+    """Rows [rows, k] in 8-bit floats: q [rows, 128 ceil(k / 128)] uint8 (E4M3 bytes; 128
+    more where that is a multiple of 16384), exps [rows, 4 ceil(k / 512)] uint8 (a power of two for 128 entries), and the dtype
     they had."""
 
     __slots__ = ("q", "exps", "k", "dtype")
@@ -403,17 +403,23 @@ class Fp8:
         return self.q.numel() + self.exps.numel()
 
 
-def _fp8_room(rows, k, dtype, dev):
+def _fp8_widths(k):
+    """Bytes of a row of values and of exponents."""
     kp = (k + BLOCK - 1) // BLOCK * BLOCK
-    return Fp8(torch.empty((rows, kp), dtype=torch.uint8, device=dev),
-               torch.empty((rows, (kp + 511) // 512 * 4), dtype=torch.uint8, device=dev), k, dtype)
+    return kp + (BLOCK if kp and kp % 16384 == 0 else 0), (k + 511) // 512 * 4
+
+
+def _fp8_room(rows, k, dtype, dev):
+    kp, ep = _fp8_widths(k)
+    return Fp8(torch.empty((rows, kp), dtype=torch.uint8, device=dev), torch.empty((rows, ep), dtype=torch.uint8, device=dev),
+               k, dtype)
 
 
 def _check_fp8(f, name):
-    kp = (f.k + BLOCK - 1) // BLOCK * BLOCK
+    kp, ep = _fp8_widths(f.k)
     if f.q.dtype != torch.uint8 or f.exps.dtype != torch.uint8 or not f.q.is_contiguous() or not f.exps.is_contiguous():
         raise ValueError(f"{name} must hold contiguous uint8 values and exponents")
-    if f.q.dim() != 2 or f.q.shape[1] != kp or f.exps.shape != (f.q.shape[0], (kp + 511) // 512 * 4):
+    if f.q.dim() != 2 or f.q.shape[1] != kp or f.exps.shape != (f.q.shape[0], ep):
         raise ValueError(f"{name}: values {tuple(f.q.shape)} and exponents {tuple(f.exps.shape)} do not fit rows of {f.k}")
 
 
@@ -452,10 +458,14 @@ def fp8_unpack(f: Fp8):
 
 
 def _out16(dtype, bias, m):
+    """Checks what a product comes in; the bias as the kernels take it."""
     if dtype not in (torch.bfloat16, torch.float16):
         raise TypeError(f"products of 8-bit floats come in bfloat16 or float16, got {dtype}")
-    if bias is not None and (bias.shape != (m,) or bias.dtype != dtype or not bias.is_contiguous()):
+    if bias is None:
+        return None
+    if bias.shape != (m,) or bias.dtype != dtype or not bias.is_contiguous():
         raise ValueError(f"the bias must be contiguous [{m}] of {dtype}, got {bias.dtype} {tuple(bias.shape)}")
+    return bias if bias.data_ptr() % 4 == 0 else bias.clone()  # (a view may begin at an odd entry)
 
 
 def fp8_matmul(a: Fp8, b: Fp8, bias=None, dtype=None):
@@ -468,7 +478,7 @@ def fp8_matmul(a: Fp8, b: Fp8, bias=None, dtype=None):
     if k != bk:
         raise ValueError(f"a and b must have rows of one length, got {k} and {bk}")
     dtype = a.dtype if dtype is None else dtype
-    _out16(dtype, bias, m)
+    bias = _out16(dtype, bias, m)
     out = torch.empty((n, m), dtype=dtype, device=dev)
     if out.numel() == 0:
         return out
@@ -559,7 +569,7 @@ def _linear_packed(x, w, b):
     m = w.shape[0]
     if k != w.k:
         raise ValueError(f"x must have rows of {w.k}, got {tuple(x.shape)}")
-    _out16(x.dtype, b, m)
+    b = _out16(x.dtype, b, m)
     out = torch.empty((*x.shape[:-1], m), dtype=x.dtype, device=dev)
     if out.numel() == 0:
         return out

@@ -19,15 +19,22 @@ namespace {
 
 struct PackArgs {
   const void* x;
-  int64_t xs, n, d, kp, ep, tp, tep;  // tp, tep: of the transpose
+  int64_t xs, n, d, blocks, kp, ep, tp, tep;  // blocks and pitches of a row; tp, tep: of the transpose
   uint8_t *q, *ex, *qt, *ext;
   float* sums;  // [ceil(n / 128)][d]
 };
 
+// The exponent of block b of a row; after the last block, 127 to the end of its word.
+__device__ __forceinline__ void put_exponent(uint8_t* row, int64_t b, int64_t blocks, uint32_t byte) {
+  row[b] = (uint8_t)byte;
+  if (b == blocks - 1)
+    for (int64_t i = blocks; i & 3; ++i) row[i] = 127;
+}
+
 // Along rows alone: 16 lanes take a block.
 template <int T>
 __global__ void __launch_bounds__(256) pack_rows(const PackArgs a) {
-  const int64_t blocks = a.kp / 128, total = a.n * blocks, step = (int64_t)gridDim.x * 16;
+  const int64_t blocks = a.blocks, total = a.n * blocks, step = (int64_t)gridDim.x * 16;
   const int lane = threadIdx.x & 15;
   for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < total; i += step) {
     const int64_t r = i / blocks, b = i - r * blocks, col = b * 128 + 8 * lane;
@@ -41,7 +48,7 @@ __global__ void __launch_bounds__(256) pack_rows(const PackArgs a) {
     uint2 w = make_uint2(fp8_pack4(v[0], v[1], v[2], v[3], inv), fp8_pack4(v[4], v[5], v[6], v[7], inv));
     if (byte == 255) w = make_uint2(kFp8Nan, kFp8Nan);
     *(uint2*)(a.q + r * a.kp + col) = w;
-    if (lane == 0) a.ex[r * a.ep + b] = (uint8_t)byte;
+    if (lane == 0) put_exponent(a.ex + r * a.ep, b, blocks, byte);
   }
 }
 
@@ -53,7 +60,7 @@ __global__ void __launch_bounds__(256, 2) pack_tile(const PackArgs a) {
   __shared__ float sum[4][128];
   __shared__ __attribute__((aligned(16))) uint8_t tile[128 * 144];  // [feature][row], 16 bytes between rows of it
   const int c = threadIdx.x & 15, g = threadIdx.x >> 4, wave = threadIdx.x >> 6;
-  const int64_t tiles = a.kp / 128, rt = blockIdx.x / tiles, ct = blockIdx.x - rt * tiles;
+  const int64_t tiles = a.blocks, rt = blockIdx.x / tiles, ct = blockIdx.x - rt * tiles;
   const int64_t row0 = rt * 128 + 8 * g, col = ct * 128 + 8 * c;
   float v[8][8];
 #pragma unroll
@@ -74,7 +81,7 @@ __global__ void __launch_bounds__(256, 2) pack_tile(const PackArgs a) {
       if (byte == 255) w = make_uint2(kFp8Nan, kFp8Nan);
       if (row0 + r < a.n) {
         *(uint2*)(a.q + (row0 + r) * a.kp + col) = w;
-        if (c == 0) a.ex[(row0 + r) * a.ep + ct] = (uint8_t)byte;
+        if (c == 0) put_exponent(a.ex + (row0 + r) * a.ep, ct, tiles, byte);
       }
     }
   }
@@ -113,7 +120,7 @@ __global__ void __launch_bounds__(256, 2) pack_tile(const PackArgs a) {
     uint2 w = make_uint2(fp8_pack4(v[0][e], v[1][e], v[2][e], v[3][e], inv), fp8_pack4(v[4][e], v[5][e], v[6][e], v[7][e], inv));
     if (byte == 255) w = make_uint2(kFp8Nan, kFp8Nan);
     *(uint2*)(tile + f * 144 + 8 * g) = w;
-    if (g == 0 && ct * 128 + f < a.d) a.ext[(ct * 128 + f) * a.tep + rt] = (uint8_t)byte;
+    if (g == 0 && ct * 128 + f < a.d) put_exponent(a.ext + (ct * 128 + f) * a.tep, rt, (a.n + 127) / 128, byte);
   }
   __syncthreads();
 #pragma unroll
@@ -188,12 +195,12 @@ __global__ void __launch_bounds__(256) unpack_rows(const uint8_t* __restrict__ q
 template <int T>
 void pack_t(const PackArgs& a, void* colsum, hipStream_t st) {
   if (!a.qt && !a.sums) {
-    const int64_t need = (a.n * (a.kp / 128) + 15) / 16;
+    const int64_t need = (a.n * a.blocks + 15) / 16;
     hipLaunchKernelGGL((pack_rows<T>), dim3((unsigned)(need < 16384 ? need : 16384)), dim3(256), 0, st, a);
     return;
   }
   const int64_t rows = (a.n + 127) / 128;
-  if (rows > 0) hipLaunchKernelGGL((pack_tile<T>), dim3((unsigned)(rows * (a.kp / 128))), dim3(256), 0, st, a);
+  if (rows > 0) hipLaunchKernelGGL((pack_tile<T>), dim3((unsigned)(rows * a.blocks)), dim3(256), 0, st, a);
   if (a.sums)
     hipLaunchKernelGGL((join_columns<T>), dim3((unsigned)((a.d + 31) / 32)), dim3(512), 0, st, (const float*)a.sums, rows, a.d, colsum);
 }
@@ -233,7 +240,7 @@ extern "C" infcl_status infcl_fp8_pack(const void* x, int64_t x_stride, int64_t 
   }
   if (n == 0 && !colsum) return INFCL_OK;
   PackArgs a;
-  a.x = x, a.xs = x_stride, a.n = n, a.d = d, a.kp = fp8_kp(d), a.ep = fp8_ep(d), a.tp = fp8_kp(n), a.tep = fp8_ep(n);
+  a.x = x, a.xs = x_stride, a.n = n, a.d = d, a.blocks = fp8_blocks(d), a.kp = fp8_pitch(d), a.ep = fp8_ep(d), a.tp = fp8_pitch(n), a.tep = fp8_ep(n);
   a.q = (uint8_t*)q, a.ex = (uint8_t*)exps, a.qt = (uint8_t*)qt, a.ext = (uint8_t*)expst;
   a.sums = colsum ? (float*)workspace : nullptr;
   hipStream_t st = (hipStream_t)stream;
@@ -255,7 +262,7 @@ extern "C" infcl_status infcl_fp8_unpack(const void* q, const void* exps, int64_
   const int64_t need = (rows * ((k + 3) / 4) + 255) / 256;
   const dim3 grid((unsigned)(need < 16384 ? need : 16384));
   hipStream_t st = (hipStream_t)stream;
-  const int64_t kp = fp8_kp(k), ep = fp8_ep(k);
+  const int64_t kp = fp8_pitch(k), ep = fp8_ep(k);
   const uint8_t *b = (const uint8_t*)q, *e = (const uint8_t*)exps;
   if (dtype == INFCL_BF16)
     hipLaunchKernelGGL((unpack_rows<kBF16>), grid, dim3(256), 0, st, b, e, kp, ep, rows, k, out);

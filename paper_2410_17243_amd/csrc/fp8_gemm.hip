@@ -52,15 +52,18 @@ struct MatmulArgs {
   int tm, tn, tiles, stages, steps;  // tiles along m and n; stages in all, of a part
 };
 
-template <class W, bool F16, bool PARTS>
+// OUT: sums of a part, the output, or the output past the caches.
+enum Out { kParts, kOutput, kPastCaches };
+template <class W, bool F16, Out OUT>
 __global__ void __launch_bounds__(W::kThreads, 2) matmul_kernel(const MatmulArgs p) {
+  constexpr bool PARTS = OUT == kParts;
   __shared__ __attribute__((aligned(1024))) char lds[kStages * W::kStage];
   __shared__ uint32_t exps[kGroups * W::kRows];
   const uint32_t slot = xcd_slot(blockIdx.x, gridDim.x);
   const int part = (int)(slot / (uint32_t)p.tiles), tile = (int)(slot % (uint32_t)p.tiles);
-  // four tiles along m for each along n, so that the workgroups of an XCD share rows of both
-  const int band = tile / (4 * p.tn), in = tile - band * 4 * p.tn, wide = p.tm - 4 * band < 4 ? p.tm - 4 * band : 4;
-  const int64_t m0 = (int64_t)(4 * band + in % wide) * W::BM, n0 = (int64_t)(in / wide) * W::BN;
+  // eight tiles along m for each along n, so that the workgroups of an XCD share rows of both
+  const int band = tile / (8 * p.tn), in = tile - band * 8 * p.tn, wide = p.tm - 8 * band < 8 ? p.tm - 8 * band : 8;
+  const int64_t m0 = (int64_t)(8 * band + in % wide) * W::BM, n0 = (int64_t)(in / wide) * W::BN;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int s0 = part * p.steps, ns = p.stages - s0 < p.steps ? p.stages - s0 : p.steps;
   const int rows_b = (int)(p.m - m0 < W::BM ? p.m - m0 : W::BM), rows_a = (int)(p.n - n0 < W::BN ? p.n - n0 : W::BN);
@@ -216,8 +219,12 @@ __global__ void __launch_bounds__(W::kThreads, 2) matmul_kernel(const MatmulArgs
         const int r = t * (64 / kAcross) + lane / kAcross, c = lane % kAcross;
         const i32x4 v = *(const INFCL_LDS i32x4*)(mine + (r * kAcross + (c ^ (r & (kAcross - 1)))) * 16);
         const int64_t row = r0 + 32 * j0 + r, col = c0 + c * (16 / kSize);
-        if (row < p.n && col < p.m)
-          *(i32x4*)((char*)(PARTS ? (void*)(p.part + part * p.nm) : p.out) + (row * p.m + col) * kSize) = v;
+        if (row >= p.n || col >= p.m) continue;
+        i32x4* out = (i32x4*)((char*)(PARTS ? (void*)(p.part + part * p.nm) : p.out) + (row * p.m + col) * kSize);
+        if constexpr (OUT == kPastCaches)
+          __builtin_nontemporal_store(v, out);
+        else
+          *out = v;
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
@@ -279,7 +286,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) few_kernel(const uint16_t* __r
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
   const int64_t m0 = (int64_t)blockIdx.x * 16, wrow = m0 + r < m ? m0 + r : m - 1;
   f32x4v acc = {0.f, 0.f, 0.f, 0.f};
-  const int blocks = (int)(kp / 128);
+  const int blocks = (int)((k + 127) / 128);
 #pragma unroll 2
   for (int b = wave; b < blocks; b += kFewWaves) {
     const int64_t at = (int64_t)128 * b + 32 * q;
@@ -328,32 +335,58 @@ struct MatmulPlan {
   int parts, stages, steps;
   size_t total;
 };
+// What a form of the product takes, in us, from the times of some thirty shapes: a round of
+// workgroups is as long as its stages (of the small tiles 0.3 us with one to a compute
+// unit, 0.6 with two; of the large ones 0.65 to 0.87 with what the chip's clock then is)
+// and a start and an end; parts cost a launch and the traffic of their sums.  Measured, chosen and
+// left: 4096 x 1024 x 1024 9.8 in small tiles, 16.5 in large ones, 28.5 in two parts; 776 x 1000 x
+// 10007 22 in four parts of small tiles, 50 in one, 32 in large ones; 8192^3 454 in large
+// tiles, 4096 x 4096 x 2048 37 and 51; 512 x 512 x 65536 31 in 16 parts, 39 in 32, 244 in one.
+double estimate(bool big, int64_t tiles, int64_t parts, int64_t steps, int64_t nm) {
+  const int64_t slots = big ? 256 : 512, wgs = tiles * parts, rest = wgs % slots;
+  const double start = big ? 8. : 4., full = steps * (big ? 0.87 : 0.6) + start;
+  double t = (double)(wgs / slots) * full;
+  if (rest > slots / 2)
+    t += full;
+  else if (rest > 0)
+    t += steps * (big ? 0.65 : 0.3) + start;
+  return parts > 1 ? t + 6. + (double)parts * (double)nm * 8. / 3.5e6 : t;
+}
 MatmulPlan plan_of(int64_t n, int64_t m, int64_t k) {
-  MatmulPlan p;
-  p.stages = (int)(fp8_kp(k) / kStep);
-  p.big = n >= 256 && m >= 256 && ((m + 255) / 256) * ((n + 255) / 256) * p.stages >= 256 * 16;
-  const int64_t b = p.big ? 256 : 128;
-  p.tm = (m + b - 1) / b, p.tn = (n + b - 1) / b;
-  const int64_t tiles = p.tm * p.tn, slots = p.big ? 256 : 512, groups = (p.stages + 7) / 8;
-  int64_t parts = tiles > 0 ? slots / tiles : 1;
-  if (parts > groups) parts = groups;
-  if (parts > 64) parts = 64;
-  if (parts < 1) parts = 1;
-  p.steps = (int)((groups + parts - 1) / parts * 8);
-  if (p.steps < 8) p.steps = 8;
-  p.parts = (int)((p.stages + p.steps - 1) / p.steps);
-  if (p.parts < 1) p.parts = 1;
+  MatmulPlan p = {};
+  p.stages = (int)(fp8_blocks(k) * (kFp8Block / kStep));
+  const int64_t groups = (p.stages + 7) / 8;  // parts begin with a word of exponents
+  double best = 0.;
+  for (int big = 0; big < 2; ++big) {
+    const int64_t b = big ? 256 : 128, tm = (m + b - 1) / b, tn = (n + b - 1) / b, tiles = tm * tn;
+    for (int64_t asked : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      if (asked > 1 && (asked > groups || tiles * asked > 2048)) break;
+      const int64_t steps = groups < 1 ? 8 : (groups + asked - 1) / asked * 8;
+      const int64_t parts = p.stages < 1 ? 1 : (p.stages + steps - 1) / steps;
+      const double t = estimate(big, tiles, parts, steps < p.stages ? steps : p.stages, n * m);
+      if (p.parts > 0 && t >= best) continue;
+      best = t;
+      p.big = big, p.tm = tm, p.tn = tn, p.parts = (int)parts, p.steps = (int)steps;
+    }
+  }
   p.total = p.parts > 1 ? up256((size_t)p.parts * ((size_t)(n * m + 3) & ~(size_t)3) * 4) : 0;
   return p;
 }
+
+// An output larger than the L2s would push the operands out of them (65536 x 4096 x 1024: 370 us
+// past them, 415 through); a smaller one is left for who reads it next (10007 x 1000 x 776: 20 us,
+// 21 past them).
+constexpr int64_t kCaches = (int64_t)32 << 20;
 
 template <class W, bool F16>
 void launch_tiles(const MatmulPlan& p, const MatmulArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)(p.tm * p.tn * p.parts));
   if (p.parts > 1)
-    hipLaunchKernelGGL((matmul_kernel<W, F16, true>), grid, dim3(W::kThreads), 0, st, a);
+    hipLaunchKernelGGL((matmul_kernel<W, F16, kParts>), grid, dim3(W::kThreads), 0, st, a);
+  else if (a.n * a.m * 2 > kCaches)
+    hipLaunchKernelGGL((matmul_kernel<W, F16, kPastCaches>), grid, dim3(W::kThreads), 0, st, a);
   else
-    hipLaunchKernelGGL((matmul_kernel<W, F16, false>), grid, dim3(W::kThreads), 0, st, a);
+    hipLaunchKernelGGL((matmul_kernel<W, F16, kOutput>), grid, dim3(W::kThreads), 0, st, a);
 }
 
 template <bool F16>
@@ -362,7 +395,7 @@ infcl_status matmul_t(const uint8_t* aq, const uint8_t* ae, int64_t n, const uin
   const MatmulPlan p = plan_of(n, m, k);
   MatmulArgs a;
   a.a = aq, a.ae = ae, a.b = bq, a.be = be, a.bias = bias, a.out = out, a.part = (float*)ws, a.n = n, a.m = m;
-  a.kp = fp8_kp(k), a.ep = fp8_ep(k), a.nm = (n * m + 3) & ~(int64_t)3;
+  a.kp = fp8_pitch(k), a.ep = fp8_ep(k), a.nm = (n * m + 3) & ~(int64_t)3;
   a.tm = (int)p.tm, a.tn = (int)p.tn, a.tiles = (int)(p.tm * p.tn), a.stages = p.stages, a.steps = p.steps;
   if (p.big)
     launch_tiles<Big, F16>(p, a, st);
@@ -380,7 +413,7 @@ infcl_status matmul_t(const uint8_t* aq, const uint8_t* ae, int64_t n, const uin
 infcl_status sizes_status(int64_t n, int64_t m, int64_t k) {
   if (n < 0 || m < 1 || k < 0) return INFCL_ERR_INVALID;
   const int64_t most = (int64_t)1 << 27;
-  if (n > most || m > most || k > ((int64_t)1 << 23) || (n > 0 && m > ((int64_t)1 << 38) / n) ||
+  if (n > most || m > ((int64_t)1 << 24) || k > ((int64_t)1 << 23) || (n > 0 && m > ((int64_t)1 << 38) / n) ||
       ((n + 127) / 128) * ((m + 127) / 128) > ((int64_t)1 << 22))
     return INFCL_ERR_UNSUPPORTED;
   return INFCL_OK;
@@ -408,7 +441,7 @@ extern "C" infcl_status infcl_fp8_matmul(const void* aq, const void* aexps, int6
   if (dtype == INFCL_F32) return INFCL_ERR_UNSUPPORTED;
   if (n == 0) return INFCL_OK;
   if ((k > 0 && (!block_aligned(aq, 16) || !block_aligned(aexps, 4) || !block_aligned(bq, 16) || !block_aligned(bexps, 4))) ||
-      ((uintptr_t)bias % 2) != 0 || !block_aligned(out, 16))
+      ((uintptr_t)bias % 4) != 0 || !block_aligned(out, 16))
     return INFCL_ERR_INVALID;
   const size_t need = plan_of(n, m, k).total;
   if (need > 0 && !block_aligned(workspace, 256)) return INFCL_ERR_INVALID;
@@ -422,7 +455,7 @@ extern "C" infcl_status infcl_fp8_linear_workspace(int64_t n, int64_t m, int64_t
   if (!bytes) return INFCL_ERR_INVALID;
   const infcl_status s = sizes_status(n, m, k);
   if (s != INFCL_OK) return s;
-  *bytes = few(n) ? 0 : up256((size_t)n * (size_t)fp8_kp(k)) + up256((size_t)n * (size_t)fp8_ep(k)) + plan_of(n, m, k).total;
+  *bytes = few(n) ? 0 : up256((size_t)n * (size_t)fp8_pitch(k)) + up256((size_t)n * (size_t)fp8_ep(k)) + plan_of(n, m, k).total;
   return INFCL_OK;
 }
 
@@ -435,7 +468,7 @@ extern "C" infcl_status infcl_fp8_linear(const void* x, int64_t x_stride, int64_
   if (dtype == INFCL_F32 || k % 8 != 0 || x_stride % 8 != 0 || x_stride > ((int64_t)1 << 32) || n > ((int64_t)1 << 37) / k)
     return INFCL_ERR_UNSUPPORTED;
   if (n == 0) return INFCL_OK;
-  if (!block_aligned(x, 16) || !block_aligned(wq, 16) || !block_aligned(wexps, 4) || ((uintptr_t)bias % 2) != 0 ||
+  if (!block_aligned(x, 16) || !block_aligned(wq, 16) || !block_aligned(wexps, 4) || ((uintptr_t)bias % 4) != 0 ||
       !block_aligned(out, 16))
     return INFCL_ERR_INVALID;
   size_t need = 0;
@@ -447,14 +480,14 @@ extern "C" infcl_status infcl_fp8_linear(const void* x, int64_t x_stride, int64_
     const dim3 grid((unsigned)((m + 15) / 16)), block(64 * kFewWaves);
     if (dtype == INFCL_BF16)
       hipLaunchKernelGGL((few_kernel<false>), grid, block, 0, st, (const uint16_t*)x, x_stride, (int)n, k, (const uint8_t*)wq,
-                         (const uint8_t*)wexps, m, fp8_kp(k), fp8_ep(k), (const __bf16*)bias, (__bf16*)out);
+                         (const uint8_t*)wexps, m, fp8_pitch(k), fp8_ep(k), (const __bf16*)bias, (__bf16*)out);
     else
       hipLaunchKernelGGL((few_kernel<true>), grid, block, 0, st, (const uint16_t*)x, x_stride, (int)n, k, (const uint8_t*)wq,
-                         (const uint8_t*)wexps, m, fp8_kp(k), fp8_ep(k), (const __bf16*)bias, (__bf16*)out);
+                         (const uint8_t*)wexps, m, fp8_pitch(k), fp8_ep(k), (const __bf16*)bias, (__bf16*)out);
     return launch_status();
   }
   char* q = (char*)workspace;
-  char* e = q + up256((size_t)n * (size_t)fp8_kp(k));
+  char* e = q + up256((size_t)n * (size_t)fp8_pitch(k));
   char* rest = e + up256((size_t)n * (size_t)fp8_ep(k));
   s = infcl_fp8_pack(x, x_stride, n, k, dtype, q, e, nullptr, nullptr, nullptr, nullptr, 0, stream);
   if (s != INFCL_OK) return s;

@@ -119,7 +119,7 @@ def test_fp8_unpack(lib, kw, want):
 @pytest.mark.parametrize("kw,want", [
     (dict(n=-1), INVALID), (dict(m=0), INVALID), (dict(k=-1), INVALID), (dict(dt=8), INVALID), (dict(dt=1), UNSUPPORTED),
     (dict(k=(1 << 23) + 1), UNSUPPORTED), (dict(n=1 << 28), UNSUPPORTED), (dict(n=1 << 26, m=1 << 20), UNSUPPORTED), (dict(a=A + 8), INVALID),
-    (dict(be=None), INVALID), (dict(out=A + 2), INVALID), (dict(bias=A + 1), INVALID), (dict(ws=None), INVALID), (dict(wsb=0), WORKSPACE),
+    (dict(be=None), INVALID), (dict(out=A + 2), INVALID), (dict(bias=A + 2), INVALID), (dict(m=(1 << 24) + 1), UNSUPPORTED), (dict(ws=None), INVALID), (dict(wsb=0), WORKSPACE),
     (dict(n=0, a=None, ae=None, out=None), OK),
 ])
 def test_fp8_matmul(lib, kw, want):

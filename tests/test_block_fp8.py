@@ -31,8 +31,15 @@ TABLE = torch.tensor([_value(b) for b in range(256)], dtype=torch.float64)
 def _held(f):
     """(values in units of the block's power of two [rows, k], exponents) of an Fp8."""
     q = TABLE[f.q.cpu().long()]
-    assert (f.q.cpu()[:, f.k:] == 0).all() or torch.isnan(q).any()  # (what fills up a row)
-    return q[:, :f.k], f.exps.cpu().long()[:, :(f.k + 127) // 128]
+    assert (f.q.cpu()[:, f.k:(f.k + 127) // 128 * 128] == 0).all() or torch.isnan(q).any()  # (what fills up a row)
+    e = f.exps.cpu().long()
+    assert (e[:, (f.k + 127) // 128:] == 127).all()
+    return q[:, :f.k], e[:, :(f.k + 127) // 128]
+
+
+def _q(f):
+    """Its bytes, without what may follow a row's last block."""
+    return f.q[:, :(f.k + 127) // 128 * 128]
 
 
 def _same(f, x):
@@ -43,7 +50,7 @@ def _same(f, x):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("n,d,dtype", [(1, 8, "bf16"), (3, 136, "f16"), (130, 40, "f32"), (5, 1032, "bf16"), (257, 264, "f16"),
-                                       (128, 128, "f32"), (127, 248, "bf16")])
+                                       (128, 128, "f32"), (127, 248, "bf16"), (9, 16384, "bf16")])
 def test_packing_both_ways(n, d, dtype):
     x = _x(n, d, dtype)
     if n > 2:
@@ -52,14 +59,14 @@ def test_packing_both_ways(n, d, dtype):
     a, t = infcl.fp8_pack_both(x.cuda())
     assert a.shape == (n, d) and t.shape == (d, n) and _same(a, x) and _same(t, x.t())
     only = infcl.fp8_pack(x.cuda())
-    assert torch.equal(only.q, a.q) and torch.equal(_held(only)[1], _held(a)[1])
+    assert torch.equal(_q(only), _q(a)) and torch.equal(_held(only)[1], _held(a)[1])
     want = block.unfp8(*block.fp8(x)).to(DT[dtype])
     assert torch.equal(infcl.fp8_unpack(a).cpu(), want)
     assert torch.equal(infcl.fp8_unpack(t).cpu(), block.unfp8(*block.fp8(x.t())).to(DT[dtype]))
     wide = torch.full((n, d + 24), math.nan, dtype=DT[dtype])
     wide[:, 8:8 + d] = x
     v, w = infcl.fp8_pack_both(wide.cuda()[:, 8:8 + d])
-    assert torch.equal(v.q, a.q) and torch.equal(w.q, t.q)
+    assert torch.equal(_q(v), _q(a)) and torch.equal(_q(w), _q(t))
 
 
 @pytest.mark.gpu
@@ -88,6 +95,7 @@ def _whole(n, k, dtype, seed):
 SIZES = [  # n, m, k
     (1, 1, 1), (1, 3, 130), (16, 40, 512), (17, 5, 300), (33, 129, 1), (130, 257, 640), (128, 128, 4096), (300, 24, 9001),
     (520, 300, 4200), (1000, 513, 72), (256, 256, 33000), (700, 2056, 1160), (4099, 1030, 513),
+    (40, 264, 16384), (9000, 1032, 200), (9000, 1031, 136), (20000, 520, 1160), (4096, 4096, 520),
 ]
 
 
