@@ -156,6 +156,22 @@ infcl_status infcl_fp8_linear(const void* x, int64_t x_stride, int64_t n, int64_
                               int64_t m, const void* bias, int dtype, void* out, void* workspace, size_t ws_bytes,
                               void* stream);
 
+/* A layer that learns: out [n, m] = x w^T + bias of x [n, k] and w [m, k] (k and m
+ * multiples of 8), packed here; then dx = dy w, dw = dy^T x and db, the sums of dy's
+ * columns (each may be NULL), of the operands packed along the other side, and dy both
+ * ways.  keeps: INFCL_KEEP_W where dx is to come, INFCL_KEEP_X for dw; `kept` is the same
+ * memory and keeps the same number in both calls (NULL and 0 where neither is to come).
+ * Everything is of dtype, INFCL_BF16 or INFCL_F16. */
+enum { INFCL_KEEP_W = 1, INFCL_KEEP_X = 2 };
+infcl_status infcl_fp8_layer_sizes(int64_t n, int64_t k, int64_t m, int keeps, size_t* kept_bytes, size_t* fwd_bytes,
+                                   size_t* bwd_bytes);
+infcl_status infcl_fp8_layer_fwd(const void* x, int64_t x_stride, int64_t n, int64_t k, const void* w,
+                                 int64_t w_stride, int64_t m, const void* bias, int dtype, int keeps, void* out,
+                                 void* kept, void* workspace, size_t ws_bytes, void* stream);
+infcl_status infcl_fp8_layer_bwd(const void* dy, int64_t dy_stride, int64_t n, int64_t k, int64_t m, int dtype,
+                                 int keeps, const void* kept, void* dx, void* dw, void* db, void* workspace,
+                                 size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

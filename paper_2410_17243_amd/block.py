@@ -88,6 +88,9 @@ def _load():
             "infcl_fp8_matmul_workspace": [i64, i64, i64, psz],
             "infcl_fp8_matmul": [vp, vp, i64, vp, vp, i64, i64, vp, ip, vp, vp, sz, vp],
             "infcl_fp8_linear_workspace": [i64, i64, i64, psz],
+            "infcl_fp8_layer_sizes": [i64, i64, i64, ip, psz, psz, psz],
+            "infcl_fp8_layer_fwd": [vp, i64, i64, i64, vp, i64, i64, vp, ip, ip, vp, vp, vp, sz, vp],
+            "infcl_fp8_layer_bwd": [vp, i64, i64, i64, i64, ip, ip, vp, vp, vp, vp, vp, sz, vp],
             "infcl_fp8_linear": [vp, i64, i64, i64, vp, vp, i64, vp, ip, vp, vp, sz, vp],
         }.items():
             fn = getattr(lib, name)
@@ -489,56 +492,72 @@ def fp8_matmul(a: Fp8, b: Fp8, bias=None, dtype=None):
     return out
 
 
-def _weights(x, w, b):
-    if w.dim() != 2 or w.shape[1] != x.shape[-1] or w.dtype != x.dtype:
-        raise ValueError(f"w must be [m, {x.shape[-1]}] of {x.dtype}, got {tuple(w.shape)} of {w.dtype}")
-    _device(("x", x), ("w", w), *([("b", b)] if b is not None else []))
-    _out16(x.dtype, b, w.shape[0])
+@functools.lru_cache(maxsize=4096)
+def _layer_sizes(n, k, m, keeps):
+    """Bytes of what is kept, of the forward's and of the backward's workspace."""
+    sizes = [ctypes.c_size_t(0) for _ in range(3)]
+    _check(_load().infcl_fp8_layer_sizes(n, k, m, keeps, *(ctypes.byref(s) for s in sizes)), "infcl_fp8_layer_sizes")
+    return tuple(s.value for s in sizes)
 
 
-def _learns(w):
-    if w.shape[0] % 8:
-        raise ValueError(f"linear_fp8: a layer with gradients has a multiple of 8 outputs, got {w.shape[0]}")
+def _learns(m):
+    if m % 8:
+        raise ValueError(f"linear_fp8: a layer with gradients has a multiple of 8 outputs, got {m}")
 
 
 def linear_fp8_fwd(x, w, b=None, need_dx: bool = True, need_dw: bool = True):
     """(x w^T + b from x and w in 8-bit floats, what linear_fp8_bwd needs: both packed the
     other way round, where asked for).  x [*, k], w [m, k], b [m] of one 16-bit dtype."""
-    _weights(x, w, b)
-    if need_dx or need_dw:
-        _learns(w)
-    xq, xt, _ = _fp8_pack(x, True, need_dw)
-    wq, wt, _ = _fp8_pack(w, True, need_dx, name="w")
-    return fp8_matmul(xq, wq, b).view(*x.shape[:-1], w.shape[0]), (xt, wt, b is not None)
+    dev, code = _device(("x", x), ("w", w), *([("b", b)] if b is not None else [])), _code(x, "x")
+    if w.dim() != 2 or w.shape[1] != x.shape[-1] or w.dtype != x.dtype:
+        raise ValueError(f"w must be [m, {x.shape[-1]}] of {x.dtype}, got {tuple(w.shape)} of {w.dtype}")
+    (n, k, xs), (m, _, ws) = _rows(x, "x"), _rows(w, "w")
+    b = _out16(x.dtype, b, m)
+    keeps = need_dx + 2 * need_dw
+    if keeps:
+        _learns(m)
+    elif m % 8:  # (a forward alone takes any number of outputs)
+        return linear_fp8(x, fp8_pack(w), b), (None, (n, k, m, x.dtype, 0, b is not None))
+    size, scratch, _ = _layer_sizes(n, k, m, keeps)
+    out = torch.empty((*x.shape[:-1], m), dtype=x.dtype, device=dev)
+    kept, space = _scratch(size, dev), _scratch(scratch, dev)
+    _call("infcl_fp8_layer_fwd", dev, x.data_ptr(), xs, n, k, w.data_ptr(), ws, m, _ptr(b), code, keeps, out.data_ptr(),
+          _ptr(kept), space.data_ptr(), scratch)
+    return out, (kept, (n, k, m, x.dtype, keeps, b is not None))
 
 
 def linear_fp8_bwd(dy, kept, need=(True, True, True)):
     """(dx, dw, db) of linear_fp8_fwd, None where not kept for or not needed: products of
     dy in 8-bit floats, along its features for dx and along its rows for dw, and its sums."""
-    xt, wt, has_b = kept
-    need_dx, need_dw, need_db = need[0] and wt is not None, need[1] and xt is not None, need[2] and has_b
-    if not (need_dx or need_dw or need_db):
-        return None, None, None
-    dq, dt, db = _fp8_pack(dy, need_dx, need_dw, need_db, name="dy")
-    dx = fp8_matmul(dq, wt).view(*dy.shape[:-1], wt.shape[0]) if need_dx else None
-    return dx, fp8_matmul(dt, xt) if need_dw else None, db
+    kept, (n, k, m, dtype, keeps, has_b) = kept
+    dev = _device(("dy", dy), *([("what was kept", kept)] if kept is not None else []))
+    rows, width, stride = _rows(dy, "dy")
+    if (rows, width, dy.dtype) != (n, m, dtype):
+        raise ValueError(f"dy must be [{n}, {m}] of {dtype}, got {tuple(dy.shape)} of {dy.dtype}")
+    size, _, scratch = _layer_sizes(n, k, m, keeps)
+    if keeps and (kept.dtype != torch.uint8 or kept.numel() != size):
+        raise ValueError(f"what was kept must be {size} bytes, got {kept.numel()} of {kept.dtype}")
+    dx = torch.empty((*dy.shape[:-1], k), dtype=dtype, device=dev) if need[0] and keeps & 1 else None
+    dw = torch.empty((m, k), dtype=dtype, device=dev) if need[1] and keeps & 2 else None
+    db = torch.empty(m, dtype=dtype, device=dev) if need[2] and has_b else None
+    if dx is not None or dw is not None or db is not None:
+        space = _scratch(scratch, dev)
+        _call("infcl_fp8_layer_bwd", dev, dy.data_ptr(), stride, n, k, m, _CODES[dtype], keeps, _ptr(kept), _ptr(dx), _ptr(dw),
+              _ptr(db), space.data_ptr(), scratch)
+    return dx, dw, db
 
 
 class _LinearFp8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, b):
-        y, (xt, wt, has_b) = linear_fp8_fwd(x, w, b, ctx.needs_input_grad[0], ctx.needs_input_grad[1])
-        ctx.save_for_backward(*(p for t in (xt, wt) for p in ((t.q, t.exps) if t else (None, None))))
-        ctx.rest = (xt and (xt.k, xt.dtype), wt and (wt.k, wt.dtype), has_b)
+        y, (kept, ctx.rest) = linear_fp8_fwd(x, w, b, ctx.needs_input_grad[0], ctx.needs_input_grad[1])
+        ctx.save_for_backward(kept)
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        xq, xe, wq, we = ctx.saved_tensors
-        x, w, has_b = ctx.rest
-        kept = (Fp8(xq, xe, *x) if x else None, Fp8(wq, we, *w) if w else None, has_b)
-        return linear_fp8_bwd(dy.contiguous(), kept, ctx.needs_input_grad)
+        return linear_fp8_bwd(dy.contiguous(), (ctx.saved_tensors[0], ctx.rest), ctx.needs_input_grad)
 
 
 def linear_fp8(x, w, b=None):
@@ -553,7 +572,7 @@ def linear_fp8(x, w, b=None):
         dtype = torch.get_autocast_dtype("cuda")
         x, w, b = x.to(dtype), w.to(dtype), None if b is None else b.to(dtype)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, w, b)):
-        _learns(w)
+        _learns(w.shape[0])
     return _LinearFp8.apply(x, w, b)
 
 

@@ -52,15 +52,16 @@ __global__ void __launch_bounds__(256) pack_rows(const PackArgs a) {
   }
 }
 
-// Both, or along columns alone: a tile of 128 x 128.  Lane (g, c), c = 0..15, of the
+// Both, or along columns alone, of one array or of two: a tile of 128 x 128.  Lane (g, c), c = 0..15, of the
 // workgroup's 16 groups: rows 8 g .. 8 g + 7, features 8 c .. 8 c + 7.
 template <int T>
-__global__ void __launch_bounds__(256, 2) pack_tile(const PackArgs a) {
+__global__ void __launch_bounds__(256, 2) pack_tile(const PackArgs one, const PackArgs two, unsigned first) {
+  const PackArgs& a = blockIdx.x < first ? one : two;
   __shared__ uint32_t top[4][128];
   __shared__ float sum[4][128];
   __shared__ __attribute__((aligned(16))) uint8_t tile[128 * 144];  // [feature][row], 16 bytes between rows of it
   const int c = threadIdx.x & 15, g = threadIdx.x >> 4, wave = threadIdx.x >> 6;
-  const int64_t tiles = a.blocks, rt = blockIdx.x / tiles, ct = blockIdx.x - rt * tiles;
+  const int64_t tiles = a.blocks, at = blockIdx.x < first ? blockIdx.x : blockIdx.x - first, rt = at / tiles, ct = at - rt * tiles;
   const int64_t row0 = rt * 128 + 8 * g, col = ct * 128 + 8 * c;
   float v[8][8];
 #pragma unroll
@@ -192,6 +193,8 @@ __global__ void __launch_bounds__(256) unpack_rows(const uint8_t* __restrict__ q
   }
 }
 
+unsigned tiles_of(const PackArgs& a) { return (unsigned)((a.n + 127) / 128 * a.blocks); }
+
 template <int T>
 void pack_t(const PackArgs& a, void* colsum, hipStream_t st) {
   if (!a.qt && !a.sums) {
@@ -199,17 +202,40 @@ void pack_t(const PackArgs& a, void* colsum, hipStream_t st) {
     hipLaunchKernelGGL((pack_rows<T>), dim3((unsigned)(need < 16384 ? need : 16384)), dim3(256), 0, st, a);
     return;
   }
-  const int64_t rows = (a.n + 127) / 128;
-  if (rows > 0) hipLaunchKernelGGL((pack_tile<T>), dim3((unsigned)(rows * a.blocks)), dim3(256), 0, st, a);
+  const unsigned tiles = tiles_of(a);
+  if (tiles > 0) hipLaunchKernelGGL((pack_tile<T>), dim3(tiles), dim3(256), 0, st, a, a, tiles);
   if (a.sums)
-    hipLaunchKernelGGL((join_columns<T>), dim3((unsigned)((a.d + 31) / 32)), dim3(512), 0, st, (const float*)a.sums, rows, a.d, colsum);
+    hipLaunchKernelGGL((join_columns<T>), dim3((unsigned)((a.d + 31) / 32)), dim3(512), 0, st, (const float*)a.sums,
+                       (a.n + 127) / 128, a.d, colsum);
 }
 
 bool sizes_ok(int64_t n, int64_t d) {
   return d % 8 == 0 && d <= ((int64_t)1 << 23) && n <= ((int64_t)1 << 27) && n <= ((int64_t)1 << 37) / d;
 }
 
+PackArgs args_of(const void* x, int64_t x_stride, int64_t n, int64_t d, void* q, void* exps, void* qt, void* expst) {
+  PackArgs a;
+  a.x = x, a.xs = x_stride, a.n = n, a.d = d, a.blocks = fp8_blocks(d), a.kp = fp8_pitch(d), a.ep = fp8_ep(d);
+  a.tp = fp8_pitch(n), a.tep = fp8_ep(n);
+  a.q = (uint8_t*)q, a.ex = (uint8_t*)exps, a.qt = (uint8_t*)qt, a.ext = (uint8_t*)expst, a.sums = nullptr;
+  return a;
+}
+
 }  // namespace
+
+// Two arrays, each along its rows and (qt) along its columns, in one launch; 16 bits.
+infcl_status fp8_pack_two(const void* x, int64_t x_stride, int64_t n, const void* w, int64_t w_stride, int64_t m, int64_t k,
+                          int dtype, void* xq, void* xe, void* xqt, void* xet, void* wq, void* we, void* wqt, void* wet,
+                          hipStream_t st) {
+  const PackArgs a = args_of(x, x_stride, n, k, xq, xe, xqt, xet), b = args_of(w, w_stride, m, k, wq, we, wqt, wet);
+  const unsigned first = tiles_of(a), all = first + tiles_of(b);
+  if (dtype == INFCL_BF16)
+    hipLaunchKernelGGL((pack_tile<kBF16>), dim3(all), dim3(256), 0, st, a, b, first);
+  else
+    hipLaunchKernelGGL((pack_tile<kF16>), dim3(all), dim3(256), 0, st, a, b, first);
+  return launch_status();
+}
+
 }  // namespace infcl
 
 using namespace infcl;
@@ -239,9 +265,7 @@ extern "C" infcl_status infcl_fp8_pack(const void* x, int64_t x_stride, int64_t 
     if (ws_bytes < need) return INFCL_ERR_WORKSPACE;
   }
   if (n == 0 && !colsum) return INFCL_OK;
-  PackArgs a;
-  a.x = x, a.xs = x_stride, a.n = n, a.d = d, a.blocks = fp8_blocks(d), a.kp = fp8_pitch(d), a.ep = fp8_ep(d), a.tp = fp8_pitch(n), a.tep = fp8_ep(n);
-  a.q = (uint8_t*)q, a.ex = (uint8_t*)exps, a.qt = (uint8_t*)qt, a.ext = (uint8_t*)expst;
+  PackArgs a = args_of(x, x_stride, n, d, q, exps, qt, expst);
   a.sums = colsum ? (float*)workspace : nullptr;
   hipStream_t st = (hipStream_t)stream;
   if (dtype == INFCL_BF16)

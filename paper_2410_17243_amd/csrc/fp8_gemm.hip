@@ -22,6 +22,9 @@
 #include "grid.hpp"
 
 namespace infcl {
+infcl_status fp8_pack_two(const void* x, int64_t x_stride, int64_t n, const void* w, int64_t w_stride, int64_t m, int64_t k,
+                          int dtype, void* xq, void* xe, void* xqt, void* xet, void* wq, void* we, void* wqt, void* wet,
+                          hipStream_t st);
 namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -420,6 +423,54 @@ infcl_status sizes_status(int64_t n, int64_t m, int64_t k) {
 }
 bool few(int64_t n) { return n <= 16; }
 
+// Packed operands one after the other in a block of memory: rows x k, values and exponents.
+struct Places {
+  char* at;
+  size_t used = 0;
+  explicit Places(void* p) : at((char*)p) {}
+  void* take(size_t bytes) {
+    void* p = at + used;
+    used += up256(bytes);
+    return p;
+  }
+  void operand(int64_t rows, int64_t k, void*& q, void*& e) {
+    q = take((size_t)rows * (size_t)fp8_pitch(k));
+    e = take((size_t)rows * (size_t)fp8_ep(k));
+  }
+};
+struct LayerPlaces {
+  void *xt = nullptr, *xte = nullptr, *wt = nullptr, *wte = nullptr;  // kept
+  void *x, *xe, *w, *we, *fwd;                                        // the forward's
+  void *dy, *dye, *dyt, *dyte, *sums, *bwd;                           // the backward's
+  size_t kept, fwd_bytes, bwd_bytes;
+};
+LayerPlaces layer_places(int64_t n, int64_t k, int64_t m, int keeps, void* kept, void* ws) {
+  LayerPlaces r;
+  Places p(kept), f(ws), b(ws);
+  if (keeps & INFCL_KEEP_X) p.operand(k, n, r.xt, r.xte);
+  if (keeps & INFCL_KEEP_W) p.operand(k, m, r.wt, r.wte);
+  f.operand(n, k, r.x, r.xe);
+  f.operand(m, k, r.w, r.we);
+  r.fwd = f.take(plan_of(n, m, k).total);
+  b.operand(n, m, r.dy, r.dye);
+  b.operand(m, n, r.dyt, r.dyte);
+  size_t sums = 0;
+  infcl_fp8_pack_workspace(n, m, &sums);
+  r.sums = b.take(sums);
+  const size_t dx = plan_of(n, k, m).total, dw = plan_of(m, k, n).total;
+  r.bwd = b.take(dx > dw ? dx : dw);
+  r.kept = p.used, r.fwd_bytes = f.used, r.bwd_bytes = b.used;
+  return r;
+}
+infcl_status layer_status(int64_t n, int64_t k, int64_t m, int keeps) {
+  if (n < 0 || k < 1 || m < 1 || keeps < 0 || keeps > 3) return INFCL_ERR_INVALID;
+  if (k % 8 != 0 || m % 8 != 0 || n > ((int64_t)1 << 23) || m > ((int64_t)1 << 23) || n > ((int64_t)1 << 37) / (k > m ? k : m))
+    return INFCL_ERR_UNSUPPORTED;
+  infcl_status s = sizes_status(n, m, k);
+  if (s == INFCL_OK) s = sizes_status(n, k, m);
+  return s == INFCL_OK ? sizes_status(m, k, n) : s;
+}
+
 }  // namespace
 }  // namespace infcl
 
@@ -492,4 +543,56 @@ extern "C" infcl_status infcl_fp8_linear(const void* x, int64_t x_stride, int64_
   s = infcl_fp8_pack(x, x_stride, n, k, dtype, q, e, nullptr, nullptr, nullptr, nullptr, 0, stream);
   if (s != INFCL_OK) return s;
   return infcl_fp8_matmul(q, e, n, wq, wexps, m, k, bias, dtype, out, rest, ws_bytes - (size_t)(rest - q), stream);
+}
+
+extern "C" infcl_status infcl_fp8_layer_sizes(int64_t n, int64_t k, int64_t m, int keeps, size_t* kept_bytes,
+                                              size_t* fwd_bytes, size_t* bwd_bytes) {
+  const infcl_status s = layer_status(n, k, m, keeps);
+  if (s != INFCL_OK) return s;
+  if (!kept_bytes || !fwd_bytes || !bwd_bytes) return INFCL_ERR_INVALID;
+  const LayerPlaces r = layer_places(n, k, m, keeps, nullptr, nullptr);
+  *kept_bytes = r.kept, *fwd_bytes = r.fwd_bytes, *bwd_bytes = r.bwd_bytes;
+  return INFCL_OK;
+}
+
+extern "C" infcl_status infcl_fp8_layer_fwd(const void* x, int64_t x_stride, int64_t n, int64_t k, const void* w,
+                                            int64_t w_stride, int64_t m, const void* bias, int dtype, int keeps,
+                                            void* out, void* kept, void* workspace, size_t ws_bytes, void* stream) {
+  infcl_status s = layer_status(n, k, m, keeps);
+  if (s != INFCL_OK) return s;
+  if (!type_known(dtype) || x_stride < k || w_stride < k) return INFCL_ERR_INVALID;
+  if (dtype == INFCL_F32 || x_stride % 8 != 0 || w_stride % 8 != 0 || x_stride > ((int64_t)1 << 32) ||
+      w_stride > ((int64_t)1 << 32))
+    return INFCL_ERR_UNSUPPORTED;
+  if ((n > 0 && (!block_aligned(x, 16) || !block_aligned(out, 16))) || !block_aligned(w, 16) || ((uintptr_t)bias % 4) != 0 ||
+      (keeps && !block_aligned(kept, 256)) || !block_aligned(workspace, 256))
+    return INFCL_ERR_INVALID;
+  const LayerPlaces r = layer_places(n, k, m, keeps, kept, workspace);
+  if (ws_bytes < r.fwd_bytes) return INFCL_ERR_WORKSPACE;
+  hipStream_t st = (hipStream_t)stream;
+  s = fp8_pack_two(x, x_stride, n, w, w_stride, m, k, dtype, r.x, r.xe, r.xt, r.xte, r.w, r.we, r.wt, r.wte, st);
+  if (s != INFCL_OK || n == 0) return s;
+  return infcl_fp8_matmul(r.x, r.xe, n, r.w, r.we, m, k, bias, dtype, out, r.fwd, ws_bytes, stream);
+}
+
+extern "C" infcl_status infcl_fp8_layer_bwd(const void* dy, int64_t dy_stride, int64_t n, int64_t k, int64_t m,
+                                            int dtype, int keeps, const void* kept, void* dx, void* dw, void* db,
+                                            void* workspace, size_t ws_bytes, void* stream) {
+  infcl_status s = layer_status(n, k, m, keeps);
+  if (s != INFCL_OK) return s;
+  if (!type_known(dtype) || dy_stride < m || (dx && !(keeps & INFCL_KEEP_W)) || (dw && !(keeps & INFCL_KEEP_X)))
+    return INFCL_ERR_INVALID;
+  if (dtype == INFCL_F32 || dy_stride % 8 != 0 || dy_stride > ((int64_t)1 << 32)) return INFCL_ERR_UNSUPPORTED;
+  if (!dx && !dw && !db) return INFCL_OK;
+  if ((n > 0 && !block_aligned(dy, 16)) || ((uintptr_t)dx % 16) != 0 || ((uintptr_t)dw % 16) != 0 || ((uintptr_t)db % 4) != 0 ||
+      ((dx || dw) && !block_aligned(kept, 256)) || !block_aligned(workspace, 256))
+    return INFCL_ERR_INVALID;
+  const LayerPlaces r = layer_places(n, k, m, keeps, (void*)kept, workspace);
+  if (ws_bytes < r.bwd_bytes) return INFCL_ERR_WORKSPACE;
+  s = infcl_fp8_pack(dy, dy_stride, n, m, dtype, dx ? r.dy : nullptr, dx ? r.dye : nullptr, dw ? r.dyt : nullptr,
+                     dw ? r.dyte : nullptr, db, r.sums, ws_bytes, stream);
+  if (s != INFCL_OK) return s;
+  if (dx && n > 0) s = infcl_fp8_matmul(r.dy, r.dye, n, r.wt, r.wte, k, m, nullptr, dtype, dx, r.bwd, ws_bytes, stream);
+  if (s != INFCL_OK || !dw) return s;
+  return infcl_fp8_matmul(r.dyt, r.dyte, m, r.xt, r.xte, k, n, nullptr, dtype, dw, r.bwd, ws_bytes, stream);
 }

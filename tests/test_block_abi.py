@@ -21,7 +21,7 @@ def lib():
 
 def test_exports_every_declared_function(lib):
     names = infcl.header_functions(infcl.BLOCK_HEADER_PATH)
-    assert len(names) == 12
+    assert len(names) == 15
     for n in names:
         assert hasattr(lib, n), n
 
@@ -137,6 +137,30 @@ def test_fp8_linear(lib, kw, want):
     a = dict(x=A, stride=4096, n=40, k=4096, w=A, we=A, m=8, bias=None, dt=0, out=A, ws=A, wsb=BIG) | kw
     assert lib.infcl_fp8_linear(a["x"], a["stride"], a["n"], a["k"], a["w"], a["we"], a["m"], a["bias"], a["dt"], a["out"], a["ws"],
                                 a["wsb"], None) == want
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(n=-1), INVALID), (dict(k=0), INVALID), (dict(keeps=4), INVALID), (dict(dt=9), INVALID), (dict(xs=8), INVALID), (dict(ws=8), INVALID),
+    (dict(x=A + 2), INVALID), (dict(w=None), INVALID), (dict(b=A + 2), INVALID), (dict(kept=None), INVALID), (dict(space=A + 16), INVALID),
+    (dict(out=A + 8), INVALID), (dict(bytes=256), WORKSPACE), (dict(k=12), UNSUPPORTED), (dict(m=12), UNSUPPORTED), (dict(dt=1), UNSUPPORTED),
+    (dict(xs=20), UNSUPPORTED), (dict(ws=20), UNSUPPORTED), (dict(n=(1 << 23) + 1), UNSUPPORTED),
+])
+def test_fp8_layer_forward(lib, kw, want):
+    a = dict(x=A, xs=16, n=3, k=16, w=A, ws=16, m=8, b=A, dt=0, keeps=3, out=A, kept=A, space=A, bytes=BIG) | kw
+    assert lib.infcl_fp8_layer_fwd(a["x"], a["xs"], a["n"], a["k"], a["w"], a["ws"], a["m"], a["b"], a["dt"], a["keeps"], a["out"],
+                                   a["kept"], a["space"], a["bytes"], None) == want
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(n=-1), INVALID), (dict(keeps=-1), INVALID), (dict(dys=4), INVALID), (dict(keeps=1), INVALID), (dict(keeps=2), INVALID),
+    (dict(dy=A + 2), INVALID), (dict(dx=A + 2), INVALID), (dict(dw=A + 2), INVALID), (dict(db=A + 2), INVALID), (dict(kept=None), INVALID),
+    (dict(space=None), INVALID), (dict(bytes=256), WORKSPACE), (dict(dt=1), UNSUPPORTED), (dict(dys=12), UNSUPPORTED),
+    (dict(dx=None, dw=None, db=None, dy=None), OK),
+])
+def test_fp8_layer_backward(lib, kw, want):
+    a = dict(dy=A, dys=8, n=3, k=16, m=8, dt=0, keeps=3, kept=A, dx=A, dw=A, db=A, space=A, bytes=BIG) | kw
+    assert lib.infcl_fp8_layer_bwd(a["dy"], a["dys"], a["n"], a["k"], a["m"], a["dt"], a["keeps"], a["kept"], a["dx"], a["dw"], a["db"],
+                                   a["space"], a["bytes"], None) == want
 
 
 def test_workspaces(lib):
