@@ -19,6 +19,28 @@ __device__ __forceinline__ void load8(const void* p, int64_t at, float (&x)[8]) 
     Chunk<T>::load(*(const u32x4*)((const uint16_t*)p + at), x);
   }
 }
+// The bits of a chunk, for loads that are to be under way together before the first is used.
+template <int T>
+struct Raw8 {
+  u32x4 w[T == kF32 ? 2 : 1];
+  __device__ __forceinline__ void load(const void* p, int64_t at) {
+    const u32x4* q = (const u32x4*)((const char*)p + at * (T == kF32 ? 4 : 2));
+#pragma unroll
+    for (int i = 0; i < (T == kF32 ? 2 : 1); ++i) w[i] = q[i];
+  }
+  // (zeros where the chunk is not there)
+  __device__ __forceinline__ void get(bool there, float (&x)[8]) const {
+    if constexpr (T == kF32) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = there ? __uint_as_float(w[e >> 2][e & 3]) : 0.f;
+    } else {
+      u32x4 c = w[0];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[i] = there ? c[i] : 0;
+      Chunk<T>::load(c, x);
+    }
+  }
+};
 template <int T>
 __device__ __forceinline__ void store8(void* p, int64_t at, const float (&x)[8]) {
   if constexpr (T == kF32) {

@@ -61,15 +61,17 @@ __global__ void __launch_bounds__(256, 2) pack_tile(const PackArgs one, const Pa
   __shared__ float sum[4][128];
   __shared__ __attribute__((aligned(16))) uint8_t tile[128 * 144];  // [feature][row], 16 bytes between rows of it
   const int c = threadIdx.x & 15, g = threadIdx.x >> 4, wave = threadIdx.x >> 6;
-  const int64_t tiles = a.blocks, at = blockIdx.x < first ? blockIdx.x : blockIdx.x - first, rt = at / tiles, ct = at - rt * tiles;
+  const uint32_t at = blockIdx.x < first ? blockIdx.x : blockIdx.x - first, across = (uint32_t)a.blocks;
+  const int64_t tiles = a.blocks, rt = at / across, ct = at % across;
   const int64_t row0 = rt * 128 + 8 * g, col = ct * 128 + 8 * c;
+  // all loads first, of some other row or chunk where there is none (one at a time, each in a
+  // branch of its own, 10007 x 776 took 16 us instead of 10)
+  Raw8<T> raw[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) raw[r].load(a.x, (row0 + r < a.n ? row0 + r : a.n - 1) * a.xs + (col < a.d ? col : 0));
   float v[8][8];
 #pragma unroll
-  for (int r = 0; r < 8; ++r) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[r][e] = 0.f;
-    if (row0 + r < a.n && col < a.d) load8<T>(a.x, (row0 + r) * a.xs + col, v[r]);
-  }
+  for (int r = 0; r < 8; ++r) raw[r].get(row0 + r < a.n && col < a.d, v[r]);
   if (a.q) {
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
