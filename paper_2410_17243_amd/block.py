@@ -117,6 +117,19 @@ def _bytes(name, *sizes) -> int:
     return n.value
 
 
+def _where(names, tensors):
+    """The one device of the tensors that are there, the first of which is (small calls are
+    bound by host time: _device names what is wrong)."""
+    dev = tensors[0].device
+    if dev.type == "cuda":
+        for t in tensors:
+            if t is not None and t.device != dev:
+                break
+        else:
+            return dev
+    return _device(*((k, t) for k, t in zip(names, tensors) if t is not None))
+
+
 def _scratch(n, dev):
     return torch.empty(n, dtype=torch.uint8, device=dev) if n else None
 
@@ -129,36 +142,40 @@ def rotary_freqs(sections, base: float = 10000.0, device="cuda"):
     return torch.cat([base ** (-torch.arange(s, dtype=torch.float64) / s) for s in sections]).float().to(device)
 
 
-def _turn(x, pos, freqs, sections, turned, paired, back, name):
-    dev = _device((name, x), ("pos", pos), ("freqs", freqs))
-    code, view = _code(x, name), _heads_view(x, name)
-    n, heads, hd = x.shape
-    if pos.dtype not in (torch.int32, torch.float32):
-        raise TypeError(f"pos must be int32 or float32, got {pos.dtype}")
-    if pos.dim() not in (1, 2) or pos.shape[0] != n or pos.dim() == 2 and pos.stride(1) != 1 and pos.shape[1] > 1:
-        raise ValueError(f"pos must be [{n}] or [{n}, axes] with a token's positions next to each other, got "
-                         f"{tuple(pos.shape)}, strides {pos.stride()}")
-    axes = 1 if pos.dim() == 1 else pos.shape[1]
-    if freqs.dtype != torch.float32 or freqs.dim() != 1 or not freqs.is_contiguous():
-        raise ValueError(f"freqs must be a contiguous float32 vector, got {freqs.dtype} {tuple(freqs.shape)}")
+@functools.lru_cache(maxsize=4096)
+def _rotary_plan(n, heads, hd, code, turned, paired, back, axes, pos_f32, stride, pairs, sections):
+    """infcl_rotary_shape for these sizes."""
     if sections is None:
-        sections = (freqs.numel(),)
+        sections = (pairs,)
     sections = (sections,) if isinstance(sections, int) else tuple(int(s) for s in sections)
-    if len(sections) != axes or not 1 <= axes <= 4 or sum(sections) != freqs.numel():
-        raise ValueError(f"sections must be the pairs of each of {axes} axes (1 to 4), {freqs.numel()} in all, got {sections}")
+    if len(sections) != axes or not 1 <= axes <= 4 or sum(sections) != pairs:
+        raise ValueError(f"sections must be the pairs of each of {axes} axes (1 to 4), {pairs} in all, got {sections}")
     if paired not in PAIRED:
         raise ValueError(f"paired must be one of {list(PAIRED)}, got {paired!r}")
     turned = heads if turned is None else int(turned)
     if not 0 <= turned <= heads:
         raise ValueError(f"turned must be 0 to {heads} heads, got {turned}")
+    return ctypes.byref(_Rotary(n, heads, turned, hd, code, PAIRED[paired], back, axes, pos_f32, (_i32 * 4)(*sections), stride))
+
+
+def _turn(x, pos, freqs, sections, turned, paired, back, name):
+    dev = _where((name, "pos", "freqs"), (x, pos, freqs))
+    code, view = _code(x, name), _heads_view(x, name)
+    n, heads, hd = x.shape
+    if pos.dtype not in (torch.int32, torch.float32):
+        raise TypeError(f"pos must be int32 or float32, got {pos.dtype}")
+    shape, stride = pos.shape, pos.stride()
+    if len(shape) not in (1, 2) or shape[0] != n or len(shape) == 2 and stride[1] != 1 and shape[1] > 1:
+        raise ValueError(f"pos must be [{n}] or [{n}, axes] with a token's positions next to each other, got "
+                         f"{tuple(shape)}, strides {stride}")
+    if freqs.dtype != torch.float32 or freqs.dim() != 1 or not freqs.is_contiguous():
+        raise ValueError(f"freqs must be a contiguous float32 vector, got {freqs.dtype} {tuple(freqs.shape)}")
+    plan = _rotary_plan(n, heads, hd, code, turned, paired, back, 1 if len(shape) == 1 else shape[1],
+                        int(pos.dtype == torch.float32), stride[0] if n > 1 else 0, freqs.shape[0],
+                        tuple(sections) if isinstance(sections, list) else sections)
     out = torch.empty((n, heads, hd), dtype=x.dtype, device=dev)
-    if out.numel() == 0:
-        return out
-    stride = pos.stride(0) if n > 1 else 0
-    shape = _Rotary(n, heads, turned, hd, code, PAIRED[paired], back, axes, int(pos.dtype == torch.float32),
-                    (_i32 * 4)(*sections), stride)
-    _call("infcl_rotary", dev, ctypes.byref(shape), view, _View(out.data_ptr(), heads * hd, hd), pos.data_ptr(),
-          freqs.data_ptr())
+    if n:
+        _call("infcl_rotary", dev, plan, view, _View(out.data_ptr(), heads * hd, hd), pos.data_ptr(), freqs.data_ptr())
     return out
 
 
@@ -213,7 +230,7 @@ def _drop(p, seed, site, row0, dev):
 
 
 def _dropped(x, p, seed, site, row0, name):
-    dev, code = _device((name, x)), _code(x, name)
+    dev, code = _where((name,), (x,)), _code(x, name)
     n, d, stride = _rows(x, name)
     drop = _drop(p, seed, site, row0, dev)
     out = torch.empty(x.shape, dtype=x.dtype, device=dev)
@@ -258,6 +275,7 @@ def dropout(x, p: float, seed, site: int = 0, row0: int = 0):
 # -------------------------------------------------------------- residual norms
 
 _VECTORS = ("gate", "post_w", "post_b", "pre_w", "pre_b")
+_NAMES = ("x", "y", *_VECTORS)
 
 
 class AddNormKept:
@@ -272,7 +290,7 @@ class AddNormKept:
 def _norm_call(x, y, vectors, options):
     """Checks the arguments; (device, infcl_add_norm)."""
     norm, eps, alpha, p, seed, site, row0 = options
-    dev = _device(("x", x), *((k, t) for k, t in zip(("y", *_VECTORS), (y, *vectors)) if t is not None))
+    dev = _where(_NAMES, (x, y, *vectors))
     n, d, xs = _rows(x, "x")
     ys = 0
     gate, post_w, post_b, pre_w, pre_b = vectors
@@ -288,18 +306,25 @@ def _norm_call(x, y, vectors, options):
         raise ValueError(f"norm must be one of {list(NORMS)}, got {norm!r}")
     if post_b is not None and post_w is None or pre_b is not None and pre_w is None:
         raise ValueError("a norm's bias comes with its weight")
-    wdtype = None
-    for k, t in zip(_VECTORS, vectors):
+    wdtype, dtype, ptrs = None, x.dtype, []
+    for t in vectors:
         if t is None:
+            ptrs.append(None)
             continue
-        if t.shape != (d,) or not t.is_contiguous() or t.dtype not in (torch.float32, x.dtype):
-            raise ValueError(f"{k} must be contiguous [{d}] of float32 or {x.dtype}, got {t.dtype} {tuple(t.shape)}")
-        if wdtype not in (None, t.dtype):
-            raise ValueError(f"gate and the norms' vectors must be of one dtype, got {wdtype} and {t.dtype}")
+        if t.dtype is not wdtype and (wdtype is not None or t.dtype not in (torch.float32, dtype)) or t.shape != (d,) or not t.is_contiguous():
+            _wrong_vector(vectors, d, dtype)
         wdtype = t.dtype
+        ptrs.append(t.data_ptr())
     code = _code(x, "x")
     return dev, _AddNorm(n, d, code, code if wdtype is None else _CODES[wdtype], NORMS[norm], eps, alpha,
-                         _drop(p, seed, site, row0, dev), xs, ys, *(_ptr(t) for t in vectors))
+                         _drop(p, seed, site, row0, dev), xs, ys, *ptrs)
+
+
+def _wrong_vector(vectors, d, dtype):
+    for k, t in zip(_VECTORS, vectors):
+        if t is not None and (t.shape != (d,) or not t.is_contiguous() or t.dtype not in (torch.float32, dtype)):
+            raise ValueError(f"{k} must be contiguous [{d}] of float32 or {dtype}, got {t.dtype} {tuple(t.shape)}")
+    raise ValueError(f"gate and the norms' vectors must be of one dtype, got {[t.dtype for t in vectors if t is not None]}")
 
 
 def add_norm_fwd(x, y=None, gate=None, post_w=None, post_b=None, pre_w=None, pre_b=None, norm: str = "layer",
@@ -322,6 +347,14 @@ def add_norm_fwd(x, y=None, gate=None, post_w=None, post_b=None, pre_w=None, pre
     return h, z, AddNormKept(x, y, vectors, stats, options) if need_grad else None
 
 
+@functools.lru_cache(maxsize=4096)
+def _norm_bytes(n, d):
+    """Bytes of the backward's workspace, which rows and features alone decide."""
+    a, size = _AddNorm(n, d, 0, 0, 0, 0.0, 1.0, _Drop(), d, d), ctypes.c_size_t(0)
+    _check(_load().infcl_add_norm_bwd_workspace(ctypes.byref(a), ctypes.byref(size)), "infcl_add_norm_bwd_workspace")
+    return size.value
+
+
 def add_norm_bwd(dh, dz, kept: AddNormKept, need=(True,) * 7):
     """Gradients from those of h and z (None: zeros): (dx, dy, dgate, dpost_w, dpost_b,
     dpre_w, dpre_b), None for what was not given or is not needed.  Without y, dx counts
@@ -335,18 +368,17 @@ def add_norm_bwd(dh, dz, kept: AddNormKept, need=(True,) * 7):
     strides = [0, 0]
     for i, (name, t) in enumerate((("dh", dh), ("dz", dz))):
         if t is not None:
-            _device(("x", x), (name, t))
+            _where(("x", name), (x, t))
             if t.shape != x.shape or t.dtype != x.dtype:
                 raise ValueError(f"{name} must be {tuple(x.shape)} of {x.dtype}, got {tuple(t.shape)} of {t.dtype}")
             strides[i] = _rows(t, name)[2]
     grads = [torch.empty(x.shape, dtype=x.dtype, device=dev) if t is not None and w else None for t, w in zip((x, y), need)]
     grads += [torch.empty_like(t) if t is not None and w else None for t, w in zip(vectors, need[2:])]
-    n = ctypes.c_size_t(0)
-    _check(_load().infcl_add_norm_bwd_workspace(ctypes.byref(a), ctypes.byref(n)), "infcl_add_norm_bwd_workspace")
-    ws = _scratch(n.value, dev)
+    size = _norm_bytes(a.n, a.d)
+    ws = _scratch(size, dev)
     g = _AddNormGrads(_ptr(dh), _ptr(dz), *strides, *(_ptr(t) for t in grads))
     _call("infcl_add_norm_bwd", dev, ctypes.byref(a), x.data_ptr(), _ptr(y), kept.stats.data_ptr(), ctypes.byref(g),
-          ws.data_ptr(), n.value)
+          ws.data_ptr(), size)
     return tuple(grads)
 
 
@@ -427,7 +459,7 @@ def _check_fp8(f, name):
 
 
 def _fp8_pack(x, along=True, across=False, sums=False, name="x"):
-    dev, code = _device((name, x)), _code(x, name)
+    dev, code = _where((name,), (x,)), _code(x, name)
     n, d, stride = _rows(x, name)
     a = _fp8_room(n, d, x.dtype, dev) if along else None
     t = _fp8_room(d, n, x.dtype, dev) if across else None
@@ -475,8 +507,7 @@ def fp8_matmul(a: Fp8, b: Fp8, bias=None, dtype=None):
     """a b^T + bias, [rows of a, rows of b] in dtype (a's by default; bfloat16 or float16)."""
     _check_fp8(a, "a")
     _check_fp8(b, "b")
-    dev = _device(("a", a.q), ("a's exponents", a.exps), ("b", b.q), ("b's exponents", b.exps),
-                  *([("bias", bias)] if bias is not None else []))
+    dev = _where(("a", "a's exponents", "b", "b's exponents", "bias"), (a.q, a.exps, b.q, b.exps, bias))
     (n, k), (m, bk) = a.shape, b.shape
     if k != bk:
         raise ValueError(f"a and b must have rows of one length, got {k} and {bk}")
@@ -508,7 +539,7 @@ def _learns(m):
 def linear_fp8_fwd(x, w, b=None, need_dx: bool = True, need_dw: bool = True):
     """(x w^T + b from x and w in 8-bit floats, what linear_fp8_bwd needs: both packed the
     other way round, where asked for).  x [*, k], w [m, k], b [m] of one 16-bit dtype."""
-    dev, code = _device(("x", x), ("w", w), *([("b", b)] if b is not None else [])), _code(x, "x")
+    dev, code = _where(("x", "w", "b"), (x, w, b)), _code(x, "x")
     if w.dim() != 2 or w.shape[1] != x.shape[-1] or w.dtype != x.dtype:
         raise ValueError(f"w must be [m, {x.shape[-1]}] of {x.dtype}, got {tuple(w.shape)} of {w.dtype}")
     (n, k, xs), (m, _, ws) = _rows(x, "x"), _rows(w, "w")
@@ -530,7 +561,7 @@ def linear_fp8_bwd(dy, kept, need=(True, True, True)):
     """(dx, dw, db) of linear_fp8_fwd, None where not kept for or not needed: products of
     dy in 8-bit floats, along its features for dx and along its rows for dw, and its sums."""
     kept, (n, k, m, dtype, keeps, has_b) = kept
-    dev = _device(("dy", dy), *([("what was kept", kept)] if kept is not None else []))
+    dev = _where(("dy", "what was kept"), (dy, kept))
     rows, width, stride = _rows(dy, "dy")
     if (rows, width, dy.dtype) != (n, m, dtype):
         raise ValueError(f"dy must be [{n}, {m}] of {dtype}, got {tuple(dy.shape)} of {dy.dtype}")
@@ -583,7 +614,7 @@ def _linear_packed(x, w, b):
     if torch.is_autocast_enabled("cuda"):
         x = x.to(torch.get_autocast_dtype("cuda"))
         b = None if b is None else b.to(x.dtype)
-    dev = _device(("x", x), ("w", w.q), ("w's exponents", w.exps), *([("b", b)] if b is not None else []))
+    dev = _where(("x", "w", "w's exponents", "b"), (x, w.q, w.exps, b))
     n, k, stride = _rows(x, "x")
     m = w.shape[0]
     if k != w.k:

@@ -111,8 +111,8 @@ __device__ __forceinline__ void load_vectors(const NormArgs& a, bool in, int64_t
 
 // WIDE: 0, rows within a wave; else rows of up to that many lanes.  FULL: with a gate, a
 // norm of y or a dropout; without, the registers of their vectors and sums are free for
-// more waves.
-template <int T, int WIDE, bool FULL>
+// more waves.  FAR: rows' outputs are past the caches.
+template <int T, int WIDE, bool FULL, bool FAR>
 __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE == 1024 ? 4 : 2) norm_fwd(const NormArgs a) {
   __shared__ float buf[2][16][2];
   int64_t row, step;
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE == 1024 ? 4 : 2) norm_
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = fmaf(a.alpha, x[e], FULL ? w.gate[e] * t[e] : t[e]);
-      if (in) store8<T>(a.h, row * (8 * (int64_t)a.c) + col, x);
+      if (in) store8<T, FAR>(a.h, row * (8 * (int64_t)a.c) + col, x);
     }
     if (a.pre_w) {
       if (!in)
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE == 1024 ? 4 : 2) norm_
       norm_row<WIDE>(x, in, a, m2, r2, buf, turn);
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], w.w2[e], w.b2[e]);
-      if (in) store8<T>(a.z, row * (8 * (int64_t)a.c) + col, x);
+      if (in) store8<T, FAR>(a.z, row * (8 * (int64_t)a.c) + col, x);
     }
     if (a.stats && chunk == 0) a.stats[row] = make_float4(m1, r1, m2, r2);
   }
@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE == 1024 ? 4 : 2) norm_
 // first bias and the gate are in LDS, each lane its own 32 bytes of them, and 16 waves fit
 // (everything, us with registers and with LDS: 50001 x 1160 348 and 320, 8001 x 8192 457 and 294;
 // but 50001 x 768 174 and 205, 30001 x 2048 214 and 265).
-template <int T, int WIDE, bool FULL, bool BIAS>
+template <int T, int WIDE, bool FULL, bool BIAS, bool FAR>
 __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE >= 512 || !BIAS ? 4 : 2) norm_bwd(const NormArgs a) {
   __shared__ float buf[2][16][2];
   __shared__ float joined[WIDE ? 1 : 4][WIDE ? 1 : 512];
@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE >= 512 || !BIAS ? 4 : 
       float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = a.alpha * e8[e];
-      store8<T>(a.dx, row * (8 * (int64_t)a.c) + col, o);
+      store8<T, FAR>(a.dx, row * (8 * (int64_t)a.c) + col, o);
     }
     if (!a.y) continue;
     if constexpr (FULL) {
@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE >= 512 || !BIAS ? 4 : 
         for (int e = 0; e < 8; ++e) e8[e] = st.y * (e8[e] - fmaf(v[e], k, m));
       }
     }
-    if (a.dy && in) store8<T>(a.dy, row * (8 * (int64_t)a.c) + col, e8);
+    if (a.dy && in) store8<T, FAR>(a.dy, row * (8 * (int64_t)a.c) + col, e8);
   }
   if (FULL && drop)
 #pragma unroll
@@ -441,42 +441,54 @@ NormArgs args_of(const infcl_add_norm* a, const Shape& s, const void* x, const v
   return r;
 }
 
-template <int T, bool FULL>
+template <int T, bool FULL, bool FAR>
 void fwd_t(const NormArgs& r, const Shape& s, hipStream_t st) {
   const dim3 grid(grid_of(s, r.n, kFwdWaves)), block(s.threads);
   if (s.threads > 512)
-    hipLaunchKernelGGL((norm_fwd<T, 1024, FULL>), grid, block, 0, st, r);
+    hipLaunchKernelGGL((norm_fwd<T, 1024, FULL, FAR>), grid, block, 0, st, r);
   else if (s.wide)
-    hipLaunchKernelGGL((norm_fwd<T, 512, FULL>), grid, block, 0, st, r);
+    hipLaunchKernelGGL((norm_fwd<T, 512, FULL, FAR>), grid, block, 0, st, r);
   else
-    hipLaunchKernelGGL((norm_fwd<T, 0, FULL>), grid, block, 0, st, r);
+    hipLaunchKernelGGL((norm_fwd<T, 0, FULL, FAR>), grid, block, 0, st, r);
 }
-template <int T, bool FULL, bool BIAS>
+template <int T, bool FULL, bool BIAS, bool FAR>
 void bwd_t(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
   const dim3 grid(wgs), block(s.threads);
   const size_t own = FULL && BIAS ? 8 * 16 * (size_t)s.threads : 0;
   if (all_in_registers(s) && FULL && BIAS)
-    hipLaunchKernelGGL((norm_bwd<T, FULL && BIAS ? 256 : 512, FULL, BIAS>), grid, block, 0, st, r);
+    hipLaunchKernelGGL((norm_bwd<T, FULL && BIAS ? 256 : 512, FULL, BIAS, FAR>), grid, block, 0, st, r);
   else if (s.threads > 512)
-    hipLaunchKernelGGL((norm_bwd<T, 1024, FULL, BIAS>), grid, block, own, st, r);
+    hipLaunchKernelGGL((norm_bwd<T, 1024, FULL, BIAS, FAR>), grid, block, own, st, r);
   else if (s.wide)
-    hipLaunchKernelGGL((norm_bwd<T, 512, FULL, BIAS>), grid, block, own, st, r);
+    hipLaunchKernelGGL((norm_bwd<T, 512, FULL, BIAS, FAR>), grid, block, own, st, r);
   else
-    hipLaunchKernelGGL((norm_bwd<T, 0, FULL, BIAS>), grid, block, 0, st, r);
+    hipLaunchKernelGGL((norm_bwd<T, 0, FULL, BIAS, FAR>), grid, block, 0, st, r);
 }
 bool full(const NormArgs& r) { return r.gate || r.post_w || r.drop.cut; }
+template <int T, bool FAR>
+void fwd_far(const NormArgs& r, const Shape& s, hipStream_t st) {
+  full(r) ? fwd_t<T, true, FAR>(r, s, st) : fwd_t<T, false, FAR>(r, s, st);
+}
+template <int T, bool FAR>
+void bwd_far(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
+  if (!full(r))
+    bwd_t<T, false, true, FAR>(r, s, wgs, st);
+  else if (r.post_b || r.pre_b)
+    bwd_t<T, true, true, FAR>(r, s, wgs, st);
+  else
+    bwd_t<T, true, false, FAR>(r, s, wgs, st);
+}
+template <int T>
+bool far(const NormArgs& r) {
+  return r.n * r.c * 8 * (T == kF32 ? 4 : 2) > kL2Bytes;
+}
 template <int T>
 void fwd_any(const NormArgs& r, const Shape& s, hipStream_t st) {
-  full(r) ? fwd_t<T, true>(r, s, st) : fwd_t<T, false>(r, s, st);
+  far<T>(r) ? fwd_far<T, true>(r, s, st) : fwd_far<T, false>(r, s, st);
 }
 template <int T>
 void bwd_any(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
-  if (!full(r))
-    bwd_t<T, false, true>(r, s, wgs, st);
-  else if (r.post_b || r.pre_b)
-    bwd_t<T, true, true>(r, s, wgs, st);
-  else
-    bwd_t<T, true, false>(r, s, wgs, st);
+  far<T>(r) ? bwd_far<T, true>(r, s, wgs, st) : bwd_far<T, false>(r, s, wgs, st);
 }
 template <int T>
 void join_t(const NormArgs& r, unsigned wgs, int sums, void* const* o, hipStream_t st) {

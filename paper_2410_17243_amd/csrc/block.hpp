@@ -51,6 +51,22 @@ __device__ __forceinline__ void store8(void* p, int64_t at, const float (&x)[8])
     *(u32x4*)((uint16_t*)p + at) = Chunk<T>::store(x);
   }
 }
+// ... past the caches with FAR: outputs larger than the L2s only push out what is read
+// (dropout of 65536 x 4096 both ways 384 us, 397 through them; 50001 x 16 heads of 80 turned both ways
+// 115 and 118; smaller outputs are left for who reads them next).
+constexpr int64_t kL2Bytes = (int64_t)32 << 20;
+template <int T, bool FAR>
+__device__ __forceinline__ void store8(void* p, int64_t at, const float (&x)[8]) {
+  if constexpr (!FAR) {
+    store8<T>(p, at, x);
+  } else if constexpr (T == kF32) {
+    f32x4* q = (f32x4*)((float*)p + at);
+    __builtin_nontemporal_store(f32x4{x[0], x[1], x[2], x[3]}, q);
+    __builtin_nontemporal_store(f32x4{x[4], x[5], x[6], x[7]}, q + 1);
+  } else {
+    __builtin_nontemporal_store(Chunk<T>::store(x), (u32x4*)((uint16_t*)p + at));
+  }
+}
 // The same where the type is one of two at run time: fp32, or T.
 template <int T>
 __device__ __forceinline__ void load8_or_f32(const void* p, int64_t at, bool f32, float (&x)[8]) {

@@ -11,7 +11,7 @@
 namespace infcl {
 namespace {
 
-template <int T>
+template <int T, bool FAR>
 __global__ void __launch_bounds__(256) dropout_kernel(const void* __restrict__ x, int64_t stride, int64_t chunks,
                                                       uint32_t c, const Drop drop, void* __restrict__ out) {
   const uint64_t seed = drop.the_seed();
@@ -28,8 +28,18 @@ __global__ void __launch_bounds__(256) dropout_kernel(const void* __restrict__ x
     const Random128 r = philox(drop.first + (uint64_t)i, drop.site, seed);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = r.bits16(e) >= drop.cut ? v[e] * drop.unit : 0.f;
-    store8<T>(out, i * 8, v);
+    store8<T, FAR>(out, i * 8, v);
   }
+}
+
+template <int T>
+void dropout_t(const void* x, int64_t stride, int64_t n, int64_t d, const Drop& r, void* out, hipStream_t st) {
+  const int64_t chunks = n * (d / 8), blocks = (chunks + 255) / 256;
+  const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384));
+  if (n * d * (T == kF32 ? 4 : 2) > kL2Bytes)
+    hipLaunchKernelGGL((dropout_kernel<T, true>), grid, dim3(256), 0, st, x, stride, chunks, (uint32_t)(d / 8), r, out);
+  else
+    hipLaunchKernelGGL((dropout_kernel<T, false>), grid, dim3(256), 0, st, x, stride, chunks, (uint32_t)(d / 8), r, out);
 }
 
 }  // namespace
@@ -45,16 +55,13 @@ extern "C" infcl_status infcl_dropout(const void* x, int64_t x_stride, int64_t n
     return INFCL_ERR_UNSUPPORTED;
   if (n == 0) return INFCL_OK;
   if (!block_aligned(x, 16) || !block_aligned(out, 16)) return INFCL_ERR_INVALID;
-  const int64_t chunks = n * (d / 8), blocks = (chunks + 255) / 256;
   const Drop r = drop_of(drop, d);
-  const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384));
-  hipStream_t st = (hipStream_t)stream;
   const int64_t stride = n == 1 ? d : x_stride;
   if (dtype == INFCL_BF16)
-    hipLaunchKernelGGL((dropout_kernel<kBF16>), grid, dim3(256), 0, st, x, stride, chunks, (uint32_t)(d / 8), r, out);
+    dropout_t<kBF16>(x, stride, n, d, r, out, (hipStream_t)stream);
   else if (dtype == INFCL_F16)
-    hipLaunchKernelGGL((dropout_kernel<kF16>), grid, dim3(256), 0, st, x, stride, chunks, (uint32_t)(d / 8), r, out);
+    dropout_t<kF16>(x, stride, n, d, r, out, (hipStream_t)stream);
   else
-    hipLaunchKernelGGL((dropout_kernel<kF32>), grid, dim3(256), 0, st, x, stride, chunks, (uint32_t)(d / 8), r, out);
+    dropout_t<kF32>(x, stride, n, d, r, out, (hipStream_t)stream);
   return launch_status();
 }

@@ -47,7 +47,7 @@ __device__ __forceinline__ float load1(const void* p, int64_t at) {
 
 // WHOLE: pairs are halves and a multiple of 8, an item is 8 pairs (two chunks), or a
 // chunk that is copied.  Otherwise an item is one chunk of 8 features.
-template <int T, bool HALVES, bool WHOLE>
+template <int T, bool HALVES, bool WHOLE, bool FAR>
 __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
   __shared__ float2 table[kTable];
   const int64_t t0 = (int64_t)blockIdx.x * a.tokens;
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
       if (c >= half) {  // past the pairs: copied
         float u[8];
         load8<T>(a.x, xi + 8 * (c + half), u);
-        store8<T>(a.out, oi + 8 * (c + half), u);
+        store8<T, FAR>(a.out, oi + 8 * (c + half), u);
         continue;
       }
       float u[8], v[8];
@@ -89,8 +89,8 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
           u[e] = p, v[e] = q;
         }
       }
-      store8<T>(a.out, oi + 8 * c, u);
-      store8<T>(a.out, oi + 8 * c + a.pairs, v);
+      store8<T, FAR>(a.out, oi + 8 * c, u);
+      store8<T, FAR>(a.out, oi + 8 * c + a.pairs, v);
     } else {
       float u[8];
       load8<T>(a.x, xi + 8 * c, u);
@@ -118,19 +118,26 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
           }
         }
       }
-      store8<T>(a.out, oi + 8 * c, u);
+      store8<T, FAR>(a.out, oi + 8 * c, u);
     }
   }
 }
 
+template <int T, bool FAR>
+void rotary_far(const RotaryArgs& a, int paired, bool whole, unsigned grid, hipStream_t st) {
+  if (paired == INFCL_PAIRED_NEIGHBOURS)
+    hipLaunchKernelGGL((rotary_kernel<T, false, false, FAR>), dim3(grid), dim3(256), 0, st, a);
+  else if (whole)
+    hipLaunchKernelGGL((rotary_kernel<T, true, true, FAR>), dim3(grid), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((rotary_kernel<T, true, false, FAR>), dim3(grid), dim3(256), 0, st, a);
+}
 template <int T>
 void rotary_t(const RotaryArgs& a, int paired, bool whole, unsigned grid, hipStream_t st) {
-  if (paired == INFCL_PAIRED_NEIGHBOURS)
-    hipLaunchKernelGGL((rotary_kernel<T, false, false>), dim3(grid), dim3(256), 0, st, a);
-  else if (whole)
-    hipLaunchKernelGGL((rotary_kernel<T, true, true>), dim3(grid), dim3(256), 0, st, a);
+  if (a.n * a.heads * a.hd * (T == kF32 ? 4 : 2) > kL2Bytes)
+    rotary_far<T, true>(a, paired, whole, grid, st);
   else
-    hipLaunchKernelGGL((rotary_kernel<T, true, false>), dim3(grid), dim3(256), 0, st, a);
+    rotary_far<T, false>(a, paired, whole, grid, st);
 }
 
 uint32_t by(int d) { return d == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d); }
