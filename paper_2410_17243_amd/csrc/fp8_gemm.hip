@@ -78,24 +78,27 @@ __global__ void __launch_bounds__(W::kThreads, 2) matmul_kernel(const MatmulArgs
   const uint32_t voff = (uint32_t)(first + (lane >> 2)) * kp + 16 * ((lane & 3) ^ ((lane >> 4) & 3));
   const uint64_t base = (uint64_t)(of_b ? p.b + m0 * p.kp : p.a + n0 * p.kp) + (uint64_t)s0 * kStep;
   const uint32_t limit = (uint32_t)((of_b ? rows_b : rows_a) - 1) * kp + kStep;
-  auto issue = [&](int s) {  // stage s of this part; past its end: zeros
+  auto source = [&](int s) {  // stage s of this part; past its end: zeros
     const uint64_t at = base + (uint64_t)s * kStep;
     u32x4 r;
     r[0] = (uint32_t)at, r[1] = (uint32_t)(at >> 32) & 0xFFFFu, r[2] = s < ns ? limit : 0, r[3] = 0x00020000u;
-    INFCL_LDS char* to = (INFCL_LDS char*)lds + (s % kStages) * W::kStage + 1024 * W::kCopies * wave;
-#pragma unroll
-    for (int i = 0; i < W::kCopies; ++i) dma16_asm(r, to + 1024 * i, voff, (uint32_t)(16 * i) * kp);
+    return r;
   };
-  auto exponents = [&](int s) {  // of 64 stages from s (a multiple of 64) on
-    const int64_t word0 = (int64_t)(s0 + s) / 8;
-#pragma unroll 1
-    for (int i = threadIdx.x; i < kGroups * W::kRows; i += W::kThreads) {
-      const int r = i % W::kRows, g = i / W::kRows;
-      const bool isb = r < W::BM;
-      const int row = isb ? r : r - W::BM, rows = isb ? rows_b : rows_a;
-      const int64_t word = word0 + g, at = ((isb ? m0 : n0) + row) * (p.ep / 4) + word;
-      exps[i] = row < rows && word < p.ep / 4 ? ((const uint32_t*)(isb ? p.be : p.ae))[at] : 0x7F7F7F7Fu;
-    }
+  auto copy = [&](const u32x4& r, int s, int i) {  // the i-th of a wave's copies
+    dma16_asm(r, (INFCL_LDS char*)lds + (s % kStages) * W::kStage + 1024 * (W::kCopies * wave + i), voff, (uint32_t)(16 * i) * kp);
+  };
+  auto exponents = [&](int s) {  // of 64 stages from s (a multiple of 64) on: a row for each thread, all loads at once
+    static_assert(W::kRows == W::kThreads, "a row for each thread");
+    const int r = threadIdx.x;
+    const bool isb = r < W::BM;
+    const int row = isb ? r : r - W::BM, rows = isb ? rows_b : rows_a;
+    const int64_t word0 = (int64_t)(s0 + s) / 8, words = p.ep / 4;
+    const uint32_t* e = (const uint32_t*)(isb ? p.be : p.ae) + ((isb ? m0 : n0) + (row < rows ? row : rows - 1)) * words;
+    uint32_t w[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) w[g] = e[word0 + g < words ? word0 + g : words - 1];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) exps[g * W::kRows + r] = w[g];
   };
 
   const int wm = wave / W::WN, wn = wave % W::WN, h = lane >> 5;
@@ -127,10 +130,11 @@ __global__ void __launch_bounds__(W::kThreads, 2) matmul_kernel(const MatmulArgs
   // One stage: its fragments are in registers, those of the next one are read beside its
   // products, b's into the registers that a product has just read.  At the barrier this
   // wave's copies of stage s + 1 are done (those of two later ones may not be) and with it
-  // every wave's; all reads of stage s are done too, so its place takes stage s + 4.
+  // every wave's; all reads of stage s are done too, so its place takes stage s + 4, whose
+  // copies go out between the products (right after the barrier they cost 2 to 4 percent).
   auto step = [&](int s, const i32x8 (&a)[W::FN], i32x8 (&next)[W::FN]) {
     asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    issue(s + kStages);
+    const u32x4 later = source(s + kStages);
 #pragma unroll
     for (int j = 0; j < W::FN; ++j) next[j] = frag(s + 1, bn + 32 * j);
 #pragma unroll
@@ -139,13 +143,19 @@ __global__ void __launch_bounds__(W::kThreads, 2) matmul_kernel(const MatmulArgs
       for (int j = 0; j < W::FN; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b[i], a[j], acc[i][j], 0, 0, 0, (int)eb[i], 0, (int)ea[j]);
       __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int c = i * W::kCopies / W::FM; c < (i + 1) * W::kCopies / W::FM; ++c) copy(later, s + kStages, c);
       b[i] = frag(s + 1, bm + 32 * i);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
 #pragma unroll
-  for (int s = 0; s < kStages; ++s) issue(s);
-  exponents(0);
+  for (int s = 0; s < kStages; ++s) {
+    const u32x4 r = source(s);
+#pragma unroll
+    for (int i = 0; i < W::kCopies; ++i) copy(r, s, i);
+  }
+  if (ns > 0) exponents(0);  // (no blocks, no words)
   asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
   for (int j = 0; j < W::FN; ++j) a0[j] = frag(0, bn + 32 * j);
@@ -493,7 +503,8 @@ LayerPlaces layer_places(int64_t n, int64_t k, int64_t m, int keeps, void* kept,
 }
 infcl_status layer_status(int64_t n, int64_t k, int64_t m, int keeps) {
   if (n < 0 || k < 1 || m < 1 || keeps < 0 || keeps > 3) return INFCL_ERR_INVALID;
-  if (k % 8 != 0 || m % 8 != 0 || n > ((int64_t)1 << 23) || m > ((int64_t)1 << 23) || n > ((int64_t)1 << 37) / (k > m ? k : m))
+  if (k % 8 != 0 || m % 8 != 0 || n > ((int64_t)1 << 23) || m > ((int64_t)1 << 23) || m > ((int64_t)1 << 36) / k ||
+      n > ((int64_t)1 << 37) / (k > m ? k : m))
     return INFCL_ERR_UNSUPPORTED;
   infcl_status s = sizes_status(n, m, k);
   if (s == INFCL_OK) s = sizes_status(n, k, m);
