@@ -69,8 +69,9 @@ __device__ __forceinline__ void norm_row(float (&t)[8], bool in, const NormArgs&
     for (int e = 0; e < 8; ++e) s[0] += t[e];
     row_sums<WIDE, 1>(s, a.ls, buf, turn);
     mean = s[0] * a.by_d;
+    const float here = in ? mean : 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) t[e] = in ? t[e] - mean : 0.f;
+    for (int e = 0; e < 8; ++e) t[e] -= here;
   }
   float s[1] = {0.f};
 #pragma unroll
@@ -109,10 +110,20 @@ __device__ __forceinline__ void load_vectors(const NormArgs& a, bool in, int64_t
   if (BIAS && a.pre_b) load8_or_f32<T>(a.pre_b, col, a.wf32, w.b2);
 }
 
+// Rows to be read, or others that are there in the place of rows that are not: every load
+// is issued, without a branch, and what should not be there is made zero afterwards.
+struct Source {
+  const void* p;
+  int64_t stride;
+  bool there;
+  __device__ __forceinline__ Source(const void* q, int64_t s, const void* other) : p(q ? q : other), stride(q ? s : 0), there(q != nullptr) {}
+  __device__ __forceinline__ int64_t at(int64_t row, bool in, int64_t col) const { return row * stride + (in ? col : 0); }
+};
+
 // WIDE: 0, rows within a wave; else rows of up to that many lanes.  FULL: with a gate, a
-// norm of y or a dropout; without, the registers of their vectors and sums are free for
-// more waves.  FAR: rows' outputs are past the caches.
-template <int T, int WIDE, bool FULL, bool FAR>
+// norm of y or a dropout (DROP); without, the registers of their vectors and sums are free
+// for more waves.  FAR: rows' outputs are past the caches.
+template <int T, int WIDE, bool FULL, bool DROP, bool FAR>
 __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE == 1024 ? 4 : 2) norm_fwd(const NormArgs a) {
   __shared__ float buf[2][16][2];
   int64_t row, step;
@@ -122,20 +133,23 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE == 1024 ? 4 : 2) norm_
   const int64_t col = 8 * (int64_t)chunk;
   Vectors w;
   load_vectors<T, FULL, true>(a, in, col, w);
-  const bool drop = FULL && a.drop.cut;
-  const uint64_t seed = drop ? a.drop.the_seed() : 0;
+  const uint64_t seed = DROP ? a.drop.the_seed() : 0;
+  const Source from_x(a.x, a.xs, a.x), from_y(a.y, a.ys, a.x);
   for (; row < a.n; row += step) {
-    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, t[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (in) load8<T>(a.x, row * a.xs + col, x);
+    Raw8<T> rx, ry;
+    rx.load(from_x.p, from_x.at(row, in, col));
+    ry.load(from_y.p, from_y.at(row, in, col));
+    float x[8], t[8];
+    rx.get(in, x);
     float m1 = 0.f, r1 = 0.f, m2 = 0.f, r2 = 0.f;
     if (a.y) {
-      if (in) load8<T>(a.y, row * a.ys + col, t);
+      ry.get(in, t);
       if (FULL && a.post_w) {
         norm_row<WIDE>(t, in, a, m1, r1, buf, turn);
 #pragma unroll
         for (int e = 0; e < 8; ++e) t[e] = fmaf(t[e], w.w1[e], w.b1[e]);
       }
-      if (drop) {
+      if constexpr (DROP) {
         const Random128 u = philox(a.drop.first + (uint64_t)row * a.c + chunk, a.drop.site, seed);
 #pragma unroll
         for (int e = 0; e < 8; ++e) t[e] = u.bits16(e) >= a.drop.cut ? t[e] * a.drop.unit : 0.f;
@@ -162,7 +176,7 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE == 1024 ? 4 : 2) norm_
 // first bias and the gate are in LDS, each lane its own 32 bytes of them, and 16 waves fit
 // (everything, us with registers and with LDS: 50001 x 1160 348 and 320, 8001 x 8192 457 and 294;
 // but 50001 x 768 174 and 205, 30001 x 2048 214 and 265).
-template <int T, int WIDE, bool FULL, bool BIAS, bool FAR>
+template <int T, int WIDE, bool FULL, bool BIAS, bool DROP, bool FAR>
 __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE >= 512 || !BIAS ? 4 : 2) norm_bwd(const NormArgs a) {
   __shared__ float buf[2][16][2];
   __shared__ float joined[WIDE ? 1 : 4][WIDE ? 1 : 512];
@@ -200,27 +214,25 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE >= 512 || !BIAS ? 4 : 
   float sg[8], sw1[8], sb1[8], sw2[8], sb2[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) sg[e] = sw1[e] = sb1[e] = sw2[e] = sb2[e] = 0.f;
-  const bool drop = FULL && a.drop.cut;
-  const uint64_t seed = drop ? a.drop.the_seed() : 0;
+  const uint64_t seed = DROP ? a.drop.the_seed() : 0;
   // dropout's factor is the gate's, and that of the gate's sums
-  if (FULL)
+  if (DROP)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w.gate[e] *= drop ? a.drop.unit : 1.f;
+    for (int e = 0; e < 8; ++e) w.gate[e] *= a.drop.unit;
   if (kOwn) put_own(2, w.b1), put_own(3, w.gate);
+  const Source from_x(a.x, a.xs, a.x), from_y(a.y, a.ys, a.x), from_dh(a.dh, a.dhs, a.x), from_dz(a.dz, a.dzs, a.x);
+  const bool post = FULL && a.post_w;
   for (; row < a.n; row += step) {
-    float h[8] = {0, 0, 0, 0, 0, 0, 0, 0}, v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, e8[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    float g[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    Raw8<T> rx, ry, rh, rz;
+    rx.load(from_x.p, from_x.at(row, in, col));
+    ry.load(from_y.p, from_y.at(row, in, col));
+    rh.load(from_dh.p, from_dh.at(row, in, col));
+    rz.load(from_dz.p, from_dz.at(row, in, col));
     float4 st = a.stats[row];
-    if (in) {
-      load8<T>(a.x, row * a.xs + col, h);
-      if (a.y) load8<T>(a.y, row * a.ys + col, v);
-      if (a.dh) load8<T>(a.dh, row * a.dhs + col, e8);
-      if (a.dz) load8<T>(a.dz, row * a.dzs + col, g);
-    } else {
-      st.y = st.w = 0.f;  // (normed rows of lanes past the row are zeros)
-    }
+    if (!post) st.x = 0.f, st.y = 1.f;
+    if (!in) st.y = st.w = 0.f;  // (normed rows of lanes past the row are zeros)
     bool keep[8];
-    if (drop) {
+    if constexpr (DROP) {
       const Random128 u = philox(a.drop.first + (uint64_t)row * a.c + chunk, a.drop.site, seed);
 #pragma unroll
       for (int e = 0; e < 8; ++e) keep[e] = u.bits16(e) >= a.drop.cut;
@@ -228,9 +240,14 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE >= 512 || !BIAS ? 4 : 
 #pragma unroll
       for (int e = 0; e < 8; ++e) keep[e] = true;
     }
+    float h[8], v[8], e8[8], g[8];
+    rx.get(in, h);
+    ry.get(in && from_y.there, v);
+    rh.get(in && from_dh.there, e8);
+    rz.get(in && from_dz.there, g);
     // what the gate took (without dropout's factor), from the normed y
     auto taken = [&](int e, const float (&b)[8]) {
-      const float t = a.post_w ? (BIAS ? fmaf(v[e], w.w1[e], b[e]) : v[e] * w.w1[e]) : v[e];
+      const float t = BIAS ? fmaf(v[e], w.w1[e], b[e]) : v[e] * w.w1[e];
       return keep[e] ? t : 0.f;
     };
     float b1[8], gate[8];
@@ -246,7 +263,7 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE >= 512 || !BIAS ? 4 : 
     if (a.y) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if (FULL && a.post_w) v[e] = (v[e] - st.x) * st.y;
+        if (FULL) v[e] = (v[e] - st.x) * st.y;
         h[e] = fmaf(a.alpha, h[e], FULL ? gate[e] * taken(e, b1) : v[e]);
       }
     }
@@ -280,16 +297,14 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE >= 512 || !BIAS ? 4 : 
       for (int e = 0; e < 8; ++e) {
         sg[e] = fmaf(e8[e], taken(e, b1), sg[e]);
         float q = keep[e] ? e8[e] * gate[e] : 0.f;
-        if (a.post_w) {
-          sw1[e] = fmaf(q, v[e], sw1[e]);
-          if (BIAS && !kOwn) sb1[e] += q;
-          qs[e] = q;
-          q *= w.w1[e];
-          s[0] += q, s[1] = fmaf(q, v[e], s[1]);
-        }
+        sw1[e] = fmaf(q, v[e], sw1[e]);
+        if (BIAS && !kOwn) sb1[e] += q;
+        qs[e] = q;
+        q *= w.w1[e];
+        s[0] += q, s[1] = fmaf(q, v[e], s[1]);
         e8[e] = q;
       }
-      if (a.post_w) {
+      if (post) {
         if (kOwn && a.want_post_b) add_own(1, qs);
         row_sums<WIDE, 2>(s, a.ls, buf, turn);
         const float m = a.rms ? 0.f : s[0] * a.by_d, k = s[1] * a.by_d;
@@ -299,7 +314,7 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE >= 512 || !BIAS ? 4 : 
     }
     if (a.dy && in) store8<T, FAR>(a.dy, row * (8 * (int64_t)a.c) + col, e8);
   }
-  if (FULL && drop)
+  if (DROP)
 #pragma unroll
     for (int e = 0; e < 8; ++e) sg[e] *= a.drop.unit;
 
@@ -441,42 +456,45 @@ NormArgs args_of(const infcl_add_norm* a, const Shape& s, const void* x, const v
   return r;
 }
 
-template <int T, bool FULL, bool FAR>
+template <int T, bool FULL, bool DROP, bool FAR>
 void fwd_t(const NormArgs& r, const Shape& s, hipStream_t st) {
   const dim3 grid(grid_of(s, r.n, kFwdWaves)), block(s.threads);
-  if (s.threads > 512)
-    hipLaunchKernelGGL((norm_fwd<T, 1024, FULL, FAR>), grid, block, 0, st, r);
-  else if (s.wide)
-    hipLaunchKernelGGL((norm_fwd<T, 512, FULL, FAR>), grid, block, 0, st, r);
+  if (s.wide)
+    hipLaunchKernelGGL((norm_fwd<T, 1024, FULL, DROP, FAR>), grid, block, 0, st, r);
   else
-    hipLaunchKernelGGL((norm_fwd<T, 0, FULL, FAR>), grid, block, 0, st, r);
+    hipLaunchKernelGGL((norm_fwd<T, 0, FULL, DROP, FAR>), grid, block, 0, st, r);
 }
-template <int T, bool FULL, bool BIAS, bool FAR>
+template <int T, bool FULL, bool BIAS, bool DROP, bool FAR>
 void bwd_t(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
   const dim3 grid(wgs), block(s.threads);
   const size_t own = FULL && BIAS ? 8 * 16 * (size_t)s.threads : 0;
-  if (all_in_registers(s) && FULL && BIAS)
-    hipLaunchKernelGGL((norm_bwd<T, FULL && BIAS ? 256 : 512, FULL, BIAS, FAR>), grid, block, 0, st, r);
-  else if (s.threads > 512)
-    hipLaunchKernelGGL((norm_bwd<T, 1024, FULL, BIAS, FAR>), grid, block, own, st, r);
-  else if (s.wide)
-    hipLaunchKernelGGL((norm_bwd<T, 512, FULL, BIAS, FAR>), grid, block, own, st, r);
+  if (!s.wide)
+    hipLaunchKernelGGL((norm_bwd<T, 0, FULL, BIAS, DROP, FAR>), grid, block, 0, st, r);
+  else if (FULL && BIAS && all_in_registers(s))
+    hipLaunchKernelGGL((norm_bwd<T, FULL && BIAS ? 256 : 1024, FULL, BIAS, DROP, FAR>), grid, block, 0, st, r);
   else
-    hipLaunchKernelGGL((norm_bwd<T, 0, FULL, BIAS, FAR>), grid, block, 0, st, r);
+    hipLaunchKernelGGL((norm_bwd<T, 1024, FULL, BIAS, DROP, FAR>), grid, block, own, st, r);
 }
 bool full(const NormArgs& r) { return r.gate || r.post_w || r.drop.cut; }
 template <int T, bool FAR>
 void fwd_far(const NormArgs& r, const Shape& s, hipStream_t st) {
-  full(r) ? fwd_t<T, true, FAR>(r, s, st) : fwd_t<T, false, FAR>(r, s, st);
+  if (!full(r))
+    fwd_t<T, false, false, FAR>(r, s, st);
+  else if (r.drop.cut)
+    fwd_t<T, true, true, FAR>(r, s, st);
+  else
+    fwd_t<T, true, false, FAR>(r, s, st);
+}
+template <int T, bool FAR, bool BIAS>
+void bwd_full(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
+  r.drop.cut ? bwd_t<T, true, BIAS, true, FAR>(r, s, wgs, st) : bwd_t<T, true, BIAS, false, FAR>(r, s, wgs, st);
 }
 template <int T, bool FAR>
 void bwd_far(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
   if (!full(r))
-    bwd_t<T, false, true, FAR>(r, s, wgs, st);
-  else if (r.post_b || r.pre_b)
-    bwd_t<T, true, true, FAR>(r, s, wgs, st);
+    bwd_t<T, false, true, false, FAR>(r, s, wgs, st);
   else
-    bwd_t<T, true, false, FAR>(r, s, wgs, st);
+    r.post_b || r.pre_b ? bwd_full<T, FAR, true>(r, s, wgs, st) : bwd_full<T, FAR, false>(r, s, wgs, st);
 }
 template <int T>
 bool far(const NormArgs& r) {
