@@ -16,7 +16,10 @@
 // taken again from x and y there (as many bytes as reading it back, and not rounded).
 // What a lane adds up for its features over all its rows are 40 registers at most, then
 // one row of partial sums for each workgroup, joined in order by a second launch.
-// Bound by the rows' bytes.
+// Bound by the rows' bytes without gate, first norm and dropout (17408 x 512: 13 us forward and 21
+// backward for 71 and 107 MB; 50001 x 1160: 78 and 142), with them by the vector unit: 400 to 500
+// instructions for 8 features (50001 x 1160 with everything: 125 and 190 us, of a floor of 92
+// and 138).
 #include "block.hpp"
 
 namespace infcl {
@@ -36,9 +39,9 @@ struct NormArgs {
 };
 
 // Sums over a row of K values of each lane: over its group of lanes, or over all waves
-// of the workgroup (WAVES > 0) through one of two buffers in turn, so that one barrier
+// of the workgroup (WIDE) through one of two buffers in turn, so that one barrier
 // does for each.
-template <int WIDE, int K>
+template <bool WIDE, int K>
 __device__ __forceinline__ void row_sums(float (&s)[K], int ls, float (*buf)[16][2], int& turn) {
 #pragma unroll
   for (int i = 0; i < K; ++i) s[i] = group_sum(s[i], ls);
@@ -59,7 +62,7 @@ __device__ __forceinline__ void row_sums(float (&s)[K], int ls, float (*buf)[16]
 
 // N(t): the mean and factor of the row, t becomes the normed row.  Lanes past the row
 // (`in` false) hold zeros before and after.
-template <int WIDE>
+template <bool WIDE>
 __device__ __forceinline__ void norm_row(float (&t)[8], bool in, const NormArgs& a, float& mean, float& r,
                                          float (*buf)[16][2], int& turn) {
   mean = 0.f;
@@ -83,7 +86,7 @@ __device__ __forceinline__ void norm_row(float (&t)[8], bool in, const NormArgs&
 }
 
 // A lane's place: its row of the launch's first sweep, the step between rows, its chunk.
-template <int WIDE>
+template <bool WIDE>
 __device__ __forceinline__ void place(const NormArgs& a, int64_t& row, int64_t& step, int& chunk) {
   if constexpr (WIDE) {
     row = blockIdx.x, step = gridDim.x, chunk = threadIdx.x;
@@ -120,11 +123,11 @@ struct Source {
   __device__ __forceinline__ int64_t at(int64_t row, bool in, int64_t col) const { return row * stride + (in ? col : 0); }
 };
 
-// WIDE: 0, rows within a wave; else rows of up to that many lanes.  FULL: with a gate, a
+// WIDE: rows of several waves, up to 1024 lanes; else rows within a wave.  FULL: with a gate, a
 // norm of y or a dropout (DROP); without, the registers of their vectors and sums are free
 // for more waves.  FAR: rows' outputs are past the caches.
-template <int T, int WIDE, bool FULL, bool DROP, bool FAR>
-__global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE == 1024 ? 4 : 2) norm_fwd(const NormArgs a) {
+template <int T, bool WIDE, bool FULL, bool DROP, bool FAR>
+__global__ void __launch_bounds__(WIDE ? 1024 : 256, WIDE ? 4 : 2) norm_fwd(const NormArgs a) {
   __shared__ float buf[2][16][2];
   int64_t row, step;
   int chunk, turn = 0;
@@ -171,13 +174,13 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE == 1024 ? 4 : 2) norm_
   }
 }
 
-// BIAS: with sums for biases.  With everything (FULL, BIAS) a lane takes 153 registers, three
-// waves on a SIMD.  Where the rows' waves do not divide those twelve, the biases' sums, the
-// first bias and the gate are in LDS, each lane its own 32 bytes of them, and 16 waves fit
-// (everything, us with registers and with LDS: 50001 x 1160 348 and 320, 8001 x 8192 457 and 294;
-// but 50001 x 768 174 and 205, 30001 x 2048 214 and 265).
-template <int T, int WIDE, bool FULL, bool BIAS, bool DROP, bool FAR>
-__global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE >= 512 || !BIAS ? 4 : 2) norm_bwd(const NormArgs a) {
+// BIAS: with sums for biases.  With everything (FULL, BIAS) a lane would take 151 registers,
+// three waves on a SIMD.  In rows of several waves the biases' sums, the first bias and the
+// gate are in LDS instead, each lane its own 32 bytes of them, and 16 waves fit a compute unit
+// (50001 x 768 131 us, 141 in registers; 30001 x 2048 176 and 180; where the waves of a row do not
+// divide twelve, 16001 x 4096, 184 and 280).
+template <int T, bool WIDE, bool FULL, bool BIAS, bool DROP, bool FAR>
+__global__ void __launch_bounds__(WIDE ? 1024 : 256, WIDE || !BIAS ? 4 : 2) norm_bwd(const NormArgs a) {
   __shared__ float buf[2][16][2];
   __shared__ float joined[WIDE ? 1 : 4][WIDE ? 1 : 512];
   int64_t row, step;
@@ -186,7 +189,7 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE >= 512 || !BIAS ? 4 : 
   const bool in = chunk < a.c;
   const int64_t col = 8 * (int64_t)chunk;
   extern __shared__ f32x4 own[];  // kOwn: [sb2, sb1, b1, gate][halves][lanes]
-  constexpr bool kOwn = WIDE >= 512 && FULL && BIAS;
+  constexpr bool kOwn = WIDE && FULL && BIAS;
   auto add_own = [&](int k, const float (&q)[8]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -357,11 +360,11 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE >= 512 || !BIAS ? 4 : 
 }
 
 // Sums of parts [parts][sums][d] in a fixed order: 32 columns of one vector for each
-// workgroup, 16 slices of the parts, joined through LDS.
+// workgroup, 32 slices of the parts, sixteen loads at a time, joined through LDS.
 template <int T>
-__global__ void __launch_bounds__(512) norm_join(const float* __restrict__ part, int parts, int sums, int d, int wf32,
+__global__ void __launch_bounds__(1024) norm_join(const float* __restrict__ part, int parts, int sums, int d, int wf32,
                                                  void* o0, void* o1, void* o2, void* o3, void* o4) {
-  __shared__ float lds[16][33];
+  __shared__ float lds[32][33];
   const int cols = (d + 31) / 32, k = blockIdx.x / cols, col = (blockIdx.x - k * cols) * 32 + (threadIdx.x & 31);
   const int slice = threadIdx.x >> 5;
   float s = 0.f;
@@ -369,21 +372,20 @@ __global__ void __launch_bounds__(512) norm_join(const float* __restrict__ part,
     const float* p = part + (int64_t)k * d + col;
     const int64_t row = (int64_t)sums * d;
     int i = slice;
-    for (; i + 16 * 7 < parts; i += 16 * 8) {
-      float v[8];
+    for (; i < parts; i += 32 * 16) {
+      float v[16];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = p[(i + 16 * j) * row];
+      for (int j = 0; j < 16; ++j) v[j] = p[(i + 32 * j < parts ? i + 32 * j : i) * row];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s += v[j];
+      for (int j = 0; j < 16; ++j) s += i + 32 * j < parts ? v[j] : 0.f;
     }
-    for (; i < parts; i += 16) s += p[i * row];
   }
   lds[slice][threadIdx.x & 31] = s;
   __syncthreads();
   if (slice == 0 && col < d) {
     float t = 0.f;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) t += lds[j][threadIdx.x];
+    for (int j = 0; j < 32; ++j) t += lds[j][threadIdx.x];
     void* const to = k == 0 ? o0 : k == 1 ? o1 : k == 2 ? o2 : k == 3 ? o3 : o4;
     if (T == kF32 || wf32)
       ((float*)to)[col] = t;
@@ -416,11 +418,10 @@ unsigned grid_of(const Shape& s, int64_t n, int waves) {
   return (unsigned)(need < most ? need : most);
 }
 // The forward starts more than that: nothing is left to be joined.  The backward's kernels
-// have registers for 16 or more waves, with everything and biases for 12 (17408 x 512: 37 us
-// with 12, 46 with 16; 30001 x 2048 without gate and norm of y: 144 us with 16, 151 with 20).
+// have registers for 16 or more waves, with everything and biases in rows of one wave for 12
+// (17408 x 512: 37 us with 12, 46 with 16; 30001 x 2048 without gate and norm of y: 144 us with
+// 16, 151 with 20).
 constexpr int kFwdWaves = 32, kBwdWaves = 16, kBwdWavesAll = 12;
-
-bool all_in_registers(const Shape& s) { return s.wide && (s.threads == 128 || s.threads == 256); }
 
 infcl_status check(const infcl_add_norm* a) {
   if (!a || a->n < 0 || a->d < 1 || !type_known(a->dtype) || !type_known(a->wdtype) ||
@@ -460,20 +461,18 @@ template <int T, bool FULL, bool DROP, bool FAR>
 void fwd_t(const NormArgs& r, const Shape& s, hipStream_t st) {
   const dim3 grid(grid_of(s, r.n, kFwdWaves)), block(s.threads);
   if (s.wide)
-    hipLaunchKernelGGL((norm_fwd<T, 1024, FULL, DROP, FAR>), grid, block, 0, st, r);
+    hipLaunchKernelGGL((norm_fwd<T, true, FULL, DROP, FAR>), grid, block, 0, st, r);
   else
-    hipLaunchKernelGGL((norm_fwd<T, 0, FULL, DROP, FAR>), grid, block, 0, st, r);
+    hipLaunchKernelGGL((norm_fwd<T, false, FULL, DROP, FAR>), grid, block, 0, st, r);
 }
 template <int T, bool FULL, bool BIAS, bool DROP, bool FAR>
 void bwd_t(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
   const dim3 grid(wgs), block(s.threads);
   const size_t own = FULL && BIAS ? 8 * 16 * (size_t)s.threads : 0;
   if (!s.wide)
-    hipLaunchKernelGGL((norm_bwd<T, 0, FULL, BIAS, DROP, FAR>), grid, block, 0, st, r);
-  else if (FULL && BIAS && all_in_registers(s))
-    hipLaunchKernelGGL((norm_bwd<T, FULL && BIAS ? 256 : 1024, FULL, BIAS, DROP, FAR>), grid, block, 0, st, r);
+    hipLaunchKernelGGL((norm_bwd<T, false, FULL, BIAS, DROP, FAR>), grid, block, 0, st, r);
   else
-    hipLaunchKernelGGL((norm_bwd<T, 1024, FULL, BIAS, DROP, FAR>), grid, block, own, st, r);
+    hipLaunchKernelGGL((norm_bwd<T, true, FULL, BIAS, DROP, FAR>), grid, block, own, st, r);
 }
 bool full(const NormArgs& r) { return r.gate || r.post_w || r.drop.cut; }
 template <int T, bool FAR>
@@ -511,7 +510,7 @@ void bwd_any(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
 template <int T>
 void join_t(const NormArgs& r, unsigned wgs, int sums, void* const* o, hipStream_t st) {
   const int d = 8 * r.c;
-  hipLaunchKernelGGL((norm_join<T>), dim3((unsigned)(sums * ((d + 31) / 32))), dim3(512), 0, st, r.part, (int)wgs, sums, d,
+  hipLaunchKernelGGL((norm_join<T>), dim3((unsigned)(sums * ((d + 31) / 32))), dim3(1024), 0, st, r.part, (int)wgs, sums, d,
                      r.wf32, o[0], o[1], o[2], o[3], o[4]);
 }
 
@@ -582,7 +581,7 @@ extern "C" infcl_status infcl_add_norm_bwd(const infcl_add_norm* a, const void* 
   for (void* o : {g->dgate, g->dpost_w, g->dpost_b, g->dpre_w, g->dpre_b})
     if (o) outs[sums++] = o;
   hipStream_t st = (hipStream_t)stream;
-  const unsigned wgs = grid_of(sh, a->n, full(r) && (r.post_b || r.pre_b) && (!sh.wide || all_in_registers(sh)) ? kBwdWavesAll : kBwdWaves);
+  const unsigned wgs = grid_of(sh, a->n, !sh.wide && full(r) && (r.post_b || r.pre_b) ? kBwdWavesAll : kBwdWaves);
   if (wgs > 0) {
     if (a->dtype == INFCL_BF16)
       bwd_any<kBF16>(r, sh, wgs, st);
