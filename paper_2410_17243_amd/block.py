@@ -422,8 +422,8 @@ def add_norm(x, y=None, gate=None, post_w=None, post_b=None, pre_w=None, pre_b=N
 
 class Fp8:
     """Rows [rows, k] in 8-bit floats: q [rows, 128 ceil(k / 128)] uint8 (E4M3 bytes; 128
-    more where that is a multiple of 16384), exps [rows, 4 ceil(k / 512)] uint8 (a power of two for 128 entries), and the dtype
-    they had."""
+    more where that is a multiple of 16384), exps [rows, 4 ceil(k / 512)] uint8 (a power of
+    two for 128 entries), and the dtype they had."""
 
     __slots__ = ("q", "exps", "k", "dtype")
 
@@ -548,7 +548,7 @@ def linear_fp8_fwd(x, w, b=None, need_dx: bool = True, need_dw: bool = True):
     if keeps:
         _learns(m)
     elif m % 8:  # (a forward alone takes any number of outputs)
-        return linear_fp8(x, fp8_pack(w), b), (None, (n, k, m, x.dtype, 0, b is not None))
+        return _times_packed(x, fp8_pack(w), b), (None, (n, k, m, x.dtype, 0, b is not None))
     size, scratch, _ = _layer_sizes(n, k, m, keeps)
     out = torch.empty((*x.shape[:-1], m), dtype=x.dtype, device=dev)
     kept, space = _scratch(size, dev), _scratch(scratch, dev)
@@ -614,6 +614,10 @@ def _linear_packed(x, w, b):
     if torch.is_autocast_enabled("cuda"):
         x = x.to(torch.get_autocast_dtype("cuda"))
         b = None if b is None else b.to(x.dtype)
+    return _times_packed(x, w, b)
+
+
+def _times_packed(x, w, b):
     dev = _where(("x", "w", "w's exponents", "b"), (x, w.q, w.exps, b))
     n, k, stride = _rows(x, "x")
     m = w.shape[0]

@@ -191,6 +191,8 @@ def test_frozen_arguments_keep_and_compute_nothing():
         infcl.linear_fp8(*args).square().sum().backward()
         assert torch.equal(args[i].grad, full[i].grad)
     odd = infcl.linear_fp8(x, w[:5], b[:5])  # (no gradient: any number of outputs)
+    leaf = x.clone().requires_grad_()
+    assert torch.equal(infcl.linear_fp8_fwd(leaf, w[:5], b[:5], need_dx=False, need_dw=False)[0], odd)
     assert torch.equal(odd, infcl.linear_fp8(x, w, b)[:, :5])
     with pytest.raises(ValueError, match="multiple of 8"):
         infcl.linear_fp8(x, w[:5].clone().requires_grad_(), b[:5])
