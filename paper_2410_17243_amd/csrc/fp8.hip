@@ -11,7 +11,9 @@
 // contracts along the features of, so x (and dy, and the weights) is wanted in blocks
 // along both, the second transposed.  One workgroup takes a tile of 128 rows and 128
 // features, a lane 8 of each: the tile stays in registers while both kinds of maxima
-// are taken, so x is read once.
+// are taken, so x is read once.  Bound by the bytes: 65536 x 4096 both ways with column
+// sums (1.09 GB) 207 to 210 us, 65536 x 1024 with 4096 x 1024 (278 MB) 55 to 57, 5.0 to 5.3 TB/s;
+// 10007 x 776 with 1000 x 776 14 us; 4096 x 2048 along rows 7.3.
 #include "fp8.hpp"
 
 namespace infcl {
