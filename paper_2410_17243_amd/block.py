@@ -602,8 +602,9 @@ def linear_fp8(x, w, b=None):
     if torch.is_autocast_enabled("cuda"):
         dtype = torch.get_autocast_dtype("cuda")
         x, w, b = x.to(dtype), w.to(dtype), None if b is None else b.to(dtype)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, w, b)):
-        _learns(w.shape[0])
+    if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in (x, w, b)):
+        return linear_fp8_fwd(x, w, b, False, False)[0]
+    _learns(w.shape[0])
     return _LinearFp8.apply(x, w, b)
 
 

@@ -7,6 +7,7 @@ import torch
 
 import paper_2410_17243_amd as infcl
 from oracle import block
+from paper_2410_17243_amd import block as binding
 
 DT = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
 HALF = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11, "f32": 2.0 ** -24}
@@ -196,6 +197,19 @@ def test_frozen_arguments_keep_and_compute_nothing():
     assert torch.equal(odd, infcl.linear_fp8(x, w, b)[:, :5])
     with pytest.raises(ValueError, match="multiple of 8"):
         infcl.linear_fp8(x, w[:5].clone().requires_grad_(), b[:5])
+
+
+@pytest.mark.gpu
+def test_without_gradients_nothing_is_kept(monkeypatch):
+    x = torch.randn(64, 256, device="cuda").bfloat16().requires_grad_()
+    w, b = (torch.randn(s, device="cuda").bfloat16().requires_grad_() for s in ((40, 256), (40,)))
+    y = infcl.linear_fp8(x, w, b)
+    keeps = []
+    sizes = binding._layer_sizes
+    monkeypatch.setattr(binding, "_layer_sizes", lambda *a: keeps.append(a[3]) or sizes(*a))
+    with torch.no_grad():
+        assert torch.equal(infcl.linear_fp8(x, w, b), y) and keeps == [0]
+        assert torch.equal(infcl.linear_fp8(x, w[:5], b[:5]), y[:, :5])  # (any number of outputs)
 
 
 @pytest.mark.gpu
