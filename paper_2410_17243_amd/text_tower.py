@@ -16,9 +16,11 @@ By choice: rotary positions instead of learned ones (rotary), dropout of what th
 blocks add, gates and norms of it, with the residual sum and the next norm in one pass
 (add_norm), and products of 8-bit floats (linear_fp8).  Dropout's masks are functions of
 the tower's seed, the layer, and the token's place in the whole batch, so both passes of
-the gradient cache have the same ones, however the batch is cut.  The command trains a small random-initialised tower against fixed
-random image embeddings for a few steps and prints the loss and what a chunk
-keeps for its backward pass.
+the gradient cache have the same ones, however the batch is cut.
+
+The command trains a small random-initialised tower against fixed random image
+embeddings for a few steps and prints the loss and what a chunk keeps for its backward
+pass.
 """
 
 from __future__ import annotations
@@ -169,7 +171,8 @@ class TextTower(torch.nn.Module):
 
         def add(x, y, post, gate, pre, site):
             w = (None, None) if post is None else (post.weight, post.bias)
-            return add_norm(x, y, gate, *w, pre.weight, pre.bias, eps=pre.eps, site=site, **drop)
+            # (under autocast the blocks' outputs have 16 bits, the residual rows those of the table)
+            return add_norm(x, y.to(x.dtype), gate, *w, pre.weight, pre.bias, eps=pre.eps, site=site, **drop)
 
         z = add_norm(x, pre_w=blocks[0].n1.weight, pre_b=blocks[0].n1.bias, eps=blocks[0].n1.eps)[1] if blocks else None
         for i, (b, after) in enumerate(zip(blocks, nexts)):

@@ -45,6 +45,29 @@ def test_gates_of_one_change_nothing():
 
 
 @pytest.mark.gpu
+def test_fp32_parameters_under_autocast():
+    """Residual rows in fp32 and blocks in bf16: with gates of one again alike up to the
+    blocks' roundings (2^-8 each, a few in a row); on 8-bit products as far off as operands
+    of 2^-5 are, through three products of two layers both ways."""
+    c = synthetic_captions(40, 300, 40, seed=2)
+    d = torch.randn((40, 64), device="cuda")
+    plain, fused, eight = (_tower(dtype=torch.float32, **kw) for kw in ({}, {"gates": 1.0}, {"gates": 1.0, "products": "fp8"}))
+    rows = []
+    for t in (plain, fused, eight):
+        t.load_state_dict(plain.state_dict(), strict=False)
+        with torch.autocast("cuda", torch.bfloat16):
+            rows.append(t(c))
+        (rows[-1] * d).sum().backward()
+    assert float((rows[0] - rows[1]).detach().norm(dim=1).max()) < 8 * 2.0 ** -8
+    for t, bound in ((fused, 16 * 2.0 ** -8), (eight, 0.35)):
+        grads = dict(t.named_parameters())
+        for n, p in plain.named_parameters():
+            assert grads[n].grad.dtype == torch.float32
+            off = float((p.grad.double() - grads[n].grad.double()).norm())
+            assert off <= bound * float(p.grad.double().norm()) + 1e-12, n
+
+
+@pytest.mark.gpu
 def test_chunks_have_the_whole_batchs_masks_and_gradient():
     """A step with dropout in one chunk and in four: the masks are functions of the token's
     place in the batch, so the parameters' gradients are alike up to the bf16 rounding of
