@@ -6,7 +6,8 @@ operators of tower.py: rotary positions, dropout, residual sums with their norms
 layers on 8-bit floats.  As there, this module only marshals arguments; the work is
 done by the HIP kernels of libinfcl.so on the current stream, and nothing falls back.
 The autograd functions are differentiable once: a gradient of their gradient is an
-error.
+error.  They may be captured into a HIP graph with their backward pass, while no eager
+graph of the same leaves is alive (as torch asks of every captured backward pass).
 
 Rotary positions
     rotary_freqs(sections, base=10000.0) -> freqs

@@ -179,3 +179,62 @@ def test_runs_repeat_bit_for_bit():
     first = once()
     for _ in range(3):
         assert all(a is None or torch.equal(a, b) for a, b in zip(once(), first))
+
+
+def _learn(x, w, b, o, gate, n, pos, freqs, seed):
+    """A run of the differentiable calls, and its gradients."""
+    q = infcl.rotary(infcl.linear_fp8(x, w, b).view(-1, 6, 32), pos, freqs, turned=4)
+    t = infcl.dropout(infcl.linear_fp8(q.reshape(-1, 192), o), 0.1, seed)
+    h, z = infcl.add_norm(x, t, gate, pre_w=n, p=0.2, seed=seed, site=1)
+    return [h.detach(), z.detach(), *torch.autograd.grad((h * z).float().sum(), (x, w, b, o, gate, n))]
+
+
+def _leaves(rows):
+    r = lambda *s: torch.randn(s, device="cuda").bfloat16().requires_grad_()  # noqa: E731
+    return [r(rows, 64), r(192, 64), r(192), r(64, 192), r(64), r(64)]
+
+
+@pytest.mark.gpu
+def test_a_step_with_autograd_captured_into_a_graph():
+    """The differentiable calls and their gradients in a graph (no eager graph of the leaves
+    is alive while it is captured): replays with new inputs and seeds, between eager work."""
+    args = _leaves(300)
+    pos, freqs, seed = torch.arange(300, dtype=torch.int32, device="cuda"), infcl.rotary_freqs(16), torch.tensor([5], device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        _learn(*args, pos, freqs, seed)
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = _learn(*args, pos, freqs, seed)
+    for rep in range(4):
+        with torch.no_grad():
+            args[0].copy_(torch.randn(300, 64, device="cuda"))
+        seed.fill_(rep)
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        want = _learn(*args, pos, freqs, seed)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(got, want)), rep
+
+
+@pytest.mark.gpu
+def test_two_streams_at_once():
+    """Calls on two streams share nothing: the results of each alone."""
+    freqs, seed = infcl.rotary_freqs(16), torch.tensor([3], device="cuda")
+    sets = [(_leaves(n), torch.arange(n, dtype=torch.int32, device="cuda")) for n in (2000, 1777)]
+    want = [_learn(*a, pos, freqs, seed) for a, pos in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    got = [[], []]
+    for _ in range(5):
+        for i, (a, pos) in enumerate(sets):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(_learn(*a, pos, freqs, seed))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for g in got[i]:
+            assert all(torch.equal(a, c) for a, c in zip(g, want[i]))
