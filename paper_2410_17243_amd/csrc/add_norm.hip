@@ -40,24 +40,27 @@ struct NormArgs {
 
 // Sums over a row of K values of each lane: over its group of lanes, or over all waves
 // of the workgroup (WIDE) through one of two buffers in turn, so that one barrier
-// does for each.
+// does for each: 16 lanes read the 16 waves' sums (zeros of waves that are not there) and
+// add them up as they do their own.
 template <bool WIDE, int K>
 __device__ __forceinline__ void row_sums(float (&s)[K], int ls, float (*buf)[16][2], int& turn) {
 #pragma unroll
-  for (int i = 0; i < K; ++i) s[i] = group_sum(s[i], ls);
+  for (int i = 0; i < K; ++i) s[i] = group_sum(s[i], WIDE ? 6 : ls);
   if constexpr (WIDE) {
-    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
-      for (int i = 0; i < K; ++i) buf[turn][wave][i] = s[i];
+      for (int i = 0; i < K; ++i) buf[turn][threadIdx.x >> 6][i] = s[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < K; ++i) s[i] = 0.f;
-    for (int w = 0; w < waves; ++w)
+    for (int i = 0; i < K; ++i) s[i] = buf[turn][threadIdx.x & 15][i];
 #pragma unroll
-      for (int i = 0; i < K; ++i) s[i] += buf[turn][w][i];
+    for (int i = 0; i < K; ++i) s[i] = group_sum(s[i], 4);
     turn ^= 1;
   }
+}
+__device__ __forceinline__ void clear(float (*buf)[16][2]) {
+  if (threadIdx.x < 64) ((float*)buf)[threadIdx.x] = 0.f;
+  __syncthreads();
 }
 
 // N(t): the mean and factor of the row, t becomes the normed row.  Lanes past the row
@@ -136,6 +139,7 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, WIDE ? 4 : 2) norm_fwd(cons
   const int64_t col = 8 * (int64_t)chunk;
   Vectors w;
   load_vectors<T, FULL, true>(a, in, col, w);
+  if constexpr (WIDE) clear(buf);
   const uint64_t seed = DROP ? a.drop.the_seed() : 0;
   const Source from_x(a.x, a.xs, a.x), from_y(a.y, a.ys, a.x);
   for (; row < a.n; row += step) {
@@ -217,6 +221,7 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, WIDE || !BIAS ? 4 : 2) norm
   float sg[8], sw1[8], sb1[8], sw2[8], sb2[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) sg[e] = sw1[e] = sb1[e] = sw2[e] = sb2[e] = 0.f;
+  if constexpr (WIDE) clear(buf);
   const uint64_t seed = DROP ? a.drop.the_seed() : 0;
   // dropout's factor is the gate's, and that of the gate's sums
   if (DROP)
