@@ -14,12 +14,12 @@
 // wave, or several waves.  It stays in registers from its load to its last use, so the
 // variance is that of the centred row and the backward reads each input once; h is
 // taken again from x and y there (as many bytes as reading it back, and not rounded).
-// What a lane adds up for its features over all its rows are 40 registers at most, then
+// What a lane adds up for its features over all its rows are 32 registers at most, then
 // one row of partial sums for each workgroup, joined in order by a second launch.
 // Bound by the rows' bytes without gate, first norm and dropout (17408 x 512: 13 us forward and 21
-// backward for 71 and 107 MB; 50001 x 1160: 78 and 142), with them by the vector unit: 400 to 500
-// instructions for 8 features (50001 x 1160 with everything: 128 and 190 us, of a floor of 92
-// and 138).  8 rows of 4096 forward: 4.8 us.
+// backward for 71 and 107 MB; 50001 x 1160: 77 and 138, of a floor of 92 and 138).  With
+// everything the vector unit has about as much to do, some 400 instructions for 8 features:
+// 50001 x 1160 108 and 154 us, 20001 x 2568 117 and 134 of 82 and 122.  8 rows of 4096 forward: 4.2 to 4.8 us.
 #include "block.hpp"
 
 namespace infcl {
@@ -188,13 +188,16 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, WIDE ? 4 : 2) norm_fwd(cons
   }
 }
 
-// BIAS: with sums for biases.  With everything (FULL, BIAS) a lane would take 151 registers,
-// three waves on a SIMD.  In rows of several waves the biases' sums, the first bias and the
-// gate are in LDS instead, each lane its own 32 bytes of them, and 16 waves fit a compute unit
-// (50001 x 768 131 us, 141 in registers; 30001 x 2048 176 and 180; where the waves of a row do not
-// divide twelve, 16001 x 4096, 184 and 280).
+// The sums of the first norm and the gate are two for each feature, S = sum e D v and
+// B = sum e D, whatever of them is asked for:
+//   dgate = post_w S + post_b B,  dpost_w = gate S,  dpost_b = gate B
+// and the rows' loop needs the vectors as gate post_w and gate post_b alone.
+// BIAS: with sums for biases.  In rows of several waves with everything their sums and gate
+// post_b are in LDS, each lane its own 32 bytes of them, so that 16 waves fit a compute unit with
+// the next row's loads (116 to 118 registers; 106 without).  With sums for each vector instead of
+// S and B: 151 registers, 50001 x 1160 188 us for 173, 20001 x 2568 183 for 164.
 template <int T, bool WIDE, bool FULL, bool BIAS, bool DROP, bool FAR>
-__global__ void __launch_bounds__(WIDE ? 1024 : 256, WIDE || !BIAS ? 4 : 2) norm_bwd(const NormArgs a) {
+__global__ void __launch_bounds__(WIDE ? 1024 : 256, 4) norm_bwd(const NormArgs a) {
   __shared__ float buf[2][16][2];
   __shared__ float joined[WIDE ? 1 : 4][WIDE ? 1 : 512];
   int64_t row, step;
@@ -202,13 +205,8 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, WIDE || !BIAS ? 4 : 2) norm
   place<WIDE>(a, row, step, chunk);
   const bool in = chunk < a.c;
   const int64_t col = 8 * (int64_t)chunk;
-  extern __shared__ f32x4 own[];  // kOwn: [sb2, sb1, b1, gate][halves][lanes]
+  extern __shared__ f32x4 own[];  // kOwn: [sb2, B, gate post_b][halves][lanes]
   constexpr bool kOwn = WIDE && FULL && BIAS;
-  auto add_own = [&](int k, const float (&q)[8]) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      own[(2 * k + i) * blockDim.x + threadIdx.x] += f32x4{q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]};
-  };
   auto get_own = [&](int k, float (&q)[8]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -217,36 +215,51 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, WIDE || !BIAS ? 4 : 2) norm
       for (int e = 0; e < 4; ++e) q[4 * i + e] = x[e];
     }
   };
-  Vectors w;
-  load_vectors<T, FULL, BIAS>(a, in, col, w);
-  if constexpr (kOwn) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) own[i * blockDim.x + threadIdx.x] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
   auto put_own = [&](int k, const float (&q)[8]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       own[(2 * k + i) * blockDim.x + threadIdx.x] = f32x4{q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]};
   };
-  float sg[8], sw1[8], sb1[8], sw2[8], sb2[8];
+  auto add_own = [&](int k, const float (&q)[8]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sg[e] = sw1[e] = sb1[e] = sw2[e] = sb2[e] = 0.f;
+    for (int i = 0; i < 2; ++i)
+      own[(2 * k + i) * blockDim.x + threadIdx.x] += f32x4{q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]};
+  };
+  float gw[8], gb[8], w2[8], S[8], B[8], sw2[8], sb2[8];
+  const float unit = DROP ? a.drop.unit : 1.f;
+  {
+    Vectors w;
+    load_vectors<T, FULL, BIAS>(a, in, col, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float g = DROP ? w.gate[e] * unit : w.gate[e];  // dropout's factor is the gate's
+      gw[e] = g * w.w1[e], gb[e] = g * w.b1[e], w2[e] = w.w2[e];
+      S[e] = B[e] = sw2[e] = sb2[e] = 0.f;
+    }
+  }
+  if constexpr (kOwn) put_own(0, sb2), put_own(1, B), put_own(2, gb);
   if constexpr (WIDE) clear(buf);
   const uint64_t seed = DROP ? a.drop.the_seed() : 0;
-  // dropout's factor is the gate's, and that of the gate's sums
-  if (DROP)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w.gate[e] *= a.drop.unit;
-  if (kOwn) put_own(2, w.b1), put_own(3, w.gate);
   const Source from_x(a.x, a.xs, a.x), from_y(a.y, a.ys, a.x), from_dh(a.dh, a.dhs, a.x), from_dz(a.dz, a.dzs, a.x);
   const bool post = FULL && a.post_w;
+  // The next row beside the sums, as in the forward (50001 x 1160 154 us for 173, 20001 x 2568 134 for
+  // 164, 16001 x 4096 168 for 162); fp32 rows and biases' sums leave no registers for it.
+  constexpr bool kAhead = WIDE && FULL && !(BIAS && T == kF32);
+  Raw8<T> next_x, next_y, next_dh, next_dz;
+  float4 next_st;
+  auto load = [&](int64_t r) {
+    next_x.load(from_x.p, from_x.at(r, in, col));
+    next_y.load(from_y.p, from_y.at(r, in, col));
+    next_dh.load(from_dh.p, from_dh.at(r, in, col));
+    next_dz.load(from_dz.p, from_dz.at(r, in, col));
+    next_st = a.stats[r];
+  };
+  if (kAhead && row < a.n) load(row);
   for (; row < a.n; row += step) {
-    Raw8<T> rx, ry, rh, rz;
-    rx.load(from_x.p, from_x.at(row, in, col));
-    ry.load(from_y.p, from_y.at(row, in, col));
-    rh.load(from_dh.p, from_dh.at(row, in, col));
-    rz.load(from_dz.p, from_dz.at(row, in, col));
-    float4 st = a.stats[row];
+    if (!kAhead) load(row);
+    const Raw8<T> rx = next_x, ry = next_y, rh = next_dh, rz = next_dz;
+    float4 st = next_st;
+    if (kAhead) load(row + step < a.n ? row + step : row);
     if (!post) st.x = 0.f, st.y = 1.f;
     if (!in) st.y = st.w = 0.f;  // (normed rows of lanes past the row are zeros)
     bool keep[8];
@@ -263,26 +276,13 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, WIDE || !BIAS ? 4 : 2) norm
     ry.get(in && from_y.there, v);
     rh.get(in && from_dh.there, e8);
     rz.get(in && from_dz.there, g);
-    // what the gate took (without dropout's factor), from the normed y
-    auto taken = [&](int e, const float (&b)[8]) {
-      const float t = BIAS ? fmaf(v[e], w.w1[e], b[e]) : v[e] * w.w1[e];
-      return keep[e] ? t : 0.f;
-    };
-    float b1[8], gate[8];
-    auto get = [&]() {
-      if constexpr (kOwn) {
-        get_own(2, b1), get_own(3, gate);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) b1[e] = w.b1[e], gate[e] = w.gate[e];
-      }
-    };
-    get();
     if (a.y) {
+      if constexpr (kOwn) get_own(2, gb);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if (FULL) v[e] = (v[e] - st.x) * st.y;
-        h[e] = fmaf(a.alpha, h[e], FULL ? gate[e] * taken(e, b1) : v[e]);
+        const float t = !FULL ? v[e] : BIAS ? fmaf(v[e], gw[e], gb[e]) : v[e] * gw[e];
+        h[e] = fmaf(a.alpha, h[e], keep[e] ? t : 0.f);
       }
     }
     if (a.pre_w) {
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, WIDE || !BIAS ? 4 : 2) norm
         h[e] = (h[e] - st.z) * st.w;
         sw2[e] = fmaf(g[e], h[e], sw2[e]);
         if (BIAS && !kOwn) sb2[e] += g[e];
-        g[e] *= w.w2[e];
+        g[e] *= w2[e];
         s[0] += g[e], s[1] = fmaf(g[e], h[e], s[1]);
       }
       row_sums<WIDE, 2>(s, a.ls, buf, turn);
@@ -309,21 +309,20 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, WIDE || !BIAS ? 4 : 2) norm
     }
     if (!a.y) continue;
     if constexpr (FULL) {
-      get();
-      float s[2] = {0.f, 0.f}, qs[8];
+      float s[2] = {0.f, 0.f};
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        sg[e] = fmaf(e8[e], taken(e, b1), sg[e]);
-        float q = keep[e] ? e8[e] * gate[e] : 0.f;
-        sw1[e] = fmaf(q, v[e], sw1[e]);
-        if (BIAS && !kOwn) sb1[e] += q;
-        qs[e] = q;
-        q *= w.w1[e];
-        s[0] += q, s[1] = fmaf(q, v[e], s[1]);
-        e8[e] = q;
+        S[e] = fmaf(e8[e], keep[e] ? v[e] : 0.f, S[e]);
+        e8[e] = keep[e] ? e8[e] : 0.f;
+        if (BIAS && !kOwn) B[e] += e8[e];
+      }
+      if (kOwn && (a.want_post_b || (a.want_gate && a.post_b))) add_own(1, e8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        e8[e] *= gw[e];
+        s[0] += e8[e], s[1] = fmaf(e8[e], v[e], s[1]);
       }
       if (post) {
-        if (kOwn && a.want_post_b) add_own(1, qs);
         row_sums<WIDE, 2>(s, a.ls, buf, turn);
         const float m = a.rms ? 0.f : s[0] * a.by_d, k = s[1] * a.by_d;
 #pragma unroll
@@ -332,11 +331,17 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, WIDE || !BIAS ? 4 : 2) norm
     }
     if (a.dy && in) store8<T, FAR>(a.dy, row * (8 * (int64_t)a.c) + col, e8);
   }
-  if (DROP)
+  if constexpr (kOwn) get_own(0, sb2), get_own(1, B);
+  float sg[8];
+  if constexpr (FULL) {  // the vectors' own sums
+    Vectors w;
+    load_vectors<T, FULL, BIAS>(a, in, col, w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sg[e] *= a.drop.unit;
-
-  if constexpr (kOwn) get_own(0, sb2), get_own(1, sb1);
+    for (int e = 0; e < 8; ++e) {
+      sg[e] = unit * (BIAS ? fmaf(w.b1[e], B[e], w.w1[e] * S[e]) : w.w1[e] * S[e]);
+      S[e] *= w.gate[e] * unit, B[e] *= w.gate[e] * unit;
+    }
+  }
 
   // One row of sums of the workgroup: groups of a wave, then waves, in order.
   const int d = 8 * a.c;
@@ -368,8 +373,8 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, WIDE || !BIAS ? 4 : 2) norm
     }
   };
   if (FULL && a.want_gate) put(sg);
-  if (FULL && a.want_post) put(sw1);
-  if (FULL && BIAS && a.want_post_b) put(sb1);
+  if (FULL && a.want_post) put(S);
+  if (FULL && BIAS && a.want_post_b) put(B);
   if (a.want_pre) put(sw2);
   if (BIAS && a.want_pre_b) put(sb2);
 }
@@ -433,10 +438,9 @@ unsigned grid_of(const Shape& s, int64_t n, int waves) {
   return (unsigned)(need < most ? need : most);
 }
 // The forward starts more than that: nothing is left to be joined.  The backward's kernels
-// have registers for 16 or more waves, with everything and biases in rows of one wave for 12
-// (17408 x 512: 37 us with 12, 46 with 16; 30001 x 2048 without gate and norm of y: 144 us with
-// 16, 151 with 20).
-constexpr int kFwdWaves = 32, kBwdWaves = 16, kBwdWavesAll = 12;
+// have registers for 16 waves (30001 x 2048 without gate and norm of y: 144 us with 16, 151
+// with 20).
+constexpr int kFwdWaves = 32, kBwdWaves = 16;
 
 infcl_status check(const infcl_add_norm* a) {
   if (!a || a->n < 0 || a->d < 1 || !type_known(a->dtype) || !type_known(a->wdtype) ||
@@ -483,7 +487,7 @@ void fwd_t(const NormArgs& r, const Shape& s, hipStream_t st) {
 template <int T, bool FULL, bool BIAS, bool DROP, bool FAR>
 void bwd_t(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
   const dim3 grid(wgs), block(s.threads);
-  const size_t own = FULL && BIAS ? 8 * 16 * (size_t)s.threads : 0;
+  const size_t own = FULL && BIAS ? 6 * 16 * (size_t)s.threads : 0;
   if (!s.wide)
     hipLaunchKernelGGL((norm_bwd<T, false, FULL, BIAS, DROP, FAR>), grid, block, 0, st, r);
   else
@@ -596,7 +600,7 @@ extern "C" infcl_status infcl_add_norm_bwd(const infcl_add_norm* a, const void* 
   for (void* o : {g->dgate, g->dpost_w, g->dpost_b, g->dpre_w, g->dpre_b})
     if (o) outs[sums++] = o;
   hipStream_t st = (hipStream_t)stream;
-  const unsigned wgs = grid_of(sh, a->n, !sh.wide && full(r) && (r.post_b || r.pre_b) ? kBwdWavesAll : kBwdWaves);
+  const unsigned wgs = grid_of(sh, a->n, kBwdWaves);
   if (wgs > 0) {
     if (a->dtype == INFCL_BF16)
       bwd_any<kBF16>(r, sh, wgs, st);
