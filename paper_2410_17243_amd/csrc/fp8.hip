@@ -36,10 +36,11 @@ __device__ __forceinline__ void put_exponent(uint8_t* row, int64_t b, int64_t bl
 // Along rows alone: 16 lanes take a block.
 template <int T>
 __global__ void __launch_bounds__(256) pack_rows(const PackArgs a) {
-  const int64_t blocks = a.blocks, total = a.n * blocks, step = (int64_t)gridDim.x * 16;
+  const uint32_t blocks = (uint32_t)a.blocks, total = (uint32_t)a.n * blocks, step = gridDim.x * 16;  // (below 2^31)
   const int lane = threadIdx.x & 15;
-  for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < total; i += step) {
-    const int64_t r = i / blocks, b = i - r * blocks, col = b * 128 + 8 * lane;
+  for (uint32_t i = blockIdx.x * 16 + (threadIdx.x >> 4); i < total; i += step) {
+    const uint32_t at = i / blocks, block = i - at * blocks;
+    const int64_t r = at, b = block, col = b * 128 + 8 * lane;
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (col < a.d) load8<T>(a.x, r * a.xs + col, v);
     uint32_t m = 0;
@@ -66,15 +67,25 @@ __global__ void __launch_bounds__(256, 2) pack_tile(const PackArgs one, const Pa
   const uint32_t at = blockIdx.x < first ? blockIdx.x : blockIdx.x - first, across = (uint32_t)a.blocks;
   const int64_t tiles = a.blocks, rt = at / across, ct = at % across;
   const int64_t row0 = rt * 128 + 8 * g, col = ct * 128 + 8 * c;
-  // all loads first, of some other row or chunk where there is none (one at a time, each in a
-  // branch of its own, 10007 x 776 took 16 us instead of 10)
+  const int rows = a.n - row0 < 8 ? (int)(a.n - row0) : 8;  // (none or fewer: this lane's rows are not there)
+  const int cols = a.d - ct * 128 < 128 ? (int)(a.d - ct * 128) : 128;  // of the tile
+  // Addresses go from row to row by additions (with products of 64 bits for each, 1366
+  // instructions instead of 1147, a hundred of them at a quarter of the rate).  All loads first, of some other row
+  // or chunk where there is none (one at a time, each in a branch of its own, 10007 x 776 took 16 us
+  // instead of 10).
+  constexpr int kSize = T == kF32 ? 4 : 2;
   Raw8<T> raw[8];
+  const char* from = (const char*)a.x + ((row0 < a.n ? row0 : a.n - 1) * a.xs + (col < a.d ? col : 0)) * kSize;
 #pragma unroll
-  for (int r = 0; r < 8; ++r) raw[r].load(a.x, (row0 + r < a.n ? row0 + r : a.n - 1) * a.xs + (col < a.d ? col : 0));
+  for (int r = 0; r < 8; ++r) {
+    raw[r].load(from, 0);
+    from += r + 1 < rows ? a.xs * kSize : 0;
+  }
   float v[8][8];
 #pragma unroll
-  for (int r = 0; r < 8; ++r) raw[r].get(row0 + r < a.n && col < a.d, v[r]);
+  for (int r = 0; r < 8; ++r) raw[r].get(r < rows && col < a.d, v[r]);
   if (a.q) {
+    uint8_t *to = a.q + row0 * a.kp + col, *ex = a.ex + row0 * a.ep + ct;
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
       uint32_t m = 0;
@@ -84,11 +95,14 @@ __global__ void __launch_bounds__(256, 2) pack_tile(const PackArgs one, const Pa
       const float inv = fp8_inverse(byte);
       uint2 w = make_uint2(fp8_pack4(v[r][0], v[r][1], v[r][2], v[r][3], inv), fp8_pack4(v[r][4], v[r][5], v[r][6], v[r][7], inv));
       if (byte == 255) w = make_uint2(kFp8Nan, kFp8Nan);
-      if (row0 + r < a.n) {
-        *(uint2*)(a.q + (row0 + r) * a.kp + col) = w;
-        if (c == 0) put_exponent(a.ex + (row0 + r) * a.ep, ct, tiles, byte);
+      if (r < rows) {
+        *(uint2*)to = w;
+        if (c == 0) *ex = (uint8_t)byte;
       }
+      to += a.kp, ex += a.ep;
     }
+    if (ct == tiles - 1 && threadIdx.x < 128 && rt * 128 + threadIdx.x < a.n)  // 127 to the end of the last word
+      for (int64_t i = tiles; i & 3; ++i) a.ex[(rt * 128 + threadIdx.x) * a.ep + i] = 127;
   }
   if (a.qt) {
 #pragma unroll
@@ -117,6 +131,7 @@ __global__ void __launch_bounds__(256, 2) pack_tile(const PackArgs one, const Pa
     a.sums[rt * a.d + ct * 128 + i] = sum[0][i] + sum[1][i] + sum[2][i] + sum[3][i];
   }
   if (!a.qt) return;
+  uint8_t* ext = a.ext + col * a.tep + rt;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int f = 8 * c + e;
@@ -125,13 +140,19 @@ __global__ void __launch_bounds__(256, 2) pack_tile(const PackArgs one, const Pa
     uint2 w = make_uint2(fp8_pack4(v[0][e], v[1][e], v[2][e], v[3][e], inv), fp8_pack4(v[4][e], v[5][e], v[6][e], v[7][e], inv));
     if (byte == 255) w = make_uint2(kFp8Nan, kFp8Nan);
     *(uint2*)(tile + f * 144 + 8 * g) = w;
-    if (g == 0 && ct * 128 + f < a.d) put_exponent(a.ext + (ct * 128 + f) * a.tep, rt, (a.n + 127) / 128, byte);
+    if (g == 0 && f < cols) *ext = (uint8_t)byte;
+    ext += a.tep;
   }
+  const int64_t down = (a.n + 127) / 128;
+  if (rt == down - 1 && (int)threadIdx.x < cols)
+    for (int64_t i = down; i & 3; ++i) a.ext[(ct * 128 + threadIdx.x) * a.tep + i] = 127;
   __syncthreads();
+  const int f0 = threadIdx.x >> 3, byte0 = 16 * (threadIdx.x & 7);
+  uint8_t* to = a.qt + (ct * 128 + f0) * a.tp + rt * 128 + byte0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {  // 8 lanes write the 128 bytes of a feature
-    const int f = 32 * i + (threadIdx.x >> 3), at = 16 * (threadIdx.x & 7);
-    if (ct * 128 + f < a.d) *(u32x4*)(a.qt + (ct * 128 + f) * a.tp + rt * 128 + at) = *(const u32x4*)(tile + f * 144 + at);
+    if (32 * i + f0 < cols) *(u32x4*)to = *(const u32x4*)(tile + (32 * i + f0) * 144 + byte0);
+    to += 32 * a.tp;
   }
 }
 
