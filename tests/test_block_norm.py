@@ -50,6 +50,12 @@ CASES = [  # rows, features, dtype, parts, the vectors' dtype, norm, alpha, p
     (4, 8184, "f32", ("y",), "f32", "rms", 0.25, 0.0),
     (5000, 24, "f32", ALL, "f32", "layer", 1.0, 0.1),          # many rows of few lanes
     (1100, 1032, "bf16", ("pre_w",), "f32", "rms", 1.0, 0.0),  # more rows than workgroups
+    (3001, 1160, "bf16", ALL, "f32", "layer", 1.0, 0.1),       # ... with everything, in each form that has
+    (2701, 1032, "f32", ALL, "f32", "layer", -0.5, 0.1),
+    (2701, 776, "f32", ("y", "post_w", "gate", "pre_w"), "f32", "rms", 1.0, 0.25),
+    (601, 8192, "f16", ALL, "f16", "layer", 1.0, 0.0),
+    (601, 6008, "f16", ("y", "post_w", "gate", "pre_w", "pre_b"), "f16", "layer", 1.0, 0.1),
+    (601, 4104, "bf16", ("y", "gate"), "bf16", "rms", 1.0, 0.5),
 ]
 
 
