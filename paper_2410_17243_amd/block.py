@@ -6,8 +6,10 @@ operators of tower.py: rotary positions, dropout, residual sums with their norms
 layers on 8-bit floats.  As there, this module only marshals arguments; the work is
 done by the HIP kernels of libinfcl.so on the current stream, and nothing falls back.
 The autograd functions are differentiable once: a gradient of their gradient is an
-error.  They may be captured into a HIP graph with their backward pass, while no eager
-graph of the same leaves is alive (as torch asks of every captured backward pass).
+error, and so is a forward-mode derivative.  torch.jit.trace records their calls, with
+the options and whether gradients were on.  They may be captured into a HIP graph with
+their backward pass, while no eager graph of the same leaves is alive (as torch asks of
+every captured backward pass).
 
 Rotary positions
     rotary_freqs(sections, base=10000.0) -> freqs
@@ -37,6 +39,7 @@ import ctypes
 import functools
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from . import _check, _ptr, _raw_stream, load_library
@@ -217,8 +220,6 @@ def rotary(x, pos, freqs, sections=None, turned=None, paired: str = "halves"):
     """rotary_fwd's out; differentiable with respect to x (positions and frequencies are
     constants).  The queries and keys of a projection at once: rotary(qkv, ...,
     turned=heads + kv_heads), then packed_attn_qkv."""
-    if not torch.is_grad_enabled() or not x.requires_grad:
-        return rotary_fwd(x, pos, freqs, sections, turned, paired)
     return _RotaryFn.apply(x, pos, freqs, sections, turned, paired)
 
 
@@ -278,8 +279,6 @@ class _DropoutFn(torch.autograd.Function):
 
 def dropout(x, p: float, seed, site: int = 0, row0: int = 0):
     """dropout_fwd's out; differentiable with respect to x."""
-    if not torch.is_grad_enabled() or not x.requires_grad:
-        return dropout_fwd(x, p, seed, site, row0)
     return _DropoutFn.apply(x, p, seed, site, row0)
 
 
@@ -395,12 +394,15 @@ def add_norm_bwd(dh, dz, kept: AddNormKept, need=(True,) * 7):
 
 class _AddNormFn(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, options, x, y, *vectors):
-        norm, eps, alpha, p, seed, site, row0 = options
-        h, z, kept = add_norm_fwd(x, y, *vectors, norm=norm, eps=eps, alpha=alpha, p=p, seed=seed, site=site, row0=row0)
-        tensor = isinstance(seed, torch.Tensor)
-        ctx.save_for_backward(x, y, *vectors, kept.stats, seed if tensor else None)
-        ctx.options = (*options[:4], None if tensor else seed, *options[5:])
+    def forward(ctx, grads, options, seed, x, y, *vectors):
+        norm, eps, alpha, p, site, row0 = options
+        learns = grads and any(ctx.needs_input_grad)
+        h, z, kept = add_norm_fwd(x, y, *vectors, norm=norm, eps=eps, alpha=alpha, p=p, seed=seed, site=site, row0=row0,
+                                  need_grad=learns)
+        if learns:
+            tensor = isinstance(seed, torch.Tensor)
+            ctx.save_for_backward(x, y, *vectors, kept.stats, seed if tensor else None)
+            ctx.options = (*options[:4], None if tensor else seed, *options[4:])
         ctx.set_materialize_grads(False)
         ctx.both = y is not None and z is not None
         return (h, z) if ctx.both else h if z is None else z
@@ -411,10 +413,11 @@ class _AddNormFn(torch.autograd.Function):
         x, y, *vectors, stats, seed = ctx.saved_tensors
         dh, dz = d if ctx.both else (d[0], None) if vectors[3] is None else (None, d[0])
         if dh is None and dz is None:
-            return (None,) * 8
+            return (None,) * 10
         options = ctx.options if seed is None else (*ctx.options[:4], seed, *ctx.options[5:])
         dh, dz = (t if t is None else t.contiguous() for t in (dh, dz))
-        return (None, *add_norm_bwd(dh, dz, AddNormKept(x, y, tuple(vectors), stats, options), ctx.needs_input_grad[1:]))
+        kept = AddNormKept(x, y, tuple(vectors), stats, options)
+        return (None, None, None, *add_norm_bwd(dh, dz, kept, ctx.needs_input_grad[3:]))
 
 
 def add_norm(x, y=None, gate=None, post_w=None, post_b=None, pre_w=None, pre_b=None, norm: str = "layer",
@@ -422,10 +425,7 @@ def add_norm(x, y=None, gate=None, post_w=None, post_b=None, pre_w=None, pre_b=N
     """add_norm_fwd's (h, z); differentiable with respect to x, y, gate and the norms'
     vectors."""
     args = (x, y, gate, post_w, post_b, pre_w, pre_b)
-    options = (norm, float(eps), float(alpha), float(p), seed, site, row0)
-    if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in args):
-        return add_norm_fwd(*args, *options, need_grad=False)[:2]
-    res = _AddNormFn.apply(options, *args)
+    res = _AddNormFn.apply(torch.is_grad_enabled(), (norm, float(eps), float(alpha), float(p), site, row0), seed, *args)
     return (x, res) if y is None else (res, None) if pre_w is None else res
 
 
@@ -591,15 +591,24 @@ def linear_fp8_bwd(dy, kept, need=(True, True, True)):
 
 class _LinearFp8(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, b):
-        y, (kept, ctx.rest) = linear_fp8_fwd(x, w, b, ctx.needs_input_grad[0], ctx.needs_input_grad[1])
+    def forward(ctx, grads, x, w, b):
+        need_dx, need_dw = (grads and n for n in ctx.needs_input_grad[1:3])
+        y, (kept, ctx.rest) = linear_fp8_fwd(x, w, b, need_dx, need_dw)
         ctx.save_for_backward(kept)
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        return linear_fp8_bwd(dy.contiguous(), (ctx.saved_tensors[0], ctx.rest), ctx.needs_input_grad)
+        return (None, *linear_fp8_bwd(dy.contiguous(), (ctx.saved_tensors[0], ctx.rest), ctx.needs_input_grad[1:]))
+
+
+class _LinearPacked(torch.autograd.Function):
+    """The forward alone, for a trace to record and forward mode to refuse."""
+
+    @staticmethod
+    def forward(ctx, x, q, exps, k, dtype, b):
+        return _times_packed(x, Fp8(q, exps, k, dtype), b)
 
 
 def linear_fp8(x, w, b=None):
@@ -613,10 +622,10 @@ def linear_fp8(x, w, b=None):
     if torch.is_autocast_enabled("cuda"):
         dtype = torch.get_autocast_dtype("cuda")
         x, w, b = x.to(dtype), w.to(dtype), None if b is None else b.to(dtype)
-    if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in (x, w, b)):
-        return linear_fp8_fwd(x, w, b, False, False)[0]
-    _learns(w.shape[0])
-    return _LinearFp8.apply(x, w, b)
+    grads = torch.is_grad_enabled()
+    if grads and any(t is not None and t.requires_grad for t in (x, w, b)):
+        _learns(w.shape[0])
+    return _LinearFp8.apply(grads, x, w, b)
 
 
 def _linear_packed(x, w, b):
@@ -626,7 +635,9 @@ def _linear_packed(x, w, b):
     if torch.is_autocast_enabled("cuda"):
         x = x.to(torch.get_autocast_dtype("cuda"))
         b = None if b is None else b.to(x.dtype)
-    return _times_packed(x, w, b)
+    if forward_ad._current_level < 0 and not torch.jit.is_tracing():  # (2.5 us less a call)
+        return _times_packed(x, w, b)
+    return _LinearPacked.apply(x, w.q, w.exps, w.k, w.dtype, b)
 
 
 def _times_packed(x, w, b):

@@ -103,6 +103,74 @@ def test_only_what_is_asked_for_has_a_gradient(plain_kernels, name):
         assert torch.equal(some[i].grad, full[i]) and all(a.grad is None for j, a in enumerate(some) if j != i)
 
 
+def _opaque(fn):
+    """fn as a kernel is to torch: what it computes is not seen as torch operations."""
+    def call(*args, **kw):
+        plain = lambda t: torch.from_numpy(t.detach().numpy().copy()) if isinstance(t, torch.Tensor) and t.is_floating_point() else t  # noqa: E731
+        res = fn(*(plain(a) for a in args), **{k: plain(a) for k, a in kw.items()})
+        return plain(res) if isinstance(res, torch.Tensor) else tuple(plain(r) for r in res)
+    return call
+
+
+@pytest.fixture
+def opaque_kernels(plain_kernels, monkeypatch):
+    for name in ("rotary_fwd", "dropout_fwd", "add_norm_fwd", "linear_fp8_fwd"):
+        monkeypatch.setattr(block, name, _opaque(getattr(block, name)))
+    monkeypatch.setattr(block, "_times_packed", _opaque(lambda x, w, b: torch.nn.functional.linear(x, w.q.double(), b)))
+
+
+def _apart(name):
+    """_call with the arguments as tensors without gradients, and products of packed weights."""
+    if name == "packed":
+        g = torch.Generator().manual_seed(4)
+        w = infcl.Fp8(torch.randint(0, 5, (16, 128), generator=g, dtype=torch.uint8), torch.full((16, 4), 127, dtype=torch.uint8), 128, torch.float64)
+        return lambda x: infcl.linear_fp8(x, w), [torch.randn((3, 128), generator=g, dtype=torch.float64)]
+    f, args = _call(name)
+    return f, [a.detach() for a in args]
+
+
+@pytest.mark.parametrize("grad", [True, False])
+@pytest.mark.parametrize("name", [*NAMES, "packed"])
+def test_forward_mode_is_refused(opaque_kernels, name, grad):
+    """A tensor that carries a tangent, and none that has gradients: no derivative is lost silently."""
+    f, args = _apart(name)
+    for i in range(len(args)):
+        with torch.set_grad_enabled(grad), torch.autograd.forward_ad.dual_level():
+            dual = [torch.autograd.forward_ad.make_dual(a, torch.ones_like(a)) if j == i else a for j, a in enumerate(args)]
+            with pytest.raises(NotImplementedError):
+                f(*dual)
+
+
+@pytest.mark.parametrize("name", [*NAMES, "packed"])
+def test_traced_calls_compute(opaque_kernels, name):
+    """A trace of inputs without gradients holds the call, not one call's results."""
+    f, args = _apart(name)
+    traced = torch.jit.trace(f, tuple(args), check_trace=False)
+    for seed in range(2):
+        g = torch.Generator().manual_seed(seed)
+        new = [torch.randn(a.shape, generator=g, dtype=a.dtype) for a in args]
+        want = f(*new)
+        assert torch.equal(traced(*new), want) and float(want.norm()) > 0
+        with torch.no_grad():
+            assert torch.equal(traced(*new), want)
+        if name != "packed":  # (and its gradients, where they are asked for later)
+            leaves = [a.requires_grad_() for a in new]
+            assert all(torch.equal(p, q) for p, q in zip(torch.autograd.grad(traced(*leaves).sum(), leaves),
+                                                         torch.autograd.grad(f(*leaves).sum(), leaves)))
+
+
+@pytest.mark.parametrize("name", ["dropout", "add_norm"])
+def test_a_traced_seed_is_an_input(monkeypatch, name):
+    """A seed in a tensor is read anew at every call of a trace."""
+    seen = []
+    monkeypatch.setattr(block, "dropout_fwd", lambda x, p, seed, *a: seen.append(int(seed)) or torch.zeros(x.shape))
+    monkeypatch.setattr(block, "add_norm_fwd", lambda x, y, *v, seed, **k: seen.append(int(seed)) or (torch.zeros(x.shape), None, None))
+    f = {"dropout": lambda x, s: infcl.dropout(x, 0.5, s), "add_norm": lambda x, s: infcl.add_norm(x, x, p=0.5, seed=s)[0]}[name]
+    traced = torch.jit.trace(f, (torch.ones((6, 8)), torch.tensor([3])), check_trace=False)
+    traced(torch.ones((6, 8)), torch.tensor([8]))
+    assert seen == [3, 8]
+
+
 @pytest.mark.gpu
 def test_a_block_captured_into_a_graph():
     """Forward and backward of a run of all of them, captured once and replayed with new
@@ -238,3 +306,35 @@ def test_two_streams_at_once():
     for i in range(2):
         for g in got[i]:
             assert all(torch.equal(a, c) for a, c in zip(g, want[i]))
+
+
+@pytest.mark.gpu
+def test_a_trace_of_a_run():
+    """torch.jit.trace of inputs without gradients: other inputs, and leaves, go through the
+    kernels.  A tangent is refused."""
+    args = [a.detach() for a in _leaves(40)]
+    pos, freqs, seed = torch.arange(40, dtype=torch.int32, device="cuda"), infcl.rotary_freqs(16), torch.tensor([5], device="cuda")
+    packed = infcl.fp8_pack(torch.randn((24, 64), device="cuda").bfloat16())
+
+    def run(x, w, b, o, gate, n, seed):
+        q = infcl.rotary(infcl.linear_fp8(x, w, b).view(-1, 6, 32), pos, freqs, turned=4)
+        t = infcl.dropout(infcl.linear_fp8(q.reshape(-1, 192), o), 0.1, seed)
+        return infcl.add_norm(x, t, gate, pre_w=n, p=0.2, seed=seed, site=1)
+
+    traced = torch.jit.trace(run, (*args, seed), check_trace=False)
+    last = torch.jit.trace(lambda x: infcl.linear_fp8(x, packed), (args[0],), check_trace=False)
+    for rep in range(2):
+        leaves, seed = _leaves(40), torch.tensor([rep], device="cuda")
+        want, got = run(*leaves, seed), traced(*leaves, seed)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        grads = [torch.autograd.grad((h * z).float().sum(), leaves) for h, z in (want, got)]
+        assert all(torch.equal(a, b) for a, b in zip(*grads))
+        with torch.no_grad():
+            assert all(torch.equal(a, b) for a, b in zip(traced(*leaves, seed), want))
+            assert torch.equal(last(leaves[0]), infcl.linear_fp8(leaves[0], packed))
+    with torch.no_grad(), torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(args[0], torch.ones_like(args[0]))
+        for f in (lambda: infcl.dropout(dual, 0.1, 3), lambda: infcl.add_norm(dual, pre_w=args[5]), lambda: infcl.linear_fp8(dual, packed),
+                  lambda: infcl.linear_fp8(dual, args[1]), lambda: infcl.rotary(dual.view(40, 2, 32), pos, freqs)):
+            with pytest.raises(NotImplementedError):
+                f()
