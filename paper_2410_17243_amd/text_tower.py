@@ -120,6 +120,8 @@ class TextTower(torch.nn.Module):
         super().__init__()
         if products not in ("16bit", "fp8"):
             raise ValueError(f'products must be "16bit" or "fp8", got {products!r}')
+        if act not in ("gelu", "quick_gelu"):
+            raise ValueError(f'act must be "gelu" or "quick_gelu", got {act!r}')
         if not 0.0 <= dropout < 1.0:
             raise ValueError(f"dropout must be from 0 to below 1, got {dropout}")
         if width % heads or (width // heads) % 8 or width // heads > 128:

@@ -26,6 +26,14 @@ def test_choices_are_checked(kw):
         TextTower(300, 128, 2, 4, 64, 40, **kw)
 
 
+@pytest.mark.parametrize("products", ["16bit", "fp8"])
+@pytest.mark.parametrize("act", ["silu", "none", "GELU", None])
+def test_an_activation_that_is_not_there_is_refused(act, products):
+    """On 8-bit products as on 16-bit ones, and before a step is taken with another."""
+    with pytest.raises(ValueError, match="act must be"):
+        TextTower(300, 128, 2, 4, 64, 40, act=act, products=products)
+
+
 @pytest.mark.gpu
 def test_gates_of_one_change_nothing():
     """The same parameters with torch's sums and norms, and with add_norm: features and
