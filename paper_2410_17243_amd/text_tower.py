@@ -137,6 +137,16 @@ class TextTower(torch.nn.Module):
         self.norm = torch.nn.LayerNorm(width, dtype=dtype)
         self.proj = torch.nn.Parameter((torch.randn(out_dim, width) / width ** 0.5).to(dtype))
 
+    def _apply(self, fn, *args, **kw):
+        """.to(), .half() and their like: the frequencies move with the parameters and stay
+        fp32, the same bits (8 bits of a frequency are 0.007 rad at position 39)."""
+        freqs = self.freqs
+        super()._apply(fn, *args, **kw)
+        if freqs is not None:
+            dev = self.freqs.device
+            self.freqs = rotary_freqs(freqs.numel(), device=dev) if freqs.is_meta else freqs.to(dev)
+        return self
+
     def _features(self, x):
         return self._project(self.norm(x))
 

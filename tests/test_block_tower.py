@@ -4,6 +4,7 @@ products of 8-bit floats: chunked steps and single tokens."""
 import pytest
 import torch
 
+import paper_2410_17243_amd as infcl
 from paper_2410_17243_amd.gradcache import gradcache_step
 from paper_2410_17243_amd.text_tower import PackedCaptions, TextTower, synthetic_captions
 
@@ -32,6 +33,39 @@ def test_an_activation_that_is_not_there_is_refused(act, products):
     """On 8-bit products as on 16-bit ones, and before a step is taken with another."""
     with pytest.raises(ValueError, match="act must be"):
         TextTower(300, 128, 2, 4, 64, 40, act=act, products=products)
+
+
+def test_frequencies_outlive_a_cast():
+    """There and back, alone and inside another module, they are the same fp32 numbers; a
+    tower from the meta device has those of a new one."""
+    t = TextTower(300, 128, 1, 2, 64, 40, rotary=True)
+    want = infcl.rotary_freqs(32, device="cpu")
+    assert torch.equal(t.freqs, want)
+    for cast in (lambda m: m.half(), lambda m: m.bfloat16(), lambda m: m.to("cpu", torch.float16), lambda m: m.double(), lambda m: m.float()):
+        assert cast(t) is t and t.freqs.dtype == torch.float32 and torch.equal(t.freqs, want)
+    torch.nn.Sequential(t).half()
+    assert t.table.dtype == torch.float16 and torch.equal(t.freqs, want)
+    t.to("meta")
+    assert t.freqs.is_meta
+    t.to_empty(device="cpu")
+    assert t.freqs.dtype == torch.float32 and torch.equal(t.freqs, want)
+    t.freqs = 2 * want  # (another base is kept as well)
+    assert torch.equal(t.bfloat16().freqs, 2 * want) and "freqs" not in t.state_dict()
+    assert TextTower(300, 128, 1, 2, 64, 40).half().freqs is None
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_a_tower_that_was_cast_is_the_one_made_so(dtype):
+    """Rotary positions after .to(dtype) and .cuda(): the features of a tower of that dtype."""
+    dt = {"f16": torch.float16, "bf16": torch.bfloat16}[dtype]
+    torch.manual_seed(3)
+    made = TextTower(300, 128, 2, 4, 64, 40, dtype=dt, **ALL)
+    cast = TextTower(300, 128, 2, 4, 64, 40, dtype=torch.float32, **ALL)
+    cast.load_state_dict({k: v.float() for k, v in made.state_dict().items()})
+    c = synthetic_captions(40, 300, 40, seed=2)
+    with torch.no_grad():
+        assert torch.equal(cast.to(dt).cuda()(c), made.cuda()(c))
 
 
 @pytest.mark.gpu
