@@ -88,9 +88,9 @@ class _Block(torch.nn.Module):
     def heads_of(self, y):
         return y.view(-1, self.heads + 2 * self.kv_heads, self.hd)
 
-    def packed(self):
-        """The weights in 8-bit floats, for calls without gradients."""
-        return {k: fp8_pack(getattr(self, k).detach()) for k in ("qkv_w", "out_w", "w1", "w2")}
+    def packed(self, dtype):
+        """The weights, as layers of dtype take them, in 8-bit floats, for calls without gradients."""
+        return {k: fp8_pack(getattr(self, k).detach().to(dtype)) for k in ("qkv_w", "out_w", "w1", "w2")}
 
     def layer(self, x, w, b, packed=None):
         if self.products == "16bit":
@@ -126,7 +126,7 @@ class TextTower(torch.nn.Module):
             raise ValueError(f"dropout must be from 0 to below 1, got {dropout}")
         if width % heads or (width // heads) % 8 or width // heads > 128:
             raise ValueError(f"width {width} must be heads times a multiple of 8 up to 128, got {heads} heads")
-        self.max_len, self.dtype = max_len, dtype
+        self.max_len = max_len
         self.table = torch.nn.Parameter((0.02 * torch.randn(vocab, width)).to(dtype))
         self.places = None if rotary else torch.nn.Parameter((0.01 * torch.randn(max_len, width)).to(dtype))
         self.register_buffer("freqs", rotary_freqs(width // heads // 2, device="cpu") if rotary else None, persistent=False)
@@ -146,6 +146,14 @@ class TextTower(torch.nn.Module):
             dev = self.freqs.device
             self.freqs = rotary_freqs(freqs.numel(), device=dev) if freqs.is_meta else freqs.to(dev)
         return self
+
+    @property
+    def dtype(self):
+        return self.table.dtype
+
+    def _block_dtype(self):
+        """What the blocks' layers compute in."""
+        return torch.get_autocast_dtype("cuda") if torch.is_autocast_enabled("cuda") else self.dtype
 
     def _features(self, x):
         return self._project(self.norm(x))
@@ -196,13 +204,14 @@ class TextTower(torch.nn.Module):
 
     def new_cache(self, n: int):
         """Room for the keys and values of n captions, empty; with products of 8-bit floats
-        also the weights packed as they are now."""
-        dev = self.table.device
+        also the weights packed as they are now.  It is for calls of extend under the
+        autocast that it was made under, or none."""
+        dev, dtype = self.table.device, self._block_dtype()
         cu = torch.arange(n + 1, dtype=torch.int32, device=dev)
-        kv = [torch.zeros((2, n * self.max_len, b.kv_heads, b.hd), dtype=self.dtype, device=dev) for b in self.blocks]
-        packed = [b.packed() if b.products == "fp8" else {} for b in self.blocks]
+        kv = [torch.zeros((2, n * self.max_len, b.kv_heads, b.hd), dtype=dtype, device=dev) for b in self.blocks]
+        packed = [b.packed(dtype) if b.products == "fp8" else {} for b in self.blocks]
         return {"kv": kv, "cu_q": cu, "cu_k": cu * self.max_len, "len": torch.zeros(n, dtype=torch.int32, device=dev),
-                "taken": 0, "packed": packed}
+                "taken": 0, "packed": packed, "dtype": dtype}
 
     @torch.no_grad()
     def extend(self, tokens, cache):
@@ -211,6 +220,8 @@ class TextTower(torch.nn.Module):
         has room for max_len tokens of each."""
         if cache["taken"] == self.max_len or tokens.numel() != cache["len"].numel():
             raise ValueError(f"a token for each of {cache['len'].numel()} captions, {self.max_len} times at most")
+        if cache["dtype"] != self._block_dtype():
+            raise ValueError(f"the cache is of {cache['dtype']}, the blocks compute in {self._block_dtype()}: make it where it is used")
         cache["taken"] += 1
         at = cache["cu_k"][:-1].long() + cache["len"].long()
         x, pos = self._rows(tokens, cache["len"].clone())

@@ -151,6 +151,52 @@ def test_extending_token_by_token_gives_the_whole_captions_features(kw):
     assert float((whole - last).norm(dim=1).max()) < bound
 
 
+def _extended(t, tokens):
+    cache = t.new_cache(tokens.shape[0])
+    for i in range(tokens.shape[1]):
+        last = t.extend(tokens[:, i].contiguous(), cache)
+    return last, cache
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kw", [dict(), dict(rotary=True, gates=1.0), dict(products="fp8", **ALL)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_extending_under_autocast(kw, dtype):
+    """A tower of fp32 parameters over a cache made under the same autocast: the weights are
+    packed from what forward packs, byte for byte, and the features are those of whole
+    captions, with the bounds of bf16 parameters (above).  A cache of another dtype is
+    refused before anything of it changes."""
+    t = _tower(dtype=torch.float32, **kw).eval()
+    tokens = torch.randint(0, 300, (5, 9), generator=torch.Generator().manual_seed(5)).cuda()
+    with torch.no_grad(), torch.autocast("cuda", dtype):
+        whole = t(PackedCaptions(tokens.reshape(-1), [9] * 5))
+        last, cache = _extended(t, tokens)
+    bound = 16 ** 0.5 * 2.0 ** -6.5 if "products" in kw else 8 * 2.0 ** -8
+    assert float((whole - last).norm(dim=1).max()) < bound
+    for b, packed in zip(t.blocks, cache["packed"]):
+        for name, f in packed.items():
+            want = infcl.fp8_pack(getattr(b, name).detach().to(dtype))
+            assert torch.equal(f.q, want.q) and torch.equal(f.exps, want.exps) and f.dtype == dtype
+    taken = cache["len"].clone()
+    other = torch.float16 if dtype == torch.bfloat16 else torch.bfloat16
+    for context in (torch.autocast("cuda", enabled=False), torch.autocast("cuda", other)):
+        with context, pytest.raises(ValueError, match="cache"):
+            t.extend(tokens[:, 0].contiguous(), cache)
+    assert torch.equal(cache["len"], taken) and cache["taken"] == 9
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kw", [dict(), dict(products="fp8", **ALL)])
+def test_extending_a_tower_that_was_cast(kw):
+    """The cache has the dtype that the parameters have now."""
+    t = _tower(dtype=torch.float32, **kw).half().eval()
+    tokens = torch.randint(0, 300, (5, 9), generator=torch.Generator().manual_seed(5)).cuda()
+    with torch.no_grad():
+        whole = t(PackedCaptions(tokens.reshape(-1), [9] * 5))
+    last = _extended(t, tokens)[0]
+    assert float((whole - last).norm(dim=1).max()) < (16 ** 0.5 * 2.0 ** -6.5 if "products" in kw else 8 * 2.0 ** -8)
+
+
 @pytest.mark.gpu
 def test_a_step_on_8_bit_products():
     """Every parameter has a gradient, near that of 16-bit products: each operand is off by
