@@ -190,22 +190,32 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, WIDE ? 4 : 2) norm_fwd(cons
 
 // The sums of the first norm and the gate are two for each feature, S = sum e D v and
 // B = sum e D, whatever of them is asked for:
-//   dgate = post_w S + post_b B,  dpost_w = gate S,  dpost_b = gate B
-// and the rows' loop needs the vectors as gate post_w and gate post_b alone.
+//   dgate = post_w S,  dpost_w = gate S,  dpost_b = gate B
+// and the rows' loop needs the vectors as gate post_w and gate post_b alone.  The gradient of a
+// gate behind a norm with a bias (kGate) has a sum of its own, G = sum e D (v post_w + post_b): as
+// post_w S + post_b B it would have the roundings of both where they cancel.  Its vectors are
+// apart then, those of rows within a wave in LDS; backward and join, with it and from S and B:
+// 20001 x 2568 in fp32 260 us and 257, 17408 x 512 in bf16 34 and 33, and where it takes the
+// next row's registers 16001 x 4096 in bf16 181 and 169, 50001 x 1160 in fp16 196 and 174.
 // BIAS: with sums for biases.  In rows of several waves with everything their sums and gate
 // post_b are in LDS, each lane its own 32 bytes of them, so that 16 waves fit a compute unit with
 // the next row's loads (116 to 118 registers; 106 without).  With sums for each vector instead of
 // S and B: 151 registers, 50001 x 1160 188 us for 173, 20001 x 2568 183 for 164.
-template <int T, bool WIDE, bool FULL, bool BIAS, bool DROP, bool FAR>
+enum Bias { kNoBias, kBias, kGateBias };
+template <int T, bool WIDE, bool FULL, Bias BIASES, bool DROP, bool FAR>
 __global__ void __launch_bounds__(WIDE ? 1024 : 256, 4) norm_bwd(const NormArgs a) {
   __shared__ float buf[2][16][2];
   __shared__ float joined[WIDE ? 1 : 4][WIDE ? 1 : 512];
+  constexpr bool BIAS = BIASES != kNoBias, kGate = BIASES == kGateBias;
+  // kGate in rows within a wave: all rows' gate, post_w, post_b and pre_w
+  constexpr bool kTable = kGate && !WIDE;
+  __shared__ __attribute__((aligned(16))) float table[kTable ? 4 : 1][kTable ? 512 : 4];
   int64_t row, step;
   int chunk, turn = 0;
   place<WIDE>(a, row, step, chunk);
   const bool in = chunk < a.c;
   const int64_t col = 8 * (int64_t)chunk;
-  extern __shared__ f32x4 own[];  // kOwn: [sb2, B, gate post_b][halves][lanes]
+  extern __shared__ f32x4 own[];  // kOwn: [sb2, B, gate post_b (kGate: post_b, G)][halves][lanes]
   constexpr bool kOwn = WIDE && FULL && BIAS;
   auto get_own = [&](int k, float (&q)[8]) {
 #pragma unroll
@@ -226,6 +236,7 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, 4) norm_bwd(const NormArgs 
       own[(2 * k + i) * blockDim.x + threadIdx.x] += f32x4{q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]};
   };
   float gw[8], gb[8], w2[8], S[8], B[8], sw2[8], sb2[8];
+  float w1[8], b1[8], g1[8], G[8];  // kGate: the vectors apart
   const float unit = DROP ? a.drop.unit : 1.f;
   {
     Vectors w;
@@ -234,17 +245,31 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, 4) norm_bwd(const NormArgs 
     for (int e = 0; e < 8; ++e) {
       const float g = DROP ? w.gate[e] * unit : w.gate[e];  // dropout's factor is the gate's
       gw[e] = g * w.w1[e], gb[e] = g * w.b1[e], w2[e] = w.w2[e];
-      S[e] = B[e] = sw2[e] = sb2[e] = 0.f;
+      w1[e] = w.w1[e], b1[e] = w.b1[e], g1[e] = g;
+      S[e] = B[e] = sw2[e] = sb2[e] = G[e] = 0.f;
     }
   }
-  if constexpr (kOwn) put_own(0, sb2), put_own(1, B), put_own(2, gb);
+  if constexpr (kOwn) put_own(0, sb2), put_own(1, B), put_own(2, kGate ? b1 : gb);
+  if constexpr (kOwn && kGate) put_own(3, G);
+  if constexpr (kTable) {
+    if (threadIdx.x < 1u << a.ls) {
+      store8<kF32>(table[0], col, g1), store8<kF32>(table[1], col, w1);
+      store8<kF32>(table[2], col, b1), store8<kF32>(table[3], col, w2);
+    }
+    __syncthreads();
+  }
+  auto get_vectors = [&] {
+    if constexpr (kOwn) get_own(2, kGate ? b1 : gb);
+    if constexpr (kTable) load8<kF32>(table[0], col, g1), load8<kF32>(table[1], col, w1), load8<kF32>(table[2], col, b1);
+  };
   if constexpr (WIDE) clear(buf);
   const uint64_t seed = DROP ? a.drop.the_seed() : 0;
   const Source from_x(a.x, a.xs, a.x), from_y(a.y, a.ys, a.x), from_dh(a.dh, a.dhs, a.x), from_dz(a.dz, a.dzs, a.x);
   const bool post = FULL && a.post_w;
   // The next row beside the sums, as in the forward (50001 x 1160 154 us for 173, 20001 x 2568 134 for
-  // 164, 16001 x 4096 168 for 162); fp32 rows and biases' sums leave no registers for it.
-  constexpr bool kAhead = WIDE && FULL && !(BIAS && T == kF32);
+  // 164, 16001 x 4096 168 for 162); fp32 rows with biases' sums, and kGate, leave no registers for it
+  // (kGate with 24 to 32 bytes of them spilled: 50001 x 1160 214 for 196, 20001 x 2568 178 for 180).
+  constexpr bool kAhead = WIDE && FULL && !(BIAS && T == kF32) && !kGate;
   Raw8<T> next_x, next_y, next_dh, next_dz;
   float4 next_st;
   auto load = [&](int64_t r) {
@@ -277,15 +302,16 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, 4) norm_bwd(const NormArgs 
     rh.get(in && from_dh.there, e8);
     rz.get(in && from_dz.there, g);
     if (a.y) {
-      if constexpr (kOwn) get_own(2, gb);
+      get_vectors();
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if (FULL) v[e] = (v[e] - st.x) * st.y;
-        const float t = !FULL ? v[e] : BIAS ? fmaf(v[e], gw[e], gb[e]) : v[e] * gw[e];
+        const float t = !FULL ? v[e] : kGate ? g1[e] * fmaf(v[e], w1[e], b1[e]) : BIAS ? fmaf(v[e], gw[e], gb[e]) : v[e] * gw[e];
         h[e] = fmaf(a.alpha, h[e], keep[e] ? t : 0.f);
       }
     }
     if (a.pre_w) {
+      if constexpr (kTable) load8<kF32>(table[3], col, w2);
       if (kOwn && a.want_pre_b) add_own(0, g);
       float s[2] = {0.f, 0.f};
 #pragma unroll
@@ -316,10 +342,17 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, 4) norm_bwd(const NormArgs 
         e8[e] = keep[e] ? e8[e] : 0.f;
         if (BIAS && !kOwn) B[e] += e8[e];
       }
-      if (kOwn && (a.want_post_b || (a.want_gate && a.post_b))) add_own(1, e8);
+      if (kOwn && a.want_post_b) add_own(1, e8);
+      if constexpr (kGate) {
+        get_vectors();
+        if constexpr (kOwn) get_own(3, G);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) G[e] = fmaf(e8[e], keep[e] ? fmaf(v[e], w1[e], b1[e]) : 0.f, G[e]);
+        if constexpr (kOwn) put_own(3, G);
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        e8[e] *= gw[e];
+        e8[e] = kGate ? e8[e] * g1[e] * w1[e] : e8[e] * gw[e];
         s[0] += e8[e], s[1] = fmaf(e8[e], v[e], s[1]);
       }
       if (post) {
@@ -332,13 +365,14 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, 4) norm_bwd(const NormArgs 
     if (a.dy && in) store8<T, FAR>(a.dy, row * (8 * (int64_t)a.c) + col, e8);
   }
   if constexpr (kOwn) get_own(0, sb2), get_own(1, B);
+  if constexpr (kOwn && kGate) get_own(3, G);
   float sg[8];
   if constexpr (FULL) {  // the vectors' own sums
     Vectors w;
     load_vectors<T, FULL, BIAS>(a, in, col, w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      sg[e] = unit * (BIAS ? fmaf(w.b1[e], B[e], w.w1[e] * S[e]) : w.w1[e] * S[e]);
+      sg[e] = unit * (kGate ? G[e] : w.w1[e] * S[e]);
       S[e] *= w.gate[e] * unit, B[e] *= w.gate[e] * unit;
     }
   }
@@ -484,10 +518,10 @@ void fwd_t(const NormArgs& r, const Shape& s, hipStream_t st) {
   else
     hipLaunchKernelGGL((norm_fwd<T, false, FULL, DROP, FAR>), grid, block, 0, st, r);
 }
-template <int T, bool FULL, bool BIAS, bool DROP, bool FAR>
+template <int T, bool FULL, Bias BIAS, bool DROP, bool FAR>
 void bwd_t(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
   const dim3 grid(wgs), block(s.threads);
-  const size_t own = FULL && BIAS ? 6 * 16 * (size_t)s.threads : 0;
+  const size_t own = FULL && BIAS != kNoBias ? (BIAS == kGateBias ? 8 : 6) * 16 * (size_t)s.threads : 0;
   if (!s.wide)
     hipLaunchKernelGGL((norm_bwd<T, false, FULL, BIAS, DROP, FAR>), grid, block, 0, st, r);
   else
@@ -503,16 +537,18 @@ void fwd_far(const NormArgs& r, const Shape& s, hipStream_t st) {
   else
     fwd_t<T, true, false, FAR>(r, s, st);
 }
-template <int T, bool FAR, bool BIAS>
+template <int T, bool FAR, Bias BIAS>
 void bwd_full(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
   r.drop.cut ? bwd_t<T, true, BIAS, true, FAR>(r, s, wgs, st) : bwd_t<T, true, BIAS, false, FAR>(r, s, wgs, st);
 }
 template <int T, bool FAR>
 void bwd_far(const NormArgs& r, const Shape& s, unsigned wgs, hipStream_t st) {
   if (!full(r))
-    bwd_t<T, false, true, false, FAR>(r, s, wgs, st);
+    bwd_t<T, false, kBias, false, FAR>(r, s, wgs, st);
+  else if (r.gate && r.post_b)  // (whether dgate is asked for or not: the other results are the same bits)
+    bwd_full<T, FAR, kGateBias>(r, s, wgs, st);
   else
-    r.post_b || r.pre_b ? bwd_full<T, FAR, true>(r, s, wgs, st) : bwd_full<T, FAR, false>(r, s, wgs, st);
+    r.post_b || r.pre_b ? bwd_full<T, FAR, kBias>(r, s, wgs, st) : bwd_full<T, FAR, kNoBias>(r, s, wgs, st);
 }
 template <int T>
 bool far(const NormArgs& r) {

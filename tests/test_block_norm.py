@@ -103,6 +103,42 @@ def test_rows_far_from_zero(d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,d,dtype,p,pre", [(3000, 64, "f32", 0.0, False), (3000, 1024, "f32", 0.0, False), (3001, 512, "f32", 0.25, True),
+                                             (2999, 2048, "f32", 0.25, True), (3000, 128, "bf16", 0.25, True), (3000, 4096, "bf16", 0.0, True),
+                                             (601, 8192, "f32", 0.25, True), (3000, 1024, "f16", 0.25, False)])
+def test_a_gates_gradient_where_the_norm_and_its_bias_cancel(n, d, dtype, p, pre):
+    """Rows whose entries are 2 or -2 have norms of 1 or -1, without a rounding, and biases of
+    -post_w (1 - 2^-12) leave t = post_w 2^-12 of each such entry, again without one, whatever its
+    sign of even features is; odd ones have t = 0.  dgate = sum e D t is then a sum of entries that
+    each carry one rounding (and that of D's factor), added in fp32: up to 16 (n / 1280 rows and
+    more) in a lane, 4 in a workgroup, 36 in the join, 64 in all, relative to what is added.
+    The entries' own size, 2^12 times that, does not count."""
+    g = torch.Generator().manual_seed(d)
+    sign = torch.where(torch.arange(d) % 2 == 0, 1.0, -1.0)  # (of a feature: the same in all rows)
+    v = {"x": torch.randn((n, d), generator=g).to(DT[dtype]), "y": (2 * sign).expand(n, d).contiguous().to(DT[dtype])}
+    w = 1.0 + torch.randint(0, 8, (d,), generator=g) / 8.0
+    v["post_w"], v["post_b"] = w, -sign * w * (1 - 2.0 ** -12 * (torch.arange(d) % 2 == 0))
+    v["gate"] = torch.where(torch.arange(d) % 16 == 3, 0.0, 1.5)
+    if pre:
+        v["pre_w"], v["pre_b"] = torch.ones(d), torch.zeros(d)
+    dh = (1 + torch.rand((n, d), generator=g)).to(DT[dtype])
+    dz = torch.zeros((n, d), dtype=DT[dtype]) if pre else None  # (e = dh, without a rounding)
+    dev = {k: t.cuda() for k, t in v.items()}
+    _, _, kept = infcl.add_norm_fwd(**dev, norm="rms", eps=0.0, p=p, seed=9)
+    grads = dict(zip(NAMES, infcl.add_norm_bwd(dh.cuda(), None if dz is None else dz.cuda(), kept)))
+    # (the masks themselves have tests of their own)
+    keep = (infcl.dropout_fwd(torch.ones((n, d), device="cuda"), p, 9).cpu() != 0) * (65536 / (65536 - round(p * 65536)))
+    t = w.double() * 2.0 ** -12 * (torch.arange(d) % 2 == 0)
+    want = (dh.double() * keep * t).sum(0)  # (all terms of one sign: their sizes' sum too)
+    got = grads["dgate"].cpu().double()
+    assert (got[1::2] == 0).all()
+    assert ((got - want).abs() <= 64 * F32 * want).all(), float(((got - want).abs() / (F32 * want + 1e-30))[0::2].max())
+    for k, scale in (("dpost_w", sign), ("dpost_b", torch.ones(d))):
+        full = (dh.double() * keep).sum(0) * v["gate"].double() * scale.double()
+        assert ((grads[k].cpu().double() - full).abs() <= 64 * F32 * full.abs()).all(), k
+
+
+@pytest.mark.gpu
 def test_equal_rows_and_zeros():
     """Rows without a spread: eps alone is their size; the gradient is finite."""
     x = torch.zeros((3, 64), device="cuda")
