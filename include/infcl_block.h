@@ -161,6 +161,7 @@ infcl_status infcl_fp8_linear(const void* x, int64_t x_stride, int64_t n, int64_
  * columns (each may be NULL), of the operands packed along the other side, and dy both
  * ways.  keeps: INFCL_KEEP_W where dx is to come, INFCL_KEEP_X for dw; `kept` is the same
  * memory and keeps the same number in both calls (NULL and 0 where neither is to come).
+ * n up to 2^27, with INFCL_KEEP_X up to 2^23; m up to 2^23.
  * Everything is of dtype, INFCL_BF16 or INFCL_F16. */
 enum { INFCL_KEEP_W = 1, INFCL_KEEP_X = 2 };
 infcl_status infcl_fp8_layer_sizes(int64_t n, int64_t k, int64_t m, int keeps, size_t* kept_bytes, size_t* fwd_bytes,

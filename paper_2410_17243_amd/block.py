@@ -542,9 +542,12 @@ def _layer_sizes(n, k, m, keeps):
     return tuple(s.value for s in sizes)
 
 
+_MOST_OUT = 1 << 23  # outputs of a layer with gradients
+
+
 def _learns(m):
-    if m % 8:
-        raise ValueError(f"linear_fp8: a layer with gradients has a multiple of 8 outputs, got {m}")
+    if m % 8 or m > _MOST_OUT:
+        raise ValueError(f"linear_fp8: a layer with gradients has a multiple of 8 outputs, up to 2^23, got {m}")
 
 
 def linear_fp8_fwd(x, w, b=None, need_dx: bool = True, need_dw: bool = True):
@@ -558,7 +561,7 @@ def linear_fp8_fwd(x, w, b=None, need_dx: bool = True, need_dw: bool = True):
     keeps = need_dx + 2 * need_dw
     if keeps:
         _learns(m)
-    elif m % 8:  # (a forward alone takes any number of outputs)
+    elif m % 8 or m > _MOST_OUT:  # (a forward alone takes any number of outputs)
         return _times_packed(x, fp8_pack(w), b), (None, (n, k, m, x.dtype, 0, b is not None))
     size, scratch, _ = _layer_sizes(n, k, m, keeps)
     out = x.new_empty((*x.shape[:-1], m))

@@ -487,7 +487,7 @@ struct Places {
 struct LayerPlaces {
   void *xt = nullptr, *xte = nullptr, *wt = nullptr, *wte = nullptr;  // kept
   void *x, *xe, *w, *we, *fwd;                                        // the forward's
-  void *dy, *dye, *dyt, *dyte, *sums, *bwd;                           // the backward's
+  void *dy = nullptr, *dye = nullptr, *dyt = nullptr, *dyte = nullptr, *sums, *bwd;  // the backward's
   size_t kept, fwd_bytes, bwd_bytes;
 };
 LayerPlaces layer_places(int64_t n, int64_t k, int64_t m, int keeps, void* kept, void* ws) {
@@ -498,24 +498,25 @@ LayerPlaces layer_places(int64_t n, int64_t k, int64_t m, int keeps, void* kept,
   f.operand(n, k, r.x, r.xe);
   f.operand(m, k, r.w, r.we);
   r.fwd = f.take(plan_of(n, m, k).total);
-  b.operand(n, m, r.dy, r.dye);
-  b.operand(m, n, r.dyt, r.dyte);
+  if (keeps & INFCL_KEEP_W) b.operand(n, m, r.dy, r.dye);
+  if (keeps & INFCL_KEEP_X) b.operand(m, n, r.dyt, r.dyte);
   size_t sums = 0;
   infcl_fp8_pack_workspace(n, m, &sums);
   r.sums = b.take(sums);
-  const size_t dx = plan_of(n, k, m).total, dw = plan_of(m, k, n).total;
+  const size_t dx = keeps & INFCL_KEEP_W ? plan_of(n, k, m).total : 0, dw = keeps & INFCL_KEEP_X ? plan_of(m, k, n).total : 0;
   r.bwd = b.take(dx > dw ? dx : dw);
   r.kept = p.used, r.fwd_bytes = f.used, r.bwd_bytes = b.used;
   return r;
 }
+// The limits of the products that there are: the rows are a contraction for dw alone.
 infcl_status layer_status(int64_t n, int64_t k, int64_t m, int keeps) {
   if (n < 0 || k < 1 || m < 1 || keeps < 0 || keeps > 3) return INFCL_ERR_INVALID;
-  if (k % 8 != 0 || m % 8 != 0 || n > ((int64_t)1 << 23) || m > ((int64_t)1 << 23) || m > ((int64_t)1 << 36) / k ||
+  if (k % 8 != 0 || m % 8 != 0 || m > ((int64_t)1 << 23) || m > ((int64_t)1 << 36) / k ||
       n > ((int64_t)1 << 37) / (k > m ? k : m))
     return INFCL_ERR_UNSUPPORTED;
   infcl_status s = sizes_status(n, m, k);
-  if (s == INFCL_OK) s = sizes_status(n, k, m);
-  return s == INFCL_OK ? sizes_status(m, k, n) : s;
+  if (s == INFCL_OK && keeps & INFCL_KEEP_W) s = sizes_status(n, k, m);
+  return s == INFCL_OK && keeps & INFCL_KEEP_X ? sizes_status(m, k, n) : s;
 }
 
 }  // namespace

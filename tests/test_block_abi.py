@@ -163,6 +163,22 @@ def test_fp8_layer_backward(lib, kw, want):
                                    a["space"], a["bytes"], None) == want
 
 
+@pytest.mark.parametrize("n,k,m,keeps,want", [
+    (1 << 27, 8, 8, 0, OK), ((1 << 27) + 1, 8, 8, 0, UNSUPPORTED), (1 << 26, 8, 64, 1, OK), (1 << 23, 8, 8, 3, OK),
+    ((1 << 23) + 1, 8, 8, 2, UNSUPPORTED), ((1 << 23) + 1, 8, 8, 3, UNSUPPORTED), (8, 8, 1 << 23, 3, OK), (8, 8, (1 << 23) + 8, 0, UNSUPPORTED),
+    (8, 1 << 23, 8, 3, OK), (8, (1 << 23) + 8, 8, 0, UNSUPPORTED), (1 << 27, 8, 2048, 0, UNSUPPORTED),
+])
+def test_fp8_layer_sizes(lib, n, k, m, keeps, want):
+    """The limits are those of the products that there are; what is not kept for has no room."""
+    sizes = [ctypes.c_size_t(0) for _ in range(3)]
+    assert lib.infcl_fp8_layer_sizes(n, k, m, keeps, *(ctypes.byref(s) for s in sizes)) == want
+    if want == OK:
+        sums = ctypes.c_size_t(0)
+        assert lib.infcl_fp8_pack_workspace(n, m, ctypes.byref(sums)) == OK
+        assert (sizes[0].value > 0) == (keeps > 0) and sizes[1].value >= 128 * (n + m)
+        assert sizes[2].value >= 128 * n + sums.value if keeps & 1 else keeps or sizes[2].value == sums.value
+
+
 def test_workspaces(lib):
     def size(name, *a):
         n = ctypes.c_size_t(0)

@@ -213,6 +213,25 @@ def test_without_gradients_nothing_is_kept(monkeypatch):
 
 
 @pytest.mark.gpu
+def test_more_rows_than_a_weights_gradient_takes():
+    """The rows are a contraction for dw alone, up to 2^23: without it there may be more, as
+    with packed weights.  The last rows are what they are alone."""
+    n = (1 << 23) + 40
+    x = torch.randn((n, 8), device="cuda").bfloat16()
+    w, b = torch.randn((8, 8), device="cuda").bfloat16(), torch.randn(8, device="cuda").bfloat16()
+    y = infcl.linear_fp8(x, w, b)
+    assert torch.equal(y, infcl.linear_fp8(x, infcl.fp8_pack(w), b)) and torch.equal(y[-50:], infcl.linear_fp8(x[-50:], w, b))
+    del y
+    tail = x[-50:].clone().requires_grad_()
+    xr, br, dy = x.requires_grad_(), b.clone().requires_grad_(), torch.ones((n, 8), dtype=torch.bfloat16, device="cuda")
+    dx, db = torch.autograd.grad(infcl.linear_fp8(xr, w, br), (xr, br), dy)
+    assert torch.equal(dx[-50:], torch.autograd.grad(infcl.linear_fp8(tail, w), tail, dy[:50])[0])
+    assert (db == float(torch.tensor(n).bfloat16())).all()  # (sums of up to 128 ones, then of 65537 of them: whole numbers)
+    with pytest.raises(infcl.InfclError):  # (in the forward)
+        infcl.linear_fp8(x.detach(), w.requires_grad_(), b)
+
+
+@pytest.mark.gpu
 def test_no_rows_and_autocast():
     w, b = torch.randn((16, 64), device="cuda"), torch.randn(16, device="cuda")
     x = torch.zeros((0, 64), dtype=torch.bfloat16, device="cuda").requires_grad_()
