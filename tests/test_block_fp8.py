@@ -124,6 +124,35 @@ def test_products_of_whole_numbers_are_exact(n, m, k, dtype):
         assert torch.equal(infcl.linear_fp8(x.cuda(), c, b.cuda() if b is not None else None), out)
 
 
+# powers of two of a's and b's rows; the last ones' results are subnormal in fp32 and bf16
+FAR = [(100, -100), (-100, 100), (60, -63), (-60, -60), (-60, 60), (110, 0), (0, -118), (-117, 117), (119, -119), (-110, 106),
+       (-64, -64), (-33, -100), (-126, -10)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [3, 16, 40, 300])
+@pytest.mark.parametrize("ea,eb", FAR)
+def test_products_of_exponents_far_apart_are_exact(ea, eb, n):
+    """Whole numbers up to 4 times powers of two at both ends of bf16, in the kernel of few rows
+    and that of tiles: each scale may be next to its end, and sums that fp32 holds as subnormals
+    are kept.  Blocks beside them in the contraction are zeros (exponent byte 1), or
+    of the other end against zeros: they add nothing."""
+    k, m = 1032, 72
+    x, w = _whole(n, k, "bf16", 7), _whole(m, k, "bf16", 8)
+    x, w = x * torch.tensor(2.0 ** ea).bfloat16(), w * torch.tensor(2.0 ** eb).bfloat16()
+    x[:, 128:256], w[:, 256:384] = 0, 0
+    w[:, 128:256] = 2.0 ** 126  # against zeros
+    x[:, 256:384] = -(2.0 ** 126)
+    x[:, 384:512], w[:, 384:512] = 0, 0
+    a, c = infcl.fp8_pack(x.cuda()), infcl.fp8_pack(w.cuda())
+    e = infcl.fp8_unpack(a)
+    assert torch.equal(e.cpu(), x)
+    want = (x.cuda().double() @ w.cuda().double().t()).to(torch.bfloat16)
+    assert torch.isfinite(want).all() and float(want.float().abs().max()) > 0
+    assert torch.equal(infcl.fp8_matmul(a, c), want)
+    assert torch.equal(infcl.linear_fp8(x.cuda(), c), want)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("n,m,k,dtype", [(5, 48, 264, "bf16"), (16, 100, 4096, "f16"), (40, 72, 1032, "bf16"), (300, 520, 2048, "f16"),
                                          (1025, 264, 776, "bf16")])
