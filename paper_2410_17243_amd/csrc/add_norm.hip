@@ -14,12 +14,14 @@
 // wave, or several waves.  It stays in registers from its load to its last use, so the
 // variance is that of the centred row and the backward reads each input once; h is
 // taken again from x and y there (as many bytes as reading it back, and not rounded).
-// What a lane adds up for its features over all its rows are 32 registers at most, then
+// What a lane adds up for its features over all its rows are 32 registers at most (40 with gate
+// and biases; some of them in LDS where rows take several waves), then
 // one row of partial sums for each workgroup, joined in order by a second launch.
 // Bound by the rows' bytes without gate, first norm and dropout (17408 x 512: 13 us forward and 21
-// backward for 71 and 107 MB; 50001 x 1160: 77 and 138, of a floor of 92 and 138).  With
-// everything the vector unit has about as much to do, some 400 instructions for 8 features:
-// 50001 x 1160 108 and 154 us, 20001 x 2568 117 and 134 of 82 and 122.  8 rows of 4096 forward: 4.2 to 4.8 us.
+// backward for 71 and 107 MB; 50001 x 1160: 77 and 138 for 464 and 696 MB, part of them from the
+// last-level cache).  With everything the vector unit has about as much to do, some 400 instructions
+// for 8 features: 50001 x 1160 108 to 116 and 154 to 171 us, 20001 x 2568 117 and 134, of 82 and 122 at a
+// copy's 5.04 TB/s.  8 rows of 4096 forward: 4.2 to 4.8 us.
 #include "block.hpp"
 
 namespace infcl {
@@ -267,8 +269,9 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256, 4) norm_bwd(const NormArgs 
   const Source from_x(a.x, a.xs, a.x), from_y(a.y, a.ys, a.x), from_dh(a.dh, a.dhs, a.x), from_dz(a.dz, a.dzs, a.x);
   const bool post = FULL && a.post_w;
   // The next row beside the sums, as in the forward (50001 x 1160 154 us for 173, 20001 x 2568 134 for
-  // 164, 16001 x 4096 168 for 162); fp32 rows with biases' sums, and kGate, leave no registers for it
-  // (kGate with 24 to 32 bytes of them spilled: 50001 x 1160 214 for 196, 20001 x 2568 178 for 180).
+  // 164; 16001 x 4096 168 for 162, the one size of these that loses, and not worth a rule); fp32 rows
+  // with biases' sums, and kGate, leave no registers for it (kGate with 24 to 32 bytes of them spilled:
+  // 50001 x 1160 214 for 196, 20001 x 2568 178 for 180).
   constexpr bool kAhead = WIDE && FULL && !(BIAS && T == kF32) && !kGate;
   Raw8<T> next_x, next_y, next_dh, next_dz;
   float4 next_st;

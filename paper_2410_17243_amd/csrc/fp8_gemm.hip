@@ -20,11 +20,12 @@
 // units idle; their sums are added in order by a second launch, with the bias.
 //
 // 8192^3 takes 427 to 505 us with the clock of the card at hand (2575 to 2180 TFLOP/s): a stage's
-// LDS traffic, 96 KiB read and 32 written, is about as long as its products, and a workgroup's start
-// and end are some 8 us, which short contractions feel: 65536 x 4096 x 1024 300 to 372 us, 65536 x
-// 1024 x 4096 235 to 257, 4096 x 1024 x 65536 242 to 260 in four parts and their join.  Two
-// workgroups of 256 x 128 to a compute unit, one's end beside the other's products, lose in the
-// loop what they gain there (8192^3 536 us for 427, 65536 x 4096 x 1024 304 for 300).
+// LDS traffic, 96 KiB read and 32 written, is about as long as its products.  65536 x 1024 x 4096
+// takes 235 to 260, 4096 x 1024 x 65536 241 to 260 in four parts and their join.  Short contractions
+// are further from the unit's rate (65536 x 4096 x 1024 300 to 372 us of 197, 17408 x 2048 x 512 34 of
+// 13); a workgroup's start and end are some 8 us, but that is not all of it: two workgroups of 256 x
+// 128 to a compute unit, one's end beside the other's products, do not gain (8192^3 536 us for 427,
+// 65536 x 4096 x 1024 304 for 300), nor does a stream of stages over several tiles.
 #include "fp8.hpp"
 #include "grid.hpp"
 
@@ -297,8 +298,9 @@ __global__ void __launch_bounds__(256) matmul_join(const float* __restrict__ par
 // block of the contraction, straight from memory; the waves' sums meet in LDS.  Every
 // workgroup packs x itself (as infcl_fp8_pack does), 4096 entries of the contraction at a
 // time, into LDS while the weights for them are on their way.  Bound by the weights' bytes
-// and the latency of one such pass: 4 x 4096 -> 4096 7.1 us, 16 rows 10.7 (9.3 and 9.4 where each
-// wave packs what it needs in its operand's layout, 16 rows whatever n).
+// and the latency of one such pass: 4 x 4096 -> 4096 7.1 us, 16 rows 10.7.  (Where each wave packs what
+// it needs in its operand's layout, 16 rows whatever n, 9.3 and 9.4: better near 16 rows only, and
+// not kept as a second form.)
 constexpr int kFewWaves = 8, kFewBlocks = 4, kFewSpan = 128 * kFewWaves * kFewBlocks, kFewPitch = kFewSpan + 16;
 template <bool F16>
 __global__ void __launch_bounds__(64 * kFewWaves) few_kernel(const uint16_t* __restrict__ x, int64_t xs, int n, int64_t k,

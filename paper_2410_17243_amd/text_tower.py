@@ -14,9 +14,10 @@ values.
 
 By choice: rotary positions instead of learned ones (rotary), dropout of what the
 blocks add, gates and norms of it, with the residual sum and the next norm in one pass
-(add_norm), and products of 8-bit floats (linear_fp8).  Dropout's masks are functions of
-the tower's seed, the layer, and the token's place in the whole batch, so both passes of
-the gradient cache have the same ones, however the batch is cut.
+(add_norm), and products of 8-bit floats (linear_fp8; the activation between them is
+torch's and keeps 16 bits).  Dropout's masks are functions of the tower's seed, the layer,
+and the token's place in the whole batch, so both passes of the gradient cache have the
+same ones, however the batch is cut.
 
 The command trains a small random-initialised tower against fixed random image
 embeddings for a few steps and prints the loss and what a chunk keeps for its backward
